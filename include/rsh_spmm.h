@@ -265,6 +265,53 @@ int rsh_act_backward(const void *dY_dev, const void *Y_dev, void *dZ_dev, float 
                      void *hip_stream);
 
 /*
+ * Matrices in microscaled 4-bit floating point, row-major, k > 0 elements a row in blocks of 32 (the last may be short):
+ *   scales  uint8 [rows][B], B = ceil(k / 32): byte s stands for 2^(s - 127), 255 for NaN
+ *   codes   uint8 [rows][16 B]: element 2i of a row in the low half of byte i, 2i + 1 in the high half; bit 3 the sign, bits 0..2
+ *           one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  Cells past k are zero.  16-byte aligned.
+ *   rsh_mx4_quantize    s brings the largest magnitude of a block into [4, 8): floor(log2 max) - 2 + 127, at least 0; elements go
+ *                       to the nearest value, ties to the even code, above 6 to 6.  A block of zeros: s = 0.  A block with an
+ *                       infinity or a NaN: s = 255, codes 0.
+ *   rsh_mx4_dequantize  the values, rounded once (to RSH_F32 and RSH_BF16 they are exact)
+ * type: RSH_F32, RSH_F16 or RSH_BF16, of X and Y, whose rows are ld elements apart (ld >= k); no alignment beyond the element's.
+ *
+ *   rsh_mx4_product     Y[i][j] = sum over k of X[i][k] w[j][k], fp32 sums, rounded once to y_type (RSH_F16 or RSH_BF16);
+ *                       w: [n][k] in 4 bits.  x_type RSH_F16 or RSH_BF16 (then y_type is the same): X [t][k], rows ld_x apart,
+ *                       x_scales NULL.  x_type RSH_MX4: X and x_scales in 4 bits like w, ld_x unused.  Y: rows of n.
+ *                       Beside binary16 activations a value of w enters as binary16 relative to its row: exactly, but for
+ *                       blocks whose scale is below 2^-33 of the row's largest.
+ *
+ * The gated block H = act(G) * U, G = X Wg^T, U = X Wu^T, and its gradients for dH:
+ *   dU = dH act(G), dG = dH U act'(G);  dX = dG Wg + dU Wu, dWg = dG^T X, dWu = dU^T X
+ * X [t][d], Wg and Wu [f][d] with rows ld_x and ld_w elements apart, H [t][f], dX [t][d], dWg and dWu [f][d] without gaps; all of
+ * `type` (RSH_F16 or RSH_BF16), no alignment beyond the element's.  act: RSH_ACT_SILU, RSH_ACT_GELU (with the error function) or
+ * RSH_ACT_RELU.  fp32 sums, each result rounded once.
+ *   rsh_gated_forward   g_scales and u_scales not NULL: Wg and Wu in 4 bits (ld_w unused).  G and U: NULL, or kept for the
+ *                       gradients: [t][f rounded up to a multiple of 8] of `type`, 16-byte aligned
+ *   rsh_gated_backward  dX, dWg, dWu: NULL where not wanted.  dH: rows ld_h apart.  dG and dU are rounded to `type`.
+ * work: device, 16-byte aligned, of the bytes that the *_work function of the same sizes reports (0: may be NULL), rewritten by
+ * every call.  Sizes are positive and below 2^31.  Results never depend on the order in which waves run.
+ * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE
+ * for more tiles than a launch takes.
+ */
+enum { RSH_F32 = 0, RSH_F16 = 1, RSH_BF16 = 2, RSH_MX4 = 3 };
+enum { RSH_ACT_SILU = 0, RSH_ACT_GELU = 1, RSH_ACT_RELU = 2 };
+int rsh_mx4_quantize(const void *X_dev, int32_t type, int64_t rows, int64_t k, int64_t ld, void *codes_dev, void *scales_dev, void *hip_stream);
+int rsh_mx4_dequantize(const void *codes_dev, const void *scales_dev, int64_t rows, int64_t k, void *Y_dev, int32_t type, int64_t ld,
+                       void *hip_stream);
+int rsh_mx4_product_work(int32_t x_type, int64_t t, int64_t n, int64_t k, int64_t *bytes);
+int rsh_mx4_product(const void *X_dev, const void *x_scales_dev, int32_t x_type, int64_t ld_x, const void *W_dev, const void *w_scales_dev,
+                    void *Y_dev, int32_t y_type, int64_t t, int64_t n, int64_t k, void *work_dev, void *hip_stream);
+int rsh_gated_forward_work(int32_t w_type, int64_t t, int64_t d, int64_t f, int64_t *bytes);
+int rsh_gated_forward(const void *X_dev, int32_t type, int64_t ld_x, const void *Wg_dev, const void *Wu_dev, int64_t ld_w, const void *g_scales_dev,
+                      const void *u_scales_dev, int32_t act, void *H_dev, void *G_dev, void *U_dev, int64_t t, int64_t d, int64_t f,
+                      void *work_dev, void *hip_stream);
+int rsh_gated_backward_work(int64_t t, int64_t d, int64_t f, int64_t *bytes);
+int rsh_gated_backward(const void *X_dev, int32_t type, int64_t ld_x, const void *Wg_dev, const void *Wu_dev, int64_t ld_w, const void *G_dev,
+                       const void *U_dev, const void *dH_dev, int64_t ld_h, int32_t act, void *dX_dev, void *dWg_dev, void *dWu_dev, int64_t t,
+                       int64_t d, int64_t f, void *work_dev, void *hip_stream);
+
+/*
  * Same work as rsh_spmm, but brackets each kernel with HIP events on hip_stream,
  * waits for the stream, and reports the elapsed milliseconds of the tile kernel,
  * the irregular kernel and the combine kernel (0 for a kernel that was not

@@ -17,6 +17,9 @@ RSH_OK = 0
 (RSH_ERR_NULL, RSH_ERR_INVALID_CSR, RSH_ERR_UNSUPPORTED_N, RSH_ERR_BAD_OPTION, RSH_ERR_OOM,
  RSH_ERR_HIP, RSH_ERR_NOT_UPLOADED, RSH_ERR_TOO_LARGE) = range(1, 9)
 
+RSH_F32, RSH_F16, RSH_BF16, RSH_MX4 = range(4)
+RSH_ACT_SILU, RSH_ACT_GELU, RSH_ACT_RELU = range(3)
+
 (RSH_ARR_WIN_ROW, RSH_ARR_WIN_TILE_OFF, RSH_ARR_TILE_COLID, RSH_ARR_TILE_MASK, RSH_ARR_TILE_VAL_OFF,
  RSH_ARR_TILE_VAL, RSH_ARR_TILE_ITEM, RSH_ARR_IRR_COL, RSH_ARR_IRR_VAL, RSH_ARR_IRR_WAVE, RSH_ARR_IRR_ROW,
  RSH_ARR_COMBINE, RSH_ARR_TILE_XCD, RSH_ARR_IRR_XCD, RSH_ARR_PANEL_COL0, RSH_ARR_PANEL_OFF, RSH_ARR_PANEL_ENT,
@@ -35,7 +38,9 @@ _ARRAY_DTYPES = {
 
 EXPORTED_SYMBOLS = [
     "rsh_plan_opts_default", "rsh_plan_create", "rsh_spmm", "rsh_spmm_noalloc", "rsh_spmm_f16", "rsh_spmm_profile",
-    "rsh_dense_forward", "rsh_dense_backward", "rsh_act_backward", "rsh_copy_probe", "rsh_plan_destroy", "rsh_plan_stats",
+    "rsh_dense_forward", "rsh_dense_backward", "rsh_act_backward", "rsh_mx4_quantize", "rsh_mx4_dequantize",
+    "rsh_mx4_product_work", "rsh_mx4_product", "rsh_gated_forward_work", "rsh_gated_forward", "rsh_gated_backward_work", "rsh_gated_backward",
+    "rsh_copy_probe", "rsh_plan_destroy", "rsh_plan_stats",
     "rsh_plan_decode", "rsh_plan_row_order", "rsh_reorder_knn", "rsh_plan_array", "rsh_plan_teams_per_wave",
     "rsh_plan_kernels", "rsh_plan_strip", "rsh_plan_operand",
     "rsh_struct_sizes", "rsh_status_string", "rsh_last_hip_error",
@@ -120,6 +125,15 @@ def lib() -> ctypes.CDLL:
         L.rsh_dense_forward.argtypes = [vp, vp, vp, ctypes.c_int64, i32, i32, vp]
         L.rsh_dense_backward.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_int64, i32, i32, vp]
         L.rsh_act_backward.argtypes = [vp, vp, vp, vp, vp, ctypes.c_int64, i32, vp]
+        i64 = ctypes.c_int64
+        L.rsh_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+        L.rsh_mx4_dequantize.argtypes = [vp, vp, i64, i64, vp, i32, i64, vp]
+        L.rsh_mx4_product_work.argtypes = [i32, i64, i64, i64, i64p]
+        L.rsh_mx4_product.argtypes = [vp, vp, i32, i64, vp, vp, vp, i32, i64, i64, i64, vp, vp]
+        L.rsh_gated_forward_work.argtypes = [i32, i64, i64, i64, i64p]
+        L.rsh_gated_forward.argtypes = [vp, i32, i64, vp, vp, i64, vp, vp, i32, vp, vp, vp, i64, i64, i64, vp, vp]
+        L.rsh_gated_backward_work.argtypes = [i64, i64, i64, i64p]
+        L.rsh_gated_backward.argtypes = [vp, i32, i64, vp, vp, i64, vp, vp, vp, i64, i32, vp, vp, vp, i64, i64, i64, vp, vp]
         L.rsh_copy_probe.argtypes = [vp, vp, ctypes.c_int64, vp]
         L.rsh_plan_destroy.argtypes = [vp]
         L.rsh_plan_stats.argtypes = [vp, ctypes.POINTER(rsh_plan_stats_t)]
@@ -224,6 +238,64 @@ def act_backward(dY, Y, want_dbias: bool):
     _check(lib().rsh_act_backward(dY.data_ptr(), _address(Y), None if Y is None else dZ.data_ptr(), _address(dbias), _address(work), n, d,
                                   current_stream()))
     return dZ, dbias
+
+
+def _work(function, device, *sizes):
+    """The work array that a *_work function asks for, or None."""
+    import torch
+    n = ctypes.c_int64()
+    _check(function(*sizes, ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+
+
+def mx4_quantize(X, x_type: int, ld: int):
+    """(codes, scales) of a matrix whose rows are ld elements apart (rsh_mx4_quantize)."""
+    import torch
+    rows, k = X.shape
+    blocks = -(-k // 32)
+    codes = torch.empty((rows, 16 * blocks), dtype=torch.uint8, device=X.device)
+    scales = torch.empty((rows, blocks), dtype=torch.uint8, device=X.device)
+    _check(lib().rsh_mx4_quantize(X.data_ptr(), x_type, rows, k, ld, codes.data_ptr(), scales.data_ptr(), current_stream()))
+    return codes, scales
+
+
+def mx4_dequantize(codes, scales, Y, y_type: int) -> None:
+    """Write the values into Y, contiguous [rows, k] (rsh_mx4_dequantize)."""
+    rows, k = Y.shape
+    _check(lib().rsh_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, Y.data_ptr(), y_type, k, current_stream()))
+
+
+def mx4_product(X, x_scales, x_type: int, ld_x: int, codes, scales, Y, y_type: int, k: int) -> None:
+    """Y = X W^T with W in 4 bits (rsh_mx4_product); Y contiguous [t, n]."""
+    t, n = Y.shape
+    work = _work(lib().rsh_mx4_product_work, Y.device, x_type, t, n, k)
+    _check(lib().rsh_mx4_product(X.data_ptr(), _address(x_scales), x_type, ld_x, codes.data_ptr(), scales.data_ptr(), Y.data_ptr(), y_type, t, n, k,
+                                 _address(work), current_stream()))
+
+
+def gated_forward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, g_scales, u_scales, act: int, f: int, keep: bool):
+    """(H, G, U) of the gated block (rsh_gated_forward); G and U None unless they are kept."""
+    import torch
+    t, d = X.shape
+    H = torch.empty((t, f), dtype=X.dtype, device=X.device)
+    G = U = None
+    if keep:
+        G, U = (torch.empty((t, -(-f // 8) * 8), dtype=X.dtype, device=X.device) for _ in range(2))
+    work = _work(lib().rsh_gated_forward_work, X.device, x_type if g_scales is None else RSH_MX4, t, d, f)
+    _check(lib().rsh_gated_forward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, _address(g_scales), _address(u_scales), act,
+                                   H.data_ptr(), _address(G), _address(U), t, d, f, _address(work), current_stream()))
+    return H, G, U
+
+
+def gated_backward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, G, U, dH, ld_h: int, act: int, want):
+    """Gradients (dX, dWg, dWu) of the gated block, None where not wanted (rsh_gated_backward)."""
+    import torch
+    (t, d), f = X.shape, Wg.shape[0]
+    out = [torch.empty(s, dtype=X.dtype, device=X.device) if w else None for s, w in zip(((t, d), (f, d), (f, d)), want)]
+    work = _work(lib().rsh_gated_backward_work, X.device, t, d, f)
+    _check(lib().rsh_gated_backward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, G.data_ptr(), U.data_ptr(), dH.data_ptr(), ld_h,
+                                    act, *(_address(o) for o in out), t, d, f, _address(work), current_stream()))
+    return out
 
 
 def rsh_copy_probe(src, dst, nbytes: int, stream=None) -> None:

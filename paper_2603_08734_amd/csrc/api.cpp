@@ -638,6 +638,93 @@ int rsh_act_backward(const void* dY, const void* Y, void* dZ, float* dbias, floa
     return launch_status(rsh::launch_act_backward(dY, Y, dZ, dbias, work, n, d, hip_stream));
 }
 
+namespace {
+constexpr int64_t kMaxSize = (int64_t)1 << 31;
+// Sizes of a product; its tiles are no smaller than 64 by 64.
+int sizes_ok(int64_t a, int64_t b, int64_t c) {
+    if (a <= 0 || b <= 0 || c <= 0 || a >= kMaxSize || b >= kMaxSize || c >= kMaxSize) return RSH_ERR_BAD_OPTION;
+    for (const auto& [x, y] : {std::pair(a, b), std::pair(a, c), std::pair(b, c)})
+        if (((x + 63) / 64) * ((y + 63) / 64) > kMaxSize / 64) return RSH_ERR_TOO_LARGE;
+    return RSH_OK;
+}
+bool half_type(int32_t type) { return type == RSH_F16 || type == RSH_BF16; }
+int matrix_ok(int32_t type, int64_t rows, int64_t k, int64_t ld, const void* X, const void* codes, const void* scales) {
+    if (!X || !codes || !scales) return RSH_ERR_NULL;
+    if ((type != RSH_F32 && !half_type(type)) || rows <= 0 || k <= 0 || ld < k || !aligned_to({X}, type == RSH_F32 ? 4 : 2) || !aligned_to({codes}, 16))
+        return RSH_ERR_BAD_OPTION;
+    if (rows >= kMaxSize || k >= kMaxSize || ld >= kMaxSize || rows * ((k + 31) / 32) > kMaxSize * 16) return RSH_ERR_TOO_LARGE;
+    return RSH_OK;
+}
+}  // namespace
+
+int rsh_mx4_quantize(const void* X, int32_t type, int64_t rows, int64_t k, int64_t ld, void* codes, void* scales, void* hip_stream) {
+    const int rc = matrix_ok(type, rows, k, ld, X, codes, scales);
+    return rc ? rc : launch_status(rsh::launch_mx4_quantize(X, type, rows, k, ld, codes, scales, hip_stream));
+}
+
+int rsh_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t k, void* Y, int32_t type, int64_t ld, void* hip_stream) {
+    const int rc = matrix_ok(type, rows, k, ld, Y, codes, scales);
+    return rc ? rc : launch_status(rsh::launch_mx4_dequantize(codes, scales, rows, k, Y, type, ld, hip_stream));
+}
+
+int rsh_mx4_product_work(int32_t x_type, int64_t t, int64_t n, int64_t k, int64_t* bytes) {
+    if (!bytes) return RSH_ERR_NULL;
+    if (x_type != RSH_MX4 && !half_type(x_type)) return RSH_ERR_BAD_OPTION;
+    *bytes = 0;
+    return sizes_ok(t, n, k);
+}
+
+int rsh_mx4_product(const void* X, const void* x_scales, int32_t x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int32_t y_type,
+                    int64_t t, int64_t n, int64_t k, void* work, void* hip_stream) {
+    int64_t bytes;
+    if (const int rc = rsh_mx4_product_work(x_type, t, n, k, &bytes)) return rc;
+    const bool four = x_type == RSH_MX4;
+    if (!X || !W || !w_scales || !Y || (four && !x_scales) || (bytes && !work)) return RSH_ERR_NULL;
+    if (!half_type(y_type) || (!four && (y_type != x_type || x_scales || ld_x < k || ld_x >= kMaxSize)) || !aligned_to({W}, 16) || !aligned_to({Y}, 2) ||
+        !aligned_to({X}, four ? 16 : 2) || !aligned_to({work}, 16))
+        return RSH_ERR_BAD_OPTION;
+    return launch_status(rsh::launch_mx4_product(X, x_scales, x_type, ld_x, W, w_scales, Y, y_type, t, n, k, hip_stream));
+}
+
+int rsh_gated_forward_work(int32_t w_type, int64_t t, int64_t d, int64_t f, int64_t* bytes) {
+    if (!bytes) return RSH_ERR_NULL;
+    if (w_type != RSH_MX4 && !half_type(w_type)) return RSH_ERR_BAD_OPTION;
+    *bytes = 0;
+    return sizes_ok(t, d, f);
+}
+
+int rsh_gated_forward(const void* X, int32_t type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
+                      const void* u_scales, int32_t act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* work, void* hip_stream) {
+    int64_t bytes;
+    if (!half_type(type) || act < RSH_ACT_SILU || act > RSH_ACT_RELU) return RSH_ERR_BAD_OPTION;
+    if (const int rc = rsh_gated_forward_work(g_scales ? RSH_MX4 : type, t, d, f, &bytes)) return rc;
+    if (!X || !Wg || !Wu || !H || !g_scales != !u_scales || !G != !U || (bytes && !work)) return RSH_ERR_NULL;
+    if (ld_x < d || ld_x >= kMaxSize || (!g_scales && (ld_w < d || ld_w >= kMaxSize)) || !aligned_to({X, H}, 2) ||
+        !aligned_to({Wg, Wu}, g_scales ? 16 : 2) || !aligned_to({G, U, work}, 16))
+        return RSH_ERR_BAD_OPTION;
+    return launch_status(rsh::launch_gated_forward(X, type, ld_x, Wg, Wu, ld_w, g_scales, u_scales, act, H, G, U, t, d, f, hip_stream));
+}
+
+int rsh_gated_backward_work(int64_t t, int64_t d, int64_t f, int64_t* bytes) {
+    if (!bytes) return RSH_ERR_NULL;
+    const int rc = sizes_ok(t, d, f);
+    *bytes = rc ? 0 : 4 * t * ((f + 7) / 8 * 8);
+    return rc;
+}
+
+int rsh_gated_backward(const void* X, int32_t type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* G, const void* U,
+                       const void* dH, int64_t ld_h, int32_t act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
+                       void* hip_stream) {
+    int64_t bytes;
+    if (!half_type(type) || act < RSH_ACT_SILU || act > RSH_ACT_RELU) return RSH_ERR_BAD_OPTION;
+    if (const int rc = rsh_gated_backward_work(t, d, f, &bytes)) return rc;
+    if (!X || !G || !U || !dH || !work || (dX && (!Wg || !Wu)) || (!dX && !dWg && !dWu)) return RSH_ERR_NULL;
+    if (ld_x < d || ld_x >= kMaxSize || (dX && (ld_w < d || ld_w >= kMaxSize)) || ld_h < f || ld_h >= kMaxSize ||
+        !aligned_to({X, Wg, Wu, dH, dX, dWg, dWu}, 2) || !aligned_to({G, U, work}, 16))
+        return RSH_ERR_BAD_OPTION;
+    return launch_status(rsh::launch_gated_backward(X, type, ld_x, Wg, Wu, ld_w, G, U, dH, ld_h, act, dX, dWg, dWu, t, d, f, work, hip_stream));
+}
+
 int rsh_copy_probe(const void* src_dev, void* dst_dev, int64_t bytes, void* hip_stream) {
     if (!src_dev || !dst_dev) return RSH_ERR_NULL;
     if (bytes < 0 || (bytes & 15) || ((uintptr_t)src_dev & 15u) || ((uintptr_t)dst_dev & 15u)) return RSH_ERR_BAD_OPTION;

@@ -1,0 +1,432 @@
+// Products of the feed-forward block: activations with weights in 16 or 4 bits, the gated block, and its gradients.
+//
+// Every product is C[r][c] = sum over k of Q[r][k] P[c][k], rows r of the result (tokens, or hidden features where a weight's
+// gradient is formed) by columns c, in fp32 on the matrix units with one rounding at the end:
+//   product    Q = X [t][d]             P = W [n][d]                  both with k running along memory
+//   gated      Q = X [t][d]             P = Wg and Wu [f][d]          G and U side by side; H = act(G) U before the rounding
+//   dX         Q = dG, then dU [t][f]   P = Wg, then Wu [f][d]        k runs along memory in Q, across it in P; two sums in one
+//   dWg, dWu   Q = dG / dU [t][f]       P = X [t][d]                  k (tokens) runs across memory in both
+// P is the first operand of the matrix instruction, so a lane ends up with runs of four columns of one row.
+#include <algorithm>
+
+#include "../../include/rsh_spmm.h"
+#include "mx4.hpp"
+
+namespace rsh {
+
+namespace {
+
+// How an operand lies in memory.
+enum Form {
+    kAlong,     // k along memory: row i at i * ld
+    kAcross,    // k across memory: k at k * ld
+    kCodes,     // blocks of codes and their scales, k along memory; turned into 16 bits on the way into LDS
+    kFours      // the same, multiplied as it is
+};
+
+struct Operand {
+    const void* data[2];           // two matrices of equal shape (gate and up), or one
+    const uint8_t* scales[2];
+    int64_t ld;                    // elements (kAlong, kAcross) or blocks (kCodes, kFours) from row to row
+};
+
+enum Act { kSilu = RSH_ACT_SILU, kGelu = RSH_ACT_GELU, kRelu = RSH_ACT_RELU };
+
+struct Result {
+    uint16_t* out[2];              // C, or H; [1]: the second of two results that share P (dWu)
+    uint16_t* gate;                // G and U where they are wanted
+    uint16_t* up;
+    int64_t ld, ld_gate;
+    int act;
+};
+
+struct Shape {
+    int64_t rows, cols, k;         // of one product
+    int tiles_r, tiles_c;
+};
+
+constexpr int kRowBytes = 128;     // of k in one step: 64 elements of 16 bits, 256 of 4
+
+// act(g) and its derivative.  silu: g s with s = 1 / (1 + exp(-g)); gelu: g times the normal distribution function.
+__device__ __forceinline__ float act_of(int act, float g) {
+    if (act == kSilu) return g / (1.f + __expf(-g));
+    if (act == kGelu) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+    return g * (g > 0.f ? 1.f : 0.f);
+}
+__device__ __forceinline__ float act_of(int act, float g, float* slope) {
+    if (act == kSilu) {
+        const float s = 1.f / (1.f + __expf(-g));
+        *slope = s * (1.f + g * (1.f - s));
+        return g * s;
+    }
+    if (act == kGelu) {
+        const float c = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        *slope = c + g * __expf(-0.5f * g * g) * 0.3989422804014327f;
+        return g * c;
+    }
+    *slope = g > 0.f ? 1.f : 0.f;
+    return g * *slope;
+}
+
+// Value of the other lane of a pair.
+__device__ __forceinline__ int swap_pair(int v) { return __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, false); }
+
+__device__ __forceinline__ half4_t read_transposed(const unsigned char* p) {
+    return __builtin_bit_cast(half4_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4_t __attribute__((address_space(3)))*)p));
+}
+
+// Byte of chunk c (16 bytes) of row r in LDS.  Rows of kRowBytes with k along them are read by 32 lanes at a time, a row each,
+// and rows with k across by 16 lanes, four rows each: the chunks of neighbouring rows are dealt to other banks.
+__device__ __forceinline__ int along_at(int r, int c) { return r * kRowBytes + ((c ^ (r & 7)) << 4); }
+template <int WIDTH>
+__device__ __forceinline__ int across_at(int k, int c) {
+    return k * (2 * WIDTH) + ((c ^ ((k & 7) << 1 & (WIDTH / 8 - 1))) << 4);
+}
+
+// Source of row `i` of a tile of P: where two matrices run side by side, 32 columns of one, then 32 of the other.
+template <bool PAIR>
+__device__ __forceinline__ int64_t column_of(int64_t tile, int i, int width, int* which) {
+    *which = PAIR ? i >> 5 & 1 : 0;
+    return PAIR ? tile * (width / 2) + (i >> 6) * 32 + (i & 31) : tile * width + i;
+}
+
+// Pieces of one operand's tile on their way through registers into LDS: N = chunks of 16 bytes per thread.
+template <Form FORM, int WIDTH, int THREADS, bool PAIR>
+struct Stage {
+    static constexpr int kChunks = FORM == kCodes ? WIDTH * 2 / THREADS : WIDTH * 8 / THREADS;
+    static_assert(kChunks > 0);
+    uint4_t v[kChunks];
+    uint32_t s[FORM == kCodes ? kChunks : 1];
+
+    __device__ __forceinline__ void load(const Operand& o, int seg, int64_t tile, int64_t extent, int64_t k0, int64_t k) {
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int i = threadIdx.x + THREADS * j;
+            if constexpr (FORM == kAlong) {
+                int which;
+                const int64_t row = column_of<PAIR>(tile, i >> 3, WIDTH, &which), at = k0 + 8 * (i & 7);
+                v[j] = load8((const uint16_t*)o.data[PAIR ? which : seg] + row * o.ld + at, row < extent ? k - at : 0);
+            } else if constexpr (FORM == kAcross) {
+                const int64_t kk = k0 + i / (WIDTH / 8), col = tile * WIDTH + 8 * (i % (WIDTH / 8));
+                v[j] = load8((const uint16_t*)o.data[seg] + kk * o.ld + col, kk < k ? extent - col : 0);
+            } else if constexpr (FORM == kCodes) {
+                int which;
+                const int64_t row = column_of<PAIR>(tile, i >> 1, WIDTH, &which), b = k0 / kBlock + (i & 1);
+                const bool in = row < extent && b < o.ld;
+                v[j] = in ? *reinterpret_cast<const uint4_t*>((const uint8_t*)o.data[which] + (row * o.ld + b) * kBlockBytes) : (uint4_t){0, 0, 0, 0};
+                s[j] = in ? o.scales[which][row * o.ld + b] : 0u;
+            } else {
+                const int64_t row = tile * WIDTH + (i >> 3), b = k0 / kBlock + (i & 7);
+                v[j] = row < extent && b < o.ld ? *reinterpret_cast<const uint4_t*>((const uint8_t*)o.data[0] + (row * o.ld + b) * kBlockBytes)
+                                                : (uint4_t){0, 0, 0, 0};
+            }
+        }
+    }
+    // shift: added to the scale bytes of a thread's rows (kCodes; rows stay a thread's own through all steps)
+    template <class T>
+    __device__ __forceinline__ void store(unsigned char* lds, const int* shift) const {
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int i = threadIdx.x + THREADS * j;
+            if constexpr (FORM == kAcross) {
+                *reinterpret_cast<uint4_t*>(lds + across_at<WIDTH>(i / (WIDTH / 8), i % (WIDTH / 8))) = v[j];
+            } else if constexpr (FORM == kCodes) {
+                const float scale = scale_of(s[j] == 255u ? 255u : (uint32_t)max(0, (int)s[j] + shift[j]));
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    *reinterpret_cast<uint4_t*>(lds + along_at(i >> 1, 4 * (i & 1) + c)) = from_codes8<T>(v[j][c], scale);
+            } else {
+                *reinterpret_cast<uint4_t*>(lds + along_at(i >> 3, i & 7)) = v[j];
+            }
+        }
+    }
+};
+
+// The 16 bytes of an operand that a lane feeds to the matrix unit: row `base` + lane % 32 of the tile, step s.
+template <Form FORM, int WIDTH>
+__device__ __forceinline__ uint4_t fragment(const unsigned char* lds, int base, int s, int lane) {
+    if constexpr (FORM == kAcross) {
+        const int k = 16 * s + 8 * (lane >> 5) + (lane >> 2 & 3), col = base + (lane & 16) + 4 * (lane & 3);
+        const half4_t a = read_transposed(lds + across_at<WIDTH>(k, col >> 3) + 2 * (col & 7));
+        const half4_t b = read_transposed(lds + across_at<WIDTH>(k + 4, col >> 3) + 2 * (col & 7));
+        return __builtin_bit_cast(uint4_t, (half8_t){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+    } else {
+        return *reinterpret_cast<const uint4_t*>(lds + along_at(base + (lane & 31), 2 * s + (lane >> 5)));
+    }
+}
+
+constexpr int kSpan = 10;   // binary16: the largest scale of a row of codes is brought to 2^kSpan
+
+}  // namespace
+
+// T: F16 or BF16 (results, and operands unless they are kFours).  WP x WQ waves, each TP x TQ tiles of 32 x 32.
+template <class T, Form FP, Form FQ, bool GATED, int SEGS, int WP, int WQ, int TP, int TQ>
+__global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Operand Q, Result res, Shape sh) {
+    constexpr int kThreads = 64 * WP * WQ, kWidthP = 32 * WP * TP, kWidthQ = 32 * WQ * TQ;
+    constexpr int kBytesP = kWidthP * kRowBytes, kBytesQ = kWidthQ * kRowBytes;
+    constexpr int kStep = FP == kFours ? 256 : 64;       // k of a step
+    constexpr bool kShifted = FP == kCodes && std::is_same<T, F16>::value;
+    constexpr bool kScaled = FP == kFours;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[2][kBytesP + kBytesQ];
+    __shared__ uint2_t scales[kScaled ? 2 : 1][kScaled ? kWidthP + kWidthQ : 1];
+    __shared__ int tops[kShifted ? kWidthP : 1];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % WP, wq = wave / WP;
+    // Tiles are dealt to the XCDs in runs of their order, which goes through eight tiles of rows before the next column, so that
+    // the workgroups of an XCD share rows of both operands in its L2.
+    const int64_t tiles = (int64_t)sh.tiles_r * sh.tiles_c, chunk = (tiles + 7) / 8;
+    const int64_t tile = (int64_t)(blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= chunk || tile >= tiles) return;
+    const int64_t strip = tile / (8 * sh.tiles_c), in_strip = tile % (8 * sh.tiles_c), tall = min((int64_t)8, sh.tiles_r - 8 * strip);
+    const int64_t tr = 8 * strip + in_strip % tall, tc = in_strip / tall;
+    const int second = SEGS == 1 ? blockIdx.y : 0;       // which of two results that share P
+
+    Stage<FP, kWidthP, kThreads, GATED> sp;
+    Stage<FQ, kWidthQ, kThreads, false> sq;
+    int shift[Stage<FP, kWidthP, kThreads, GATED>::kChunks] = {};
+    if constexpr (kShifted) {
+        // the largest scale of each row; two threads share a row
+#pragma unroll
+        for (int j = 0; j < Stage<FP, kWidthP, kThreads, GATED>::kChunks; ++j) {
+            const int i = threadIdx.x + kThreads * j;
+            int which;
+            const int64_t row = column_of<GATED>(tc, i >> 1, kWidthP, &which);
+            int top = 0;
+            if (row < sh.cols)
+                for (int64_t b = i & 1; b < P.ld; b += 2) {
+                    const int s = P.scales[which][row * P.ld + b];
+                    top = max(top, s == 255 ? 0 : s);
+                }
+            top = max(top, swap_pair(top));
+            shift[j] = 127 + kSpan - top;
+            if ((i & 1) == 0) tops[i >> 1] = top;
+        }
+    }
+
+    float16_t acc[TP][TQ];
+#pragma unroll
+    for (int a = 0; a < TP; ++a)
+#pragma unroll
+        for (int b = 0; b < TQ; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+
+    const int64_t steps = (sh.k + kStep - 1) / kStep;
+    uint2_t sc = {0, 0};
+    auto load = [&](int64_t step) {
+        const int seg = SEGS == 2 ? (int)(step / steps) : 0;
+        const int64_t k0 = (SEGS == 2 ? step - seg * steps : step) * kStep;
+        sp.load(P, seg, tc, sh.cols, k0, sh.k);
+        sq.load(Q, SEGS == 2 ? seg : second, tr, sh.rows, k0, sh.k);
+        if constexpr (kScaled) {
+            // the eight scales of one row of either operand
+            const int i = threadIdx.x;
+            if (i < kWidthP + kWidthQ) {
+                const Operand& o = i < kWidthP ? P : Q;
+                const int64_t row = i < kWidthP ? tc * kWidthP + i : tr * kWidthQ + (i - kWidthP), b = k0 / kBlock;
+                sc = (uint2_t){0, 0};
+                if (row < (i < kWidthP ? sh.cols : sh.rows)) {
+                    const uint8_t* const at = o.scales[0] + row * o.ld + b;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (b + j < o.ld) sc[j / 4] |= (uint32_t)at[j] << (8 * (j & 3));
+                }
+            }
+        }
+    };
+    auto store = [&](int buf) {
+        sp.template store<T>(lds[buf], shift);
+        sq.template store<T>(lds[buf] + kBytesP, nullptr);
+        if constexpr (kScaled)
+            if (threadIdx.x < kWidthP + kWidthQ) scales[buf][threadIdx.x] = sc;
+    };
+
+    load(0);
+    store(0);
+    __syncthreads();
+    for (int64_t step = 0; step < SEGS * steps; ++step) {
+        const int buf = (int)(step & 1);
+        if (step + 1 < SEGS * steps) load(step + 1);
+        const unsigned char *lp = lds[buf], *lq = lds[buf] + kBytesP;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            uint4_t a[TP], b[TQ];
+#pragma unroll
+            for (int i = 0; i < TP; ++i) a[i] = fragment<FP == kAcross ? kAcross : kAlong, kWidthP>(lp, 32 * (wp * TP + i), s, lane);
+#pragma unroll
+            for (int i = 0; i < TQ; ++i) b[i] = fragment<FQ == kAcross ? kAcross : kAlong, kWidthQ>(lq, 32 * (wq * TQ + i), s, lane);
+            if constexpr (kScaled) {
+                int ea[TP], eb[TQ];
+#pragma unroll
+                for (int i = 0; i < TP; ++i) ea[i] = reinterpret_cast<const uint8_t*>(&scales[buf][32 * (wp * TP + i) + (lane & 31)])[2 * s + (lane >> 5)];
+#pragma unroll
+                for (int i = 0; i < TQ; ++i)
+                    eb[i] = reinterpret_cast<const uint8_t*>(&scales[buf][kWidthP + 32 * (wq * TQ + i) + (lane & 31)])[2 * s + (lane >> 5)];
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int j = 0; j < TQ; ++j) {
+                        const int8v_t fa = {(int)a[i][0], (int)a[i][1], (int)a[i][2], (int)a[i][3], 0, 0, 0, 0};
+                        const int8v_t fb = {(int)b[j][0], (int)b[j][1], (int)b[j][2], (int)b[j][3], 0, 0, 0, 0};
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 0, ea[i], 0, eb[j]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int j = 0; j < TQ; ++j) acc[i][j] = T::mfma32(a[i], b[j], acc[i][j]);
+            }
+        }
+        if (step + 1 < SEGS * steps) store(buf ^ 1);
+        __syncthreads();
+    }
+
+    // A lane has columns 8 g + 4 (lane / 32) .. + 3, g = 0 .. 3, of row lane % 32 of every tile of 32 x 32.
+    uint16_t* const out = res.out[second];
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+        const int64_t row = tr * kWidthQ + 32 * (wq * TQ + j) + (lane & 31);
+        if (row >= sh.rows) continue;
+#pragma unroll
+        for (int i = 0; i < TP; i += GATED ? 2 : 1) {
+            const int at = 32 * (wp * TP + i);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int in_tile = 8 * g + 4 * (lane >> 5);
+                const int64_t col = GATED ? tc * (kWidthP / 2) + at / 2 + in_tile : tc * kWidthP + at + in_tile;
+                const int64_t left = sh.cols - col;
+                if (left <= 0) continue;
+                float x[4], y[4];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    x[v] = acc[i][j][4 * g + v];
+                    if constexpr (kShifted) x[v] = ldexpf(x[v], tops[at + in_tile + v] - (127 + kSpan));
+                }
+                if constexpr (GATED) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        y[v] = acc[i + 1][j][4 * g + v];
+                        if constexpr (kShifted) y[v] = ldexpf(y[v], tops[at + 32 + in_tile + v] - (127 + kSpan));
+                    }
+                    if (res.gate) {
+                        store4(res.gate + row * res.ld_gate + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
+                        store4(res.up + row * res.ld_gate + col, (uint2_t){T::pair(y[0], y[1]), T::pair(y[2], y[3])}, left);
+                    }
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) x[v] = act_of(res.act, x[v]) * y[v];
+                }
+                store4(out + row * res.ld + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
+            }
+        }
+    }
+}
+
+// dU = dH act(G) and dG = dH U act'(G), eight elements a thread, rounded to the 16 bits that the matrix units take.
+template <class T>
+__global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* __restrict__ dH, const uint16_t* __restrict__ G,
+                                                                const uint16_t* __restrict__ U, uint16_t* __restrict__ dG,
+                                                                uint16_t* __restrict__ dU, int64_t t, int64_t f, int64_t ld, int64_t ld_gate, int act) {
+    const int64_t pieces = ld_gate / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= t * pieces) return;
+    const int64_t row = i / pieces, col = 8 * (i - row * pieces), at = row * ld_gate + col;
+    const uint4_t h = load8(dH + row * ld + col, f - col);
+    const uint4_t g = *reinterpret_cast<const uint4_t*>(G + at), u = *reinterpret_cast<const uint4_t*>(U + at);
+    uint4_t a, b;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        float dg[2], du[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float hv = T::widen((uint16_t)(h[w] >> 16 * e)), gv = T::widen((uint16_t)(g[w] >> 16 * e)), uv = T::widen((uint16_t)(u[w] >> 16 * e));
+            float slope;
+            du[e] = hv * act_of(act, gv, &slope);
+            dg[e] = hv * uv * slope;
+            if (col + 2 * w + e >= f) du[e] = dg[e] = 0.f;
+        }
+        a[w] = T::pair(dg[0], dg[1]);
+        b[w] = T::pair(du[0], du[1]);
+    }
+    *reinterpret_cast<uint4_t*>(dG + at) = a;
+    *reinterpret_cast<uint4_t*>(dU + at) = b;
+}
+
+// ---------------------------------------------------------------------------
+// launchers
+// ---------------------------------------------------------------------------
+namespace {
+
+int launched() { return hipGetLastError() == hipSuccess ? RSH_OK : RSH_ERR_HIP; }
+
+template <class T, Form FP, Form FQ, bool GATED, int SEGS>
+void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, int results, hipStream_t st) {
+    constexpr int WP = 4, WQ = 2, TP = 2, TQ = 4;
+    const int64_t wide = 32 * WP * TP / (GATED ? 2 : 1), tall = 32 * WQ * TQ;
+    Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
+    const int64_t tiles = (int64_t)sh.tiles_r * sh.tiles_c;
+    hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, WP, WQ, TP, TQ>), dim3((unsigned)((tiles + 7) / 8 * 8), results),
+                       dim3(64 * WP * WQ), 0, st, P, Q, res, sh);
+}
+
+template <class F>
+void by_half(int type, F f) {
+    if (type == RSH_F16) f(F16());
+    else f(BF16());
+}
+
+}  // namespace
+
+int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int y_type,
+                       int64_t t, int64_t n, int64_t k, void* stream) {
+    const int64_t blocks = (k + kBlock - 1) / kBlock;
+    const Operand p = {{W, nullptr}, {(const uint8_t*)w_scales, nullptr}, blocks};
+    const Operand q = {{X, nullptr}, {(const uint8_t*)x_scales, nullptr}, x_type == RSH_MX4 ? blocks : ld_x};
+    const Result res = {{(uint16_t*)Y, nullptr}, nullptr, nullptr, n, 0, 0};
+    by_half(y_type, [&](auto half) {
+        using T = decltype(half);
+        if (x_type == RSH_MX4) product<T, kFours, kFours, false, 1>(p, q, res, t, n, k, 1, (hipStream_t)stream);
+        else product<T, kCodes, kAlong, false, 1>(p, q, res, t, n, k, 1, (hipStream_t)stream);
+    });
+    return launched();
+}
+
+int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
+                         const void* u_scales, int act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* stream) {
+    const int64_t blocks = (d + kBlock - 1) / kBlock;
+    const Operand p = {{Wg, Wu}, {(const uint8_t*)g_scales, (const uint8_t*)u_scales}, g_scales ? blocks : ld_w};
+    const Operand q = {{X, nullptr}, {nullptr, nullptr}, ld_x};
+    const Result res = {{(uint16_t*)H, nullptr}, (uint16_t*)G, (uint16_t*)U, f, (f + 7) / 8 * 8, act};
+    by_half(type, [&](auto half) {
+        using T = decltype(half);
+        if (g_scales) product<T, kCodes, kAlong, true, 1>(p, q, res, t, f, d, 1, (hipStream_t)stream);
+        else product<T, kAlong, kAlong, true, 1>(p, q, res, t, f, d, 1, (hipStream_t)stream);
+    });
+    return launched();
+}
+
+int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* G, const void* U,
+                          const void* dH, int64_t ld_h, int act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
+                          void* stream) {
+    const hipStream_t st = (hipStream_t)stream;
+    const int64_t ld_gate = (f + 7) / 8 * 8, pieces = t * (ld_gate / 8);
+    uint16_t* const dG = (uint16_t*)work;
+    uint16_t* const dU = dG + t * ld_gate;
+    const Operand gates = {{dG, dU}, {nullptr, nullptr}, ld_gate};
+    by_half(type, [&](auto half) {
+        using T = decltype(half);
+        hipLaunchKernelGGL(rsh_gate_backward_kernel<T>, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, st, (const uint16_t*)dH, (const uint16_t*)G,
+                           (const uint16_t*)U, dG, dU, t, f, ld_h, ld_gate, act);
+        if (dX) {
+            const Operand w = {{Wg, Wu}, {nullptr, nullptr}, ld_w};
+            const Result res = {{(uint16_t*)dX, nullptr}, nullptr, nullptr, d, 0, 0};
+            product<T, kAcross, kAlong, false, 2>(w, gates, res, t, d, f, 1, st);
+        }
+        if (dWg || dWu) {
+            const Operand x = {{X, nullptr}, {nullptr, nullptr}, ld_x}, only_u = {{dU, nullptr}, {nullptr, nullptr}, ld_gate};
+            const Result res = {{(uint16_t*)(dWg ? dWg : dWu), (uint16_t*)dWu}, nullptr, nullptr, d, 0, 0};
+            product<T, kAcross, kAcross, false, 1>(x, dWg ? gates : only_u, res, f, d, t, dWg && dWu ? 2 : 1, st);
+        }
+    });
+    return launched();
+}
+
+}  // namespace rsh

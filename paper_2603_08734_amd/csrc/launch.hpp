@@ -85,6 +85,20 @@ int launch_dense_backward(const void* H, const void* W, const void* dP, void* dH
                           void* stream);
 int launch_act_backward(const void* dY, const void* Y, void* dZ, float* dbias, float* work, int64_t n, int d, void* stream);
 
+// Matrices in 4 bits (mx4.hip).  type: RSH_F32, RSH_F16 or RSH_BF16; ld: elements from row to row.
+int launch_mx4_quantize(const void* X, int type, int64_t rows, int64_t k, int64_t ld, void* codes, void* scales, void* stream);
+int launch_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t k, void* Y, int type, int64_t ld, void* stream);
+
+// Products of the feed-forward block (ffn.hip).  x_type, y_type, type: RSH_F16 or RSH_BF16, x_type also RSH_MX4; scales null for
+// operands of 16 bits.  G, U, dG and dU have rows of f elements rounded up to a multiple of eight.
+int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int y_type,
+                       int64_t t, int64_t n, int64_t k, void* stream);
+int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
+                         const void* u_scales, int act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* stream);
+int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* G, const void* U,
+                          const void* dH, int64_t ld_h, int act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
+                          void* stream);
+
 // Plain device-to-device copy of `bytes` (multiple of 16) used to calibrate traffic counters.
 int launch_copy_probe(const void* src_dev, void* dst_dev, size_t bytes, void* stream);
 
