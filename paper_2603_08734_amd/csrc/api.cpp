@@ -644,7 +644,7 @@ constexpr int64_t kMaxSize = (int64_t)1 << 31;
 int sizes_ok(int64_t a, int64_t b, int64_t c) {
     if (a <= 0 || b <= 0 || c <= 0 || a >= kMaxSize || b >= kMaxSize || c >= kMaxSize) return RSH_ERR_BAD_OPTION;
     for (const auto& [x, y] : {std::pair(a, b), std::pair(a, c), std::pair(b, c)})
-        if (((x + 63) / 64) * ((y + 63) / 64) > kMaxSize / 64) return RSH_ERR_TOO_LARGE;
+        if (((x + 63) / 64) * ((y + 63) / 64) > kMaxSize / 256) return RSH_ERR_TOO_LARGE;
     return RSH_OK;
 }
 bool half_type(int32_t type) { return type == RSH_F16 || type == RSH_BF16; }
@@ -670,8 +670,9 @@ int rsh_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int6
 int rsh_mx4_product_work(int32_t x_type, int64_t t, int64_t n, int64_t k, int64_t* bytes) {
     if (!bytes) return RSH_ERR_NULL;
     if (x_type != RSH_MX4 && !half_type(x_type)) return RSH_ERR_BAD_OPTION;
-    *bytes = 0;
-    return sizes_ok(t, n, k);
+    const int rc = sizes_ok(t, n, k);
+    *bytes = rc ? 0 : rsh::mx4_product_work(x_type, t, n, k);
+    return rc;
 }
 
 int rsh_mx4_product(const void* X, const void* x_scales, int32_t x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int32_t y_type,
@@ -683,14 +684,15 @@ int rsh_mx4_product(const void* X, const void* x_scales, int32_t x_type, int64_t
     if (!half_type(y_type) || (!four && (y_type != x_type || x_scales || ld_x < k || ld_x >= kMaxSize)) || !aligned_to({W}, 16) || !aligned_to({Y}, 2) ||
         !aligned_to({X}, four ? 16 : 2) || !aligned_to({work}, 16))
         return RSH_ERR_BAD_OPTION;
-    return launch_status(rsh::launch_mx4_product(X, x_scales, x_type, ld_x, W, w_scales, Y, y_type, t, n, k, hip_stream));
+    return launch_status(rsh::launch_mx4_product(X, x_scales, x_type, ld_x, W, w_scales, Y, y_type, t, n, k, work, hip_stream));
 }
 
 int rsh_gated_forward_work(int32_t w_type, int64_t t, int64_t d, int64_t f, int64_t* bytes) {
     if (!bytes) return RSH_ERR_NULL;
     if (w_type != RSH_MX4 && !half_type(w_type)) return RSH_ERR_BAD_OPTION;
-    *bytes = 0;
-    return sizes_ok(t, d, f);
+    const int rc = sizes_ok(t, d, f);
+    *bytes = rc ? 0 : rsh::gated_forward_work(t, d, f);
+    return rc;
 }
 
 int rsh_gated_forward(const void* X, int32_t type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
@@ -702,13 +704,13 @@ int rsh_gated_forward(const void* X, int32_t type, int64_t ld_x, const void* Wg,
     if (ld_x < d || ld_x >= kMaxSize || (!g_scales && (ld_w < d || ld_w >= kMaxSize)) || !aligned_to({X, H}, 2) ||
         !aligned_to({Wg, Wu}, g_scales ? 16 : 2) || !aligned_to({G, U, work}, 16))
         return RSH_ERR_BAD_OPTION;
-    return launch_status(rsh::launch_gated_forward(X, type, ld_x, Wg, Wu, ld_w, g_scales, u_scales, act, H, G, U, t, d, f, hip_stream));
+    return launch_status(rsh::launch_gated_forward(X, type, ld_x, Wg, Wu, ld_w, g_scales, u_scales, act, H, G, U, t, d, f, work, hip_stream));
 }
 
 int rsh_gated_backward_work(int64_t t, int64_t d, int64_t f, int64_t* bytes) {
     if (!bytes) return RSH_ERR_NULL;
     const int rc = sizes_ok(t, d, f);
-    *bytes = rc ? 0 : 4 * t * ((f + 7) / 8 * 8);
+    *bytes = rc ? 0 : rsh::gated_backward_work(t, d, f);
     return rc;
 }
 

@@ -142,6 +142,70 @@ struct Stage {
     }
 };
 
+// 16 bytes a lane from byte `at` of a buffer of `size` bytes to the lane's place behind `lds`; zero past the buffer's end.  (The
+// host's pass over this file does not know the type of a buffer's description.)
+__device__ __forceinline__ void load_to_lds([[maybe_unused]] const uint8_t* buffer, [[maybe_unused]] uint32_t size, [[maybe_unused]] uint32_t at,
+                                            [[maybe_unused]] unsigned char* lds) {
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)buffer, 0, size, 0x00020000),
+                                             (__attribute__((address_space(3))) void*)lds, 16, at, 0, 0, 0);
+#endif
+}
+
+// The same straight into LDS: 16 bytes a lane, 1 KB a wave and turn, in the order of the lanes, so the chunks are dealt to their
+// banks by the lane's choice of source.  Reads past the operand's end come back as zero (the buffer's range check); rows must be
+// whole chunks at 16-byte boundaries.
+template <Form FORM, int WIDTH, int THREADS, bool PAIR>
+struct Direct {
+    static constexpr int kChunks = WIDTH * 8 / THREADS;
+    static constexpr uint32_t kNowhere = 0x80000000u;      // past every buffer
+    uint32_t at[kChunks];          // byte of the lane's chunks from the tile's first, at k = 0
+    int64_t first, span, stride;   // byte of the tile's first row (kAcross: column), bytes from there to the operand's end, row to row
+    int chunk;                     // chunk of its row that a lane loads (kAlong, kFours); the same in every turn
+
+    __device__ __forceinline__ void start(const Operand& o, int64_t tile, int64_t extent, int64_t k) {
+        const int64_t width = PAIR ? WIDTH / 2 : WIDTH;
+        stride = FORM == kFours ? o.ld * kBlockBytes : o.ld * 2;
+        if constexpr (FORM == kAcross) {
+            chunk = 0;
+            first = tile * width * 2;
+            span = (k - 1) * stride + (extent - tile * width) * 2;
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+                const int i = threadIdx.x + THREADS * j, kk = i / (WIDTH / 8), c = i % (WIDTH / 8) ^ ((kk & 7) << 1 & (WIDTH / 8 - 1));
+                at[j] = tile * width + 8 * c < extent ? (uint32_t)(kk * stride + 16 * c) : kNowhere;
+            }
+        } else {
+            chunk = (threadIdx.x & 7) ^ (threadIdx.x >> 3 & 7);
+            first = tile * width * stride;
+            span = (extent - tile * width - 1) * stride + (FORM == kFours ? stride : 2 * k);
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+                const int r = (threadIdx.x + THREADS * j) >> 3;
+                at[j] = (uint32_t)((PAIR ? (r >> 6) * 32 + (r & 31) : r) * stride + 16 * chunk);
+            }
+        }
+    }
+    __device__ __forceinline__ void issue(const Operand& o, int seg, int64_t k0, int64_t k, unsigned char* lds) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t ahead = FORM == kAcross ? k0 * stride : FORM == kFours ? k0 / 2 : k0 * 2;
+        const uint32_t left = (uint32_t)min(span - ahead, (int64_t)0x7ffffff0);
+        const bool in = FORM == kAcross || k0 + (FORM == kFours ? 32 : 8) * chunk < k;
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int which = PAIR ? (wave + THREADS / 64 * j) >> 2 & 1 : seg;
+            load_to_lds((const uint8_t*)o.data[which] + first + ahead, left, in ? at[j] : kNowhere, lds + (wave * 64 + THREADS * j) * 16);
+        }
+    }
+};
+
+// All of a wave's loads into LDS have arrived and its reads of LDS are done; then all waves'.
+__device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // The 16 bytes of an operand that a lane feeds to the matrix unit: row `base` + lane % 32 of the tile, step s.
 template <Form FORM, int WIDTH>
 __device__ __forceinline__ uint4_t fragment(const unsigned char* lds, int base, int s, int lane) {
@@ -155,18 +219,45 @@ __device__ __forceinline__ uint4_t fragment(const unsigned char* lds, int base, 
     }
 }
 
+// What becomes of the sums of four columns of a row.
+template <class T, bool GATED>
+__device__ __forceinline__ void finish(const Result& res, uint16_t* out, int64_t row, int64_t col, int64_t left, float4_t x, float4_t y) {
+    if constexpr (GATED) {
+        if (res.gate) {
+            store4(res.gate + row * res.ld_gate + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
+            store4(res.up + row * res.ld_gate + col, (uint2_t){T::pair(y[0], y[1]), T::pair(y[2], y[3])}, left);
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[v] = act_of(res.act, x[v]) * y[v];
+    }
+    store4(out + row * res.ld + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
+}
+
 constexpr int kSpan = 10;   // binary16: the largest scale of a row of codes is brought to 2^kSpan
 
 }  // namespace
 
-// T: F16 or BF16 (results, and operands unless they are kFours).  WP x WQ waves, each TP x TQ tiles of 32 x 32.
-template <class T, Form FP, Form FQ, bool GATED, int SEGS, int WP, int WQ, int TP, int TQ>
-__global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Operand Q, Result res, Shape sh) {
+// A part of the steps of k, whose sums go to `partial` as fp32 [part][result][row][columns rounded up to 4, gate before up], where
+// there is more than one.
+struct Split {
+    int parts;
+    int64_t steps;         // of one part
+    float* partial;
+};
+
+// T: F16 or BF16 (results, and operands unless they are kFours).  WP x WQ waves, each TP x TQ tiles of 32 x 32.  DIRECT: operands
+// that need no conversion go straight into LDS.
+template <class T, Form FP, Form FQ, bool GATED, int SEGS, int WP, int WQ, int TP, int TQ, bool DIRECT>
+__global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Operand Q, Result res, Shape sh, Split split) {
     constexpr int kThreads = 64 * WP * WQ, kWidthP = 32 * WP * TP, kWidthQ = 32 * WQ * TQ;
     constexpr int kBytesP = kWidthP * kRowBytes, kBytesQ = kWidthQ * kRowBytes;
     constexpr int kStep = FP == kFours ? 256 : 64;       // k of a step
     constexpr bool kShifted = FP == kCodes && std::is_same<T, F16>::value;
     constexpr bool kScaled = FP == kFours;
+    constexpr bool kDirectP = DIRECT && FP != kCodes;
+    constexpr int kTurns = kScaled ? (kWidthP + kWidthQ + kThreads - 1) / kThreads : 1;
+    using StageP = Stage<FP, kWidthP, kThreads, GATED>;
+    using StageQ = Stage<FQ, kWidthQ, kThreads, false>;
     __shared__ __attribute__((aligned(16))) unsigned char lds[2][kBytesP + kBytesQ];
     __shared__ uint2_t scales[kScaled ? 2 : 1][kScaled ? kWidthP + kWidthQ : 1];
     __shared__ int tops[kShifted ? kWidthP : 1];
@@ -179,15 +270,17 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     if ((blockIdx.x >> 3) >= chunk || tile >= tiles) return;
     const int64_t strip = tile / (8 * sh.tiles_c), in_strip = tile % (8 * sh.tiles_c), tall = min((int64_t)8, sh.tiles_r - 8 * strip);
     const int64_t tr = 8 * strip + in_strip % tall, tc = in_strip / tall;
-    const int second = SEGS == 1 ? blockIdx.y : 0;       // which of two results that share P
+    const int second = SEGS == 1 ? blockIdx.z : 0;       // which of two results that share P
 
-    Stage<FP, kWidthP, kThreads, GATED> sp;
-    Stage<FQ, kWidthQ, kThreads, false> sq;
-    int shift[Stage<FP, kWidthP, kThreads, GATED>::kChunks] = {};
+    std::conditional_t<kDirectP, Direct<FP, kWidthP, kThreads, GATED>, StageP> sp;
+    std::conditional_t<DIRECT, Direct<FQ, kWidthQ, kThreads, false>, StageQ> sq;
+    if constexpr (kDirectP) sp.start(P, tc, sh.cols, sh.k);
+    if constexpr (DIRECT) sq.start(Q, tr, sh.rows, sh.k);
+    int shift[StageP::kChunks] = {};
     if constexpr (kShifted) {
         // the largest scale of each row; two threads share a row
 #pragma unroll
-        for (int j = 0; j < Stage<FP, kWidthP, kThreads, GATED>::kChunks; ++j) {
+        for (int j = 0; j < StageP::kChunks; ++j) {
             const int i = threadIdx.x + kThreads * j;
             int which;
             const int64_t row = column_of<GATED>(tc, i >> 1, kWidthP, &which);
@@ -212,42 +305,61 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
 
     const int64_t steps = (sh.k + kStep - 1) / kStep;
-    uint2_t sc = {0, 0};
-    auto load = [&](int64_t step) {
-        const int seg = SEGS == 2 ? (int)(step / steps) : 0;
+    const int64_t begin = blockIdx.y * split.steps, end = min(SEGS * steps, begin + split.steps);
+    uint2_t sc[kTurns];
+    auto load = [&](int64_t step, int buf) {
+        const int seg = SEGS == 2 ? (int)(step >= steps) : 0;
         const int64_t k0 = (SEGS == 2 ? step - seg * steps : step) * kStep;
-        sp.load(P, seg, tc, sh.cols, k0, sh.k);
-        sq.load(Q, SEGS == 2 ? seg : second, tr, sh.rows, k0, sh.k);
+        if constexpr (kDirectP) sp.issue(P, seg, k0, sh.k, lds[buf]);
+        else sp.load(P, seg, tc, sh.cols, k0, sh.k);
+        if constexpr (DIRECT) sq.issue(Q, SEGS == 2 ? seg : second, k0, sh.k, lds[buf] + kBytesP);
+        else sq.load(Q, SEGS == 2 ? seg : second, tr, sh.rows, k0, sh.k);
         if constexpr (kScaled) {
             // the eight scales of one row of either operand
-            const int i = threadIdx.x;
-            if (i < kWidthP + kWidthQ) {
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u) {
+                const int i = threadIdx.x + kThreads * u;
+                sc[u] = (uint2_t){0, 0};
                 const Operand& o = i < kWidthP ? P : Q;
                 const int64_t row = i < kWidthP ? tc * kWidthP + i : tr * kWidthQ + (i - kWidthP), b = k0 / kBlock;
-                sc = (uint2_t){0, 0};
-                if (row < (i < kWidthP ? sh.cols : sh.rows)) {
-                    const uint8_t* const at = o.scales[0] + row * o.ld + b;
+                if (i >= kWidthP + kWidthQ || row >= (i < kWidthP ? sh.cols : sh.rows)) continue;
+                const uint8_t* const at = o.scales[0] + row * o.ld + b;
+                if (b + 8 <= o.ld) {
+                    __builtin_memcpy(&sc[u], at, 8);
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (b + j < o.ld) sc[j / 4] |= (uint32_t)at[j] << (8 * (j & 3));
+                    for (int j = 0; j < 7; ++j)
+                        if (b + j < o.ld) sc[u][j / 4] |= (uint32_t)at[j] << (8 * (j & 3));
                 }
             }
         }
     };
     auto store = [&](int buf) {
-        sp.template store<T>(lds[buf], shift);
-        sq.template store<T>(lds[buf] + kBytesP, nullptr);
-        if constexpr (kScaled)
-            if (threadIdx.x < kWidthP + kWidthQ) scales[buf][threadIdx.x] = sc;
+        if constexpr (!kDirectP) sp.template store<T>(lds[buf], shift);
+        if constexpr (!DIRECT) sq.template store<T>(lds[buf] + kBytesP, nullptr);
+        if constexpr (kScaled) {
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u)
+                if (threadIdx.x + kThreads * u < kWidthP + kWidthQ) scales[buf][threadIdx.x + kThreads * u] = sc[u];
+        }
     };
 
-    load(0);
-    store(0);
-    __syncthreads();
-    for (int64_t step = 0; step < SEGS * steps; ++step) {
-        const int buf = (int)(step & 1);
-        if (step + 1 < SEGS * steps) load(step + 1);
+    if (begin < end) {
+        load(begin, 0);
+        store(0);
+    }
+    meet();
+    for (int64_t step = begin; step < end; ++step) {
+        const int buf = (int)((step - begin) & 1);
+        if (step + 1 < end) load(step + 1, buf ^ 1);
         const unsigned char *lp = lds[buf], *lq = lds[buf] + kBytesP;
+        uint2_t ea[TP], eb[TQ];     // scales of the lane's rows: lanes from 32 on have every second block
+        if constexpr (kScaled) {
+#pragma unroll
+            for (int i = 0; i < TP; ++i) ea[i] = scales[buf][32 * (wp * TP + i) + (lane & 31)] >> (8 * (lane >> 5));
+#pragma unroll
+            for (int i = 0; i < TQ; ++i) eb[i] = scales[buf][kWidthP + 32 * (wq * TQ + i) + (lane & 31)] >> (8 * (lane >> 5));
+        }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             uint4_t a[TP], b[TQ];
@@ -256,20 +368,17 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
 #pragma unroll
             for (int i = 0; i < TQ; ++i) b[i] = fragment<FQ == kAcross ? kAcross : kAlong, kWidthQ>(lq, 32 * (wq * TQ + i), s, lane);
             if constexpr (kScaled) {
-                int ea[TP], eb[TQ];
-#pragma unroll
-                for (int i = 0; i < TP; ++i) ea[i] = reinterpret_cast<const uint8_t*>(&scales[buf][32 * (wp * TP + i) + (lane & 31)])[2 * s + (lane >> 5)];
-#pragma unroll
-                for (int i = 0; i < TQ; ++i)
-                    eb[i] = reinterpret_cast<const uint8_t*>(&scales[buf][kWidthP + 32 * (wq * TQ + i) + (lane & 31)])[2 * s + (lane >> 5)];
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
 #pragma unroll
                     for (int j = 0; j < TQ; ++j) {
                         const int8v_t fa = {(int)a[i][0], (int)a[i][1], (int)a[i][2], (int)a[i][3], 0, 0, 0, 0};
                         const int8v_t fb = {(int)b[j][0], (int)b[j][1], (int)b[j][2], (int)b[j][3], 0, 0, 0, 0};
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 0, ea[i], 0, eb[j]);
+                        // step s takes bytes 0 and 2 of the first word, then of the second
+                        if (s & 1) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 2, ea[i][s / 2], 2, eb[j][s / 2]);
+                        else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 0, ea[i][s / 2], 0, eb[j][s / 2]);
                     }
+
             } else {
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
@@ -277,12 +386,14 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
                     for (int j = 0; j < TQ; ++j) acc[i][j] = T::mfma32(a[i], b[j], acc[i][j]);
             }
         }
-        if (step + 1 < SEGS * steps) store(buf ^ 1);
-        __syncthreads();
+        if (step + 1 < end) store(buf ^ 1);
+        meet();
     }
 
     // A lane has columns 8 g + 4 (lane / 32) .. + 3, g = 0 .. 3, of row lane % 32 of every tile of 32 x 32.
     uint16_t* const out = res.out[second];
+    const int64_t wide = (sh.cols + 3) / 4 * 4, ld_partial = GATED ? 2 * wide : wide;
+    float* const partial = split.parts > 1 ? split.partial + ((int64_t)blockIdx.y * gridDim.z + blockIdx.z) * sh.rows * ld_partial : nullptr;
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
         const int64_t row = tr * kWidthQ + 32 * (wq * TQ + j) + (lane & 31);
@@ -296,29 +407,41 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
                 const int64_t col = GATED ? tc * (kWidthP / 2) + at / 2 + in_tile : tc * kWidthP + at + in_tile;
                 const int64_t left = sh.cols - col;
                 if (left <= 0) continue;
-                float x[4], y[4];
+                float4_t x, y = {};
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     x[v] = acc[i][j][4 * g + v];
                     if constexpr (kShifted) x[v] = ldexpf(x[v], tops[at + in_tile + v] - (127 + kSpan));
-                }
-                if constexpr (GATED) {
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
+                    if constexpr (GATED) {
                         y[v] = acc[i + 1][j][4 * g + v];
                         if constexpr (kShifted) y[v] = ldexpf(y[v], tops[at + 32 + in_tile + v] - (127 + kSpan));
                     }
-                    if (res.gate) {
-                        store4(res.gate + row * res.ld_gate + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
-                        store4(res.up + row * res.ld_gate + col, (uint2_t){T::pair(y[0], y[1]), T::pair(y[2], y[3])}, left);
-                    }
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) x[v] = act_of(res.act, x[v]) * y[v];
                 }
-                store4(out + row * res.ld + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
+                if (partial) {
+                    *reinterpret_cast<float4_t*>(partial + row * ld_partial + col) = x;
+                    if constexpr (GATED) *reinterpret_cast<float4_t*>(partial + row * ld_partial + wide + col) = y;
+                } else {
+                    finish<T, GATED>(res, out, row, col, left, x, y);
+                }
             }
         }
     }
+}
+
+// Sums of the parts in their order, and what a tile does with finished sums.  A thread has four columns.
+template <class T, bool GATED>
+__global__ __launch_bounds__(256) void rsh_join_parts_kernel(const float* __restrict__ partial, Result res, int64_t rows, int64_t cols, int parts) {
+    const int64_t wide = (cols + 3) / 4 * 4, ld = GATED ? 2 * wide : wide, stride = gridDim.z * rows * ld;
+    const uint32_t across = (uint32_t)((cols + 1023) / 1024), row = blockIdx.x / across;
+    const int64_t col = 4 * ((int64_t)(blockIdx.x % across) * 256 + threadIdx.x);
+    if (col >= cols) return;
+    const float* at = partial + (blockIdx.z * rows + row) * ld + col;
+    float4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    for (int p = 0; p < parts; ++p, at += stride) {
+        x += *reinterpret_cast<const float4_t*>(at);
+        if constexpr (GATED) y += *reinterpret_cast<const float4_t*>(at + wide);
+    }
+    finish<T, GATED>(res, res.out[blockIdx.z], row, col, cols - col, x, y);
 }
 
 // dU = dH act(G) and dG = dH U act'(G), eight elements a thread, rounded to the 16 bits that the matrix units take.
@@ -357,14 +480,76 @@ namespace {
 
 int launched() { return hipGetLastError() == hipSuccess ? RSH_OK : RSH_ERR_HIP; }
 
+// Tiles and parts of k for a product.
+struct Choice {
+    int form;          // 0: 256 x 256 by 8 waves, 1: 128 x 128 by 4, 2: 128 columns x 64 rows by 4
+    int parts;
+};
+
+constexpr int64_t kTall[3] = {256, 128, 64}, kWide[3] = {256, 128, 128};
+
+// The form and the parts whose rounds of workgroups take the least time, in units of a step of a lone workgroup of 256 x 256:
+// `steps` of k in all, `pairs`: columns come in two matrices, `results` products side by side.
+Choice choose(int64_t rows, int64_t cols, int64_t steps, bool pairs, int results) {
+    constexpr double step[3] = {1.0, 0.33, 0.2};      // a step of one workgroup with its neighbours on the compute unit
+    constexpr int room[3] = {1, 2, 3};                 // workgroups of a compute unit
+    Choice best = {0, 1};
+    double least = 1e300;
+    for (int form = 0; form < 3; ++form) {
+        const int64_t wide = kWide[form] / (pairs ? 2 : 1);
+        const int64_t tiles = ((rows + kTall[form] - 1) / kTall[form]) * ((cols + wide - 1) / wide) * results;
+        for (int parts = 1; parts <= 16 && parts <= steps; parts = parts < 4 ? parts + 1 : parts * 2) {
+            const int64_t each = (steps + parts - 1) / parts, work = tiles * ((steps + each - 1) / each);
+            const int64_t slots = 256 * room[form];
+            double t = (double)((work + slots - 1) / slots) * ((double)each * step[form] * room[form] + 4.0);
+            // sums through memory: written and read once, and a launch
+            if (parts > 1) t += 4.0 + 8e-6 * (double)(parts * rows * cols * results * (pairs ? 2 : 1));
+            if (t < least) {
+                least = t;
+                best = {form, parts};
+            }
+        }
+    }
+    return best;
+}
+
+int64_t partial_bytes(const Choice& c, int64_t rows, int64_t cols, bool pairs, int results) {
+    return c.parts == 1 ? 0 : (int64_t)c.parts * results * rows * ((cols + 3) / 4 * 4) * (pairs ? 2 : 1) * (int64_t)sizeof(float);
+}
+
+// Whether an operand's chunks lie at 16-byte boundaries and a tile's within a buffer's reach.
+bool whole_chunks(const Operand& o, Form form, int64_t along) {
+    if (form == kCodes) return true;
+    if (form == kFours) return o.ld < (1 << 18);
+    return ((uintptr_t)o.data[0] | (uintptr_t)o.data[1]) % 16 == 0 && o.ld % 8 == 0 && along % 8 == 0 && o.ld < (1 << 21);
+}
+
+template <class T, Form FP, Form FQ, bool GATED, int SEGS, bool DIRECT>
+void launch_tiles(int form, dim3 grid, const Operand& P, const Operand& Q, const Result& res, const Shape& sh, const Split& split, hipStream_t st) {
+    if (form == 0)
+        hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, 4, 2, 2, 4, DIRECT>), grid, dim3(512), 0, st, P, Q, res, sh, split);
+    else if (form == 1)
+        hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, 2, 2, 2, 2, DIRECT>), grid, dim3(256), 0, st, P, Q, res, sh, split);
+    else
+        hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, 2, 2, 2, 1, DIRECT>), grid, dim3(256), 0, st, P, Q, res, sh, split);
+}
+
 template <class T, Form FP, Form FQ, bool GATED, int SEGS>
-void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, int results, hipStream_t st) {
-    constexpr int WP = 4, WQ = 2, TP = 2, TQ = 4;
-    const int64_t wide = 32 * WP * TP / (GATED ? 2 : 1), tall = 32 * WQ * TQ;
-    Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
+void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, int results, void* work, hipStream_t st) {
+    constexpr int64_t kStep = FP == kFours ? 256 : 64;
+    const int64_t steps = SEGS * ((k + kStep - 1) / kStep);
+    const Choice c = choose(rows, cols, steps, GATED, results);
+    const int64_t wide = kWide[c.form] / (GATED ? 2 : 1), tall = kTall[c.form], each = (steps + c.parts - 1) / c.parts;
+    const Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
+    const Split split = {c.parts, each, (float*)work};
     const int64_t tiles = (int64_t)sh.tiles_r * sh.tiles_c;
-    hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, WP, WQ, TP, TQ>), dim3((unsigned)((tiles + 7) / 8 * 8), results),
-                       dim3(64 * WP * WQ), 0, st, P, Q, res, sh);
+    const bool direct = whole_chunks(P, FP, FP == kAcross ? cols : k) && whole_chunks(Q, FQ, FQ == kAcross ? rows : k);
+    const dim3 grid((unsigned)((tiles + 7) / 8 * 8), c.parts, results);
+    if (direct) launch_tiles<T, FP, FQ, GATED, SEGS, true>(c.form, grid, P, Q, res, sh, split, st);
+    else launch_tiles<T, FP, FQ, GATED, SEGS, false>(c.form, grid, P, Q, res, sh, split, st);
+    if (c.parts > 1)
+        hipLaunchKernelGGL((rsh_join_parts_kernel<T, GATED>), dim3((unsigned)((cols + 1023) / 1024 * rows), 1, results), dim3(256), 0, st,
+                           (const float*)work, res, rows, cols, c.parts);
 }
 
 template <class F>
@@ -375,30 +560,46 @@ void by_half(int type, F f) {
 
 }  // namespace
 
+int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k) {
+    const int64_t step = x_type == RSH_MX4 ? 256 : 64;
+    return partial_bytes(choose(t, n, (k + step - 1) / step, false, 1), t, n, false, 1);
+}
+
+int64_t gated_forward_work(int64_t t, int64_t d, int64_t f) { return partial_bytes(choose(t, f, (d + 63) / 64, true, 1), t, f, true, 1); }
+
+// dG and dU, and behind them the larger of the sums of dX and of the weights' gradients (of both, or of one alone).
+int64_t gated_backward_work(int64_t t, int64_t d, int64_t f) {
+    const int64_t gates = 4 * t * ((f + 7) / 8 * 8);
+    int64_t sums = partial_bytes(choose(t, d, 2 * ((f + 63) / 64), false, 1), t, d, false, 1);
+    for (int results = 1; results <= 2; ++results)
+        sums = std::max(sums, partial_bytes(choose(f, d, (t + 63) / 64, false, results), f, d, false, results));
+    return gates + sums;
+}
+
 int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int y_type,
-                       int64_t t, int64_t n, int64_t k, void* stream) {
+                       int64_t t, int64_t n, int64_t k, void* work, void* stream) {
     const int64_t blocks = (k + kBlock - 1) / kBlock;
     const Operand p = {{W, nullptr}, {(const uint8_t*)w_scales, nullptr}, blocks};
     const Operand q = {{X, nullptr}, {(const uint8_t*)x_scales, nullptr}, x_type == RSH_MX4 ? blocks : ld_x};
     const Result res = {{(uint16_t*)Y, nullptr}, nullptr, nullptr, n, 0, 0};
     by_half(y_type, [&](auto half) {
         using T = decltype(half);
-        if (x_type == RSH_MX4) product<T, kFours, kFours, false, 1>(p, q, res, t, n, k, 1, (hipStream_t)stream);
-        else product<T, kCodes, kAlong, false, 1>(p, q, res, t, n, k, 1, (hipStream_t)stream);
+        if (x_type == RSH_MX4) product<T, kFours, kFours, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
+        else product<T, kCodes, kAlong, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
     });
     return launched();
 }
 
 int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
-                         const void* u_scales, int act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* stream) {
+                         const void* u_scales, int act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* work, void* stream) {
     const int64_t blocks = (d + kBlock - 1) / kBlock;
     const Operand p = {{Wg, Wu}, {(const uint8_t*)g_scales, (const uint8_t*)u_scales}, g_scales ? blocks : ld_w};
     const Operand q = {{X, nullptr}, {nullptr, nullptr}, ld_x};
     const Result res = {{(uint16_t*)H, nullptr}, (uint16_t*)G, (uint16_t*)U, f, (f + 7) / 8 * 8, act};
     by_half(type, [&](auto half) {
         using T = decltype(half);
-        if (g_scales) product<T, kCodes, kAlong, true, 1>(p, q, res, t, f, d, 1, (hipStream_t)stream);
-        else product<T, kAlong, kAlong, true, 1>(p, q, res, t, f, d, 1, (hipStream_t)stream);
+        if (g_scales) product<T, kCodes, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
+        else product<T, kAlong, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
     });
     return launched();
 }
@@ -410,6 +611,7 @@ int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg,
     const int64_t ld_gate = (f + 7) / 8 * 8, pieces = t * (ld_gate / 8);
     uint16_t* const dG = (uint16_t*)work;
     uint16_t* const dU = dG + t * ld_gate;
+    void* const sums = dU + t * ld_gate;
     const Operand gates = {{dG, dU}, {nullptr, nullptr}, ld_gate};
     by_half(type, [&](auto half) {
         using T = decltype(half);
@@ -418,12 +620,12 @@ int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg,
         if (dX) {
             const Operand w = {{Wg, Wu}, {nullptr, nullptr}, ld_w};
             const Result res = {{(uint16_t*)dX, nullptr}, nullptr, nullptr, d, 0, 0};
-            product<T, kAcross, kAlong, false, 2>(w, gates, res, t, d, f, 1, st);
+            product<T, kAcross, kAlong, false, 2>(w, gates, res, t, d, f, 1, sums, st);
         }
         if (dWg || dWu) {
             const Operand x = {{X, nullptr}, {nullptr, nullptr}, ld_x}, only_u = {{dU, nullptr}, {nullptr, nullptr}, ld_gate};
             const Result res = {{(uint16_t*)(dWg ? dWg : dWu), (uint16_t*)dWu}, nullptr, nullptr, d, 0, 0};
-            product<T, kAcross, kAcross, false, 1>(x, dWg ? gates : only_u, res, f, d, t, dWg && dWu ? 2 : 1, st);
+            product<T, kAcross, kAcross, false, 1>(x, dWg ? gates : only_u, res, f, d, t, dWg && dWu ? 2 : 1, sums, st);
         }
     });
     return launched();

@@ -90,11 +90,16 @@ int launch_mx4_quantize(const void* X, int type, int64_t rows, int64_t k, int64_
 int launch_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t k, void* Y, int type, int64_t ld, void* stream);
 
 // Products of the feed-forward block (ffn.hip).  x_type, y_type, type: RSH_F16 or RSH_BF16, x_type also RSH_MX4; scales null for
-// operands of 16 bits.  G, U, dG and dU have rows of f elements rounded up to a multiple of eight.
+// operands of 16 bits.  G, U, dG and dU have rows of f elements rounded up to a multiple of eight.  work: the bytes that the
+// *_work function of the same sizes says.
+int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k);
+int64_t gated_forward_work(int64_t t, int64_t d, int64_t f);
+int64_t gated_backward_work(int64_t t, int64_t d, int64_t f);
 int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int y_type,
-                       int64_t t, int64_t n, int64_t k, void* stream);
+                       int64_t t, int64_t n, int64_t k, void* work, void* stream);
 int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
-                         const void* u_scales, int act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* stream);
+                         const void* u_scales, int act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* work,
+                         void* stream);
 int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* G, const void* U,
                           const void* dH, int64_t ld_h, int act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
                           void* stream);
