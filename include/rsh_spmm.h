@@ -290,11 +290,12 @@ int rsh_act_backward(const void *dY_dev, const void *Y_dev, void *dZ_dev, float 
  *                       gradients: [t][f rounded up to a multiple of 8] of `type`, 16-byte aligned
  *   rsh_gated_backward  dX, dWg, dWu: NULL where not wanted.  dH: rows ld_h apart.  dG and dU are rounded to `type`.
  * work: device, 16-byte aligned, of the bytes that the *_work function of the same sizes reports (0: may be NULL), rewritten by
- * every call.  Sizes are positive and below 2^31.  Results never depend on the order in which waves run.
+ * every call.  t is positive and below 2^31; n, k, d, f and the distances between rows are at most RSH_FFN_MAX_WIDTH.  Results never depend on the order in which waves run.
  * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE
- * for more tiles than a launch takes.
+ * for a width above RSH_FFN_MAX_WIDTH or more tiles than a launch takes.
  */
 enum { RSH_F32 = 0, RSH_F16 = 1, RSH_BF16 = 2, RSH_MX4 = 3 };
+#define RSH_FFN_MAX_WIDTH (1 << 21)
 enum { RSH_ACT_SILU = 0, RSH_ACT_GELU = 1, RSH_ACT_RELU = 2 };
 int rsh_mx4_quantize(const void *X_dev, int32_t type, int64_t rows, int64_t k, int64_t ld, void *codes_dev, void *scales_dev, void *hip_stream);
 int rsh_mx4_dequantize(const void *codes_dev, const void *scales_dev, int64_t rows, int64_t k, void *Y_dev, int32_t type, int64_t ld,

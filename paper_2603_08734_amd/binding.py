@@ -7,6 +7,7 @@ fallback: if the library cannot be loaded the import of a symbol fails loudly.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -240,21 +241,21 @@ def act_backward(dY, Y, want_dbias: bool):
     return dZ, dbias
 
 
-def _work(function, device, *sizes):
-    """The work array that a *_work function asks for, or None."""
-    import torch
+@functools.lru_cache(maxsize=4096)
+def _work_bytes(name: str, *sizes) -> int:
+    """What a *_work function says: a function of the sizes alone."""
     n = ctypes.c_int64()
-    _check(function(*sizes, ctypes.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+    _check(getattr(lib(), name)(*sizes, ctypes.byref(n)))
+    return n.value
 
 
 def mx4_quantize(X, x_type: int, ld: int):
     """(codes, scales) of a matrix whose rows are ld elements apart (rsh_mx4_quantize)."""
     import torch
     rows, k = X.shape
-    blocks = -(-k // 32)
-    codes = torch.empty((rows, 16 * blocks), dtype=torch.uint8, device=X.device)
-    scales = torch.empty((rows, blocks), dtype=torch.uint8, device=X.device)
+    blocks, device = -(-k // 32), X.device
+    codes = torch.empty((rows, 16 * blocks), dtype=torch.uint8, device=device)
+    scales = torch.empty((rows, blocks), dtype=torch.uint8, device=device)
     _check(lib().rsh_mx4_quantize(X.data_ptr(), x_type, rows, k, ld, codes.data_ptr(), scales.data_ptr(), current_stream()))
     return codes, scales
 
@@ -268,34 +269,38 @@ def mx4_dequantize(codes, scales, Y, y_type: int) -> None:
 def mx4_product(X, x_scales, x_type: int, ld_x: int, codes, scales, Y, y_type: int, k: int) -> None:
     """Y = X W^T with W in 4 bits (rsh_mx4_product); Y contiguous [t, n]."""
     t, n = Y.shape
-    work = _work(lib().rsh_mx4_product_work, Y.device, x_type, t, n, k)
-    _check(lib().rsh_mx4_product(X.data_ptr(), _address(x_scales), x_type, ld_x, codes.data_ptr(), scales.data_ptr(), Y.data_ptr(), y_type, t, n, k,
-                                 _address(work), current_stream()))
+    bytes_ = _work_bytes("rsh_mx4_product_work", x_type, t, n, k)
+    work = Y.new_empty(bytes_ // 2) if bytes_ else None
+    _check(lib().rsh_mx4_product(X.data_ptr(), None if x_scales is None else x_scales.data_ptr(), x_type, ld_x, codes.data_ptr(), scales.data_ptr(),
+                                 Y.data_ptr(), y_type, t, n, k, None if work is None else work.data_ptr(), current_stream()))
 
 
 def gated_forward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, g_scales, u_scales, act: int, f: int, keep: bool):
-    """(H, G, U) of the gated block (rsh_gated_forward); G and U None unless they are kept."""
-    import torch
+    """(H, G and U one behind the other or None) of the gated block (rsh_gated_forward)."""
     t, d = X.shape
-    H = torch.empty((t, f), dtype=X.dtype, device=X.device)
-    G = U = None
+    H = X.new_empty((t, f))
+    kept = g = u = None
     if keep:
-        G, U = (torch.empty((t, -(-f // 8) * 8), dtype=X.dtype, device=X.device) for _ in range(2))
-    work = _work(lib().rsh_gated_forward_work, X.device, x_type if g_scales is None else RSH_MX4, t, d, f)
+        kept = X.new_empty((2, t, (f + 7) // 8 * 8))
+        g = kept.data_ptr()
+        u = g + kept.numel()       # half of its bytes
+    bytes_ = _work_bytes("rsh_gated_forward_work", x_type if g_scales is None else RSH_MX4, t, d, f)
+    work = X.new_empty(bytes_ // 2) if bytes_ else None
     _check(lib().rsh_gated_forward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, _address(g_scales), _address(u_scales), act,
-                                   H.data_ptr(), _address(G), _address(U), t, d, f, _address(work), current_stream()))
-    return H, G, U
+                                   H.data_ptr(), g, u, t, d, f, None if work is None else work.data_ptr(), current_stream()))
+    return H, kept
 
 
-def gated_backward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, G, U, dH, ld_h: int, act: int, want):
+def gated_backward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, kept, dH, ld_h: int, act: int, want):
     """Gradients (dX, dWg, dWu) of the gated block, None where not wanted (rsh_gated_backward)."""
-    import torch
     (t, d), f = X.shape, Wg.shape[0]
-    out = [torch.empty(s, dtype=X.dtype, device=X.device) if w else None for s, w in zip(((t, d), (f, d), (f, d)), want)]
-    work = _work(lib().rsh_gated_backward_work, X.device, t, d, f)
-    _check(lib().rsh_gated_backward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, G.data_ptr(), U.data_ptr(), dH.data_ptr(), ld_h,
-                                    act, *(_address(o) for o in out), t, d, f, _address(work), current_stream()))
-    return out
+    dX = X.new_empty((t, d)) if want[0] else None
+    dWg = X.new_empty((f, d)) if want[1] else None
+    dWu = X.new_empty((f, d)) if want[2] else None
+    work, g = X.new_empty(_work_bytes("rsh_gated_backward_work", t, d, f) // 2), kept.data_ptr()
+    _check(lib().rsh_gated_backward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, g, g + kept.numel(), dH.data_ptr(), ld_h, act,
+                                    _address(dX), _address(dWg), _address(dWu), t, d, f, work.data_ptr(), current_stream()))
+    return dX, dWg, dWu
 
 
 def rsh_copy_probe(src, dst, nbytes: int, stream=None) -> None:

@@ -639,10 +639,11 @@ int rsh_act_backward(const void* dY, const void* Y, void* dZ, float* dbias, floa
 }
 
 namespace {
-constexpr int64_t kMaxSize = (int64_t)1 << 31;
-// Sizes of a product; its tiles are no smaller than 64 by 64.
+constexpr int64_t kMaxSize = (int64_t)1 << 31, kMaxWidth = RSH_FFN_MAX_WIDTH;
+// Sizes of a product: rows of activations, and the two widths of a weight.  Its tiles are no smaller than 64 by 64.
 int sizes_ok(int64_t a, int64_t b, int64_t c) {
     if (a <= 0 || b <= 0 || c <= 0 || a >= kMaxSize || b >= kMaxSize || c >= kMaxSize) return RSH_ERR_BAD_OPTION;
+    if (b > kMaxWidth || c > kMaxWidth) return RSH_ERR_TOO_LARGE;
     for (const auto& [x, y] : {std::pair(a, b), std::pair(a, c), std::pair(b, c)})
         if (((x + 63) / 64) * ((y + 63) / 64) > kMaxSize / 256) return RSH_ERR_TOO_LARGE;
     return RSH_OK;
@@ -681,7 +682,7 @@ int rsh_mx4_product(const void* X, const void* x_scales, int32_t x_type, int64_t
     if (const int rc = rsh_mx4_product_work(x_type, t, n, k, &bytes)) return rc;
     const bool four = x_type == RSH_MX4;
     if (!X || !W || !w_scales || !Y || (four && !x_scales) || (bytes && !work)) return RSH_ERR_NULL;
-    if (!half_type(y_type) || (!four && (y_type != x_type || x_scales || ld_x < k || ld_x >= kMaxSize)) || !aligned_to({W}, 16) || !aligned_to({Y}, 2) ||
+    if (!half_type(y_type) || (!four && (y_type != x_type || x_scales || ld_x < k || ld_x > kMaxWidth)) || !aligned_to({W}, 16) || !aligned_to({Y}, 2) ||
         !aligned_to({X}, four ? 16 : 2) || !aligned_to({work}, 16))
         return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_mx4_product(X, x_scales, x_type, ld_x, W, w_scales, Y, y_type, t, n, k, work, hip_stream));
@@ -701,7 +702,7 @@ int rsh_gated_forward(const void* X, int32_t type, int64_t ld_x, const void* Wg,
     if (!half_type(type) || act < RSH_ACT_SILU || act > RSH_ACT_RELU) return RSH_ERR_BAD_OPTION;
     if (const int rc = rsh_gated_forward_work(g_scales ? RSH_MX4 : type, t, d, f, &bytes)) return rc;
     if (!X || !Wg || !Wu || !H || !g_scales != !u_scales || !G != !U || (bytes && !work)) return RSH_ERR_NULL;
-    if (ld_x < d || ld_x >= kMaxSize || (!g_scales && (ld_w < d || ld_w >= kMaxSize)) || !aligned_to({X, H}, 2) ||
+    if (ld_x < d || ld_x > kMaxWidth || (!g_scales && (ld_w < d || ld_w > kMaxWidth)) || !aligned_to({X, H}, 2) ||
         !aligned_to({Wg, Wu}, g_scales ? 16 : 2) || !aligned_to({G, U, work}, 16))
         return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_gated_forward(X, type, ld_x, Wg, Wu, ld_w, g_scales, u_scales, act, H, G, U, t, d, f, work, hip_stream));
@@ -721,7 +722,7 @@ int rsh_gated_backward(const void* X, int32_t type, int64_t ld_x, const void* Wg
     if (!half_type(type) || act < RSH_ACT_SILU || act > RSH_ACT_RELU) return RSH_ERR_BAD_OPTION;
     if (const int rc = rsh_gated_backward_work(t, d, f, &bytes)) return rc;
     if (!X || !G || !U || !dH || !work || (dX && (!Wg || !Wu)) || (!dX && !dWg && !dWu)) return RSH_ERR_NULL;
-    if (ld_x < d || ld_x >= kMaxSize || (dX && (ld_w < d || ld_w >= kMaxSize)) || ld_h < f || ld_h >= kMaxSize ||
+    if (ld_x < d || ld_x > kMaxWidth || (dX && (ld_w < d || ld_w > kMaxWidth)) || ld_h < f || ld_h > kMaxWidth ||
         !aligned_to({X, Wg, Wu, dH, dX, dWg, dWu}, 2) || !aligned_to({G, U, work}, 16))
         return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_gated_backward(X, type, ld_x, Wg, Wu, ld_w, G, U, dH, ld_h, act, dX, dWg, dWu, t, d, f, work, hip_stream));

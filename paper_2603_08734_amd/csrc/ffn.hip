@@ -10,35 +10,11 @@
 #include <algorithm>
 
 #include "../../include/rsh_spmm.h"
-#include "mx4.hpp"
+#include "ffn.hpp"
 
 namespace rsh {
 
 namespace {
-
-// How an operand lies in memory.
-enum Form {
-    kAlong,     // k along memory: row i at i * ld
-    kAcross,    // k across memory: k at k * ld
-    kCodes,     // blocks of codes and their scales, k along memory; turned into 16 bits on the way into LDS
-    kFours      // the same, multiplied as it is
-};
-
-struct Operand {
-    const void* data[2];           // two matrices of equal shape (gate and up), or one
-    const uint8_t* scales[2];
-    int64_t ld;                    // elements (kAlong, kAcross) or blocks (kCodes, kFours) from row to row
-};
-
-enum Act { kSilu = RSH_ACT_SILU, kGelu = RSH_ACT_GELU, kRelu = RSH_ACT_RELU };
-
-struct Result {
-    uint16_t* out[2];              // C, or H; [1]: the second of two results that share P (dWu)
-    uint16_t* gate;                // G and U where they are wanted
-    uint16_t* up;
-    int64_t ld, ld_gate;
-    int act;
-};
 
 struct Shape {
     int64_t rows, cols, k;         // of one product
@@ -47,25 +23,21 @@ struct Shape {
 
 constexpr int kRowBytes = 128;     // of k in one step: 64 elements of 16 bits, 256 of 4
 
-// act(g) and its derivative.  silu: g s with s = 1 / (1 + exp(-g)); gelu: g times the normal distribution function.
-__device__ __forceinline__ float act_of(int act, float g) {
-    if (act == kSilu) return g / (1.f + __expf(-g));
-    if (act == kGelu) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
-    return g * (g > 0.f ? 1.f : 0.f);
-}
-__device__ __forceinline__ float act_of(int act, float g, float* slope) {
-    if (act == kSilu) {
-        const float s = 1.f / (1.f + __expf(-g));
-        *slope = s * (1.f + g * (1.f - s));
-        return g * s;
+// Sixteen scales of which `valid` exist; the others are 0.
+__device__ __forceinline__ uint4_t load_scales16(const uint8_t* p, int64_t valid) {
+    uint4_t v = {0, 0, 0, 0};
+    if (valid >= 16) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+        for (int i = 0; i < valid; ++i) {
+            const uint32_t byte = (uint32_t)p[i] << (8 * (i & 3));
+            v[0] |= i / 4 == 0 ? byte : 0u;
+            v[1] |= i / 4 == 1 ? byte : 0u;
+            v[2] |= i / 4 == 2 ? byte : 0u;
+            v[3] |= i / 4 == 3 ? byte : 0u;
+        }
     }
-    if (act == kGelu) {
-        const float c = 0.5f * (1.f + erff(g * 0.70710678118654752f));
-        *slope = c + g * __expf(-0.5f * g * g) * 0.3989422804014327f;
-        return g * c;
-    }
-    *slope = g > 0.f ? 1.f : 0.f;
-    return g * *slope;
+    return v;
 }
 
 // Value of the other lane of a pair.
@@ -83,42 +55,91 @@ __device__ __forceinline__ int across_at(int k, int c) {
     return k * (2 * WIDTH) + ((c ^ ((k & 7) << 1 & (WIDTH / 8 - 1))) << 4);
 }
 
-// Source of row `i` of a tile of P: where two matrices run side by side, 32 columns of one, then 32 of the other.
-template <bool PAIR>
-__device__ __forceinline__ int64_t column_of(int64_t tile, int i, int width, int* which) {
-    *which = PAIR ? i >> 5 & 1 : 0;
-    return PAIR ? tile * (width / 2) + (i >> 6) * 32 + (i & 31) : tile * width + i;
-}
-
-// Pieces of one operand's tile on their way through registers into LDS: N = chunks of 16 bytes per thread.
+// Chunks of one operand's tile on their way through registers into LDS: codes, which are turned into 16 bits, and rows that do not
+// lie at 16-byte boundaries.  Offsets are 32 bits from the tile's first element (launches see to it that they fit).  Lines past the
+// operand's last are read as that one: only what lies past k has to be zero, in both operands, since rows and columns past the
+// result's end are not kept.
 template <Form FORM, int WIDTH, int THREADS, bool PAIR>
 struct Stage {
     static constexpr int kChunks = FORM == kCodes ? WIDTH * 2 / THREADS : WIDTH * 8 / THREADS;
     static_assert(kChunks > 0);
     uint4_t v[kChunks];
     uint32_t s[FORM == kCodes ? kChunks : 1];
+    uint32_t line[kChunks];        // byte of the chunk's line (kCodes: of its scales)
+    int64_t first, stride;         // bytes to the tile's first element, from line to line
+    int64_t span;                  // from there to the operand's end
+    int chunk;                     // in its line; the same for all chunks of a thread
 
-    __device__ __forceinline__ void load(const Operand& o, int seg, int64_t tile, int64_t extent, int64_t k0, int64_t k) {
+    // Which of two matrices, where they run side by side: 32 lines of one, then 32 of the other.
+    static __device__ __forceinline__ int matrix(int j) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        return PAIR ? (wave + THREADS / 64 * j) >> (FORM == kCodes ? 0 : 2) & 1 : 0;
+    }
+    __device__ __forceinline__ void start(const Operand& o, int64_t tile, int64_t extent, int64_t k) {
+        const int64_t width = PAIR ? WIDTH / 2 : WIDTH, left = extent - tile * width;
+        stride = FORM == kCodes ? o.ld : 2 * o.ld;
+        if constexpr (FORM == kAcross) {
+            chunk = threadIdx.x % (WIDTH / 8);
+            first = 2 * tile * width;
+            span = (k - 1) * stride + 2 * left;
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) line[j] = (uint32_t)((threadIdx.x + THREADS * j) / (WIDTH / 8) * stride);
+        } else {
+            constexpr int kIn = FORM == kCodes ? 2 : 8;       // chunks of a line
+            chunk = threadIdx.x % kIn;
+            first = tile * width * stride;
+            span = (left - 1) * stride + 2 * k;
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+                const int i = (threadIdx.x + THREADS * j) / kIn, at = PAIR ? (i >> 6) * 32 + (i & 31) : i;
+                line[j] = (uint32_t)(min((int64_t)at, left - 1) * stride);
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const Operand& o, int seg, int64_t k0) {
+        if constexpr (FORM == kCodes) {
+            const uint32_t b = (uint32_t)min(k0 / kBlock + chunk, o.ld - 1);
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+                v[j] = *reinterpret_cast<const uint4_t*>((const uint8_t*)o.data[matrix(j)] + first * kBlockBytes + (line[j] + b) * kBlockBytes);
+                s[j] = (o.scales[matrix(j)] + first)[line[j] + b];
+            }
+        } else {
+            const int64_t ahead = FORM == kAlong ? 2 * k0 : k0 * stride;
+            const int last = (int)min(span - ahead - 16, (int64_t)0x7ffffff0);      // below 0 where less than 16 bytes are left
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+                const uint8_t* const base = (const uint8_t*)o.data[PAIR ? matrix(j) : seg] + first + ahead;
+                if (__builtin_expect(span >= 16, 1)) {      // a chunk that the operand's end cuts is read as its last 16 bytes
+                    v[j] = *reinterpret_cast<const uint4_a2*>(base + min((int)line[j] + 16 * chunk, last));
+                } else {               // seven elements at most
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t x = *reinterpret_cast<const uint16_t*>(base + min((int64_t)line[j] + 16 * chunk + 2 * e, span - ahead - 2));
+                        v[j][e / 2] = e & 1 ? v[j][e / 2] | x << 16 : x;
+                    }
+                }
+            }
+        }
+    }
+    // In the last step: the elements of a cut chunk go to its front, what lies past k becomes zero.
+    __device__ __forceinline__ void trim(const Operand& o, int64_t k0, int64_t k) {
+        if (k0 + 64 < k) return;
+        const int left = (int)(k - k0), end = (int)(span - (FORM == kAlong ? 2 * k0 : k0 * stride)) - 16;     // of k; of the operand's bytes
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
-            const int i = threadIdx.x + THREADS * j;
-            if constexpr (FORM == kAlong) {
-                int which;
-                const int64_t row = column_of<PAIR>(tile, i >> 3, WIDTH, &which), at = k0 + 8 * (i & 7);
-                v[j] = load8((const uint16_t*)o.data[PAIR ? which : seg] + row * o.ld + at, row < extent ? k - at : 0);
-            } else if constexpr (FORM == kAcross) {
-                const int64_t kk = k0 + i / (WIDTH / 8), col = tile * WIDTH + 8 * (i % (WIDTH / 8));
-                v[j] = load8((const uint16_t*)o.data[seg] + kk * o.ld + col, kk < k ? extent - col : 0);
-            } else if constexpr (FORM == kCodes) {
-                int which;
-                const int64_t row = column_of<PAIR>(tile, i >> 1, WIDTH, &which), b = k0 / kBlock + (i & 1);
-                const bool in = row < extent && b < o.ld;
-                v[j] = in ? *reinterpret_cast<const uint4_t*>((const uint8_t*)o.data[which] + (row * o.ld + b) * kBlockBytes) : (uint4_t){0, 0, 0, 0};
-                s[j] = in ? o.scales[which][row * o.ld + b] : 0u;
+            if constexpr (FORM == kCodes) {
+                if (k0 / kBlock + chunk >= o.ld) v[j] = (uint4_t){0, 0, 0, 0}, s[j] = 0;
             } else {
-                const int64_t row = tile * WIDTH + (i >> 3), b = k0 / kBlock + (i & 7);
-                v[j] = row < extent && b < o.ld ? *reinterpret_cast<const uint4_t*>((const uint8_t*)o.data[0] + (row * o.ld + b) * kBlockBytes)
-                                                : (uint4_t){0, 0, 0, 0};
+                const int past = (int)line[j] + 16 * chunk - end, drop = span >= 16 ? max(0, min(past, 16)) / 2 : 0;
+                const int keep = FORM == kAlong ? left - 8 * chunk : (int)(threadIdx.x + THREADS * j) / (WIDTH / 8) < left ? 8 : 0;
+                uint4_t x = v[j];
+                if (drop & 4) x = (uint4_t){x[2], x[3], 0, 0};
+                if (drop & 2) x = (uint4_t){x[1], x[2], x[3], 0};
+                if (drop & 1) x = (uint4_t){x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x[w] &= (2 * w < keep ? 0xffffu : 0u) | (2 * w + 1 < keep ? 0xffff0000u : 0u);
+                v[j] = x;
             }
         }
     }
@@ -219,20 +240,6 @@ __device__ __forceinline__ uint4_t fragment(const unsigned char* lds, int base, 
     }
 }
 
-// What becomes of the sums of four columns of a row.
-template <class T, bool GATED>
-__device__ __forceinline__ void finish(const Result& res, uint16_t* out, int64_t row, int64_t col, int64_t left, float4_t x, float4_t y) {
-    if constexpr (GATED) {
-        if (res.gate) {
-            store4(res.gate + row * res.ld_gate + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
-            store4(res.up + row * res.ld_gate + col, (uint2_t){T::pair(y[0], y[1]), T::pair(y[2], y[3])}, left);
-        }
-#pragma unroll
-        for (int v = 0; v < 4; ++v) x[v] = act_of(res.act, x[v]) * y[v];
-    }
-    store4(out + row * res.ld + col, (uint2_t){T::pair(x[0], x[1]), T::pair(x[2], x[3])}, left);
-}
-
 constexpr int kSpan = 10;   // binary16: the largest scale of a row of codes is brought to 2^kSpan
 
 }  // namespace
@@ -274,22 +281,25 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
 
     std::conditional_t<kDirectP, Direct<FP, kWidthP, kThreads, GATED>, StageP> sp;
     std::conditional_t<DIRECT, Direct<FQ, kWidthQ, kThreads, false>, StageQ> sq;
-    if constexpr (kDirectP) sp.start(P, tc, sh.cols, sh.k);
-    if constexpr (DIRECT) sq.start(Q, tr, sh.rows, sh.k);
+    sp.start(P, tc, sh.cols, sh.k);
+    sq.start(Q, tr, sh.rows, sh.k);
     int shift[StageP::kChunks] = {};
     if constexpr (kShifted) {
-        // the largest scale of each row; two threads share a row
+        // the largest scale of each row within the part's k; two threads share a row, 16 blocks each in turn
+        const int64_t b0 = blockIdx.y * split.steps * (kStep / kBlock), b1 = min(P.ld, b0 + split.steps * (kStep / kBlock));
 #pragma unroll
         for (int j = 0; j < StageP::kChunks; ++j) {
             const int i = threadIdx.x + kThreads * j;
-            int which;
-            const int64_t row = column_of<GATED>(tc, i >> 1, kWidthP, &which);
+            const uint8_t* const at = P.scales[sp.matrix(j)] + sp.first + sp.line[j];
             int top = 0;
-            if (row < sh.cols)
-                for (int64_t b = i & 1; b < P.ld; b += 2) {
-                    const int s = P.scales[which][row * P.ld + b];
+            for (int64_t b = b0 + 16 * (i & 1); b < b1; b += 32) {
+                const uint4_t v = load_scales16(at + b, b1 - b);
+#pragma unroll
+                for (int w = 0; w < 16; ++w) {
+                    const int s = v[w / 4] >> (8 * (w & 3)) & 255;
                     top = max(top, s == 255 ? 0 : s);
                 }
+            }
             top = max(top, swap_pair(top));
             shift[j] = 127 + kSpan - top;
             if ((i & 1) == 0) tops[i >> 1] = top;
@@ -311,9 +321,9 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
         const int seg = SEGS == 2 ? (int)(step >= steps) : 0;
         const int64_t k0 = (SEGS == 2 ? step - seg * steps : step) * kStep;
         if constexpr (kDirectP) sp.issue(P, seg, k0, sh.k, lds[buf]);
-        else sp.load(P, seg, tc, sh.cols, k0, sh.k);
+        else sp.load(P, seg, k0);
         if constexpr (DIRECT) sq.issue(Q, SEGS == 2 ? seg : second, k0, sh.k, lds[buf] + kBytesP);
-        else sq.load(Q, SEGS == 2 ? seg : second, tr, sh.rows, k0, sh.k);
+        else sq.load(Q, SEGS == 2 ? seg : second, k0);
         if constexpr (kScaled) {
             // the eight scales of one row of either operand
 #pragma unroll
@@ -334,9 +344,16 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
             }
         }
     };
-    auto store = [&](int buf) {
-        if constexpr (!kDirectP) sp.template store<T>(lds[buf], shift);
-        if constexpr (!DIRECT) sq.template store<T>(lds[buf] + kBytesP, nullptr);
+    auto store = [&](int64_t step, int buf) {
+        const int64_t k0 = (SEGS == 2 && step >= steps ? step - steps : step) * kStep;
+        if constexpr (!kDirectP) {
+            sp.trim(P, k0, sh.k);
+            sp.template store<T>(lds[buf], shift);
+        }
+        if constexpr (!DIRECT) {
+            sq.trim(Q, k0, sh.k);
+            sq.template store<T>(lds[buf] + kBytesP, nullptr);
+        }
         if constexpr (kScaled) {
 #pragma unroll
             for (int u = 0; u < kTurns; ++u)
@@ -346,7 +363,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
 
     if (begin < end) {
         load(begin, 0);
-        store(0);
+        store(begin, 0);
     }
     meet();
     for (int64_t step = begin; step < end; ++step) {
@@ -386,7 +403,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
                     for (int j = 0; j < TQ; ++j) acc[i][j] = T::mfma32(a[i], b[j], acc[i][j]);
             }
         }
-        if (step + 1 < end) store(buf ^ 1);
+        if (step + 1 < end) store(step + 1, buf ^ 1);
         meet();
     }
 
@@ -449,9 +466,9 @@ template <class T>
 __global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* __restrict__ dH, const uint16_t* __restrict__ G,
                                                                 const uint16_t* __restrict__ U, uint16_t* __restrict__ dG,
                                                                 uint16_t* __restrict__ dU, int64_t t, int64_t f, int64_t ld, int64_t ld_gate, int act) {
-    const int64_t pieces = ld_gate / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= t * pieces) return;
-    const int64_t row = i / pieces, col = 8 * (i - row * pieces), at = row * ld_gate + col;
+    const uint32_t across = (uint32_t)((ld_gate + 2047) / 2048), slab = blockIdx.x / across;
+    const int64_t row = slab, col = 8 * ((int64_t)(blockIdx.x - slab * across) * 256 + threadIdx.x), at = row * ld_gate + col;
+    if (row >= t || col >= ld_gate) return;
     const uint4_t h = load8(dH + row * ld + col, f - col);
     const uint4_t g = *reinterpret_cast<const uint4_t*>(G + at), u = *reinterpret_cast<const uint4_t*>(U + at);
     uint4_t a, b;
@@ -517,11 +534,10 @@ int64_t partial_bytes(const Choice& c, int64_t rows, int64_t cols, bool pairs, i
     return c.parts == 1 ? 0 : (int64_t)c.parts * results * rows * ((cols + 3) / 4 * 4) * (pairs ? 2 : 1) * (int64_t)sizeof(float);
 }
 
-// Whether an operand's chunks lie at 16-byte boundaries and a tile's within a buffer's reach.
+// Whether an operand's lines are whole chunks at 16-byte boundaries.
 bool whole_chunks(const Operand& o, Form form, int64_t along) {
-    if (form == kCodes) return true;
-    if (form == kFours) return o.ld < (1 << 18);
-    return ((uintptr_t)o.data[0] | (uintptr_t)o.data[1]) % 16 == 0 && o.ld % 8 == 0 && along % 8 == 0 && o.ld < (1 << 21);
+    if (form == kCodes || form == kFours) return true;
+    return ((uintptr_t)o.data[0] | (uintptr_t)o.data[1]) % 16 == 0 && o.ld % 8 == 0 && along % 8 == 0;
 }
 
 template <class T, Form FP, Form FQ, bool GATED, int SEGS, bool DIRECT>
@@ -543,10 +559,14 @@ void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows
     const Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
     const Split split = {c.parts, each, (float*)work};
     const int64_t tiles = (int64_t)sh.tiles_r * sh.tiles_c;
-    const bool direct = whole_chunks(P, FP, FP == kAcross ? cols : k) && whole_chunks(Q, FQ, FQ == kAcross ? rows : k);
     const dim3 grid((unsigned)((tiles + 7) / 8 * 8), c.parts, results);
-    if (direct) launch_tiles<T, FP, FQ, GATED, SEGS, true>(c.form, grid, P, Q, res, sh, split, st);
-    else launch_tiles<T, FP, FQ, GATED, SEGS, false>(c.form, grid, P, Q, res, sh, split, st);
+    if constexpr (FP != kFours) {
+        if (!whole_chunks(P, FP, FP == kAcross ? cols : k) || !whole_chunks(Q, FQ, FQ == kAcross ? rows : k))
+            launch_tiles<T, FP, FQ, GATED, SEGS, false>(c.form, grid, P, Q, res, sh, split, st);
+        else launch_tiles<T, FP, FQ, GATED, SEGS, true>(c.form, grid, P, Q, res, sh, split, st);
+    } else {
+        launch_tiles<T, FP, FQ, GATED, SEGS, true>(c.form, grid, P, Q, res, sh, split, st);
+    }
     if (c.parts > 1)
         hipLaunchKernelGGL((rsh_join_parts_kernel<T, GATED>), dim3((unsigned)((cols + 1023) / 1024 * rows), 1, results), dim3(256), 0, st,
                            (const float*)work, res, rows, cols, c.parts);
@@ -562,10 +582,14 @@ void by_half(int type, F f) {
 
 int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k) {
     const int64_t step = x_type == RSH_MX4 ? 256 : 64;
+    if (takes_few(t, x_type == RSH_MX4)) return 0;
     return partial_bytes(choose(t, n, (k + step - 1) / step, false, 1), t, n, false, 1);
 }
 
-int64_t gated_forward_work(int64_t t, int64_t d, int64_t f) { return partial_bytes(choose(t, f, (d + 63) / 64, true, 1), t, f, true, 1); }
+int64_t gated_forward_work(int64_t t, int64_t d, int64_t f) {
+    if (takes_few(t, false)) return 0;
+    return partial_bytes(choose(t, f, (d + 63) / 64, true, 1), t, f, true, 1);
+}
 
 // dG and dU, and behind them the larger of the sums of dX and of the weights' gradients (of both, or of one alone).
 int64_t gated_backward_work(int64_t t, int64_t d, int64_t f) {
@@ -584,7 +608,10 @@ int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t 
     const Result res = {{(uint16_t*)Y, nullptr}, nullptr, nullptr, n, 0, 0};
     by_half(y_type, [&](auto half) {
         using T = decltype(half);
-        if (x_type == RSH_MX4) product<T, kFours, kFours, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
+        if (takes_few(t, x_type == RSH_MX4)) {
+            if (x_type == RSH_MX4) launch_few<T, kFours, false>(p, q, res, t, n, k, (hipStream_t)stream);
+            else launch_few<T, kCodes, false>(p, q, res, t, n, k, (hipStream_t)stream);
+        } else if (x_type == RSH_MX4) product<T, kFours, kFours, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
         else product<T, kCodes, kAlong, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
     });
     return launched();
@@ -598,7 +625,10 @@ int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, 
     const Result res = {{(uint16_t*)H, nullptr}, (uint16_t*)G, (uint16_t*)U, f, (f + 7) / 8 * 8, act};
     by_half(type, [&](auto half) {
         using T = decltype(half);
-        if (g_scales) product<T, kCodes, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
+        if (takes_few(t, false)) {
+            if (g_scales) launch_few<T, kCodes, true>(p, q, res, t, f, d, (hipStream_t)stream);
+            else launch_few<T, kAlong, true>(p, q, res, t, f, d, (hipStream_t)stream);
+        } else if (g_scales) product<T, kCodes, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
         else product<T, kAlong, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
     });
     return launched();
@@ -608,14 +638,14 @@ int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg,
                           const void* dH, int64_t ld_h, int act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
                           void* stream) {
     const hipStream_t st = (hipStream_t)stream;
-    const int64_t ld_gate = (f + 7) / 8 * 8, pieces = t * (ld_gate / 8);
+    const int64_t ld_gate = (f + 7) / 8 * 8, blocks = t * ((ld_gate + 2047) / 2048);
     uint16_t* const dG = (uint16_t*)work;
     uint16_t* const dU = dG + t * ld_gate;
     void* const sums = dU + t * ld_gate;
     const Operand gates = {{dG, dU}, {nullptr, nullptr}, ld_gate};
     by_half(type, [&](auto half) {
         using T = decltype(half);
-        hipLaunchKernelGGL(rsh_gate_backward_kernel<T>, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, st, (const uint16_t*)dH, (const uint16_t*)G,
+        hipLaunchKernelGGL(rsh_gate_backward_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, (const uint16_t*)dH, (const uint16_t*)G,
                            (const uint16_t*)U, dG, dU, t, f, ld_h, ld_gate, act);
         if (dX) {
             const Operand w = {{Wg, Wu}, {nullptr, nullptr}, ld_w};

@@ -13,45 +13,49 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding
-from .mx4 import HALVES, Mx4, _matrix, _no_gradient, _on
+from .mx4 import HALVES, Mx4, _no_gradient, _on, _rows
 
 ACTIVATIONS = {"silu": binding.RSH_ACT_SILU, "gelu": binding.RSH_ACT_GELU, "relu": binding.RSH_ACT_RELU}
 
 
 def _weights(Wg, Wu):
     """Both weights as matrices with one row stride, and that."""
-    Wg, ld = _matrix(Wg, "W_gate", HALVES)
-    Wu, ld_u = _matrix(Wu, "W_up", HALVES)
+    Wg, ld = _rows(Wg)
+    Wu, ld_u = _rows(Wu)
     return (Wg, Wu, ld) if ld == ld_u else (Wg.contiguous(), Wu.contiguous(), Wg.shape[1])
+
+
+def _forward(X, Wg, Wu, act, keep):
+    x, ld_x = _rows(X)
+    wg, wu, ld_w = _weights(Wg, Wu)
+    with _on(x.device):
+        return binding.gated_forward(x, HALVES[x.dtype], ld_x, wg, wu, ld_w, None, None, act, wg.shape[0], keep)
+
+
+def _backward(ctx, dH):
+    X, Wg, Wu, kept = ctx.saved_tensors
+    x, ld_x = _rows(X)
+    wg, wu, ld_w = _weights(Wg, Wu)
+    dH, ld_h = _rows(dH)
+    with _on(x.device):
+        return (*binding.gated_backward(x, HALVES[x.dtype], ld_x, wg, wu, ld_w, kept, dH, ld_h, ctx.act, ctx.needs_input_grad), None)
+
+
+_backward_once = once_differentiable(_backward)
 
 
 class _Gated(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, X, Wg, Wu, act, keep):
-        x, ld_x = _matrix(X, "X", HALVES)
-        wg, wu, ld_w = _weights(Wg, Wu)
+    def forward(ctx, X, Wg, Wu, act):
+        H, kept = _forward(X, Wg, Wu, act, True)
         ctx.act = act
-        if x.numel() == 0 or wg.numel() == 0:
-            ctx.save_for_backward(X, Wg, Wu, None, None)
-            return X.new_zeros((X.shape[0], Wg.shape[0]))
-        with _on(x.device):
-            H, G, U = binding.gated_forward(x, HALVES[x.dtype], ld_x, wg, wu, ld_w, None, None, act, wg.shape[0], keep)
-        ctx.save_for_backward(X, Wg, Wu, G, U)
+        ctx.save_for_backward(X, Wg, Wu, kept)
         return H
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, dH):
-        X, Wg, Wu, G, U = ctx.saved_tensors
-        want = ctx.needs_input_grad[:3]
-        if G is None:
-            return (*(torch.zeros_like(t) if w else None for t, w in zip((X, Wg, Wu), want)), None, None)
-        x, ld_x = _matrix(X, "X", HALVES)
-        wg, wu, ld_w = _weights(Wg, Wu)
-        dH, ld_h = _matrix(dH.to(X.dtype), "dH", HALVES)
-        with _on(x.device):
-            grads = binding.gated_backward(x, HALVES[x.dtype], ld_x, wg, wu, ld_w, G, U, dH, ld_h, ctx.act, want)
-        return (*grads, None, None)
+        # where the gradients' own graph is wanted, it ends here with an error
+        return _backward_once(ctx, dH) if torch.is_grad_enabled() else _backward(ctx, dH)
 
 
 def gated(X, W_gate, W_up, activation: str = "silu"):
@@ -63,23 +67,28 @@ def gated(X, W_gate, W_up, activation: str = "silu"):
     four = isinstance(W_gate, Mx4)
     if four != isinstance(W_up, Mx4):
         raise TypeError("W_gate and W_up: either both in 4 bits or neither")
-    if tuple(W_gate.shape) != tuple(W_up.shape) or len(W_gate.shape) != 2 or W_gate.shape[1] != X.shape[-1]:
-        raise ValueError(f"X {tuple(X.shape)}, W_gate {tuple(W_gate.shape)} and W_up {tuple(W_up.shape)} do not fit")
-    if X.dtype not in HALVES or (not four and (W_gate.dtype != X.dtype or W_up.dtype != X.dtype)):
-        raise TypeError(f"expected one type for X and 16-bit weights, one of {list(HALVES)}; X is {X.dtype}")
-    if X.device.type != "cuda" or W_gate.device != X.device or W_up.device != X.device:
-        raise ValueError(f"X is on {X.device}, W_gate on {W_gate.device}, W_up on {W_up.device}; expected one GPU")
-    act, (f, d) = ACTIVATIONS[activation], W_gate.shape
-    rows = X if X.dim() == 2 else X.reshape(-1, d) if d else X.reshape(X.shape[:-1].numel(), 0)
+    shape, device, dtype = W_gate.shape, X.device, X.dtype
+    if W_up.shape != shape or len(shape) != 2 or shape[1] != X.shape[-1]:
+        raise ValueError(f"X {tuple(X.shape)}, W_gate {tuple(shape)} and W_up {tuple(W_up.shape)} do not fit")
+    if dtype not in HALVES or (not four and (W_gate.dtype != dtype or W_up.dtype != dtype)):
+        raise TypeError(f"expected one type for X and 16-bit weights, one of {list(HALVES)}; X is {dtype}")
+    if not X.is_cuda or W_gate.device != device or W_up.device != device:
+        raise ValueError(f"X is on {device}, W_gate on {W_gate.device}, W_up on {W_up.device}; expected one GPU")
+    act, (f, d) = ACTIVATIONS[activation], shape
+    flat = X.dim() == 2
+    rows = X if flat else X.reshape(-1, d) if d else X.reshape(X.shape[:-1].numel(), 0)
     if four:
         _no_gradient(X)
-        if rows.numel() == 0 or f == 0:
-            H = X.new_zeros((rows.shape[0], f))
-        else:
-            x, ld_x = _matrix(rows, "X", HALVES)
-            with _on(X.device):
-                H, _, _ = binding.gated_forward(x, HALVES[X.dtype], ld_x, W_gate.codes, W_up.codes, 0, W_gate.scales, W_up.scales, act, f, False)
+    if rows.shape[0] == 0 or f == 0 or d == 0:
+        # no sums: zeros, whose gradients are zeros
+        H = rows.sum() * 0 + rows.new_zeros((rows.shape[0], f))
+        H = H if four else H + (W_gate.sum() + W_up.sum()) * 0
+    elif four:
+        x, ld_x = _rows(rows)
+        with _on(device):
+            H = binding.gated_forward(x, HALVES[dtype], ld_x, W_gate.codes, W_up.codes, 0, W_gate.scales, W_up.scales, act, f, False)[0]
+    elif (X.requires_grad or W_gate.requires_grad or W_up.requires_grad) and torch.is_grad_enabled():
+        H = _Gated.apply(rows, W_gate, W_up, act)
     else:
-        keep = torch.is_grad_enabled() and (X.requires_grad or W_gate.requires_grad or W_up.requires_grad)
-        H = _Gated.apply(rows, W_gate, W_up, act, keep)
-    return H if X.dim() == 2 else H.reshape(*X.shape[:-1], f)
+        H = _forward(rows, W_gate, W_up, act, False)[0]
+    return H if flat else H.reshape(*X.shape[:-1], f)

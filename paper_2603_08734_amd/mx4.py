@@ -24,7 +24,7 @@ _NOTHING = contextlib.nullcontext()
 
 def _on(device):
     """Launches go to the current device: make the operands' device that."""
-    return _NOTHING if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return _NOTHING if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
 
 def _matrix(X, name: str, types):
@@ -33,16 +33,23 @@ def _matrix(X, name: str, types):
         raise TypeError(f"{name}: expected a tensor of {' or '.join(str(t) for t in types)}, got {getattr(X, 'dtype', type(X))}")
     if X.dim() != 2:
         raise ValueError(f"{name}: expected a matrix, got shape {tuple(X.shape)}")
-    if X.device.type != "cuda":
+    if not X.is_cuda:
         raise ValueError(f"{name}: expected a tensor on the GPU, got {X.device}")
+    return _rows(X)
+
+
+def _rows(X):
+    """The same for a matrix that is known to be one."""
     k = X.shape[1]
+    if X.is_contiguous():
+        return X, k
     if (k > 1 and X.stride(1) != 1) or (X.shape[0] > 1 and X.stride(0) < k):
-        X = X.contiguous()
+        return X.contiguous(), k
     return X, X.stride(0) if X.shape[0] > 1 else k
 
 
 def _no_gradient(*tensors) -> None:
-    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+    if any(t.requires_grad for t in tensors) and torch.is_grad_enabled():
         raise ValueError("products and conversions in 4 bits have no gradient: call them under torch.no_grad() or on detached operands")
 
 
@@ -63,6 +70,13 @@ class Mx4:
             raise ValueError("codes: expected 16-byte alignment")
         self.codes, self.scales, self.shape = codes, scales, (codes.shape[0], k)
 
+    @classmethod
+    def _of(cls, codes, scales, k: int):
+        """Of arrays that the library has just made."""
+        Q = cls.__new__(cls)
+        Q.codes, Q.scales, Q.shape = codes, scales, (codes.shape[0], k)
+        return Q
+
     @property
     def device(self):
         return self.codes.device
@@ -81,9 +95,9 @@ def quantize(X) -> Mx4:
     rows, k = X.shape
     if rows == 0 or k == 0:
         blocks = -(-k // BLOCK)
-        return Mx4(*(torch.empty((rows, w), dtype=torch.uint8, device=X.device) for w in (16 * blocks, blocks)), k)
+        return Mx4._of(*(torch.empty((rows, w), dtype=torch.uint8, device=X.device) for w in (16 * blocks, blocks)), k)
     with _on(X.device):
-        return Mx4(*binding.mx4_quantize(X, _TYPES[X.dtype], ld), k)
+        return Mx4._of(*binding.mx4_quantize(X, _TYPES[X.dtype], ld), k)
 
 
 def dequantize(Q: Mx4, dtype=torch.bfloat16):
