@@ -268,7 +268,8 @@ int rsh_act_backward(const void *dY_dev, const void *Y_dev, void *dZ_dev, float 
  * Matrices in microscaled 4-bit floating point, row-major, k > 0 elements a row in blocks of 32 (the last may be short):
  *   scales  uint8 [rows][B], B = ceil(k / 32): byte s stands for 2^(s - 127), 255 for NaN
  *   codes   uint8 [rows][16 B]: element 2i of a row in the low half of byte i, 2i + 1 in the high half; bit 3 the sign, bits 0..2
- *           one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  Cells past k are zero.  16-byte aligned.
+ *           one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  Cells past k are zero.  16-byte aligned, the scales
+ *           4-byte aligned.
  *   rsh_mx4_quantize    s brings the largest magnitude of a block into [4, 8): floor(log2 max) - 2 + 127, at least 0; elements go
  *                       to the nearest value, ties to the even code, above 6 to 6.  A block of zeros: s = 0.  A block with an
  *                       infinity or a NaN: s = 255, codes 0.

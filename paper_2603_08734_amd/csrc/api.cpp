@@ -651,7 +651,8 @@ int sizes_ok(int64_t a, int64_t b, int64_t c) {
 bool half_type(int32_t type) { return type == RSH_F16 || type == RSH_BF16; }
 int matrix_ok(int32_t type, int64_t rows, int64_t k, int64_t ld, const void* X, const void* codes, const void* scales) {
     if (!X || !codes || !scales) return RSH_ERR_NULL;
-    if ((type != RSH_F32 && !half_type(type)) || rows <= 0 || k <= 0 || ld < k || !aligned_to({X}, type == RSH_F32 ? 4 : 2) || !aligned_to({codes}, 16))
+    if ((type != RSH_F32 && !half_type(type)) || rows <= 0 || k <= 0 || ld < k || !aligned_to({X}, type == RSH_F32 ? 4 : 2) || !aligned_to({codes}, 16) ||
+        !aligned_to({scales}, 4))
         return RSH_ERR_BAD_OPTION;
     if (rows >= kMaxSize || k >= kMaxSize || ld >= kMaxSize || rows * ((k + 31) / 32) > kMaxSize * 16) return RSH_ERR_TOO_LARGE;
     return RSH_OK;
@@ -683,7 +684,7 @@ int rsh_mx4_product(const void* X, const void* x_scales, int32_t x_type, int64_t
     const bool four = x_type == RSH_MX4;
     if (!X || !W || !w_scales || !Y || (four && !x_scales) || (bytes && !work)) return RSH_ERR_NULL;
     if (!half_type(y_type) || (!four && (y_type != x_type || x_scales || ld_x < k || ld_x > kMaxWidth)) || !aligned_to({W}, 16) || !aligned_to({Y}, 2) ||
-        !aligned_to({X}, four ? 16 : 2) || !aligned_to({work}, 16))
+        !aligned_to({X}, four ? 16 : 2) || !aligned_to({w_scales, x_scales}, 4) || !aligned_to({work}, 16))
         return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_mx4_product(X, x_scales, x_type, ld_x, W, w_scales, Y, y_type, t, n, k, work, hip_stream));
 }
@@ -703,7 +704,7 @@ int rsh_gated_forward(const void* X, int32_t type, int64_t ld_x, const void* Wg,
     if (const int rc = rsh_gated_forward_work(g_scales ? RSH_MX4 : type, t, d, f, &bytes)) return rc;
     if (!X || !Wg || !Wu || !H || !g_scales != !u_scales || !G != !U || (bytes && !work)) return RSH_ERR_NULL;
     if (ld_x < d || ld_x > kMaxWidth || (!g_scales && (ld_w < d || ld_w > kMaxWidth)) || !aligned_to({X, H}, 2) ||
-        !aligned_to({Wg, Wu}, g_scales ? 16 : 2) || !aligned_to({G, U, work}, 16))
+        !aligned_to({Wg, Wu}, g_scales ? 16 : 2) || !aligned_to({g_scales, u_scales}, 4) || !aligned_to({G, U, work}, 16))
         return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_gated_forward(X, type, ld_x, Wg, Wu, ld_w, g_scales, u_scales, act, H, G, U, t, d, f, work, hip_stream));
 }

@@ -21,213 +21,201 @@ struct Shape {
     int tiles_r, tiles_c;
 };
 
-constexpr int kRowBytes = 128;     // of k in one step: 64 elements of 16 bits, 256 of 4
+// A part of the slices of k, whose sums go to `partial` as fp32 [part][result][row][columns rounded up to 4, gate before up], where
+// there is more than one.
+struct Split {
+    int parts, slices;             // slices of a part
+    float* partial;
+};
 
-// Sixteen scales of which `valid` exist; the others are 0.
-__device__ __forceinline__ uint4_t load_scales16(const uint8_t* p, int64_t valid) {
-    uint4_t v = {0, 0, 0, 0};
-    if (valid >= 16) {
-        __builtin_memcpy(&v, p, 16);
-    } else {
-        for (int i = 0; i < valid; ++i) {
-            const uint32_t byte = (uint32_t)p[i] << (8 * (i & 3));
-            v[0] |= i / 4 == 0 ? byte : 0u;
-            v[1] |= i / 4 == 1 ? byte : 0u;
-            v[2] |= i / 4 == 2 ? byte : 0u;
-            v[3] |= i / 4 == 3 ? byte : 0u;
-        }
-    }
-    return v;
-}
-
-// Value of the other lane of a pair.
-__device__ __forceinline__ int swap_pair(int v) { return __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, false); }
+constexpr int kRowBytes = 64;      // of a slice of k: 32 elements of 16 bits, 128 of 4
+constexpr int kRing = 4;           // slices in LDS
+constexpr int kSpan = 10;          // binary16: the largest scale of a row of codes is brought to 2^kSpan
 
 __device__ __forceinline__ half4_t read_transposed(const unsigned char* p) {
     return __builtin_bit_cast(half4_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4_t __attribute__((address_space(3)))*)p));
 }
 
-// Byte of chunk c (16 bytes) of row r in LDS.  Rows of kRowBytes with k along them are read by 32 lanes at a time, a row each,
-// and rows with k across by 16 lanes, four rows each: the chunks of neighbouring rows are dealt to other banks.
-__device__ __forceinline__ int along_at(int r, int c) { return r * kRowBytes + ((c ^ (r & 7)) << 4); }
+// Byte of chunk c (16 bytes) of row r of a slice in LDS.  The 64 banks are 256 bytes wide, four rows of kRowBytes: 16 lanes that
+// read a chunk of as many rows at once shall find the 16 different chunks of that width, and so shall 32 lanes that read halves of
+// four chunks in four rows with k across.
+__device__ __forceinline__ int along_turn(int r) { return r >> 2 & 3; }
+template <int WIDTH>
+__device__ __forceinline__ int across_turn(int k) {
+    return WIDTH >= 128 ? (k & 3) << 2 ^ (k >> 3 & 1) << 1 : (k >> 1 & 1) << 2 ^ (k >> 3 & 1) << 1;
+}
+__device__ __forceinline__ int along_at(int r, int c) { return r * kRowBytes + ((c ^ along_turn(r)) << 4); }
 template <int WIDTH>
 __device__ __forceinline__ int across_at(int k, int c) {
-    return k * (2 * WIDTH) + ((c ^ ((k & 7) << 1 & (WIDTH / 8 - 1))) << 4);
+    return k * (2 * WIDTH) + ((c ^ across_turn<WIDTH>(k)) << 4);
+}
+// Place of a row of codes, 16 bytes a slice, where two matrices run side by side: a wave loads 64 rows of one of them.
+template <bool PAIR>
+__device__ __forceinline__ int codes_place(int r) {
+    return PAIR ? (r >> 7) * 128 + (r >> 5 & 1) * 64 + (r >> 6 & 1) * 32 + (r & 31) : r;
+}
+template <bool PAIR>
+__device__ __forceinline__ int codes_row(int place) {
+    return PAIR ? (place >> 7) * 128 + (place >> 5 & 1) * 64 + (place >> 6 & 1) * 32 + (place & 31) : place;
+}
+// Line of its own matrix that row i of a tile is: 32 rows of the one, then 32 of the other.
+template <bool PAIR>
+__device__ __forceinline__ int line_of(int i) {
+    return PAIR ? (i >> 6) * 32 + (i & 31) : i;
 }
 
-// Chunks of one operand's tile on their way through registers into LDS: codes, which are turned into 16 bits, and rows that do not
-// lie at 16-byte boundaries.  Offsets are 32 bits from the tile's first element (launches see to it that they fit).  Lines past the
-// operand's last are read as that one: only what lies past k has to be zero, in both operands, since rows and columns past the
-// result's end are not kept.
+// Chunks of one operand's slice on their way through registers into LDS, for rows that do not lie at 16-byte boundaries.  Offsets
+// are 32 bits from the tile's first element (launches see to it that they fit).  Lines past the operand's last are read as that
+// one: only what lies past k has to be zero, in both operands, since rows and columns past the result's end are not kept.
 template <Form FORM, int WIDTH, int THREADS, bool PAIR>
 struct Stage {
-    static constexpr int kChunks = FORM == kCodes ? WIDTH * 2 / THREADS : WIDTH * 8 / THREADS;
-    static_assert(kChunks > 0);
-    uint4_t v[kChunks];
-    uint32_t s[FORM == kCodes ? kChunks : 1];
-    uint32_t line[kChunks];        // byte of the chunk's line (kCodes: of its scales)
-    int64_t first, stride;         // bytes to the tile's first element, from line to line
-    int64_t span;                  // from there to the operand's end
+    static constexpr int kChunks = WIDTH * 4 / THREADS;
+    uint4_t v[2][kChunks];         // slices of even and odd number
+    uint32_t line[kChunks];        // byte of the chunk's line
+    const uint8_t* base[2];        // the tile's first element of either matrix
+    int64_t stride;                // bytes from line to line
+    int64_t span;                  // from the first element to the operand's end
     int chunk;                     // in its line; the same for all chunks of a thread
 
-    // Which of two matrices, where they run side by side: 32 lines of one, then 32 of the other.
-    static __device__ __forceinline__ int matrix(int j) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        return PAIR ? (wave + THREADS / 64 * j) >> (FORM == kCodes ? 0 : 2) & 1 : 0;
-    }
+    static __device__ __forceinline__ int matrix() { return PAIR ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 7) & 1 : 0; }
     __device__ __forceinline__ void start(const Operand& o, int64_t tile, int64_t extent, int64_t k) {
         const int64_t width = PAIR ? WIDTH / 2 : WIDTH, left = extent - tile * width;
-        stride = FORM == kCodes ? o.ld : 2 * o.ld;
+        stride = 2 * o.ld;
+        const int64_t first = tile * width * (FORM == kAcross ? 2 : stride);
+        base[0] = (const uint8_t*)o.data[0] + first;
+        base[1] = (const uint8_t*)o.data[1] + first;
         if constexpr (FORM == kAcross) {
             chunk = threadIdx.x % (WIDTH / 8);
-            first = 2 * tile * width;
             span = (k - 1) * stride + 2 * left;
 #pragma unroll
             for (int j = 0; j < kChunks; ++j) line[j] = (uint32_t)((threadIdx.x + THREADS * j) / (WIDTH / 8) * stride);
         } else {
-            constexpr int kIn = FORM == kCodes ? 2 : 8;       // chunks of a line
-            chunk = threadIdx.x % kIn;
-            first = tile * width * stride;
+            chunk = threadIdx.x & 3;
             span = (left - 1) * stride + 2 * k;
 #pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-                const int i = (threadIdx.x + THREADS * j) / kIn, at = PAIR ? (i >> 6) * 32 + (i & 31) : i;
-                line[j] = (uint32_t)(min((int64_t)at, left - 1) * stride);
-            }
+            for (int j = 0; j < kChunks; ++j) line[j] = (uint32_t)(min((int64_t)line_of<PAIR>((threadIdx.x + THREADS * j) >> 2), left - 1) * stride);
         }
     }
-    __device__ __forceinline__ void load(const Operand& o, int seg, int64_t k0) {
-        if constexpr (FORM == kCodes) {
-            const uint32_t b = (uint32_t)min(k0 / kBlock + chunk, o.ld - 1);
+    __device__ __forceinline__ void load(int odd, int seg, int64_t k0) {
+        const int64_t ahead = FORM == kAlong ? 2 * k0 : k0 * stride;
+        const int last = (int)min(span - ahead - 16, (int64_t)0x7ffffff0);      // below 0 where less than 16 bytes are left
+        const uint8_t* const at = ((PAIR ? matrix() : seg) ? base[1] : base[0]) + ahead;
 #pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-                v[j] = *reinterpret_cast<const uint4_t*>((const uint8_t*)o.data[matrix(j)] + first * kBlockBytes + (line[j] + b) * kBlockBytes);
-                s[j] = (o.scales[matrix(j)] + first)[line[j] + b];
-            }
-        } else {
-            const int64_t ahead = FORM == kAlong ? 2 * k0 : k0 * stride;
-            const int last = (int)min(span - ahead - 16, (int64_t)0x7ffffff0);      // below 0 where less than 16 bytes are left
+        for (int j = 0; j < kChunks; ++j) {
+            if (__builtin_expect(span >= 16, 1)) {      // a chunk that the operand's end cuts is read as its last 16 bytes
+                v[odd][j] = *reinterpret_cast<const uint4_a2*>(at + min((int)line[j] + 16 * chunk, last));
+            } else {                                    // seven elements at most
 #pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-                const uint8_t* const base = (const uint8_t*)o.data[PAIR ? matrix(j) : seg] + first + ahead;
-                if (__builtin_expect(span >= 16, 1)) {      // a chunk that the operand's end cuts is read as its last 16 bytes
-                    v[j] = *reinterpret_cast<const uint4_a2*>(base + min((int)line[j] + 16 * chunk, last));
-                } else {               // seven elements at most
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t x = *reinterpret_cast<const uint16_t*>(base + min((int64_t)line[j] + 16 * chunk + 2 * e, span - ahead - 2));
-                        v[j][e / 2] = e & 1 ? v[j][e / 2] | x << 16 : x;
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t x = *reinterpret_cast<const uint16_t*>(at + min((int64_t)line[j] + 16 * chunk + 2 * e, span - ahead - 2));
+                    v[odd][j][e / 2] = e & 1 ? v[odd][j][e / 2] | x << 16 : x;
                 }
             }
         }
     }
-    // In the last step: the elements of a cut chunk go to its front, what lies past k becomes zero.
-    __device__ __forceinline__ void trim(const Operand& o, int64_t k0, int64_t k) {
-        if (k0 + 64 < k) return;
-        const int left = (int)(k - k0), end = (int)(span - (FORM == kAlong ? 2 * k0 : k0 * stride)) - 16;     // of k; of the operand's bytes
+    // Into LDS.  In the last slice the elements of a cut chunk go to its front, and what lies past k becomes zero.
+    __device__ __forceinline__ void store(int odd, int64_t k0, int64_t k, unsigned char* lds) {
+        const int left = (int)min(k - k0, (int64_t)32), end = (int)min(span - (FORM == kAlong ? 2 * k0 : k0 * stride) - 16, (int64_t)0x7ffffff0);
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
-            if constexpr (FORM == kCodes) {
-                if (k0 / kBlock + chunk >= o.ld) v[j] = (uint4_t){0, 0, 0, 0}, s[j] = 0;
-            } else {
+            const int i = threadIdx.x + THREADS * j;
+            uint4_t x = v[odd][j];
+            if (k0 + 32 >= k) {
                 const int past = (int)line[j] + 16 * chunk - end, drop = span >= 16 ? max(0, min(past, 16)) / 2 : 0;
-                const int keep = FORM == kAlong ? left - 8 * chunk : (int)(threadIdx.x + THREADS * j) / (WIDTH / 8) < left ? 8 : 0;
-                uint4_t x = v[j];
+                const int keep = FORM == kAlong ? left - 8 * chunk : i / (WIDTH / 8) < left ? 8 : 0;
                 if (drop & 4) x = (uint4_t){x[2], x[3], 0, 0};
                 if (drop & 2) x = (uint4_t){x[1], x[2], x[3], 0};
                 if (drop & 1) x = (uint4_t){x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) x[w] &= (2 * w < keep ? 0xffffu : 0u) | (2 * w + 1 < keep ? 0xffff0000u : 0u);
-                v[j] = x;
             }
-        }
-    }
-    // shift: added to the scale bytes of a thread's rows (kCodes; rows stay a thread's own through all steps)
-    template <class T>
-    __device__ __forceinline__ void store(unsigned char* lds, const int* shift) const {
-#pragma unroll
-        for (int j = 0; j < kChunks; ++j) {
-            const int i = threadIdx.x + THREADS * j;
-            if constexpr (FORM == kAcross) {
-                *reinterpret_cast<uint4_t*>(lds + across_at<WIDTH>(i / (WIDTH / 8), i % (WIDTH / 8))) = v[j];
-            } else if constexpr (FORM == kCodes) {
-                const float scale = scale_of(s[j] == 255u ? 255u : (uint32_t)max(0, (int)s[j] + shift[j]));
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    *reinterpret_cast<uint4_t*>(lds + along_at(i >> 1, 4 * (i & 1) + c)) = from_codes8<T>(v[j][c], scale);
-            } else {
-                *reinterpret_cast<uint4_t*>(lds + along_at(i >> 3, i & 7)) = v[j];
-            }
+            *reinterpret_cast<uint4_t*>(lds + (FORM == kAcross ? across_at<WIDTH>(i / (WIDTH / 8), chunk) : along_at(i >> 2, chunk))) = x;
         }
     }
 };
 
-// 16 bytes a lane from byte `at` of a buffer of `size` bytes to the lane's place behind `lds`; zero past the buffer's end.  (The
-// host's pass over this file does not know the type of a buffer's description.)
+// BYTES (16, 4 or 1) a lane from byte `at` of a buffer of `size` bytes to LDS: lane by lane behind byte `lds` of it, at least four
+// bytes each; zero past the buffer's end.  Written as an instruction because the compiler, which does not see that reads of LDS
+// are of other slices, has them wait for every load that it knows to be on its way there.  What a wave has in flight is counted
+// where it meets the others.
+template <int BYTES>
 __device__ __forceinline__ void load_to_lds([[maybe_unused]] const uint8_t* buffer, [[maybe_unused]] uint32_t size, [[maybe_unused]] uint32_t at,
-                                            [[maybe_unused]] unsigned char* lds) {
+                                            [[maybe_unused]] uint32_t lds) {
 #ifdef __HIP_DEVICE_COMPILE__
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)buffer, 0, size, 0x00020000),
-                                             (__attribute__((address_space(3))) void*)lds, 16, at, 0, 0, 0);
+    const uint64_t p = (uint64_t)buffer;
+    const uint4_t d = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32) & 0xffffu),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(size), 0x00020000u};
+    lds = __builtin_amdgcn_readfirstlane(lds);
+    if constexpr (BYTES == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d) : "memory");
+    else if constexpr (BYTES == 4)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d) : "memory");
 #endif
+}
+__device__ __forceinline__ uint32_t lds_byte(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)p;
 }
 
 // The same straight into LDS: 16 bytes a lane, 1 KB a wave and turn, in the order of the lanes, so the chunks are dealt to their
 // banks by the lane's choice of source.  Reads past the operand's end come back as zero (the buffer's range check); rows must be
-// whole chunks at 16-byte boundaries.
+// whole chunks at 16-byte boundaries, as those of codes always are.
 template <Form FORM, int WIDTH, int THREADS, bool PAIR>
 struct Direct {
-    static constexpr int kChunks = WIDTH * 8 / THREADS;
+    static constexpr int kChunks = FORM == kCodes ? (WIDTH + THREADS - 1) / THREADS : WIDTH * 4 / THREADS;
+    static constexpr int kBytes = kChunks * THREADS * 16;  // of a slice; a workgroup wider than a tile of codes loads zeros behind it
+    static constexpr int kSlice = FORM == kFours ? 128 : 32;
     static constexpr uint32_t kNowhere = 0x80000000u;      // past every buffer
     uint32_t at[kChunks];          // byte of the lane's chunks from the tile's first, at k = 0
-    int64_t first, span, stride;   // byte of the tile's first row (kAcross: column), bytes from there to the operand's end, row to row
-    int chunk;                     // chunk of its row that a lane loads (kAlong, kFours); the same in every turn
+    const uint8_t* base[2];        // the tile's first row (kAcross: column) of either matrix
+    int64_t span, stride;          // bytes from there to the operand's end, from row to row
+    int chunk;                     // chunk of its row that a lane loads; the same in every turn
 
     __device__ __forceinline__ void start(const Operand& o, int64_t tile, int64_t extent, int64_t k) {
-        const int64_t width = PAIR ? WIDTH / 2 : WIDTH;
-        stride = FORM == kFours ? o.ld * kBlockBytes : o.ld * 2;
-        if constexpr (FORM == kAcross) {
-            chunk = 0;
-            first = tile * width * 2;
-            span = (k - 1) * stride + (extent - tile * width) * 2;
+        const int64_t width = PAIR ? WIDTH / 2 : WIDTH, left = extent - tile * width;
+        stride = FORM == kFours || FORM == kCodes ? o.ld * kBlockBytes : o.ld * 2;
+        const int64_t first = tile * width * (FORM == kAcross ? 2 : stride);
+        base[0] = (const uint8_t*)o.data[0] + first;
+        base[1] = (const uint8_t*)o.data[1] + first;
+        chunk = FORM == kAlong || FORM == kFours ? (threadIdx.x & 3) ^ along_turn(threadIdx.x >> 2) : 0;
+        span = FORM == kAcross ? (k - 1) * stride + 2 * left : FORM == kAlong ? (left - 1) * stride + 2 * k : left * stride;
 #pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-                const int i = threadIdx.x + THREADS * j, kk = i / (WIDTH / 8), c = i % (WIDTH / 8) ^ ((kk & 7) << 1 & (WIDTH / 8 - 1));
-                at[j] = tile * width + 8 * c < extent ? (uint32_t)(kk * stride + 16 * c) : kNowhere;
-            }
-        } else {
-            chunk = (threadIdx.x & 7) ^ (threadIdx.x >> 3 & 7);
-            first = tile * width * stride;
-            span = (extent - tile * width - 1) * stride + (FORM == kFours ? stride : 2 * k);
-#pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-                const int r = (threadIdx.x + THREADS * j) >> 3;
-                at[j] = (uint32_t)((PAIR ? (r >> 6) * 32 + (r & 31) : r) * stride + 16 * chunk);
+        for (int j = 0; j < kChunks; ++j) {
+            const int i = threadIdx.x + THREADS * j;
+            if constexpr (FORM == kAcross) {
+                const int kk = i / (WIDTH / 8), c = i % (WIDTH / 8) ^ across_turn<WIDTH>(kk);
+                at[j] = 8 * c < left ? (uint32_t)(kk * stride + 16 * c) : kNowhere;
+            } else if constexpr (FORM == kCodes) {
+                at[j] = i < WIDTH ? (uint32_t)(line_of<PAIR>(codes_row<PAIR>(i)) * stride) : kNowhere;
+            } else {
+                at[j] = (uint32_t)(line_of<PAIR>(i >> 2) * stride + 16 * chunk);
             }
         }
     }
-    __device__ __forceinline__ void issue(const Operand& o, int seg, int64_t k0, int64_t k, unsigned char* lds) const {
+    // Chunk j of the slice at k0; nothing but zeros where there is none any more.
+    __device__ __forceinline__ void issue(int j, int seg, int64_t k0, int64_t k, bool live, uint32_t lds) const {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int64_t ahead = FORM == kAcross ? k0 * stride : FORM == kFours ? k0 / 2 : k0 * 2;
-        const uint32_t left = (uint32_t)min(span - ahead, (int64_t)0x7ffffff0);
-        const bool in = FORM == kAcross || k0 + (FORM == kFours ? 32 : 8) * chunk < k;
-#pragma unroll
-        for (int j = 0; j < kChunks; ++j) {
-            const int which = PAIR ? (wave + THREADS / 64 * j) >> 2 & 1 : seg;
-            load_to_lds((const uint8_t*)o.data[which] + first + ahead, left, in ? at[j] : kNowhere, lds + (wave * 64 + THREADS * j) * 16);
-        }
+        const int which = !PAIR ? seg : FORM == kCodes ? wave & 1 : wave >> 1 & 1;
+        const int64_t ahead = FORM == kAcross ? k0 * stride : FORM == kAlong ? 2 * k0 : k0 / 2;
+        const uint32_t left = live ? (uint32_t)min(span - ahead, (int64_t)0x7ffffff0) : 0u;
+        // a row's chunks past its end would be the next row's
+        const bool in = FORM == kAcross || FORM == kCodes || k0 + (FORM == kFours ? 32 : 8) * chunk < k;
+        load_to_lds<16>((which ? base[1] : base[0]) + ahead, left, in ? at[j] : kNowhere, lds + (wave * 64 + THREADS * j) * 16);
     }
 };
 
-// All of a wave's loads into LDS have arrived and its reads of LDS are done; then all waves'.
+// All reads and writes of LDS by a wave are done and all but the last PENDING of its loads have arrived (64: whatever is in
+// flight may stay so); then the same of all waves.
+template <int PENDING>
 __device__ __forceinline__ void meet() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if constexpr (PENDING < 64) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PENDING) : "memory");
+    else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// The 16 bytes of an operand that a lane feeds to the matrix unit: row `base` + lane % 32 of the tile, step s.
+// The 16 bytes of an operand that a lane feeds to the matrix unit: row `base` + lane % 32 of the tile, half s of the slice.
 template <Form FORM, int WIDTH>
 __device__ __forceinline__ uint4_t fragment(const unsigned char* lds, int base, int s, int lane) {
     if constexpr (FORM == kAcross) {
@@ -240,33 +228,28 @@ __device__ __forceinline__ uint4_t fragment(const unsigned char* lds, int base, 
     }
 }
 
-constexpr int kSpan = 10;   // binary16: the largest scale of a row of codes is brought to 2^kSpan
+constexpr int larger(int a, int b) { return a > b ? a : b; }
 
 }  // namespace
 
-// A part of the steps of k, whose sums go to `partial` as fp32 [part][result][row][columns rounded up to 4, gate before up], where
-// there is more than one.
-struct Split {
-    int parts;
-    int64_t steps;         // of one part
-    float* partial;
-};
-
 // T: F16 or BF16 (results, and operands unless they are kFours).  WP x WQ waves, each TP x TQ tiles of 32 x 32.  DIRECT: operands
-// that need no conversion go straight into LDS.
+// of 16 bits go straight into LDS.
 template <class T, Form FP, Form FQ, bool GATED, int SEGS, int WP, int WQ, int TP, int TQ, bool DIRECT>
 __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Operand Q, Result res, Shape sh, Split split) {
     constexpr int kThreads = 64 * WP * WQ, kWidthP = 32 * WP * TP, kWidthQ = 32 * WQ * TQ;
-    constexpr int kBytesP = kWidthP * kRowBytes, kBytesQ = kWidthQ * kRowBytes;
-    constexpr int kStep = FP == kFours ? 256 : 64;       // k of a step
     constexpr bool kShifted = FP == kCodes && std::is_same<T, F16>::value;
-    constexpr bool kScaled = FP == kFours;
-    constexpr bool kDirectP = DIRECT && FP != kCodes;
-    constexpr int kTurns = kScaled ? (kWidthP + kWidthQ + kThreads - 1) / kThreads : 1;
-    using StageP = Stage<FP, kWidthP, kThreads, GATED>;
-    using StageQ = Stage<FQ, kWidthQ, kThreads, false>;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2][kBytesP + kBytesQ];
-    __shared__ uint2_t scales[kScaled ? 2 : 1][kScaled ? kWidthP + kWidthQ : 1];
+    constexpr bool kFour = FP == kFours, kCode = FP == kCodes;
+    constexpr bool kDirectP = DIRECT || kCode;
+    constexpr int kSlice = kFour ? 128 : 32;                             // k of a slice
+    using DirectP = Direct<FP, kWidthP, kThreads, GATED>;
+    using DirectQ = Direct<FQ, kWidthQ, kThreads, false>;
+    constexpr int kBytesP = kCode ? DirectP::kBytes : kWidthP * kRowBytes, kBytesSlice = kBytesP + kWidthQ * kRowBytes;
+    constexpr int kWide = GATED ? kWidthP / 2 : kWidthP;                 // columns of the tile's result
+    constexpr int kScaleRows = kFour ? kWidthP + kWidthQ : kWidthP;      // rows of a slice that have scales
+    constexpr int kScaleTurns = (kScaleRows + kThreads - 1) / kThreads;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[larger(kRing * kBytesSlice, 2 * kWide * kWidthQ)];
+    // four bytes of a row of a slice, or one at the place of its codes; a workgroup with more threads than rows loads zeros behind them
+    __shared__ uint32_t scales[kFour || kCode ? kRing : 1][kFour || kCode ? kScaleTurns * kThreads : 1];
     __shared__ int tops[kShifted ? kWidthP : 1];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % WP, wq = wave / WP;
@@ -278,31 +261,51 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     const int64_t strip = tile / (8 * sh.tiles_c), in_strip = tile % (8 * sh.tiles_c), tall = min((int64_t)8, sh.tiles_r - 8 * strip);
     const int64_t tr = 8 * strip + in_strip % tall, tc = in_strip / tall;
     const int second = SEGS == 1 ? blockIdx.z : 0;       // which of two results that share P
+    const int slices = (int)((sh.k + kSlice - 1) / kSlice);
+    const int begin = blockIdx.y * split.slices, end = min(SEGS * slices, begin + split.slices);
 
-    std::conditional_t<kDirectP, Direct<FP, kWidthP, kThreads, GATED>, StageP> sp;
-    std::conditional_t<DIRECT, Direct<FQ, kWidthQ, kThreads, false>, StageQ> sq;
+    std::conditional_t<kDirectP, DirectP, Stage<FP, kWidthP, kThreads, GATED>> sp;
+    std::conditional_t<DIRECT, DirectQ, Stage<FQ, kWidthQ, kThreads, false>> sq;
     sp.start(P, tc, sh.cols, sh.k);
     sq.start(Q, tr, sh.rows, sh.k);
-    int shift[StageP::kChunks] = {};
-    if constexpr (kShifted) {
-        // the largest scale of each row within the part's k; two threads share a row, 16 blocks each in turn
-        const int64_t b0 = blockIdx.y * split.steps * (kStep / kBlock), b1 = min(P.ld, b0 + split.steps * (kStep / kBlock));
+
+    // Scales: a lane loads those of its rows, a wave those of 64 rows of one matrix.  kCodes: a byte a slice, at the place of the
+    // row's codes; kFours: the four bytes of a slice, rows of P before those of Q.
+    const int uniform = __builtin_amdgcn_readfirstlane(wave);
+    const uint8_t* scale_base[kScaleTurns];
+    uint32_t scale_at[kScaleTurns], scale_size[kScaleTurns];
+    if constexpr (kFour || kCode) {
 #pragma unroll
-        for (int j = 0; j < StageP::kChunks; ++j) {
-            const int i = threadIdx.x + kThreads * j;
-            const uint8_t* const at = P.scales[sp.matrix(j)] + sp.first + sp.line[j];
-            int top = 0;
-            for (int64_t b = b0 + 16 * (i & 1); b < b1; b += 32) {
-                const uint4_t v = load_scales16(at + b, b1 - b);
+        for (int u = 0; u < kScaleTurns; ++u) {
+            const int first = 64 * uniform + kThreads * u, i = first + lane;
+            const bool of_q = kFour && first >= kWidthP;
+            const int which = kCode && GATED ? first >> 6 & 1 : 0;
+            const Operand& o = of_q ? Q : P;
+            const int64_t row0 = of_q ? tr * kWidthQ : tc * (kCode ? kWide : kWidthP), rows = (of_q ? sh.rows : sh.cols) - row0;
+            const int line = of_q ? i - kWidthP : kCode ? line_of<GATED>(codes_row<GATED>(i)) : i;
+            scale_base[u] = (which ? o.scales[1] : o.scales[0]) + row0 * o.ld_scales;
+            scale_at[u] = i < kScaleRows ? (uint32_t)(line * o.ld_scales) : 0x80000000u;
+            scale_size[u] = (uint32_t)min(rows * o.ld_scales, (int64_t)0x7ffffff0);
+        }
+    }
+    if constexpr (kShifted) {
+        // The largest scale of each row within the part's k, and from it the lanes' shifts of their rows' scales.
+        for (int i = threadIdx.x; i < kWidthP; i += kThreads) {
+            const uint8_t* const row = (GATED && (i >> 5 & 1) ? P.scales[1] : P.scales[0]) +
+                                       min(tc * kWide + line_of<GATED>(i), sh.cols - 1) * P.ld_scales;
+            int top = 0, b = begin;
+            for (; b + 16 <= end; b += 16) {
+                uint4_t v;
+                __builtin_memcpy(&v, row + b, 16);
 #pragma unroll
                 for (int w = 0; w < 16; ++w) {
-                    const int s = v[w / 4] >> (8 * (w & 3)) & 255;
+                    const uint32_t word = v[w / 4];
+                    const int s = word >> (8 * (w & 3)) & 255;
                     top = max(top, s == 255 ? 0 : s);
                 }
             }
-            top = max(top, swap_pair(top));
-            shift[j] = 127 + kSpan - top;
-            if ((i & 1) == 0) tops[i >> 1] = top;
+            for (; b < end; ++b) top = max(top, row[b] == 255 ? 0 : (int)row[b]);
+            tops[i] = top;
         }
     }
 
@@ -314,135 +317,253 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
 
-    const int64_t steps = (sh.k + kStep - 1) / kStep;
-    const int64_t begin = blockIdx.y * split.steps, end = min(SEGS * steps, begin + split.steps);
-    uint2_t sc[kTurns];
-    auto load = [&](int64_t step, int buf) {
-        const int seg = SEGS == 2 ? (int)(step >= steps) : 0;
-        const int64_t k0 = (SEGS == 2 ? step - seg * steps : step) * kStep;
-        if constexpr (kDirectP) sp.issue(P, seg, k0, sh.k, lds[buf]);
-        else sp.load(P, seg, k0);
-        if constexpr (DIRECT) sq.issue(Q, SEGS == 2 ? seg : second, k0, sh.k, lds[buf] + kBytesP);
-        else sq.load(Q, SEGS == 2 ? seg : second, k0);
-        if constexpr (kScaled) {
-            // the eight scales of one row of either operand
+    // What goes into LDS by way of registers: two slices on the way, of even and odd number.
+    auto load = [&](int slice, int odd) {
+        slice = min(slice, end - 1);       // past the end: of no use, but the loads in flight are counted
+        [[maybe_unused]] const int seg = SEGS == 2 && slice >= slices ? 1 : 0;
+        [[maybe_unused]] const int64_t k0 = (int64_t)(slice - seg * slices) * kSlice;
+        if constexpr (!kDirectP) sp.load(odd, seg, k0);
+        if constexpr (!DIRECT) sq.load(odd, SEGS == 2 ? seg : second, k0);
+    };
+    auto store = [&](int slice, int odd) {
+        if (slice >= end) return;
+        [[maybe_unused]] const int at = (slice - begin) & (kRing - 1);
+        [[maybe_unused]] const int64_t k0 = (int64_t)(SEGS == 2 && slice >= slices ? slice - slices : slice) * kSlice;
+        if constexpr (!kDirectP) sp.store(odd, k0, sh.k, lds + at * kBytesSlice);
+        if constexpr (!DIRECT) sq.store(odd, k0, sh.k, lds + at * kBytesSlice + kBytesP);
+    };
+    // What goes straight into LDS: load j of a slice's kLoads.
+    constexpr int kLoadsP = kDirectP ? DirectP::kChunks : 0, kLoadsPQ = kLoadsP + (DIRECT ? DirectQ::kChunks : 0);
+    constexpr int kLoads = kLoadsPQ + (kFour || kCode ? kScaleTurns : 0);
+    const uint32_t lds0 = lds_byte(lds), scales0 = lds_byte(scales);
+    auto issue = [&](int slice, int j) {
+        const int seg = SEGS == 2 && slice >= slices ? 1 : 0;
+        const int64_t k0 = (int64_t)(slice - seg * slices) * kSlice;
+        const int place = (slice - begin) & (kRing - 1);
+        const uint32_t to = lds0 + place * kBytesSlice;
+        if constexpr (kDirectP)
+            if (j < kLoadsP) sp.issue(j, seg, k0, sh.k, slice < end, to);
+        if constexpr (DIRECT)
+            if (j >= kLoadsP && j < kLoadsPQ) sq.issue(j - kLoadsP, SEGS == 2 ? seg : second, k0, sh.k, slice < end, to + kBytesP);
+        if constexpr (kFour || kCode) {
+            if (j >= kLoadsPQ) {
+                const int u = j - kLoadsPQ, ahead = kFour ? 4 * slice : slice;
+                load_to_lds<kFour ? 4 : 1>(scale_base[u] + ahead, slice < end ? scale_size[u] - ahead : 0u, scale_at[u],
+                                           scales0 + place * (kScaleTurns * kThreads * 4) + (64 * uniform + kThreads * u) * 4);
+            }
+        }
+    };
+
+    // Fragment n of the kReads of half a slice.
+    constexpr int kReads = TP + TQ, kProducts = TP * TQ;
+    struct Pieces {
+        uint4_t a[TP], b[TQ];      // a[][0] alone: eight codes
+    };
+    auto read = [&](Pieces& f, int at, int s, int n) {
+        const unsigned char *lp = lds + at * kBytesSlice, *lq = lp + kBytesP;
+        if (n >= TP) f.b[n - TP] = fragment<FQ == kAcross ? kAcross : kAlong, kWidthQ>(lq, 32 * (wq * TQ + n - TP), s, lane);
+        else if constexpr (kCode)
+            f.a[n][0] = *reinterpret_cast<const uint32_t*>(lp + codes_place<GATED>(32 * (wp * TP + n) + (lane & 31)) * 16 + 8 * s + 4 * (lane >> 5));
+        else f.a[n] = fragment<FP == kAcross ? kAcross : kAlong, kWidthP>(lp, 32 * (wp * TP + n), s, lane);
+    };
+    // Scales of the lane's rows in a slice: kFours: lanes from 32 on have every second block; kCodes: one block.
+    uint32_t ea[TP], eb[TQ];
+    int shift[TP];
+    uint32_t na[TP], nb[TQ];       // of the next slice, as they lie in LDS
+    auto read_scales = [&](int at) {
+        if constexpr (kFour || kCode) {
 #pragma unroll
-            for (int u = 0; u < kTurns; ++u) {
-                const int i = threadIdx.x + kThreads * u;
-                sc[u] = (uint2_t){0, 0};
-                const Operand& o = i < kWidthP ? P : Q;
-                const int64_t row = i < kWidthP ? tc * kWidthP + i : tr * kWidthQ + (i - kWidthP), b = k0 / kBlock;
-                if (i >= kWidthP + kWidthQ || row >= (i < kWidthP ? sh.cols : sh.rows)) continue;
-                const uint8_t* const at = o.scales[0] + row * o.ld + b;
-                if (b + 8 <= o.ld) {
-                    __builtin_memcpy(&sc[u], at, 8);
+            for (int i = 0; i < TP; ++i) na[i] = scales[at][codes_place<kCode && GATED>(32 * (wp * TP + i) + (lane & 31))];
+        }
+        if constexpr (kFour) {
+#pragma unroll
+            for (int i = 0; i < TQ; ++i) nb[i] = scales[at][kWidthP + 32 * (wq * TQ + i) + (lane & 31)];
+        }
+    };
+    auto take_scales = [&]() {
+        if constexpr (kFour) {
+#pragma unroll
+            for (int i = 0; i < TP; ++i) ea[i] = na[i] >> (8 * (lane >> 5));
+#pragma unroll
+            for (int i = 0; i < TQ; ++i) eb[i] = nb[i] >> (8 * (lane >> 5));
+        }
+        if constexpr (kCode) {
+#pragma unroll
+            for (int i = 0; i < TP; ++i) ea[i] = (kShifted && na[i] != 255u ? (uint32_t)max(0, (int)na[i] + shift[i]) : na[i]) << 23;
+        }
+    };
+    // The products of half a slice, then(n) behind the n-th.
+    auto multiply = [&](const Pieces& f, int s, auto then) {
+#pragma unroll
+        for (int i = 0; i < TP; ++i) {
+            uint4_t a = f.a[i];
+            if constexpr (kCode) a = from_codes8<T>(a[0], __uint_as_float(ea[i]));
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) {
+                if constexpr (kFour) {
+                    const int8v_t fa = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+                    const int8v_t fb = {(int)f.b[j][0], (int)f.b[j][1], (int)f.b[j][2], (int)f.b[j][3], 0, 0, 0, 0};
+                    if (s) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 2, ea[i], 2, eb[j]);
+                    else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 0, ea[i], 0, eb[j]);
                 } else {
-#pragma unroll
-                    for (int j = 0; j < 7; ++j)
-                        if (b + j < o.ld) sc[u][j / 4] |= (uint32_t)at[j] << (8 * (j & 3));
+                    acc[i][j] = T::mfma32(a, f.b[j], acc[i][j]);
                 }
+                then(i * TQ + j);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
-    auto store = [&](int64_t step, int buf) {
-        const int64_t k0 = (SEGS == 2 && step >= steps ? step - steps : step) * kStep;
-        if constexpr (!kDirectP) {
-            sp.trim(P, k0, sh.k);
-            sp.template store<T>(lds[buf], shift);
-        }
-        if constexpr (!DIRECT) {
-            sq.trim(Q, k0, sh.k);
-            sq.template store<T>(lds[buf] + kBytesP, nullptr);
-        }
-        if constexpr (kScaled) {
+    // Item n of `count` things that are spread over the products.
+    auto spread = [&](int from, int to, int n, auto thing) {
 #pragma unroll
-            for (int u = 0; u < kTurns; ++u)
-                if (threadIdx.x + kThreads * u < kWidthP + kWidthQ) scales[buf][threadIdx.x + kThreads * u] = sc[u];
-        }
+        for (int j = from; j < to; ++j)
+            if ((j - from) * kProducts / (to - from) == n) thing(j);
     };
 
-    if (begin < end) {
-        load(begin, 0);
-        store(begin, 0);
+    // Slice i is multiplied in two halves.  Behind the first half all waves meet: the fragments of the second are in registers by then,
+    // slice i + 1 is in LDS, and the place of slice i is free for slice i + kRing, half of whose loads are issued during the second
+    // half and half during the first of the next slice.  So a load has nearly kRing - 1 slices to arrive, and products, reads and loads
+    // alternate, which keeps any of them from holding up the products behind it.
+    constexpr int kEarly = (kLoads + 1) / 2;
+    constexpr int kPending = kLoads ? (kRing - 2) * kLoads : 64;       // registers that loads go to are waited for where they are used
+#pragma unroll
+    for (int u = 0; u < kRing; ++u)
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) issue(begin + u, j);
+    load(begin, 0);
+    store(begin, 0);
+    load(begin + 1, 1);
+    load(begin + 2, 0);
+    meet<kLoads ? (kRing - 1) * kLoads : 64>();
+    if constexpr (kShifted) {
+#pragma unroll
+        for (int i = 0; i < TP; ++i) shift[i] = 127 + kSpan - tops[32 * (wp * TP + i) + (lane & 31)];
     }
-    meet();
-    for (int64_t step = begin; step < end; ++step) {
-        const int buf = (int)((step - begin) & 1);
-        if (step + 1 < end) load(step + 1, buf ^ 1);
-        const unsigned char *lp = lds[buf], *lq = lds[buf] + kBytesP;
-        uint2_t ea[TP], eb[TQ];     // scales of the lane's rows: lanes from 32 on have every second block
-        if constexpr (kScaled) {
+    Pieces f[2];
+    read_scales(0);
+    take_scales();
 #pragma unroll
-            for (int i = 0; i < TP; ++i) ea[i] = scales[buf][32 * (wp * TP + i) + (lane & 31)] >> (8 * (lane >> 5));
-#pragma unroll
-            for (int i = 0; i < TQ; ++i) eb[i] = scales[buf][kWidthP + 32 * (wq * TQ + i) + (lane & 31)] >> (8 * (lane >> 5));
-        }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            uint4_t a[TP], b[TQ];
-#pragma unroll
-            for (int i = 0; i < TP; ++i) a[i] = fragment<FP == kAcross ? kAcross : kAlong, kWidthP>(lp, 32 * (wp * TP + i), s, lane);
-#pragma unroll
-            for (int i = 0; i < TQ; ++i) b[i] = fragment<FQ == kAcross ? kAcross : kAlong, kWidthQ>(lq, 32 * (wq * TQ + i), s, lane);
-            if constexpr (kScaled) {
-#pragma unroll
-                for (int i = 0; i < TP; ++i)
-#pragma unroll
-                    for (int j = 0; j < TQ; ++j) {
-                        const int8v_t fa = {(int)a[i][0], (int)a[i][1], (int)a[i][2], (int)a[i][3], 0, 0, 0, 0};
-                        const int8v_t fb = {(int)b[j][0], (int)b[j][1], (int)b[j][2], (int)b[j][3], 0, 0, 0, 0};
-                        // step s takes bytes 0 and 2 of the first word, then of the second
-                        if (s & 1) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 2, ea[i][s / 2], 2, eb[j][s / 2]);
-                        else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa, fb, acc[i][j], 4, 4, 0, ea[i][s / 2], 0, eb[j][s / 2]);
-                    }
-
-            } else {
-#pragma unroll
-                for (int i = 0; i < TP; ++i)
-#pragma unroll
-                    for (int j = 0; j < TQ; ++j) acc[i][j] = T::mfma32(a[i], b[j], acc[i][j]);
-            }
-        }
-        if (step + 1 < end) store(step + 1, buf ^ 1);
-        meet();
+    for (int n = 0; n < kReads; ++n) read(f[0], 0, 0, n);
+    auto turn = [&](int slice, int odd) {
+        const int at = (slice - begin) & (kRing - 1), next = (slice + 1 - begin) & (kRing - 1);
+        multiply(f[0], 0, [&](int n) {
+            spread(0, kReads, n, [&](int r) { read(f[1], at, 1, r); });
+            if (slice > begin) spread(kEarly, kLoads, n, [&](int j) { issue(slice - 1 + kRing, j); });
+        });
+        store(slice + 1, odd ^ 1);
+        meet<kPending>();
+        load(slice + 3, odd ^ 1);
+        read_scales(next);
+        multiply(f[1], 1, [&](int n) {
+            spread(0, kReads, n, [&](int r) { read(f[0], next, 0, r); });
+            spread(0, kEarly, n, [&](int j) { issue(slice + kRing, j); });
+        });
+        take_scales();
+    };
+    for (int slice = begin; slice < end; slice += 2) {
+        turn(slice, 0);
+        if (slice + 1 < end) turn(slice + 1, 1);
     }
+    meet<0>();
 
     // A lane has columns 8 g + 4 (lane / 32) .. + 3, g = 0 .. 3, of row lane % 32 of every tile of 32 x 32.
-    uint16_t* const out = res.out[second];
-    const int64_t wide = (sh.cols + 3) / 4 * 4, ld_partial = GATED ? 2 * wide : wide;
-    float* const partial = split.parts > 1 ? split.partial + ((int64_t)blockIdx.y * gridDim.z + blockIdx.z) * sh.rows * ld_partial : nullptr;
+    const int half = 4 * (lane >> 5);
+    if constexpr (kShifted) {
 #pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-        const int64_t row = tr * kWidthQ + 32 * (wq * TQ + j) + (lane & 31);
-        if (row >= sh.rows) continue;
+        for (int i = 0; i < TP; ++i)
 #pragma unroll
-        for (int i = 0; i < TP; i += GATED ? 2 : 1) {
-            const int at = 32 * (wp * TP + i);
+            for (int v = 0; v < 16; ++v) {
+                const int e = tops[32 * (wp * TP + i) + 8 * (v / 4) + half + v % 4] - (127 + kSpan);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int in_tile = 8 * g + 4 * (lane >> 5);
-                const int64_t col = GATED ? tc * (kWidthP / 2) + at / 2 + in_tile : tc * kWidthP + at + in_tile;
-                const int64_t left = sh.cols - col;
-                if (left <= 0) continue;
-                float4_t x, y = {};
+                for (int j = 0; j < TQ; ++j) acc[i][j][v] = ldexpf(acc[i][j][v], e);
+            }
+    }
+    const int64_t col0 = tc * kWide, row0 = tr * kWidthQ;
+    if (split.parts > 1) {
+        const int64_t wide = (sh.cols + 3) / 4 * 4, ld = GATED ? 2 * wide : wide;
+        float* const partial = split.partial + ((int64_t)blockIdx.y * gridDim.z + blockIdx.z) * sh.rows * ld;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    x[v] = acc[i][j][4 * g + v];
-                    if constexpr (kShifted) x[v] = ldexpf(x[v], tops[at + in_tile + v] - (127 + kSpan));
-                    if constexpr (GATED) {
-                        y[v] = acc[i + 1][j][4 * g + v];
-                        if constexpr (kShifted) y[v] = ldexpf(y[v], tops[at + 32 + in_tile + v] - (127 + kSpan));
-                    }
+        for (int j = 0; j < TQ; ++j) {
+            const int64_t row = row0 + 32 * (wq * TQ + j) + (lane & 31);
+#pragma unroll
+            for (int i = 0; i < TP; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int at = 32 * (wp * TP + i);
+                    const int64_t col = col0 + (GATED ? at / 64 * 32 : at) + 8 * g + half;
+                    if (row < sh.rows && col < sh.cols)
+                        *reinterpret_cast<float4_t*>(partial + row * ld + (GATED && i % 2 ? wide : 0) + col) =
+                            (float4_t){acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
                 }
-                if (partial) {
-                    *reinterpret_cast<float4_t*>(partial + row * ld_partial + col) = x;
-                    if constexpr (GATED) *reinterpret_cast<float4_t*>(partial + row * ld_partial + wide + col) = y;
+        }
+        return;
+    }
+    // Rounded, a result goes through LDS (its chunks dealt to the banks by their row) and leaves in whole lines.
+    constexpr int kTurn = (kWide < 128 ? kWide : 128) / 8 - 1;
+    unsigned char* const turned = lds;
+    auto put = [&](int i, int j, int g, uint2_t v) {
+        const int row = 32 * (wq * TQ + j) + (lane & 31), at = 32 * (wp * TP + i), col = (GATED ? at / 64 * 32 : at) + 8 * g;
+        *reinterpret_cast<uint2_t*>(turned + row * (2 * kWide) + ((col / 8 ^ (row & kTurn)) << 4) + 2 * half) = v;
+    };
+    auto leave = [&](uint16_t* out, int64_t ld) {
+        __syncthreads();
+        constexpr int kIn = kWide / 8;         // chunks of a row
+#pragma unroll 4
+        for (int n = threadIdx.x; n < kIn * kWidthQ; n += kThreads) {
+            const int row = n / kIn, c = n % kIn;
+            const int64_t left = sh.cols - col0 - 8 * c;
+            const uint4_t v = *reinterpret_cast<const uint4_t*>(turned + row * (2 * kWide) + ((c ^ (row & kTurn)) << 4));
+            uint16_t* const at = out + (row0 + row) * ld + col0 + 8 * c;
+            if (row0 + row < sh.rows) {
+                if (left >= 8) {
+                    *reinterpret_cast<uint4_a2*>(at) = v;
                 } else {
-                    finish<T, GATED>(res, out, row, col, left, x, y);
+                    for (int e = 0; e < left; ++e) at[e] = (uint16_t)((e & 4 ? (e & 2 ? v[3] : v[2]) : (e & 2 ? v[1] : v[0])) >> (16 * (e & 1)));
                 }
             }
         }
+        __syncthreads();
+    };
+    auto each = [&](auto value) {
+#pragma unroll
+        for (int i = 0; i < TP; i += GATED ? 2 : 1)
+#pragma unroll
+            for (int j = 0; j < TQ; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) put(i, j, g, (uint2_t){T::pair(value(i, j, 4 * g), value(i, j, 4 * g + 1)), T::pair(value(i, j, 4 * g + 2), value(i, j, 4 * g + 3))});
+    };
+    if constexpr (GATED) {
+        if (res.gate) {
+            each([&](int i, int j, int v) { return acc[i][j][v]; });
+            leave(res.gate, res.ld_gate);
+            each([&](int i, int j, int v) { return acc[i + 1][j][v]; });
+            leave(res.up, res.ld_gate);
+        }
+        auto finished = [&](auto act) {
+            each([&](int i, int j, int v) { return act_of(decltype(act)::value, acc[i][j][v]) * acc[i + 1][j][v]; });
+        };
+        if (res.act == kSilu) finished(std::integral_constant<int, kSilu>());
+        else if (res.act == kGelu) finished(std::integral_constant<int, kGelu>());
+        else finished(std::integral_constant<int, kRelu>());
+    } else {
+        each([&](int i, int j, int v) { return acc[i][j][v]; });
     }
+    leave(res.out[second], res.ld);
+}
+
+// Rows of scales at multiples of four bytes, as lanes load them four at a time: those of W, then those of X.
+__global__ __launch_bounds__(256) void rsh_align_scales_kernel(const uint8_t* __restrict__ W, const uint8_t* __restrict__ X, uint32_t* __restrict__ out,
+                                                               int64_t n, int64_t t, int blocks) {
+    const int words = (blocks + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (n + t) * words) return;
+    const int64_t row = i / words, b = 4 * (i - row * words);
+    const uint8_t* const at = row < n ? W + row * blocks : X + (row - n) * blocks;
+    uint32_t v = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (b + j < blocks) v |= (uint32_t)at[b + j] << (8 * j);
+    out[i] = v;
 }
 
 // Sums of the parts in their order, and what a tile does with finished sums.  A thread has four columns.
@@ -508,7 +629,7 @@ constexpr int64_t kTall[3] = {256, 128, 64}, kWide[3] = {256, 128, 128};
 // The form and the parts whose rounds of workgroups take the least time, in units of a step of a lone workgroup of 256 x 256:
 // `steps` of k in all, `pairs`: columns come in two matrices, `results` products side by side.
 Choice choose(int64_t rows, int64_t cols, int64_t steps, bool pairs, int results) {
-    constexpr double step[3] = {1.0, 0.33, 0.2};      // a step of one workgroup with its neighbours on the compute unit
+    constexpr double step[3] = {0.5, 0.165, 0.1};      // a step of one workgroup with its neighbours on the compute unit
     constexpr int room[3] = {1, 2, 3};                 // workgroups of a compute unit
     Choice best = {0, 1};
     double least = 1e300;
@@ -523,7 +644,7 @@ Choice choose(int64_t rows, int64_t cols, int64_t steps, bool pairs, int results
             if (parts > 1) t += 4.0 + 8e-6 * (double)(parts * rows * cols * results * (pairs ? 2 : 1));
             if (t < least) {
                 least = t;
-                best = {form, parts};
+                best = {form, (int)((steps + each - 1) / each)};
             }
         }
     }
@@ -552,12 +673,12 @@ void launch_tiles(int form, dim3 grid, const Operand& P, const Operand& Q, const
 
 template <class T, Form FP, Form FQ, bool GATED, int SEGS>
 void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, int results, void* work, hipStream_t st) {
-    constexpr int64_t kStep = FP == kFours ? 256 : 64;
-    const int64_t steps = SEGS * ((k + kStep - 1) / kStep);
+    constexpr int64_t kSlice = FP == kFours ? 128 : 32;
+    const int64_t steps = SEGS * ((k + kSlice - 1) / kSlice);
     const Choice c = choose(rows, cols, steps, GATED, results);
     const int64_t wide = kWide[c.form] / (GATED ? 2 : 1), tall = kTall[c.form], each = (steps + c.parts - 1) / c.parts;
     const Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
-    const Split split = {c.parts, each, (float*)work};
+    const Split split = {c.parts, (int)each, (float*)work};
     const int64_t tiles = (int64_t)sh.tiles_r * sh.tiles_c;
     const dim3 grid((unsigned)((tiles + 7) / 8 * 8), c.parts, results);
     if constexpr (FP != kFours) {
@@ -580,38 +701,57 @@ void by_half(int type, F f) {
 
 }  // namespace
 
+// Bytes of the scales of both operands in rows of whole words, where theirs are not.
+int64_t aligned_scales(int x_type, int64_t t, int64_t n, int64_t k) {
+    const int64_t blocks = (k + kBlock - 1) / kBlock;
+    if (x_type != RSH_MX4 || blocks % 4 == 0) return 0;
+    return ((n + t) * ((blocks + 3) / 4) * 4 + 15) / 16 * 16;
+}
+
 int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k) {
-    const int64_t step = x_type == RSH_MX4 ? 256 : 64;
+    const int64_t step = x_type == RSH_MX4 ? 128 : 32;
     if (takes_few(t, x_type == RSH_MX4)) return 0;
-    return partial_bytes(choose(t, n, (k + step - 1) / step, false, 1), t, n, false, 1);
+    return aligned_scales(x_type, t, n, k) + partial_bytes(choose(t, n, (k + step - 1) / step, false, 1), t, n, false, 1);
 }
 
 int64_t gated_forward_work(int64_t t, int64_t d, int64_t f) {
     if (takes_few(t, false)) return 0;
-    return partial_bytes(choose(t, f, (d + 63) / 64, true, 1), t, f, true, 1);
+    return partial_bytes(choose(t, f, (d + 31) / 32, true, 1), t, f, true, 1);
 }
 
 // dG and dU, and behind them the larger of the sums of dX and of the weights' gradients (of both, or of one alone).
 int64_t gated_backward_work(int64_t t, int64_t d, int64_t f) {
     const int64_t gates = 4 * t * ((f + 7) / 8 * 8);
-    int64_t sums = partial_bytes(choose(t, d, 2 * ((f + 63) / 64), false, 1), t, d, false, 1);
+    int64_t sums = partial_bytes(choose(t, d, 2 * ((f + 31) / 32), false, 1), t, d, false, 1);
     for (int results = 1; results <= 2; ++results)
-        sums = std::max(sums, partial_bytes(choose(f, d, (t + 63) / 64, false, results), f, d, false, results));
+        sums = std::max(sums, partial_bytes(choose(f, d, (t + 31) / 32, false, results), f, d, false, results));
     return gates + sums;
 }
 
 int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int y_type,
                        int64_t t, int64_t n, int64_t k, void* work, void* stream) {
     const int64_t blocks = (k + kBlock - 1) / kBlock;
-    const Operand p = {{W, nullptr}, {(const uint8_t*)w_scales, nullptr}, blocks};
-    const Operand q = {{X, nullptr}, {(const uint8_t*)x_scales, nullptr}, x_type == RSH_MX4 ? blocks : ld_x};
+    const Operand p = {{W, nullptr}, {(const uint8_t*)w_scales, nullptr}, blocks, blocks};
+    const Operand q = {{X, nullptr}, {(const uint8_t*)x_scales, nullptr}, x_type == RSH_MX4 ? blocks : ld_x, blocks};
     const Result res = {{(uint16_t*)Y, nullptr}, nullptr, nullptr, n, 0, 0};
     by_half(y_type, [&](auto half) {
         using T = decltype(half);
         if (takes_few(t, x_type == RSH_MX4)) {
             if (x_type == RSH_MX4) launch_few<T, kFours, false>(p, q, res, t, n, k, (hipStream_t)stream);
             else launch_few<T, kCodes, false>(p, q, res, t, n, k, (hipStream_t)stream);
-        } else if (x_type == RSH_MX4) product<T, kFours, kFours, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
+        } else if (x_type == RSH_MX4) {
+            Operand w = p, x = q;
+            const int64_t bytes = aligned_scales(x_type, t, n, k);
+            if (bytes) {
+                w.ld_scales = x.ld_scales = (blocks + 3) / 4 * 4;
+                const int64_t words = (n + t) * (w.ld_scales / 4);
+                hipLaunchKernelGGL(rsh_align_scales_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, (hipStream_t)stream,
+                                   (const uint8_t*)w_scales, (const uint8_t*)x_scales, (uint32_t*)work, n, t, (int)blocks);
+                w.scales[0] = (const uint8_t*)work;
+                x.scales[0] = w.scales[0] + n * w.ld_scales;
+            }
+            product<T, kFours, kFours, false, 1>(w, x, res, t, n, k, 1, (uint8_t*)work + bytes, (hipStream_t)stream);
+        }
         else product<T, kCodes, kAlong, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
     });
     return launched();
@@ -620,8 +760,8 @@ int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t 
 int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
                          const void* u_scales, int act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* work, void* stream) {
     const int64_t blocks = (d + kBlock - 1) / kBlock;
-    const Operand p = {{Wg, Wu}, {(const uint8_t*)g_scales, (const uint8_t*)u_scales}, g_scales ? blocks : ld_w};
-    const Operand q = {{X, nullptr}, {nullptr, nullptr}, ld_x};
+    const Operand p = {{Wg, Wu}, {(const uint8_t*)g_scales, (const uint8_t*)u_scales}, g_scales ? blocks : ld_w, blocks};
+    const Operand q = {{X, nullptr}, {nullptr, nullptr}, ld_x, 0};
     const Result res = {{(uint16_t*)H, nullptr}, (uint16_t*)G, (uint16_t*)U, f, (f + 7) / 8 * 8, act};
     by_half(type, [&](auto half) {
         using T = decltype(half);
@@ -642,18 +782,18 @@ int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg,
     uint16_t* const dG = (uint16_t*)work;
     uint16_t* const dU = dG + t * ld_gate;
     void* const sums = dU + t * ld_gate;
-    const Operand gates = {{dG, dU}, {nullptr, nullptr}, ld_gate};
+    const Operand gates = {{dG, dU}, {nullptr, nullptr}, ld_gate, 0};
     by_half(type, [&](auto half) {
         using T = decltype(half);
         hipLaunchKernelGGL(rsh_gate_backward_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, (const uint16_t*)dH, (const uint16_t*)G,
                            (const uint16_t*)U, dG, dU, t, f, ld_h, ld_gate, act);
         if (dX) {
-            const Operand w = {{Wg, Wu}, {nullptr, nullptr}, ld_w};
+            const Operand w = {{Wg, Wu}, {nullptr, nullptr}, ld_w, 0};
             const Result res = {{(uint16_t*)dX, nullptr}, nullptr, nullptr, d, 0, 0};
             product<T, kAcross, kAlong, false, 2>(w, gates, res, t, d, f, 1, sums, st);
         }
         if (dWg || dWu) {
-            const Operand x = {{X, nullptr}, {nullptr, nullptr}, ld_x}, only_u = {{dU, nullptr}, {nullptr, nullptr}, ld_gate};
+            const Operand x = {{X, nullptr}, {nullptr, nullptr}, ld_x, 0}, only_u = {{dU, nullptr}, {nullptr, nullptr}, ld_gate, 0};
             const Result res = {{(uint16_t*)(dWg ? dWg : dWu), (uint16_t*)dWu}, nullptr, nullptr, d, 0, 0};
             product<T, kAcross, kAcross, false, 1>(x, dWg ? gates : only_u, res, f, d, t, dWg && dWu ? 2 : 1, sums, st);
         }

@@ -17,6 +17,7 @@ struct Operand {
     const void* data[2];           // two matrices of equal shape (gate and up), or one
     const uint8_t* scales[2];
     int64_t ld;                    // elements (kAlong, kAcross) or blocks (kCodes, kFours) from row to row
+    int64_t ld_scales;             // bytes from row to row of the scales
 };
 
 enum Act { kSilu = RSH_ACT_SILU, kGelu = RSH_ACT_GELU, kRelu = RSH_ACT_RELU };

@@ -66,8 +66,8 @@ class Mx4:
                 raise ValueError(f"{name}: expected contiguous uint8 [rows, {width}] for k = {k}, got {t.dtype} {tuple(t.shape)}")
         if codes.shape[0] != scales.shape[0] or codes.device != scales.device or codes.device.type != "cuda":
             raise ValueError(f"codes and scales: {tuple(codes.shape)} on {codes.device} against {tuple(scales.shape)} on {scales.device}")
-        if codes.data_ptr() % 16:
-            raise ValueError("codes: expected 16-byte alignment")
+        if codes.data_ptr() % 16 or scales.data_ptr() % 4:
+            raise ValueError("codes and scales: expected alignment to 16 and 4 bytes")
         self.codes, self.scales, self.shape = codes, scales, (codes.shape[0], k)
 
     @classmethod
