@@ -139,25 +139,29 @@ struct Stage {
     }
 };
 
-// BYTES (16, 4 or 1) a lane from byte `at` of a buffer of `size` bytes to LDS: lane by lane behind byte `lds` of it, at least four
-// bytes each; zero past the buffer's end.  Written as an instruction because the compiler, which does not see that reads of LDS
-// are of other slices, has them wait for every load that it knows to be on its way there.  What a wave has in flight is counted
-// where it meets the others.
-template <int BYTES>
-__device__ __forceinline__ void load_to_lds([[maybe_unused]] const uint8_t* buffer, [[maybe_unused]] uint32_t size, [[maybe_unused]] uint32_t at,
-                                            [[maybe_unused]] uint32_t lds) {
+// Where a wave reads: a buffer's description, the same in all lanes.
+struct Buffer {
+    uint64_t at;
+    uint32_t size;     // bytes; reads past them come back as zero
+};
+
+// BYTES (16, 4 or 1) a lane from byte `at` of a buffer to LDS: lane by lane behind byte `lds` + PLUS of it, at least four bytes each.
+// Written as an instruction because the compiler, which does not see that reads of LDS are of other slices, has them wait for every
+// load that it knows to be on its way there.  What a wave has in flight is counted where it meets the others.
+template <int BYTES, int PLUS>
+__device__ __forceinline__ void load_to_lds([[maybe_unused]] Buffer buffer, [[maybe_unused]] uint32_t at, [[maybe_unused]] uint32_t lds) {
 #ifdef __HIP_DEVICE_COMPILE__
-    const uint64_t p = (uint64_t)buffer;
-    const uint4_t d = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32) & 0xffffu),
-                       (uint32_t)__builtin_amdgcn_readfirstlane(size), 0x00020000u};
-    lds = __builtin_amdgcn_readfirstlane(lds);
-    if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d) : "memory");
-    else if constexpr (BYTES == 4)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d) : "memory");
-    else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d) : "memory");
+    const uint4_t d = {(uint32_t)buffer.at, (uint32_t)(buffer.at >> 32), buffer.size, 0x00020000u};
+#define RSH_LOAD(name) asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\t" name " %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d), "n"(PLUS) : "memory", "scc")
+    if constexpr (BYTES == 16) RSH_LOAD("buffer_load_dwordx4");
+    else if constexpr (BYTES == 4) RSH_LOAD("buffer_load_dword");
+    else RSH_LOAD("buffer_load_ubyte");
+#undef RSH_LOAD
 #endif
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint64_t uniform_address(const void* p) {
+    return (uint64_t)uniform((uint32_t)((uint64_t)p >> 32) & 0xffffu) << 32 | uniform((uint32_t)(uint64_t)p);
 }
 __device__ __forceinline__ uint32_t lds_byte(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)p;
@@ -171,26 +175,38 @@ struct Direct {
     static constexpr int kIn = ROW / 16;                   // chunks of a row
     static constexpr int kChunks = FORM == kCodes ? (WIDTH + THREADS - 1) / THREADS : WIDTH * kIn / THREADS;
     static constexpr int kBytes = kChunks * THREADS * 16;  // of a slice; a workgroup wider than a tile of codes loads zeros behind it
+    static constexpr int kSlice = FORM == kFours ? 2 * ROW : ROW / 2;
     static constexpr uint32_t kNowhere = 0x80000000u;      // past every buffer
-    uint32_t at[kChunks];          // byte of the lane's chunks from the tile's first, at k = 0
-    const uint8_t* base[2];        // the tile's first row (kAcross: column) of either matrix
-    int64_t span, stride;          // bytes from there to the operand's end, from row to row
+    uint32_t at[kChunks];          // byte of the lane's chunks from the tile's first, in any slice
     int chunk;                     // chunk of its row that a lane loads; the same in every turn
+    Buffer from;                   // of the slice that comes next
+    uint64_t other;                // the second segment's first byte
+    uint32_t step, whole, cut;     // bytes from slice to slice; sizes of a slice of rows of k, and of the last one
+    int left;                      // of k
 
-    __device__ __forceinline__ void start(const Operand& o, int64_t tile, int64_t extent, int64_t k) {
-        const int64_t width = PAIR ? WIDTH / 2 : WIDTH, left = extent - tile * width;
-        stride = FORM == kFours || FORM == kCodes ? o.ld * kBlockBytes : o.ld * 2;
+    // which: the matrix of a wave, or of the first segment
+    __device__ __forceinline__ void start(const Operand& o, int64_t tile, int64_t extent, int64_t k, int which, int slice) {
+        const int64_t width = PAIR ? WIDTH / 2 : WIDTH, lines = min(extent - tile * width, (int64_t)width);
+        const int64_t stride = FORM == kFours || FORM == kCodes ? o.ld * kBlockBytes : o.ld * 2;
         const int64_t first = tile * width * (FORM == kAcross ? 2 : stride);
-        base[0] = (const uint8_t*)o.data[0] + first;
-        base[1] = (const uint8_t*)o.data[1] + first;
+        step = uniform(FORM == kAcross ? (uint32_t)(kSlice * stride) : FORM == kCodes ? 16 : ROW);
+        from.at = uniform_address((const uint8_t*)(which ? o.data[1] : o.data[0]) + first + (int64_t)slice * step);
+        other = uniform_address((const uint8_t*)o.data[1] + first);
+        left = (int)uniform((uint32_t)min(k - (int64_t)slice * kSlice, (int64_t)0x7fffffff));
+        if constexpr (FORM == kAcross) {
+            whole = uniform((uint32_t)((kSlice - 1) * stride + 2 * lines));
+            cut = uniform((uint32_t)(((k - 1) % kSlice) * stride + 2 * lines));
+        } else {
+            whole = uniform((uint32_t)((lines - 1) * stride + (FORM == kAlong ? 2 * k : stride)));
+            from.size = uniform(whole - (uint32_t)slice * step);
+        }
         chunk = FORM == kAlong || FORM == kFours ? (threadIdx.x % kIn) ^ along_turn<ROW>(threadIdx.x / kIn) : 0;
-        span = FORM == kAcross ? (k - 1) * stride + 2 * left : FORM == kAlong ? (left - 1) * stride + 2 * k : left * stride;
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int i = threadIdx.x + THREADS * j;
             if constexpr (FORM == kAcross) {
                 const int kk = i / (WIDTH / 8), c = i % (WIDTH / 8) ^ across_turn<WIDTH>(kk);
-                at[j] = 8 * c < left ? (uint32_t)(kk * stride + 16 * c) : kNowhere;
+                at[j] = 8 * c < lines ? (uint32_t)(kk * stride + 16 * c) : kNowhere;
             } else if constexpr (FORM == kCodes) {
                 at[j] = i < WIDTH ? (uint32_t)(line_of<PAIR>(codes_row<PAIR>(i)) * stride) : kNowhere;
             } else {
@@ -198,15 +214,27 @@ struct Direct {
             }
         }
     }
-    // Chunk j of the slice at k0; nothing but zeros where there is none any more.
-    __device__ __forceinline__ void issue(int j, int seg, int64_t k0, int64_t k, bool live, uint32_t lds) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int which = !PAIR ? seg : FORM == kCodes ? wave & 1 : (wave * 64 + THREADS * j) / (32 * kIn) & 1;
-        const int64_t ahead = FORM == kAcross ? k0 * stride : FORM == kAlong ? 2 * k0 : k0 / 2;
-        const uint32_t left = live ? (uint32_t)min(span - ahead, (int64_t)0x7ffffff0) : 0u;
+    // Chunk J of the slice that comes next, to `lds` + PLUS; nothing but zeros where there is none any more.
+    template <int J, int PLUS>
+    __device__ __forceinline__ void issue(bool live, uint32_t lds) const {
+        Buffer b = from;
+        if constexpr (FORM == kAcross) b.size = left >= kSlice ? whole : cut;
+        b.size = live ? b.size : 0u;
         // a row's chunks past its end would be the next row's
-        const bool in = FORM == kAcross || FORM == kCodes || k0 + (FORM == kFours ? 32 : 8) * chunk < k;
-        load_to_lds<16>((which ? base[1] : base[0]) + ahead, left, in ? at[j] : kNowhere, lds + (wave * 64 + THREADS * j) * 16);
+        const bool in = FORM == kAcross || FORM == kCodes || (FORM == kFours ? 32 : 8) * chunk < left;
+        load_to_lds<16, PLUS + THREADS * J * 16>(b, in ? at[J] : kNowhere, lds);
+    }
+    // The slice after that; `turn`: the first of the second segment, whose k is `k`.
+    __device__ __forceinline__ void next(bool turn, int k) {
+        if (turn) {
+            from.at = other;
+            left = k;
+            if constexpr (FORM != kAcross) from.size = whole;
+        } else {
+            from.at += step;
+            left -= kSlice;
+            if constexpr (FORM != kAcross) from.size -= step;
+        }
     }
 };
 
@@ -220,16 +248,44 @@ __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
 }
 
-// The 16 bytes of an operand that a lane feeds to the matrix unit: row `base` + lane % 32 of the tile, piece s of the slice.
-template <Form FORM, int ROW, int WIDTH>
-__device__ __forceinline__ uint4_t fragment(const unsigned char* lds, int base, int s, int lane) {
-    if constexpr (FORM == kAcross) {
-        const int k = 16 * s + 8 * (lane >> 5) + (lane >> 2 & 3), col = base + (lane & 16) + 4 * (lane & 3);
-        const half4_t a = read_transposed(lds + across_at<WIDTH>(k, col >> 3) + 2 * (col & 7));
-        const half4_t b = read_transposed(lds + across_at<WIDTH>(k + 4, col >> 3) + 2 * (col & 7));
-        return __builtin_bit_cast(uint4_t, (half8_t){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
-    } else {
-        return *reinterpret_cast<const uint4_t*>(lds + along_at<ROW>(base + (lane & 31), 2 * s + (lane >> 5)));
+// The 16 bytes of an operand that a lane feeds to the matrix unit: row 32 i + lane % 32 of a wave's rows, piece s of a slice.  What
+// depends on the lane is found once; the rest are constants of the instruction.
+template <Form FORM, int ROW, int WIDTH, bool PAIR, int N>
+struct Reader {
+    int off[FORM == kAcross ? N : FORM == kCodes ? 1 : ROW / 32];
+    __device__ __forceinline__ void start(int first, int lane) {
+        if constexpr (FORM == kAcross) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int k = 8 * (lane >> 5) + (lane >> 2 & 3), col = first + 32 * i + (lane & 16) + 4 * (lane & 3);
+                off[i] = across_at<WIDTH>(k, col >> 3) + 2 * (col & 7);
+            }
+        } else if constexpr (FORM == kCodes) {
+            off[0] = codes_place<PAIR>(first + (lane & 31)) * 16 + 4 * (lane >> 5);
+        } else {
+#pragma unroll
+            for (int s = 0; s < ROW / 32; ++s) off[s] = along_at<ROW>(first + (lane & 31), 2 * s + (lane >> 5));
+        }
+    }
+    __device__ __forceinline__ uint4_t get(const unsigned char* lds, int i, int s) const {
+        if constexpr (FORM == kAcross) {
+            const unsigned char* const at = lds + off[i] + s * 16 * (2 * WIDTH);      // rows four on lie in the same banks
+            const half4_t a = read_transposed(at), b = read_transposed(at + 4 * (2 * WIDTH));
+            return __builtin_bit_cast(uint4_t, (half8_t){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+        } else if constexpr (FORM == kCodes) {
+            return (uint4_t){*reinterpret_cast<const uint32_t*>(lds + off[0] + (PAIR ? 64 : 32) * 16 * i + 8 * s), 0, 0, 0};     // eight codes
+        } else {
+            return *reinterpret_cast<const uint4_t*>(lds + off[s] + i * 32 * ROW);
+        }
+    }
+};
+
+// f(FROM) .. f(TO - 1), each with its own constant.
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void each_of(F f) {
+    if constexpr (FROM < TO) {
+        f(std::integral_constant<int, FROM>());
+        each_of<FROM + 1, TO>(f);
     }
 }
 
@@ -273,26 +329,32 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
 
     std::conditional_t<kDirectP, DirectP, Stage<FP, ROW, kWidthP, kThreads, GATED>> sp;
     std::conditional_t<DIRECT, DirectQ, Stage<FQ, ROW, kWidthQ, kThreads, false>> sq;
-    sp.start(P, tc, sh.cols, sh.k);
-    sq.start(Q, tr, sh.rows, sh.k);
+    const int seg0 = SEGS == 2 && begin >= slices ? 1 : 0;
+    if constexpr (kDirectP)
+        sp.start(P, tc, sh.cols, sh.k, !GATED ? seg0 : kCode ? wave & 1 : wave * 64 / (32 * DirectP::kIn) & 1, begin - seg0 * slices);
+    else sp.start(P, tc, sh.cols, sh.k);
+    if constexpr (DIRECT) sq.start(Q, tr, sh.rows, sh.k, SEGS == 2 ? seg0 : second, begin - seg0 * slices);
+    else sq.start(Q, tr, sh.rows, sh.k);
 
     // Scales: a lane loads those of its rows, a wave those of 64 rows of one matrix.  kCodes: a byte a slice, at the place of the
     // row's codes; kFours: the four bytes of a slice, rows of P before those of Q.
-    const int uniform = __builtin_amdgcn_readfirstlane(wave);
-    const uint8_t* scale_base[kScaleTurns];
-    uint32_t scale_at[kScaleTurns], scale_size[kScaleTurns];
+    const int wave0 = (int)uniform(wave);
+    Buffer scale_from[kScaleTurns];
+    uint32_t scale_at[kScaleTurns];
     if constexpr (kFour || kCode) {
 #pragma unroll
         for (int u = 0; u < kScaleTurns; ++u) {
-            const int first = 64 * uniform + kThreads * u, i = first + lane;
+            const int first = 64 * wave0 + kThreads * u, i = first + lane;
             const bool of_q = kFour && first >= kWidthP;
             const int which = kCode && GATED ? first >> 6 & 1 : 0;
             const Operand& o = of_q ? Q : P;
-            const int64_t row0 = of_q ? tr * kWidthQ : tc * (kCode ? kWide : kWidthP), rows = (of_q ? sh.rows : sh.cols) - row0;
+            const int64_t row0 = of_q ? tr * kWidthQ : tc * (kCode ? kWide : kWidthP);
+            const int64_t rows = min((of_q ? sh.rows : sh.cols) - row0, (int64_t)(of_q ? kWidthQ : kCode ? kWide : kWidthP));
             const int line = of_q ? i - kWidthP : kCode ? line_of<GATED>(codes_row<GATED>(i)) : i;
-            scale_base[u] = (which ? o.scales[1] : o.scales[0]) + row0 * o.ld_scales;
+            const int ahead = (kFour ? 4 : 1) * begin;
+            scale_from[u].at = uniform_address((which ? o.scales[1] : o.scales[0]) + row0 * o.ld_scales + ahead);
+            scale_from[u].size = uniform((uint32_t)(rows * o.ld_scales - ahead));
             scale_at[u] = i < kScaleRows ? (uint32_t)(line * o.ld_scales) : 0x80000000u;
-            scale_size[u] = (uint32_t)min(rows * o.ld_scales, (int64_t)0x7ffffff0);
         }
     }
     if constexpr (kShifted) {
@@ -342,21 +404,27 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     // What goes straight into LDS: load j of a slice's kLoads.
     constexpr int kLoadsP = kDirectP ? DirectP::kChunks : 0, kLoadsPQ = kLoadsP + (DIRECT ? DirectQ::kChunks : 0);
     constexpr int kLoads = kLoadsPQ + (kFour || kCode ? kScaleTurns : 0);
-    const uint32_t lds0 = lds_byte(lds), scales0 = lds_byte(scales);
-    auto issue = [&](int slice, int j) {
-        const int seg = SEGS == 2 && slice >= slices ? 1 : 0;
-        const int64_t k0 = (int64_t)(slice - seg * slices) * kSlice;
-        const int place = (slice - begin) & (kRing - 1);
-        const uint32_t to = lds0 + place * kBytesSlice;
+    const uint32_t lds0 = uniform(lds_byte(lds)) + wave0 * 1024, scales0 = uniform(lds_byte(scales)) + wave0 * 256;
+    // of the slice that comes next, into place PLACE of the ring
+    auto issue = [&](bool live, auto place, auto load) {
+        constexpr int kPlace = decltype(place)::value, J = decltype(load)::value;
         if constexpr (kDirectP)
-            if (j < kLoadsP) sp.issue(j, seg, k0, sh.k, slice < end, to);
+            if constexpr (J < kLoadsP) sp.template issue<J, kPlace * kBytesSlice>(live, lds0);
         if constexpr (DIRECT)
-            if (j >= kLoadsP && j < kLoadsPQ) sq.issue(j - kLoadsP, SEGS == 2 ? seg : second, k0, sh.k, slice < end, to + kBytesP);
+            if constexpr (J >= kLoadsP && J < kLoadsPQ) sq.template issue<J - kLoadsP, kPlace * kBytesSlice + kBytesP>(live, lds0);
+        if constexpr (J >= kLoadsPQ)
+            load_to_lds<kFour ? 4 : 1, (kPlace * kScaleTurns + J - kLoadsPQ) * kThreads * 4>(
+                Buffer{scale_from[J - kLoadsPQ].at, live ? scale_from[J - kLoadsPQ].size : 0u}, scale_at[J - kLoadsPQ], scales0);
+    };
+    auto issued = [&](int slice) {         // all of `slice`
+        const bool turn = SEGS == 2 && slice + 1 == slices;
+        if constexpr (kDirectP) sp.next(turn, (int)min(sh.k, (int64_t)0x7fffffff));
+        if constexpr (DIRECT) sq.next(turn, (int)min(sh.k, (int64_t)0x7fffffff));
         if constexpr (kFour || kCode) {
-            if (j >= kLoadsPQ) {
-                const int u = j - kLoadsPQ, ahead = kFour ? 4 * slice : slice;
-                load_to_lds<kFour ? 4 : 1>(scale_base[u] + ahead, slice < end ? scale_size[u] - ahead : 0u, scale_at[u],
-                                           scales0 + place * (kScaleTurns * kThreads * 4) + (64 * uniform + kThreads * u) * 4);
+#pragma unroll
+            for (int u = 0; u < kScaleTurns; ++u) {
+                scale_from[u].at += kFour ? 4 : 1;
+                scale_from[u].size -= kFour ? 4 : 1;
             }
         }
     };
@@ -366,12 +434,14 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     struct Pieces {
         uint4_t a[TP], b[TQ];      // a[][0] alone: eight codes
     };
+    Reader<kCode ? kCodes : FP == kAcross ? kAcross : kAlong, ROW, kWidthP, GATED, TP> rp;
+    Reader<FQ == kAcross ? kAcross : kAlong, ROW, kWidthQ, false, TQ> rq;
+    rp.start(32 * wp * TP, lane);
+    rq.start(32 * wq * TQ, lane);
+    static_assert(!kCode || TP == 2);
     auto read = [&](Pieces& f, int at, int s, int n) {
-        const unsigned char *lp = lds + at * kBytesSlice, *lq = lp + kBytesP;
-        if (n >= TP) f.b[n - TP] = fragment<FQ == kAcross ? kAcross : kAlong, ROW, kWidthQ>(lq, 32 * (wq * TQ + n - TP), s, lane);
-        else if constexpr (kCode)
-            f.a[n][0] = *reinterpret_cast<const uint32_t*>(lp + codes_place<GATED>(32 * (wp * TP + n) + (lane & 31)) * 16 + 8 * s + 4 * (lane >> 5));
-        else f.a[n] = fragment<FP == kAcross ? kAcross : kAlong, ROW, kWidthP>(lp, 32 * (wp * TP + n), s, lane);
+        if (n < TP) f.a[n] = rp.get(lds + at * kBytesSlice, n, s);
+        else f.b[n - TP] = rq.get(lds + at * kBytesSlice + kBytesP, n - TP, s);
     };
     // Scales of the lane's rows in a slice: kFours: lanes from 32 on have every second block; kCodes: one block.
     uint32_t ea[TP], eb[TQ];
@@ -420,11 +490,12 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
             }
         }
     };
-    // Item n of `count` things that are spread over the products.
-    auto spread = [&](int from, int to, int n, auto thing) {
-#pragma unroll
-        for (int j = from; j < to; ++j)
-            if ((j - from) * kProducts / (to - from) == n) thing(j);
+    // Of things FROM .. TO - 1, spread over the products, those behind product n.
+    auto spread = [&](auto from, auto to, int n, auto thing) {
+        constexpr int kFrom = decltype(from)::value, kTo = decltype(to)::value;
+        each_of<kFrom, kTo>([&](auto j) {
+            if ((j - kFrom) * kProducts / (kTo - kFrom) == n) thing(j);
+        });
     };
 
     // Slice i is multiplied in two halves.  Behind the first half all waves meet: the fragments of the second are in registers by then,
@@ -433,10 +504,10 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     // alternate, which keeps any of them from holding up the products behind it.
     constexpr int kEarly = (kLoads + 1) / 2;
     constexpr int kPending = kLoads ? (kRing - 2) * kLoads : 64;       // registers that loads go to are waited for where they are used
-#pragma unroll
-    for (int u = 0; u < kRing; ++u)
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) issue(begin + u, j);
+    each_of<0, kRing>([&](auto place) {
+        each_of<0, kLoads>([&](auto j) { issue(begin + place < end, place, j); });
+        issued(begin + place);
+    });
     load(begin, 0);
     store(begin, 0);
     load(begin + 1, 1);
@@ -451,29 +522,38 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     take_scales();
 #pragma unroll
     for (int n = 0; n < kReads; ++n) read(f[0], 0, 0, n);
-    auto turn = [&](int slice, int odd) {
-        const int at = (slice - begin) & (kRing - 1), next = (slice + 1 - begin) & (kRing - 1);
+    const std::integral_constant<int, 0> none;
+    const std::integral_constant<int, kEarly> early;
+    const std::integral_constant<int, kLoads> all;
+    const std::integral_constant<int, kReads> reads;
+    // Slice `slice`, which lies at place PLACE.
+    auto turn = [&](int slice, auto place) {
+        constexpr int kPlace = decltype(place)::value, kNext = (kPlace + 1) % kRing;
+        const auto before = std::integral_constant<int, (kPlace + kRing - 1) % kRing>();
 #pragma unroll
         for (int s = 0; s < kPieces - 1; ++s) {
             multiply(f[s & 1], s, [&](int n) {
-                spread(0, kReads, n, [&](int r) { read(f[(s + 1) & 1], at, s + 1, r); });
-                if (s == 0 && slice > begin) spread(kEarly, kLoads, n, [&](int j) { issue(slice - 1 + kRing, j); });
+                spread(none, reads, n, [&](auto r) { read(f[(s + 1) & 1], kPlace, s + 1, r); });
+                if (s == 0 && slice > begin) {
+                    spread(early, all, n, [&](auto j) { issue(slice - 1 + kRing < end, before, j); });
+                    if (n == kProducts - 1) issued(slice - 1 + kRing);
+                }
             });
         }
-        store(slice + 1, odd ^ 1);
+        store(slice + 1, (kPlace + 1) & 1);
         meet<kPending>();
-        load(slice + 3, odd ^ 1);
-        read_scales(next);
+        load(slice + 3, (kPlace + 1) & 1);
+        read_scales(kNext);
         multiply(f[1], kPieces - 1, [&](int n) {
-            spread(0, kReads, n, [&](int r) { read(f[0], next, 0, r); });
-            spread(0, kEarly, n, [&](int j) { issue(slice + kRing, j); });
+            spread(none, reads, n, [&](auto r) { read(f[0], kNext, 0, r); });
+            spread(none, early, n, [&](auto j) { issue(slice + kRing < end, place, j); });
         });
         take_scales();
     };
-    for (int slice = begin; slice < end; slice += 2) {
-        turn(slice, 0);
-        if (slice + 1 < end) turn(slice + 1, 1);
-    }
+    for (int slice = begin; slice < end; slice += kRing)
+        each_of<0, kRing>([&](auto place) {
+            if (slice + place < end) turn(slice + place, place);
+        });
     meet<0>();
 
     // A lane has columns 8 g + 4 (lane / 32) .. + 3, g = 0 .. 3, of row lane % 32 of every tile of 32 x 32.
@@ -672,13 +752,14 @@ bool whole_chunks(const Operand& o, Form form, int64_t along) {
 }
 
 // Bytes of a row of a slice in tiles of 256 x 256.  Whole lines of 128 bytes halve the requests that L2 serves (2048 tokens through
-// 8192 x 28672: 1.62 ms against 1.71 in rows of 64), where both operands are of 16 bits; 4-bit ones have four slices on the way.
-constexpr int row_bytes(Form p) { return p == kAlong || p == kAcross ? 128 : 64; }
+// 8192 x 28672: 1.62 ms against 1.71 in rows of 64), where both operands are of 16 bits.
+// 4-bit ones have four slices on the way, and rows that pass through registers would not fit those.
+constexpr int row_bytes(Form p, bool direct) { return direct && (p == kAlong || p == kAcross) ? 128 : 64; }
 
 template <class T, Form FP, Form FQ, bool GATED, int SEGS, bool DIRECT>
 void launch_tiles(int form, dim3 grid, const Operand& P, const Operand& Q, const Result& res, const Shape& sh, const Split& split, hipStream_t st) {
     if (form == 0)
-        hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, row_bytes(FP), 4, 2, 2, 4, DIRECT>), grid, dim3(512), 0, st, P, Q, res, sh, split);
+        hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, row_bytes(FP, DIRECT), 4, 2, 2, 4, DIRECT>), grid, dim3(512), 0, st, P, Q, res, sh, split);
     else if (form == 1)
         hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, 64, 2, 2, 2, 2, DIRECT>), grid, dim3(256), 0, st, P, Q, res, sh, split);
     else
@@ -689,20 +770,17 @@ template <class T, Form FP, Form FQ, bool GATED, int SEGS>
 void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, int results, void* work, hipStream_t st) {
     constexpr int64_t kSlice = FP == kFours ? 128 : 32;
     const Choice c = choose(rows, cols, SEGS * ((k + kSlice - 1) / kSlice), GATED, results);
-    const int64_t slice = c.form == 0 ? kSlice * row_bytes(FP) / 64 : kSlice, slices = SEGS * ((k + slice - 1) / slice);
+    const bool direct = FP == kFours || (whole_chunks(P, FP, FP == kAcross ? cols : k) && whole_chunks(Q, FQ, FQ == kAcross ? rows : k));
+    const int64_t slice = c.form == 0 ? kSlice * row_bytes(FP, direct) / 64 : kSlice, slices = SEGS * ((k + slice - 1) / slice);
     const int64_t wide = kWide[c.form] / (GATED ? 2 : 1), tall = kTall[c.form], each = (slices + c.parts - 1) / c.parts;
     const int parts = (int)((slices + each - 1) / each);
     const Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
     const Split split = {parts, (int)each, (float*)work};
     const int64_t tiles = (int64_t)sh.tiles_r * sh.tiles_c;
     const dim3 grid((unsigned)((tiles + 7) / 8 * 8), parts, results);
-    if constexpr (FP != kFours) {
-        if (!whole_chunks(P, FP, FP == kAcross ? cols : k) || !whole_chunks(Q, FQ, FQ == kAcross ? rows : k))
-            launch_tiles<T, FP, FQ, GATED, SEGS, false>(c.form, grid, P, Q, res, sh, split, st);
-        else launch_tiles<T, FP, FQ, GATED, SEGS, true>(c.form, grid, P, Q, res, sh, split, st);
-    } else {
-        launch_tiles<T, FP, FQ, GATED, SEGS, true>(c.form, grid, P, Q, res, sh, split, st);
-    }
+    if constexpr (FP != kFours)
+        if (!direct) launch_tiles<T, FP, FQ, GATED, SEGS, false>(c.form, grid, P, Q, res, sh, split, st);
+    if (direct) launch_tiles<T, FP, FQ, GATED, SEGS, true>(c.form, grid, P, Q, res, sh, split, st);
     if (parts > 1)
         hipLaunchKernelGGL((rsh_join_parts_kernel<T, GATED>), dim3((unsigned)((cols + 1023) / 1024 * rows), 1, results), dim3(256), 0, st,
                            (const float*)work, res, rows, cols, parts);
