@@ -716,33 +716,47 @@ struct Choice {
 
 constexpr int64_t kTall[3] = {256, 128, 64}, kWide[3] = {256, 128, 128};
 
-// The form and the parts whose rounds of workgroups take the least time, in units of a step of a lone workgroup of 256 x 256:
-// `steps` of k in all, `pairs`: columns come in two matrices, `results` products side by side.
-Choice choose(int64_t rows, int64_t cols, int64_t steps, bool pairs, int results) {
-    constexpr double step[3] = {0.5, 0.165, 0.1};      // a step of one workgroup with its neighbours on the compute unit
+// What the operands of a product do on their way: straight into LDS, through registers, or in 4 bits on both sides.
+enum Way { kStraight, kStaged, kFourBits };
+
+// The form and the parts of k whose workgroups take the least time by this account, fitted to products of 17 to 4096 rows by 500 to
+// 28672 columns, all forms and 1 to 16 parts of each, in microseconds: a slice of k of one workgroup alone on its compute unit, and
+// of each of several or where all of them work; what a workgroup takes besides; a join's launch and the bytes that pass through
+// memory for it.  (128 rows by 8192 columns by 28672 in 4 bits beside 16: 101 in form 1 and four parts, 110 in form 0 and eight, 225
+// in form 2 whole; 1024 rows of a gated block of 2048 x 2048: 25, 42 in form 0 and two parts, 32 in form 2.)
+Choice choose(int64_t rows, int64_t cols, int64_t slices, bool pairs, int results, Way way) {
+    constexpr double alone[3][3] = {{0.56, 0.27, 0.23}, {1.2, 0.8, 0.62}, {0.75, 0.38, 0.3}};
+    constexpr double shared[3][3] = {{0.56, 0.29, 0.2}, {1.2, 0.5, 0.37}, {1.1, 0.5, 0.32}};
+    constexpr double besides[3] = {8, 1.5, 0.7};
     constexpr int room[3] = {1, 2, 3};                 // workgroups of a compute unit
     Choice best = {0, 1};
     double least = 1e300;
     for (int form = 0; form < 3; ++form) {
         const int64_t wide = kWide[form] / (pairs ? 2 : 1);
         const int64_t tiles = ((rows + kTall[form] - 1) / kTall[form]) * ((cols + wide - 1) / wide) * results;
-        for (int parts = 1; parts <= 16 && parts <= steps; parts = parts < 4 ? parts + 1 : parts * 2) {
-            const int64_t each = (steps + parts - 1) / parts, work = tiles * ((steps + each - 1) / each);
-            const int64_t slots = 256 * room[form];
-            double t = (double)((work + slots - 1) / slots) * ((double)each * step[form] * room[form] + 4.0);
-            // sums through memory: written and read once, and a launch
-            if (parts > 1) t += 4.0 + 8e-6 * (double)(parts * rows * cols * results * (pairs ? 2 : 1));
+        for (int tried = 1; tried <= 16 && tried <= slices; tried += tried < 4 ? 1 : tried < 8 ? 2 : 4) {
+            const int64_t each = (slices + tried - 1) / tried, parts = (slices + each - 1) / each;
+            const double n = (double)((tiles * parts + 255) / 256), rounds = (double)(((int64_t)n + room[form] - 1) / room[form]);
+            double t = (double)each * std::max(alone[way][form] * rounds, n * shared[way][form]) + n * besides[form];
+            if (parts > 1) t += 5.0 + 8.0 / 5.1e6 * (double)(parts * rows * cols * results * (pairs ? 2 : 1));
             if (t < least) {
                 least = t;
-                best = {form, (int)((steps + each - 1) / each)};
+                best = {form, (int)parts};
             }
         }
     }
     return best;
 }
 
-int64_t partial_bytes(const Choice& c, int64_t rows, int64_t cols, bool pairs, int results) {
-    return c.parts == 1 ? 0 : (int64_t)c.parts * results * rows * ((cols + 3) / 4 * 4) * (pairs ? 2 : 1) * (int64_t)sizeof(float);
+// Of a product whose operands may go either way.
+int64_t partial_bytes(int64_t rows, int64_t cols, int64_t slices, bool pairs, int results, bool four) {
+    int parts = 1;
+    for (const Way way : {kStraight, kStaged, kFourBits})
+        if (four == (way == kFourBits)) {
+            const int p = choose(rows, cols, slices, pairs, results, way).parts;
+            parts = std::max(parts, p);
+        }
+    return parts == 1 ? 0 : (int64_t)parts * results * rows * ((cols + 3) / 4 * 4) * (pairs ? 2 : 1) * (int64_t)sizeof(float);
 }
 
 // Whether an operand's lines are whole chunks at 16-byte boundaries.
@@ -769,8 +783,8 @@ void launch_tiles(int form, dim3 grid, const Operand& P, const Operand& Q, const
 template <class T, Form FP, Form FQ, bool GATED, int SEGS>
 void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, int results, void* work, hipStream_t st) {
     constexpr int64_t kSlice = FP == kFours ? 128 : 32;
-    const Choice c = choose(rows, cols, SEGS * ((k + kSlice - 1) / kSlice), GATED, results);
     const bool direct = FP == kFours || (whole_chunks(P, FP, FP == kAcross ? cols : k) && whole_chunks(Q, FQ, FQ == kAcross ? rows : k));
+    const Choice c = choose(rows, cols, SEGS * ((k + kSlice - 1) / kSlice), GATED, results, FP == kFours ? kFourBits : direct ? kStraight : kStaged);
     const int64_t slice = c.form == 0 ? kSlice * row_bytes(FP, direct) / 64 : kSlice, slices = SEGS * ((k + slice - 1) / slice);
     const int64_t wide = kWide[c.form] / (GATED ? 2 : 1), tall = kTall[c.form], each = (slices + c.parts - 1) / c.parts;
     const int parts = (int)((slices + each - 1) / each);
@@ -804,20 +818,20 @@ int64_t aligned_scales(int x_type, int64_t t, int64_t n, int64_t k) {
 int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k) {
     const int64_t step = x_type == RSH_MX4 ? 128 : 32;
     if (takes_few(t, x_type == RSH_MX4)) return 0;
-    return aligned_scales(x_type, t, n, k) + partial_bytes(choose(t, n, (k + step - 1) / step, false, 1), t, n, false, 1);
+    return aligned_scales(x_type, t, n, k) + partial_bytes(t, n, (k + step - 1) / step, false, 1, x_type == RSH_MX4);
 }
 
 int64_t gated_forward_work(int64_t t, int64_t d, int64_t f) {
     if (takes_few(t, false)) return 0;
-    return partial_bytes(choose(t, f, (d + 31) / 32, true, 1), t, f, true, 1);
+    return partial_bytes(t, f, (d + 31) / 32, true, 1, false);
 }
 
 // dG and dU, and behind them the larger of the sums of dX and of the weights' gradients (of both, or of one alone).
 int64_t gated_backward_work(int64_t t, int64_t d, int64_t f) {
     const int64_t gates = 4 * t * ((f + 7) / 8 * 8);
-    int64_t sums = partial_bytes(choose(t, d, 2 * ((f + 31) / 32), false, 1), t, d, false, 1);
+    int64_t sums = partial_bytes(t, d, 2 * ((f + 31) / 32), false, 1, false);
     for (int results = 1; results <= 2; ++results)
-        sums = std::max(sums, partial_bytes(choose(f, d, (t + 31) / 32, false, results), f, d, false, results));
+        sums = std::max(sums, partial_bytes(f, d, (t + 31) / 32, false, results, false));
     return gates + sums;
 }
 
