@@ -288,7 +288,8 @@ int rsh_act_backward(const void *dY_dev, const void *Y_dev, void *dZ_dev, float 
  * `type` (RSH_F16 or RSH_BF16), no alignment beyond the element's.  act: RSH_ACT_SILU, RSH_ACT_GELU (with the error function) or
  * RSH_ACT_RELU.  fp32 sums, each result rounded once.
  *   rsh_gated_forward   g_scales and u_scales not NULL: Wg and Wu in 4 bits (ld_w unused).  G and U: NULL, or kept for the
- *                       gradients: [t][f rounded up to a multiple of 8] of `type`, 16-byte aligned
+ *                       gradients: [t][f rounded up to a multiple of 8] cells of 16 bits, 16-byte aligned, in a form of
+ *                       rsh_gated_backward's own (four numbers of 14 bits and their exponent in four cells)
  *   rsh_gated_backward  dX, dWg, dWu: NULL where not wanted.  dH: rows ld_h apart.  dG and dU are rounded to `type`.
  * work: device, 16-byte aligned, of the bytes that the *_work function of the same sizes reports (0: may be NULL), rewritten by
  * every call.  t is positive and below 2^31; n, k, d, f and the distances between rows are at most RSH_FFN_MAX_WIDTH.  Results never depend on the order in which waves run.

@@ -595,13 +595,13 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
         const int row = 32 * (wq * TQ + j) + (lane & 31), at = 32 * (wp * TP + i), col = (GATED ? at / 64 * 32 : at) + 8 * g;
         *reinterpret_cast<uint2_t*>(turned + row * (2 * kWide) + ((col / 8 ^ (row & kTurn)) << 4) + 2 * half) = v;
     };
-    auto leave = [&](uint16_t* out, int64_t ld) {
+    auto leave = [&](uint16_t* out, int64_t ld, int64_t cols) {
         __syncthreads();
         constexpr int kIn = kWide / 8;         // chunks of a row
 #pragma unroll 4
         for (int n = threadIdx.x; n < kIn * kWidthQ; n += kThreads) {
             const int row = n / kIn, c = n % kIn;
-            const int64_t left = sh.cols - col0 - 8 * c;
+            const int64_t left = cols - col0 - 8 * c;
             const uint4_t v = *reinterpret_cast<const uint4_t*>(turned + row * (2 * kWide) + ((c ^ (row & kTurn)) << 4));
             uint16_t* const at = out + (row0 + row) * ld + col0 + 8 * c;
             if (row0 + row < sh.rows) {
@@ -624,10 +624,24 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     };
     if constexpr (GATED) {
         if (res.gate) {
-            each([&](int i, int j, int v) { return acc[i][j][v]; });
-            leave(res.gate, res.ld_gate);
-            each([&](int i, int j, int v) { return acc[i + 1][j][v]; });
-            leave(res.up, res.ld_gate);
+            auto kept = [&](int which) {       // columns past the end are zero, that they do not set the scale of those before it
+#pragma unroll
+                for (int i = 0; i < TP; i += 2)
+#pragma unroll
+                    for (int j = 0; j < TQ; ++j)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const int64_t left = sh.cols - (col0 + 32 * (wp * TP + i) / 64 * 32 + 8 * g + half);
+                            float4_t x;
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) x[v] = v < left ? acc[i + which][j][4 * g + v] : 0.f;
+                            put(i, j, g, keep4(x));
+                        }
+            };
+            kept(0);
+            leave(res.gate, res.ld_gate, res.ld_gate);
+            kept(1);
+            leave(res.up, res.ld_gate, res.ld_gate);
         }
         auto finished = [&](auto act) {
             each([&](int i, int j, int v) { return act_of(decltype(act)::value, acc[i][j][v]) * acc[i + 1][j][v]; });
@@ -638,7 +652,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     } else {
         each([&](int i, int j, int v) { return acc[i][j][v]; });
     }
-    leave(res.out[second], res.ld);
+    leave(res.out[second], res.ld, sh.cols);
 }
 
 // Rows of scales at multiples of four bytes, as lanes load them four at a time: those of W, then those of X.
@@ -681,14 +695,17 @@ __global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* 
     const int64_t row = slab, col = 8 * ((int64_t)(blockIdx.x - slab * across) * 256 + threadIdx.x), at = row * ld_gate + col;
     if (row >= t || col >= ld_gate) return;
     const uint4_t h = load8(dH + row * ld + col, f - col);
-    const uint4_t g = *reinterpret_cast<const uint4_t*>(G + at), u = *reinterpret_cast<const uint4_t*>(U + at);
+    const uint4_t gk = *reinterpret_cast<const uint4_t*>(G + at), uk = *reinterpret_cast<const uint4_t*>(U + at);
+    const float4_t g[2] = {kept4((uint2_t){gk[0], gk[1]}), kept4((uint2_t){gk[2], gk[3]})};
+    const float4_t u[2] = {kept4((uint2_t){uk[0], uk[1]}), kept4((uint2_t){uk[2], uk[3]})};
     uint4_t a, b;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         float dg[2], du[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float hv = T::widen((uint16_t)(h[w] >> 16 * e)), gv = T::widen((uint16_t)(g[w] >> 16 * e)), uv = T::widen((uint16_t)(u[w] >> 16 * e));
+            const uint32_t word = h[w];
+            const float hv = T::widen((uint16_t)(word >> 16 * e)), gv = g[w / 2][2 * (w & 1) + e], uv = u[w / 2][2 * (w & 1) + e];
             float slope;
             du[e] = hv * act_of(act, gv, &slope);
             dg[e] = hv * uv * slope;

@@ -152,6 +152,31 @@ def test_gradients_against_differences(act):
         assert (got - want).abs() <= (bounds[i] * v.abs()).sum() + 1e-6 * (grads[i].double() * v).abs().sum()
 
 
+@pytest.mark.parametrize("t", [3, 40, 300])
+def test_small_numbers_beside_large_ones(t):
+    """The forward pass keeps four numbers with one exponent.  A positive one stays positive however large its neighbours are (relu's
+    slope), an infinity leaves its neighbours finite, and what is kept is off by 2^-13 of the largest of the four at most."""
+    import torch
+    from paper_2603_08734_amd import ffn
+    d, f = 64, 24
+    x = torch.full((t, d), 0.125, device="cuda").bfloat16()
+    wg = torch.full((f, d), 100.0, device="cuda").bfloat16()
+    wg[1::4], wg[2::4] = 2.0 ** -30, -(2.0 ** -30)
+    wu = torch.full((f, d), 0.5, device="cuda").bfloat16()
+    dh = torch.ones((t, f), device="cuda").bfloat16()
+    leaves = [m.clone().requires_grad_() for m in (x, wg, wu)]
+    _, dwg, dwu = torch.autograd.grad(ffn.gated(*leaves, "relu"), leaves, dh)
+    want = torch.full((f,), t * 4.0 * 0.125, device="cuda")      # sum over t of dH U x, U = 64 * 0.125 * 0.5
+    want[2::4] = 0
+    assert ((dwg[:, 0].float() - want).abs() <= 2.0 ** -8 * want).all()
+    small = t * 0.125 * 64 * 0.125 * 2.0 ** -30                  # sum over t of dH G x
+    assert ((dwu[1::4].float() - small).abs() <= 2.0 ** -8 * small + t * 0.125 * 800 * 2.0 ** -13).all() and not dwu[2::4].any()
+    wg[0, 0] = float("inf")                                      # G of column 0
+    leaves = [m.clone().requires_grad_() for m in (x, wg, wu)]
+    dx, dwg, dwu = torch.autograd.grad(ffn.gated(*leaves, "silu"), leaves, dh)
+    assert torch.isfinite(dwg[1:]).all() and torch.isfinite(dwu[1:]).all() and not torch.isfinite(dwu[0]).any()
+
+
 def test_some_gradients_only():
     import torch
     from paper_2603_08734_amd import ffn
