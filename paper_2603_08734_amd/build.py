@@ -1,9 +1,11 @@
 """Build the HIP library in-tree (``librsh.so`` next to this file) for gfx950."""
 from __future__ import annotations
 
+import concurrent.futures
 import hashlib
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -46,9 +48,13 @@ def needs_build() -> bool:
 
 
 def build(force: bool = True) -> str:
+    """Compile every source for itself, side by side, and link."""
     if force or needs_build():
-        cmd = [HIPCC, *FLAGS, "-o", LIB, *sources(), "-lpthread"]
-        subprocess.check_call(cmd)
+        with tempfile.TemporaryDirectory() as tmp, concurrent.futures.ThreadPoolExecutor(4) as pool:
+            objects = [os.path.join(tmp, name + ".o") for name in SOURCES]
+            flags = [f for f in FLAGS if f != "-shared"]
+            list(pool.map(lambda source, obj: subprocess.check_call([HIPCC, *flags, "-c", "-o", obj, source]), sources(), objects))
+            subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objects, "-lpthread"])
         with open(STAMP, "w") as f:
             f.write(source_digest() + "\n")
     return LIB

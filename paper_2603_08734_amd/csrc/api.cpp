@@ -654,7 +654,7 @@ int matrix_ok(int32_t type, int64_t rows, int64_t k, int64_t ld, const void* X, 
     if ((type != RSH_F32 && !half_type(type)) || rows <= 0 || k <= 0 || ld < k || !aligned_to({X}, type == RSH_F32 ? 4 : 2) || !aligned_to({codes}, 16) ||
         !aligned_to({scales}, 4))
         return RSH_ERR_BAD_OPTION;
-    if (rows >= kMaxSize || k >= kMaxSize || ld >= kMaxSize || rows * ((k + 31) / 32) > kMaxSize * 16) return RSH_ERR_TOO_LARGE;
+    if (rows >= kMaxSize || k >= kMaxSize || ld >= kMaxSize || rows * ((k + 31) / 32) > kMaxSize) return RSH_ERR_TOO_LARGE;
     return RSH_OK;
 }
 }  // namespace

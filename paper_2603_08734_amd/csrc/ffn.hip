@@ -691,31 +691,34 @@ template <class T>
 __global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* __restrict__ dH, const uint16_t* __restrict__ G,
                                                                 const uint16_t* __restrict__ U, uint16_t* __restrict__ dG,
                                                                 uint16_t* __restrict__ dU, int64_t t, int64_t f, int64_t ld, int64_t ld_gate, int act) {
-    const uint32_t across = (uint32_t)((ld_gate + 2047) / 2048), slab = blockIdx.x / across;
-    const int64_t row = slab, col = 8 * ((int64_t)(blockIdx.x - slab * across) * 256 + threadIdx.x), at = row * ld_gate + col;
-    if (row >= t || col >= ld_gate) return;
-    const uint4_t h = load8(dH + row * ld + col, f - col);
-    const uint4_t gk = *reinterpret_cast<const uint4_t*>(G + at), uk = *reinterpret_cast<const uint4_t*>(U + at);
-    const float4_t g[2] = {kept4((uint2_t){gk[0], gk[1]}), kept4((uint2_t){gk[2], gk[3]})};
-    const float4_t u[2] = {kept4((uint2_t){uk[0], uk[1]}), kept4((uint2_t){uk[2], uk[3]})};
-    uint4_t a, b;
+    const uint32_t across = (uint32_t)((ld_gate + 2047) / 2048);
+    const int64_t col = 8 * ((int64_t)(blockIdx.x % across) * 256 + threadIdx.x);
+    if (col >= ld_gate) return;
+    for (int64_t row = blockIdx.x / across; row < t; row += gridDim.x / across) {
+        const int64_t at = row * ld_gate + col;
+        const uint4_t h = load8(dH + row * ld + col, f - col);
+        const uint4_t gk = *reinterpret_cast<const uint4_t*>(G + at), uk = *reinterpret_cast<const uint4_t*>(U + at);
+        const float4_t g[2] = {kept4((uint2_t){gk[0], gk[1]}), kept4((uint2_t){gk[2], gk[3]})};
+        const float4_t u[2] = {kept4((uint2_t){uk[0], uk[1]}), kept4((uint2_t){uk[2], uk[3]})};
+        uint4_t a, b;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        float dg[2], du[2];
+        for (int w = 0; w < 4; ++w) {
+            float dg[2], du[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t word = h[w];
-            const float hv = T::widen((uint16_t)(word >> 16 * e)), gv = g[w / 2][2 * (w & 1) + e], uv = u[w / 2][2 * (w & 1) + e];
-            float slope;
-            du[e] = hv * act_of(act, gv, &slope);
-            dg[e] = hv * uv * slope;
-            if (col + 2 * w + e >= f) du[e] = dg[e] = 0.f;
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t word = h[w];
+                const float hv = T::widen((uint16_t)(word >> 16 * e)), gv = g[w / 2][2 * (w & 1) + e], uv = u[w / 2][2 * (w & 1) + e];
+                float slope;
+                du[e] = hv * act_of(act, gv, &slope);
+                dg[e] = hv * uv * slope;
+                if (col + 2 * w + e >= f) du[e] = dg[e] = 0.f;
+            }
+            a[w] = T::pair(dg[0], dg[1]);
+            b[w] = T::pair(du[0], du[1]);
         }
-        a[w] = T::pair(dg[0], dg[1]);
-        b[w] = T::pair(du[0], du[1]);
+        *reinterpret_cast<uint4_t*>(dG + at) = a;
+        *reinterpret_cast<uint4_t*>(dU + at) = b;
     }
-    *reinterpret_cast<uint4_t*>(dG + at) = a;
-    *reinterpret_cast<uint4_t*>(dU + at) = b;
 }
 
 // ---------------------------------------------------------------------------
@@ -902,7 +905,7 @@ int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg,
                           const void* dH, int64_t ld_h, int act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
                           void* stream) {
     const hipStream_t st = (hipStream_t)stream;
-    const int64_t ld_gate = (f + 7) / 8 * 8, blocks = t * ((ld_gate + 2047) / 2048);
+    const int64_t ld_gate = (f + 7) / 8 * 8, across = (ld_gate + 2047) / 2048, blocks = std::min<int64_t>(t, std::max<int64_t>(1, (1 << 20) / across)) * across;
     uint16_t* const dG = (uint16_t*)work;
     uint16_t* const dU = dG + t * ld_gate;
     void* const sums = dU + t * ld_gate;

@@ -13,7 +13,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding
-from .mx4 import HALVES, Mx4, _no_gradient, _on, _rows
+from .mx4 import HALVES, Mx4, _no_gradient, _on, _rows, product
 
 ACTIVATIONS = {"silu": binding.RSH_ACT_SILU, "gelu": binding.RSH_ACT_GELU, "relu": binding.RSH_ACT_RELU}
 
@@ -28,7 +28,7 @@ def _weights(Wg, Wu):
 def _forward(X, Wg, Wu, act, keep):
     x, ld_x = _rows(X)
     wg, wu, ld_w = _weights(Wg, Wu)
-    with _on(x.device):
+    with _on(x.get_device()):
         return binding.gated_forward(x, HALVES[x.dtype], ld_x, wg, wu, ld_w, None, None, act, wg.shape[0], keep)
 
 
@@ -37,7 +37,7 @@ def _backward(ctx, dH):
     x, ld_x = _rows(X)
     wg, wu, ld_w = _weights(Wg, Wu)
     dH, ld_h = _rows(dH)
-    with _on(x.device):
+    with _on(x.get_device()):
         return (*binding.gated_backward(x, HALVES[x.dtype], ld_x, wg, wu, ld_w, kept, dH, ld_h, ctx.act, ctx.needs_input_grad), None)
 
 
@@ -58,8 +58,8 @@ class _Gated(torch.autograd.Function):
         return _backward_once(ctx, dH) if torch.is_grad_enabled() else _backward(ctx, dH)
 
 
-def gated(X, W_gate, W_up, activation: str = "silu"):
-    """act(X W_gate^T) * (X W_up^T): X [..., d], weights [f, d] of X's type or in 4 bits, result [..., f]."""
+def _refuse(X, W_gate, W_up, activation):
+    """Say what does not fit."""
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation: expected one of {list(ACTIVATIONS)}, got {activation!r}")
     if not isinstance(X, torch.Tensor) or X.dim() < 1:
@@ -67,14 +67,24 @@ def gated(X, W_gate, W_up, activation: str = "silu"):
     four = isinstance(W_gate, Mx4)
     if four != isinstance(W_up, Mx4):
         raise TypeError("W_gate and W_up: either both in 4 bits or neither")
-    shape, device, dtype = W_gate.shape, X.device, X.dtype
-    if W_up.shape != shape or len(shape) != 2 or shape[1] != X.shape[-1]:
-        raise ValueError(f"X {tuple(X.shape)}, W_gate {tuple(shape)} and W_up {tuple(W_up.shape)} do not fit")
-    if dtype not in HALVES or (not four and (W_gate.dtype != dtype or W_up.dtype != dtype)):
-        raise TypeError(f"expected one type for X and 16-bit weights, one of {list(HALVES)}; X is {dtype}")
-    if not X.is_cuda or W_gate.device != device or W_up.device != device:
-        raise ValueError(f"X is on {device}, W_gate on {W_gate.device}, W_up on {W_up.device}; expected one GPU")
-    act, (f, d) = ACTIVATIONS[activation], shape
+    if tuple(W_up.shape) != tuple(W_gate.shape) or len(W_gate.shape) != 2 or W_gate.shape[1] != X.shape[-1]:
+        raise ValueError(f"X {tuple(X.shape)}, W_gate {tuple(W_gate.shape)} and W_up {tuple(W_up.shape)} do not fit")
+    if X.dtype not in HALVES or (not four and (W_gate.dtype != X.dtype or W_up.dtype != X.dtype)):
+        raise TypeError(f"expected one type for X and 16-bit weights, one of {list(HALVES)}; X is {X.dtype}")
+    raise ValueError(f"X is on {X.device}, W_gate on {W_gate.device}, W_up on {W_up.device}; expected one GPU")
+
+
+def gated(X, W_gate, W_up, activation: str = "silu"):
+    """act(X W_gate^T) * (X W_up^T): X [..., d], weights [f, d] of X's type or in 4 bits, result [..., f]."""
+    act, four = ACTIVATIONS.get(activation), isinstance(W_gate, Mx4)
+    if act is None or not isinstance(X, torch.Tensor) or X.dim() < 1 or X.dtype not in HALVES or four != isinstance(W_up, Mx4):
+        _refuse(X, W_gate, W_up, activation)
+    shape, device = W_gate.shape, X.get_device()
+    a, b = (W_gate.codes, W_up.codes) if four else (W_gate, W_up)
+    if (W_up.shape != shape or len(shape) != 2 or shape[1] != X.shape[-1] or device < 0 or a.get_device() != device or b.get_device() != device or
+            not (four or a.dtype == b.dtype == X.dtype)):
+        _refuse(X, W_gate, W_up, activation)
+    f, d = shape
     flat = X.dim() == 2
     rows = X if flat else X.reshape(-1, d) if d else X.reshape(X.shape[:-1].numel(), 0)
     if four:
@@ -86,9 +96,31 @@ def gated(X, W_gate, W_up, activation: str = "silu"):
     elif four:
         x, ld_x = _rows(rows)
         with _on(device):
-            H = binding.gated_forward(x, HALVES[dtype], ld_x, W_gate.codes, W_up.codes, 0, W_gate.scales, W_up.scales, act, f, False)[0]
+            H = binding.gated_forward(x, HALVES[x.dtype], ld_x, a, b, 0, W_gate.scales, W_up.scales, act, f, False)[0]
     elif (X.requires_grad or W_gate.requires_grad or W_up.requires_grad) and torch.is_grad_enabled():
         H = _Gated.apply(rows, W_gate, W_up, act)
     else:
         H = _forward(rows, W_gate, W_up, act, False)[0]
     return H if flat else H.reshape(*X.shape[:-1], f)
+
+
+class FeedForward:
+    """A gated feed-forward layer as it is served: Y = W_down (act(X W_gate^T) * (X W_up^T)).
+
+    W_gate, W_up: [f, d] of the activations' type, or in 4 bits (``mx4.quantize``).  W_down: [d, f] in 4 bits, or a ``Plan`` of the
+    pruned weight for exactly as many tokens as X has (binary16: the sparse product takes the tokens as columns)."""
+
+    def __init__(self, W_gate, W_up, W_down, activation: str = "silu"):
+        self.W_gate, self.W_up, self.W_down, self.activation = W_gate, W_up, W_down, activation
+
+    def __call__(self, X):
+        """X: [t, d]; result [t, d] of its type."""
+        H = gated(X, self.W_gate, self.W_up, self.activation)
+        if isinstance(self.W_down, Mx4):
+            return product(H, self.W_down)
+        if H.dtype != torch.float16 or H.shape[0] != self.W_down.N:
+            raise ValueError(f"the plan is for {self.W_down.N} tokens of binary16, got {H.shape[0]} of {H.dtype}")
+        Y = torch.empty((self.W_down.n_rows, self.W_down.N), dtype=torch.float16, device=H.device)
+        with _on(H.get_device()):
+            self.W_down.spmm_f16(H.t().contiguous(), Y)
+        return Y.t()

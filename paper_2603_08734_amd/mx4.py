@@ -22,9 +22,9 @@ _TYPES = {torch.float32: binding.RSH_F32, torch.float16: binding.RSH_F16, torch.
 _NOTHING = contextlib.nullcontext()
 
 
-def _on(device):
+def _on(index: int):
     """Launches go to the current device: make the operands' device that."""
-    return _NOTHING if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
+    return _NOTHING if index == torch._C._cuda_getDevice() else torch.cuda.device(index)
 
 
 def _matrix(X, name: str, types):
@@ -96,7 +96,7 @@ def quantize(X) -> Mx4:
     if rows == 0 or k == 0:
         blocks = -(-k // BLOCK)
         return Mx4._of(*(torch.empty((rows, w), dtype=torch.uint8, device=X.device) for w in (16 * blocks, blocks)), k)
-    with _on(X.device):
+    with _on(X.get_device()):
         return Mx4._of(*binding.mx4_quantize(X, _TYPES[X.dtype], ld), k)
 
 
@@ -106,7 +106,7 @@ def dequantize(Q: Mx4, dtype=torch.bfloat16):
         raise TypeError(f"dtype: expected one of {list(_TYPES)}, got {dtype}")
     Y = torch.empty(Q.shape, dtype=dtype, device=Q.device)
     if Y.numel():
-        with _on(Q.device):
+        with _on(Q.codes.get_device()):
             binding.mx4_dequantize(Q.codes, Q.scales, Y, _TYPES[dtype])
     return Y
 
@@ -131,11 +131,11 @@ def product(X, W: Mx4, dtype=None):
     (t, k), n = X.shape, W.shape[0]
     if k != W.shape[1]:
         raise ValueError(f"X {tuple(X.shape)} and W {W.shape}: the last sizes differ")
-    if data.device != W.device:
+    if data.get_device() != W.codes.get_device():
         raise ValueError(f"X is on {data.device}, W on {W.device}")
     if t == 0 or n == 0 or k == 0:
         return torch.zeros((t, n), dtype=dtype, device=W.device)
     Y = torch.empty((t, n), dtype=dtype, device=W.device)
-    with _on(W.device):
+    with _on(W.codes.get_device()):
         binding.mx4_product(data, x_scales, x_type, ld, W.codes, W.scales, Y, HALVES[dtype], k)
     return Y
