@@ -109,7 +109,7 @@ __device__ __forceinline__ void finish(const Result& res, uint16_t* out, int64_t
 
 // Whether the kernel for few rows (few.hip) takes a product, and its launch.  Operands as for the tiles (ffn.hip); P is kAlong,
 // kCodes or kFours, Q kAlong or, beside kFours, kFours.
-bool takes_few(int64_t rows, bool four);
+bool takes_few(int64_t rows);
 template <class T, Form FP, bool GATED>
 void launch_few(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, hipStream_t st);
 

@@ -19,7 +19,6 @@ constexpr int kBlockBytes = 16;    // their codes
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 struct F16 {
-    using Pair = half2_t;
     static __device__ __forceinline__ float16_t mfma32(uint4_t a, uint4_t b, float16_t c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
     }
@@ -37,7 +36,6 @@ struct F16 {
 };
 
 struct BF16 {
-    using Pair = bf2_t;
     static __device__ __forceinline__ float16_t mfma32(uint4_t a, uint4_t b, float16_t c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8_t, a), __builtin_bit_cast(bf8_t, b), c, 0, 0, 0);
     }
