@@ -693,7 +693,7 @@ int rsh_gated_forward_work(int32_t w_type, int64_t t, int64_t d, int64_t f, int6
     if (!bytes) return RSH_ERR_NULL;
     if (w_type != RSH_MX4 && !half_type(w_type)) return RSH_ERR_BAD_OPTION;
     const int rc = sizes_ok(t, d, f);
-    *bytes = rc ? 0 : rsh::gated_forward_work(t, d, f);
+    *bytes = rc ? 0 : rsh::gated_forward_work(w_type == RSH_MX4, t, d, f);
     return rc;
 }
 

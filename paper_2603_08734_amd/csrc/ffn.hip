@@ -14,7 +14,7 @@
 // Measured (bfloat16 unless said): 2048 tokens through a gated block of 8192 x 28672 1.46 ms, 1320 TFLOP/s where the library's product
 // of the same shape alone runs at 1490; a training step of 4096 tokens on 4096 x 16384 2.76 ms, 1200 TFLOP/s with dX at 1270 and the
 // weights' gradients at 1260 (the library's products: 1190 and 1000); 4096 tokens through 28672 x 8192, 4 bits on both sides 0.64 ms,
-// 3020 TFLOP/s; 128 tokens through 8192 x 28672 in 4 bits beside binary16 114 us, where four parts of k and a slice's latency count.
+// 3020 TFLOP/s; 128 tokens through 8192 x 28672 in 4 bits beside binary16 99 us, where four parts of k and a slice's latency count.
 #include <algorithm>
 
 #include "../../include/rsh_spmm.h"
@@ -319,8 +319,10 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     constexpr int kScaleRows = kFour ? kWidthP + kWidthQ : kWidthP;      // rows of a slice that have scales
     constexpr int kScaleTurns = (kScaleRows + kThreads - 1) / kThreads;
     __shared__ __attribute__((aligned(16))) unsigned char lds[larger(kRing * kBytesSlice, 2 * kWide * kWidthQ)];
-    // four bytes of a row of a slice, or one at the place of its codes; a workgroup with more threads than rows loads zeros behind them
-    __shared__ uint32_t scales[kFour || kCode ? kRing : 1][kFour || kCode ? kScaleTurns * kThreads : 1];
+    // Four scales of a row: those of a slice, or beside codes, at their place, those of a ring of slices (a byte with every slice took as many
+    // cycles of the loads' addresses as the codes: 128 rows through 8192 x 28672 113 us against 99).  A workgroup with more threads
+    // than rows loads zeros behind them.
+    __shared__ uint32_t scales[kFour ? kRing : 1][kFour || kCode ? kScaleTurns * kThreads : 1];
     __shared__ int tops[kShifted ? kWidthP : 1];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % WP, wq = wave / WP;
@@ -344,8 +346,8 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     if constexpr (DIRECT) sq.start(Q, tr, sh.rows, sh.k, SEGS == 2 ? seg0 : second, begin - seg0 * slices);
     else sq.start(Q, tr, sh.rows, sh.k);
 
-    // Scales: a lane loads those of its rows, a wave those of 64 rows of one matrix.  kCodes: a byte a slice, at the place of the
-    // row's codes; kFours: the four bytes of a slice, rows of P before those of Q.
+    // Scales: a lane loads those of its rows, a wave those of 64 rows of one matrix, four bytes at a time.  kCodes: for four slices, of
+    // which a part of k begins with the first; kFours: of a slice, rows of P before those of Q.
     const int wave0 = (int)uniform(wave);
     Buffer scale_from[kScaleTurns];
     uint32_t scale_at[kScaleTurns];
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
             const int64_t row0 = of_q ? tr * kWidthQ : tc * (kCode ? kWide : kWidthP);
             const int64_t rows = min((of_q ? sh.rows : sh.cols) - row0, (int64_t)(of_q ? kWidthQ : kCode ? kWide : kWidthP));
             const int line = of_q ? i - kWidthP : kCode ? line_of<GATED>(codes_row<GATED>(i)) : i;
-            const int ahead = (kFour ? 4 : 1) * begin;
+            const int ahead = kFour ? 4 * begin : begin;
             scale_from[u].at = uniform_address((which ? o.scales[1] : o.scales[0]) + row0 * o.ld_scales + ahead);
             scale_from[u].size = uniform((uint32_t)(rows * o.ld_scales - ahead));
             scale_at[u] = i < kScaleRows ? (uint32_t)(line * o.ld_scales) : 0x80000000u;
@@ -411,7 +413,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     };
     // What goes straight into LDS: load j of a slice's kLoads.
     constexpr int kLoadsP = kDirectP ? DirectP::kChunks : 0, kLoadsPQ = kLoadsP + (DIRECT ? DirectQ::kChunks : 0);
-    constexpr int kLoads = kLoadsPQ + (kFour || kCode ? kScaleTurns : 0);
+    constexpr int kLoads = kLoadsPQ + (kFour || kCode ? kScaleTurns : 0), kSure = kCode ? kLoadsPQ : kLoads;      // at most, at least
     const uint32_t lds0 = uniform(lds_byte(lds)) + wave0 * 1024, scales0 = uniform(lds_byte(scales)) + wave0 * 256;
     // of the slice that comes next, into place PLACE of the ring
     auto issue = [&](bool live, auto place, auto load) {
@@ -420,19 +422,19 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
             if constexpr (J < kLoadsP) sp.template issue<J, kPlace * kBytesSlice>(live, lds0);
         if constexpr (DIRECT)
             if constexpr (J >= kLoadsP && J < kLoadsPQ) sq.template issue<J - kLoadsP, kPlace * kBytesSlice + kBytesP>(live, lds0);
-        if constexpr (J >= kLoadsPQ)
-            load_to_lds<kFour ? 4 : 1, (kPlace * kScaleTurns + J - kLoadsPQ) * kThreads * 4>(
+        if constexpr (J >= kLoadsPQ && (kFour || kPlace == 0))
+            load_to_lds<4, (kPlace * kScaleTurns + J - kLoadsPQ) * kThreads * 4>(
                 Buffer{scale_from[J - kLoadsPQ].at, live ? scale_from[J - kLoadsPQ].size : 0u}, scale_at[J - kLoadsPQ], scales0);
     };
-    auto issued = [&](int slice) {         // all of `slice`
+    auto issued = [&](int slice, auto place) {         // all of `slice`
         const bool turn = SEGS == 2 && slice + 1 == slices;
         if constexpr (kDirectP) sp.next(turn, (int)min(sh.k, (int64_t)0x7fffffff));
         if constexpr (DIRECT) sq.next(turn, (int)min(sh.k, (int64_t)0x7fffffff));
-        if constexpr (kFour || kCode) {
+        if constexpr (kFour || (kCode && decltype(place)::value == 0)) {
 #pragma unroll
             for (int u = 0; u < kScaleTurns; ++u) {
-                scale_from[u].at += kFour ? 4 : 1;
-                scale_from[u].size -= kFour ? 4 : 1;
+                scale_from[u].at += 4;
+                scale_from[u].size -= 4;
             }
         }
     };
@@ -451,12 +453,13 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
         if (n < TP) f.a[n] = rp.get(lds + at * kBytesSlice, n, s);
         else f.b[n - TP] = rq.get(lds + at * kBytesSlice + kBytesP, n - TP, s);
     };
-    // Scales of the lane's rows in a slice: kFours: lanes from 32 on have every second block; kCodes: one block.
+    // Scales of the lane's rows in a slice: kFours: lanes from 32 on have every second block; kCodes: one block of the four at hand.
     uint32_t ea[TP], eb[TQ];
     int shift[TP];
     uint32_t na[TP], nb[TQ];       // of the next slice, as they lie in LDS
-    auto read_scales = [&](int at) {
-        if constexpr (kFour || kCode) {
+    auto read_scales = [&](auto place) {
+        constexpr int at = decltype(place)::value;
+        if constexpr (kFour || (kCode && at == 0)) {
 #pragma unroll
             for (int i = 0; i < TP; ++i) na[i] = scales[at][codes_place<kCode && GATED>(32 * (wp * TP + i) + (lane & 31))];
         }
@@ -465,7 +468,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
             for (int i = 0; i < TQ; ++i) nb[i] = scales[at][kWidthP + 32 * (wq * TQ + i) + (lane & 31)];
         }
     };
-    auto take_scales = [&]() {
+    auto take_scales = [&]([[maybe_unused]] auto place) {
         if constexpr (kFour) {
 #pragma unroll
             for (int i = 0; i < TP; ++i) ea[i] = na[i] >> (8 * (lane >> 5));
@@ -474,7 +477,10 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
         }
         if constexpr (kCode) {
 #pragma unroll
-            for (int i = 0; i < TP; ++i) ea[i] = (kShifted && na[i] != 255u ? (uint32_t)max(0, (int)na[i] + shift[i]) : na[i]) << 23;
+            for (int i = 0; i < TP; ++i) {
+                const uint32_t e = na[i] >> (8 * decltype(place)::value) & 255u;
+                ea[i] = (kShifted && e != 255u ? (uint32_t)max(0, (int)e + shift[i]) : e) << 23;
+            }
         }
     };
     // The products of a piece, then(n) behind the n-th.
@@ -511,26 +517,26 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     // last piece and half during the first of the next slice.  So a load has nearly kRing - 1 slices to arrive, and products, reads and
     // loads alternate, which keeps any of them from holding up the products behind it.  (All loads in the last piece: the same time.)
     constexpr int kEarly = (kLoads + 1) / 2;
-    constexpr int kPending = kLoads ? (kRing - 2) * kLoads : 64;       // registers that loads go to are waited for where they are used
+    constexpr int kPending = kLoads ? (kRing - 2) * kSure : 64;       // registers that loads go to are waited for where they are used
     each_of<0, kRing>([&](auto place) {
         each_of<0, kLoads>([&](auto j) { issue(begin + place < end, place, j); });
-        issued(begin + place);
+        issued(begin + place, place);
     });
     load(begin, 0);
     store(begin, 0);
     load(begin + 1, 1);
     load(begin + 2, 0);
-    meet<kLoads ? (kRing - 1) * kLoads : 64>();
+    meet<kLoads ? (kRing - 1) * kSure : 64>();
     if constexpr (kShifted) {
 #pragma unroll
         for (int i = 0; i < TP; ++i) shift[i] = 127 + kSpan - tops[32 * (wp * TP + i) + (lane & 31)];
     }
     Pieces f[2];
-    read_scales(0);
-    take_scales();
+    const std::integral_constant<int, 0> none;
+    read_scales(none);
+    take_scales(none);
 #pragma unroll
     for (int n = 0; n < kReads; ++n) read(f[0], 0, 0, n);
-    const std::integral_constant<int, 0> none;
     const std::integral_constant<int, kEarly> early;
     const std::integral_constant<int, kLoads> all;
     const std::integral_constant<int, kReads> reads;
@@ -538,25 +544,26 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     auto turn = [&](int slice, auto place) {
         constexpr int kPlace = decltype(place)::value, kNext = (kPlace + 1) % kRing;
         const auto before = std::integral_constant<int, (kPlace + kRing - 1) % kRing>();
+        const auto after = std::integral_constant<int, kNext>();
 #pragma unroll
         for (int s = 0; s < kPieces - 1; ++s) {
             multiply(f[s & 1], s, [&](int n) {
                 spread(none, reads, n, [&](auto r) { read(f[(s + 1) & 1], kPlace, s + 1, r); });
                 if (s == 0 && slice > begin) {
                     spread(early, all, n, [&](auto j) { issue(slice - 1 + kRing < end, before, j); });
-                    if (n == kProducts - 1) issued(slice - 1 + kRing);
+                    if (n == kProducts - 1) issued(slice - 1 + kRing, before);
                 }
             });
         }
         store(slice + 1, (kPlace + 1) & 1);
         meet<kPending>();
         load(slice + 3, (kPlace + 1) & 1);
-        read_scales(kNext);
+        read_scales(after);
         multiply(f[1], kPieces - 1, [&](int n) {
             spread(none, reads, n, [&](auto r) { read(f[0], kNext, 0, r); });
             spread(none, early, n, [&](auto j) { issue(slice + kRing < end, place, j); });
         });
-        take_scales();
+        take_scales(after);
     };
     for (int slice = begin; slice < end; slice += kRing)
         each_of<0, kRing>([&](auto place) {
@@ -751,8 +758,8 @@ enum Way { kStraight, kStaged, kFourBits };
 // The form and the parts of k whose workgroups take the least time by this account, fitted to products of 17 to 4096 rows by 500 to
 // 28672 columns, all forms and 1 to 16 parts of each, in microseconds: a slice of k of one workgroup alone on its compute unit, and
 // of each of several or where all of them work; what a workgroup takes besides; a join's launch and the bytes that pass through
-// memory for it.  (128 rows by 8192 columns by 28672 in 4 bits beside 16: 101 in form 1 and four parts, 110 in form 0 and eight, 225
-// in form 2 whole; 1024 rows of a gated block of 2048 x 2048: 25, 42 in form 0 and two parts, 32 in form 2.)
+// memory for it.  (1024 rows of a gated block
+// of 2048 x 2048: 25 in form 1, 42 in form 0 and two parts, 32 in form 2.)
 Choice choose(int64_t rows, int64_t cols, int64_t slices, bool pairs, int results, Way way) {
     constexpr double alone[3][3] = {{0.56, 0.27, 0.23}, {1.2, 0.8, 0.62}, {0.75, 0.38, 0.3}};
     constexpr double shared[3][3] = {{0.56, 0.29, 0.2}, {1.2, 0.5, 0.37}, {1.1, 0.5, 0.32}};
@@ -815,7 +822,8 @@ void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows
     const bool direct = FP == kFours || (whole_chunks(P, FP, FP == kAcross ? cols : k) && whole_chunks(Q, FQ, FQ == kAcross ? rows : k));
     const Choice c = choose(rows, cols, SEGS * ((k + kSlice - 1) / kSlice), GATED, results, FP == kFours ? kFourBits : direct ? kStraight : kStaged);
     const int64_t slice = c.form == 0 ? kSlice * row_bytes(FP, direct) / 64 : kSlice, slices = SEGS * ((k + slice - 1) / slice);
-    const int64_t wide = kWide[c.form] / (GATED ? 2 : 1), tall = kTall[c.form], each = (slices + c.parts - 1) / c.parts;
+    const int64_t wide = kWide[c.form] / (GATED ? 2 : 1), tall = kTall[c.form], share = (slices + c.parts - 1) / c.parts;
+    const int64_t each = FP == kCodes ? (share + 3) / 4 * 4 : share;      // parts begin where a word of scales does
     const int parts = (int)((slices + each - 1) / each);
     const Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
     const Split split = {parts, (int)each, (float*)work};
@@ -837,22 +845,37 @@ void by_half(int type, F f) {
 
 }  // namespace
 
-// Bytes of the scales of both operands in rows of whole words, where theirs are not.
-int64_t aligned_scales(int x_type, int64_t t, int64_t n, int64_t k) {
+// Bytes of `rows` rows of scales in whole words, where theirs are not.
+int64_t aligned_scales(int64_t rows, int64_t k) {
     const int64_t blocks = (k + kBlock - 1) / kBlock;
-    if (x_type != RSH_MX4 || blocks % 4 == 0) return 0;
-    return ((n + t) * ((blocks + 3) / 4) * 4 + 15) / 16 * 16;
+    return blocks % 4 == 0 ? 0 : (rows * ((blocks + 3) / 4) * 4 + 15) / 16 * 16;
+}
+
+// Puts them there: those of `a`'s n rows (second: of its second matrix too) and of b's t.  Returns what of `work` lies behind them.
+uint8_t* align_scales(Operand& a, int64_t n, bool second, Operand& b, int64_t t, int64_t k, void* work, hipStream_t st) {
+    const int64_t bytes = aligned_scales(second ? 2 * n : n + t, k), blocks = (k + kBlock - 1) / kBlock;
+    if (bytes) {
+        const uint8_t* const next = second ? a.scales[1] : b.scales[0];
+        const int64_t rest = second ? n : t;
+        a.ld_scales = b.ld_scales = (blocks + 3) / 4 * 4;
+        const int64_t words = (n + rest) * (a.ld_scales / 4);
+        hipLaunchKernelGGL(rsh_align_scales_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, st, a.scales[0], next, (uint32_t*)work, n, rest,
+                           (int)blocks);
+        a.scales[0] = (const uint8_t*)work;
+        (second ? a.scales[1] : b.scales[0]) = a.scales[0] + n * a.ld_scales;
+    }
+    return (uint8_t*)work + bytes;
 }
 
 int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k) {
     const int64_t step = x_type == RSH_MX4 ? 128 : 32;
     if (takes_few(t)) return 0;
-    return aligned_scales(x_type, t, n, k) + partial_bytes(t, n, (k + step - 1) / step, false, 1, x_type == RSH_MX4);
+    return aligned_scales(x_type == RSH_MX4 ? n + t : n, k) + partial_bytes(t, n, (k + step - 1) / step, false, 1, x_type == RSH_MX4);
 }
 
-int64_t gated_forward_work(int64_t t, int64_t d, int64_t f) {
+int64_t gated_forward_work(bool codes, int64_t t, int64_t d, int64_t f) {
     if (takes_few(t)) return 0;
-    return partial_bytes(t, f, (d + 31) / 32, true, 1, false);
+    return (codes ? aligned_scales(2 * f, d) : 0) + partial_bytes(t, f, (d + 31) / 32, true, 1, false);
 }
 
 // dG and dU, and behind them the larger of the sums of dX and of the weights' gradients (of both, or of one alone).
@@ -875,20 +898,13 @@ int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t 
         if (takes_few(t)) {
             if (x_type == RSH_MX4) launch_few<T, kFours, false>(p, q, res, t, n, k, (hipStream_t)stream);
             else launch_few<T, kCodes, false>(p, q, res, t, n, k, (hipStream_t)stream);
-        } else if (x_type == RSH_MX4) {
+        } else {
+            const bool four = x_type == RSH_MX4;
             Operand w = p, x = q;
-            const int64_t bytes = aligned_scales(x_type, t, n, k);
-            if (bytes) {
-                w.ld_scales = x.ld_scales = (blocks + 3) / 4 * 4;
-                const int64_t words = (n + t) * (w.ld_scales / 4);
-                hipLaunchKernelGGL(rsh_align_scales_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, (hipStream_t)stream,
-                                   (const uint8_t*)w_scales, (const uint8_t*)x_scales, (uint32_t*)work, n, t, (int)blocks);
-                w.scales[0] = (const uint8_t*)work;
-                x.scales[0] = w.scales[0] + n * w.ld_scales;
-            }
-            product<T, kFours, kFours, false, 1>(w, x, res, t, n, k, 1, (uint8_t*)work + bytes, (hipStream_t)stream);
+            void* const rest = align_scales(w, n, false, x, four ? t : 0, k, work, (hipStream_t)stream);
+            if (four) product<T, kFours, kFours, false, 1>(w, x, res, t, n, k, 1, rest, (hipStream_t)stream);
+            else product<T, kCodes, kAlong, false, 1>(w, x, res, t, n, k, 1, rest, (hipStream_t)stream);
         }
-        else product<T, kCodes, kAlong, false, 1>(p, q, res, t, n, k, 1, work, (hipStream_t)stream);
     });
     return launched();
 }
@@ -904,8 +920,11 @@ int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, 
         if (takes_few(t)) {
             if (g_scales) launch_few<T, kCodes, true>(p, q, res, t, f, d, (hipStream_t)stream);
             else launch_few<T, kAlong, true>(p, q, res, t, f, d, (hipStream_t)stream);
-        } else if (g_scales) product<T, kCodes, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
-        else product<T, kAlong, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
+        } else if (g_scales) {
+            Operand w = p, x = q;
+            void* const rest = align_scales(w, f, true, x, 0, d, work, (hipStream_t)stream);
+            product<T, kCodes, kAlong, true, 1>(w, x, res, t, f, d, 1, rest, (hipStream_t)stream);
+        } else product<T, kAlong, kAlong, true, 1>(p, q, res, t, f, d, 1, work, (hipStream_t)stream);
     });
     return launched();
 }

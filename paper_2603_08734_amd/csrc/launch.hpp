@@ -93,7 +93,7 @@ int launch_mx4_dequantize(const void* codes, const void* scales, int64_t rows, i
 // operands of 16 bits.  G, U, dG and dU have rows of f elements rounded up to a multiple of eight.  work: the bytes that the
 // *_work function of the same sizes says.
 int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k);
-int64_t gated_forward_work(int64_t t, int64_t d, int64_t f);
+int64_t gated_forward_work(bool codes, int64_t t, int64_t d, int64_t f);
 int64_t gated_backward_work(int64_t t, int64_t d, int64_t f);
 int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int y_type,
                        int64_t t, int64_t n, int64_t k, void* work, void* stream);
