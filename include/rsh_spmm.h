@@ -288,8 +288,7 @@ int rsh_act_backward(const void *dY_dev, const void *Y_dev, void *dZ_dev, float 
  * `type` (RSH_F16 or RSH_BF16), no alignment beyond the element's.  act: RSH_ACT_SILU, RSH_ACT_GELU (with the error function) or
  * RSH_ACT_RELU.  fp32 sums, each result rounded once.
  *   rsh_gated_forward   g_scales and u_scales not NULL: Wg and Wu in 4 bits (ld_w unused).  G and U: NULL, or kept for the
- *                       gradients: [t][f rounded up to a multiple of 8] cells of 16 bits, 16-byte aligned, in a form of
- *                       rsh_gated_backward's own (four numbers of 14 bits and their exponent in four cells)
+ *                       gradients: fp32 [t][f rounded up to a multiple of 8], 16-byte aligned
  *   rsh_gated_backward  dX, dWg, dWu: NULL where not wanted.  dH: rows ld_h apart.  dG and dU are rounded to `type`.
  * work: device, 16-byte aligned, of the bytes that the *_work function of the same sizes reports (0: may be NULL), rewritten by
  * every call.  t is positive and below 2^31; n, k, d, f and the distances between rows are at most RSH_FFN_MAX_WIDTH.  Results never depend on the order in which waves run.
@@ -307,11 +306,11 @@ int rsh_mx4_product(const void *X_dev, const void *x_scales_dev, int32_t x_type,
                     void *Y_dev, int32_t y_type, int64_t t, int64_t n, int64_t k, void *work_dev, void *hip_stream);
 int rsh_gated_forward_work(int32_t w_type, int64_t t, int64_t d, int64_t f, int64_t *bytes);
 int rsh_gated_forward(const void *X_dev, int32_t type, int64_t ld_x, const void *Wg_dev, const void *Wu_dev, int64_t ld_w, const void *g_scales_dev,
-                      const void *u_scales_dev, int32_t act, void *H_dev, void *G_dev, void *U_dev, int64_t t, int64_t d, int64_t f,
+                      const void *u_scales_dev, int32_t act, void *H_dev, float *G_dev, float *U_dev, int64_t t, int64_t d, int64_t f,
                       void *work_dev, void *hip_stream);
 int rsh_gated_backward_work(int64_t t, int64_t d, int64_t f, int64_t *bytes);
-int rsh_gated_backward(const void *X_dev, int32_t type, int64_t ld_x, const void *Wg_dev, const void *Wu_dev, int64_t ld_w, const void *G_dev,
-                       const void *U_dev, const void *dH_dev, int64_t ld_h, int32_t act, void *dX_dev, void *dWg_dev, void *dWu_dev, int64_t t,
+int rsh_gated_backward(const void *X_dev, int32_t type, int64_t ld_x, const void *Wg_dev, const void *Wu_dev, int64_t ld_w, const float *G_dev,
+                       const float *U_dev, const void *dH_dev, int64_t ld_h, int32_t act, void *dX_dev, void *dWg_dev, void *dWu_dev, int64_t t,
                        int64_t d, int64_t f, void *work_dev, void *hip_stream);
 
 /*

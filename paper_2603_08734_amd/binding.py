@@ -277,13 +277,14 @@ def mx4_product(X, x_scales, x_type: int, ld_x: int, codes, scales, Y, y_type: i
 
 def gated_forward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, g_scales, u_scales, act: int, f: int, keep: bool):
     """(H, G and U one behind the other or None) of the gated block (rsh_gated_forward)."""
+    import torch
     t, d = X.shape
     H = X.new_empty((t, f))
     kept = g = u = None
     if keep:
-        kept = X.new_empty((2, t, (f + 7) // 8 * 8))
+        kept = X.new_empty((2, t, (f + 7) // 8 * 8), dtype=torch.float32)
         g = kept.data_ptr()
-        u = g + kept.numel()       # half of its bytes
+        u = g + 2 * kept.numel()       # half of its bytes
     bytes_ = _work_bytes("rsh_gated_forward_work", x_type if g_scales is None else RSH_MX4, t, d, f)
     work = X.new_empty(bytes_ // 2) if bytes_ else None
     _check(lib().rsh_gated_forward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, _address(g_scales), _address(u_scales), act,
@@ -298,7 +299,7 @@ def gated_backward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, kept, dH, ld_h:
     dWg = X.new_empty((f, d)) if want[1] else None
     dWu = X.new_empty((f, d)) if want[2] else None
     work, g = X.new_empty(_work_bytes("rsh_gated_backward_work", t, d, f) // 2), kept.data_ptr()
-    _check(lib().rsh_gated_backward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, g, g + kept.numel(), dH.data_ptr(), ld_h, act,
+    _check(lib().rsh_gated_backward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, g, g + 2 * kept.numel(), dH.data_ptr(), ld_h, act,
                                     _address(dX), _address(dWg), _address(dWu), t, d, f, work.data_ptr(), current_stream()))
     return dX, dWg, dWu
 

@@ -698,7 +698,7 @@ int rsh_gated_forward_work(int32_t w_type, int64_t t, int64_t d, int64_t f, int6
 }
 
 int rsh_gated_forward(const void* X, int32_t type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
-                      const void* u_scales, int32_t act, void* H, void* G, void* U, int64_t t, int64_t d, int64_t f, void* work, void* hip_stream) {
+                      const void* u_scales, int32_t act, void* H, float* G, float* U, int64_t t, int64_t d, int64_t f, void* work, void* hip_stream) {
     int64_t bytes;
     if (!half_type(type) || act < RSH_ACT_SILU || act > RSH_ACT_RELU) return RSH_ERR_BAD_OPTION;
     if (const int rc = rsh_gated_forward_work(g_scales ? RSH_MX4 : type, t, d, f, &bytes)) return rc;
@@ -716,7 +716,7 @@ int rsh_gated_backward_work(int64_t t, int64_t d, int64_t f, int64_t* bytes) {
     return rc;
 }
 
-int rsh_gated_backward(const void* X, int32_t type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* G, const void* U,
+int rsh_gated_backward(const void* X, int32_t type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const float* G, const float* U,
                        const void* dH, int64_t ld_h, int32_t act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
                        void* hip_stream) {
     int64_t bytes;

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     constexpr int kWide = GATED ? kWidthP / 2 : kWidthP;                 // columns of the tile's result
     constexpr int kScaleRows = kFour ? kWidthP + kWidthQ : kWidthP;      // rows of a slice that have scales
     constexpr int kScaleTurns = (kScaleRows + kThreads - 1) / kThreads;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[larger(kRing * kBytesSlice, 2 * kWide * kWidthQ)];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[larger(kRing * kBytesSlice, (GATED ? 4 : 2) * kWide * kWidthQ)];
     // Four scales of a row: those of a slice, or beside codes, at their place, those of a ring of slices (a byte with every slice took as many
     // cycles of the loads' addresses as the codes: 128 rows through 8192 x 28672 113 us against 99).  A workgroup with more threads
     // than rows loads zeros behind them.
@@ -639,24 +639,30 @@ __global__ __launch_bounds__(64 * WP * WQ) void rsh_product_kernel(Operand P, Op
     };
     if constexpr (GATED) {
         if (res.gate) {
-            auto kept = [&](int which) {       // columns past the end are zero, that they do not set the scale of those before it
+            auto keep = [&](float* out, int which) {       // the same way, in 32 bits
+                constexpr int kIn = kWide / 4;
 #pragma unroll
                 for (int i = 0; i < TP; i += 2)
 #pragma unroll
                     for (int j = 0; j < TQ; ++j)
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
-                            const int64_t left = sh.cols - (col0 + 32 * (wp * TP + i) / 64 * 32 + 8 * g + half);
-                            float4_t x;
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) x[v] = v < left ? acc[i + which][j][4 * g + v] : 0.f;
-                            put(i, j, g, keep4(x));
+                            const int row = 32 * (wq * TQ + j) + (lane & 31), c = (32 * (wp * TP + i) / 64 * 32 + 8 * g + half) / 4;
+                            *reinterpret_cast<float4_t*>(lds + row * (4 * kWide) + ((c ^ (row & 15)) << 4)) =
+                                (float4_t){acc[i + which][j][4 * g], acc[i + which][j][4 * g + 1], acc[i + which][j][4 * g + 2], acc[i + which][j][4 * g + 3]};
                         }
+                __syncthreads();
+#pragma unroll 4
+                for (int n = threadIdx.x; n < kIn * kWidthQ; n += kThreads) {
+                    const int row = n / kIn, c = n % kIn;
+                    const float4_t v = *reinterpret_cast<const float4_t*>(lds + row * (4 * kWide) + ((c ^ (row & 15)) << 4));
+                    if (row0 + row < sh.rows && col0 + 4 * c < res.ld_gate)
+                        *reinterpret_cast<float4_t*>(out + (row0 + row) * res.ld_gate + col0 + 4 * c) = v;
+                }
+                __syncthreads();
             };
-            kept(0);
-            leave(res.gate, res.ld_gate, res.ld_gate);
-            kept(1);
-            leave(res.up, res.ld_gate, res.ld_gate);
+            keep(res.gate, 0);
+            keep(res.up, 1);
         }
         auto finished = [&](auto act) {
             each([&](int i, int j, int v) { return act_of(decltype(act)::value, acc[i][j][v]) * acc[i + 1][j][v]; });
@@ -704,8 +710,8 @@ __global__ __launch_bounds__(256) void rsh_join_parts_kernel(const float* __rest
 // dU = dH act(G) and dG = dH U act'(G), eight elements a thread, rounded to the 16 bits that the matrix units take: the gradients'
 // one rounding besides that of their results.  A pass over five arrays: 110 us at 4096 x 16384, 6.1 TB/s.
 template <class T>
-__global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* __restrict__ dH, const uint16_t* __restrict__ G,
-                                                                const uint16_t* __restrict__ U, uint16_t* __restrict__ dG,
+__global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* __restrict__ dH, const float* __restrict__ G,
+                                                                const float* __restrict__ U, uint16_t* __restrict__ dG,
                                                                 uint16_t* __restrict__ dU, int64_t t, int64_t f, int64_t ld, int64_t ld_gate, int act) {
     const uint32_t across = (uint32_t)((ld_gate + 2047) / 2048);
     const int64_t col = 8 * ((int64_t)(blockIdx.x % across) * 256 + threadIdx.x);
@@ -713,9 +719,8 @@ __global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* 
     for (int64_t row = blockIdx.x / across; row < t; row += gridDim.x / across) {
         const int64_t at = row * ld_gate + col;
         const uint4_t h = load8(dH + row * ld + col, f - col);
-        const uint4_t gk = *reinterpret_cast<const uint4_t*>(G + at), uk = *reinterpret_cast<const uint4_t*>(U + at);
-        const float4_t g[2] = {kept4((uint2_t){gk[0], gk[1]}), kept4((uint2_t){gk[2], gk[3]})};
-        const float4_t u[2] = {kept4((uint2_t){uk[0], uk[1]}), kept4((uint2_t){uk[2], uk[3]})};
+        const float4_t g[2] = {*reinterpret_cast<const float4_t*>(G + at), *reinterpret_cast<const float4_t*>(G + at + 4)};
+        const float4_t u[2] = {*reinterpret_cast<const float4_t*>(U + at), *reinterpret_cast<const float4_t*>(U + at + 4)};
         uint4_t a, b;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -914,7 +919,7 @@ int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, 
     const int64_t blocks = (d + kBlock - 1) / kBlock;
     const Operand p = {{Wg, Wu}, {(const uint8_t*)g_scales, (const uint8_t*)u_scales}, g_scales ? blocks : ld_w, blocks};
     const Operand q = {{X, nullptr}, {nullptr, nullptr}, ld_x, 0};
-    const Result res = {{(uint16_t*)H, nullptr}, (uint16_t*)G, (uint16_t*)U, f, (f + 7) / 8 * 8, act};
+    const Result res = {{(uint16_t*)H, nullptr}, (float*)G, (float*)U, f, (f + 7) / 8 * 8, act};
     by_half(type, [&](auto half) {
         using T = decltype(half);
         if (takes_few(t)) {
@@ -940,8 +945,8 @@ int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg,
     const Operand gates = {{dG, dU}, {nullptr, nullptr}, ld_gate, 0};
     by_half(type, [&](auto half) {
         using T = decltype(half);
-        hipLaunchKernelGGL(rsh_gate_backward_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, (const uint16_t*)dH, (const uint16_t*)G,
-                           (const uint16_t*)U, dG, dU, t, f, ld_h, ld_gate, act);
+        hipLaunchKernelGGL(rsh_gate_backward_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, (const uint16_t*)dH, (const float*)G,
+                           (const float*)U, dG, dU, t, f, ld_h, ld_gate, act);
         if (dX) {
             const Operand w = {{Wg, Wu}, {nullptr, nullptr}, ld_w, 0};
             const Result res = {{(uint16_t*)dX, nullptr}, nullptr, nullptr, d, 0, 0};

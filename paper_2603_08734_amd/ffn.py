@@ -4,7 +4,7 @@
     H = ffn.gated(X, Wg4, Wu4, "silu")         # the weights in 4 bits (mx4.quantize), for serving
 
 Both projections, the activation and the product run as one kernel (``rsh_gated_forward``): sums are fp32 until H is rounded.
-A forward pass that will be differentiated keeps both projections, four numbers of 14 bits to an exponent; the backward pass
+A forward pass that will be differentiated keeps both projections in fp32; the backward pass
 (``rsh_gated_backward``) forms their gradients in one pass over them, rounds those to the inputs' type, and multiplies.
 """
 from __future__ import annotations
