@@ -126,14 +126,16 @@ struct Stage {
             }
         }
     }
-    // Into LDS.  In the last slice the elements of a cut chunk go to its front, and what lies past k becomes zero.
+    // Into LDS.  The elements of a cut chunk go to its front, and what lies past k becomes zero.  Both are of the last slice, but for k
+    // across lines of one to three elements: a chunk then runs through lines behind its own, and the operand's end cuts those of the last
+    // seven lines, some of which the slice before may have.
     __device__ __forceinline__ void store(int odd, int64_t k0, int64_t k, unsigned char* lds) {
         const int left = (int)min(k - k0, (int64_t)kSlice), end = (int)min(span - (FORM == kAlong ? 2 * k0 : k0 * stride) - 16, (int64_t)0x7ffffff0);
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int i = threadIdx.x + THREADS * j;
             uint4_t x = v[odd][j];
-            if (k0 + kSlice >= k) {
+            if (k0 + kSlice + (FORM == kAcross ? 6 : 0) >= k) {
                 const int past = (int)line[j] + 16 * chunk - end, drop = span >= 16 ? max(0, min(past, 16)) / 2 : 0;
                 const int keep = FORM == kAlong ? left - 8 * chunk : i / (WIDTH / 8) < left ? 8 : 0;
                 if (drop & 4) x = (uint4_t){x[2], x[3], 0, 0};
