@@ -1,6 +1,6 @@
 """The gated feed-forward block H = act(X Wg^T) * (X Wu^T), forward and backward, in kernels of the library.
 
-    H = ffn.gated(X, W_gate, W_up, "silu")     # binary16 or bfloat16, X [..., d], weights [f, d]; autograd-aware
+    H = ffn.gated(X, W_gate, W_up, "silu")     # binary16 or bfloat16, X [..., d], weights [f, d]; autograd-aware (reverse mode)
     H = ffn.gated(X, Wg4, Wu4, "silu")         # the weights in 4 bits (mx4.quantize), for serving
 
 Both projections, the activation and the product run as one kernel (``rsh_gated_forward``): sums are fp32 until H is rounded.
@@ -13,8 +13,9 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding
-from .mx4 import HALVES, Mx4, _no_gradient, _on, _rows, product
+from .mx4 import HALVES, Mx4, _no_gradient, _on, _rows, _tangent, product
 
+_FORWARD_MODE = "the gated block and its gradients have no forward-mode derivative: call them on detached operands"
 ACTIVATIONS = {"silu": binding.RSH_ACT_SILU, "gelu": binding.RSH_ACT_GELU, "relu": binding.RSH_ACT_RELU}
 
 
@@ -33,6 +34,8 @@ def _forward(X, Wg, Wu, act, keep):
 
 
 def _backward(ctx, dH):
+    if _tangent(dH):
+        raise ValueError(_FORWARD_MODE)
     X, Wg, Wu, kept = ctx.saved_tensors
     x, ld_x = _rows(X)
     wg, wu, ld_w = _weights(Wg, Wu)
@@ -89,6 +92,8 @@ def gated(X, W_gate, W_up, activation: str = "silu"):
     rows = X if flat else X.reshape(-1, d) if d else X.reshape(X.shape[:-1].numel(), 0)
     if four:
         _no_gradient(X)
+    elif _tangent(X, W_gate, W_up):
+        raise ValueError(_FORWARD_MODE)
     if rows.shape[0] == 0 or f == 0 or d == 0:
         # no sums: zeros, whose gradients are zeros
         H = rows.sum() * 0 + rows.new_zeros((rows.shape[0], f))

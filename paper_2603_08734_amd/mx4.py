@@ -7,13 +7,15 @@
     mx4.dequantize(W4, torch.float32)    # the values
 
 All of it runs in kernels of the library (``rsh_mx4_*``) on the current stream; sums are fp32, rounded once.  Serving
-forms: nothing here records a gradient, and operands that want one are refused while gradients are recorded.
+forms: nothing here records a gradient, and operands that want one are refused while gradients are recorded; operands with a
+forward-mode tangent are refused.
 """
 from __future__ import annotations
 
 import contextlib
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 
@@ -48,9 +50,19 @@ def _rows(X):
     return X, X.stride(0) if X.shape[0] > 1 else k
 
 
+def _tangent(*tensors) -> bool:
+    """Whether one of them carries a tangent (forward-mode derivatives, which torch.no_grad() does not stop)."""
+    for t in tensors:
+        if forward_ad.unpack_dual(t).tangent is not None:
+            return True
+    return False
+
+
 def _no_gradient(*tensors) -> None:
     if any(t.requires_grad for t in tensors) and torch.is_grad_enabled():
         raise ValueError("products and conversions in 4 bits have no gradient: call them under torch.no_grad() or on detached operands")
+    if _tangent(*tensors):
+        raise ValueError("products and conversions in 4 bits have no forward-mode derivative: call them on detached operands")
 
 
 class Mx4:
