@@ -113,13 +113,15 @@ class FeedForward:
     """A gated feed-forward layer as it is served: Y = W_down (act(X W_gate^T) * (X W_up^T)).
 
     W_gate, W_up: [f, d] of the activations' type, or in 4 bits (``mx4.quantize``).  W_down: [d, f] in 4 bits, or a ``Plan`` of the
-    pruned weight for exactly as many tokens as X has (binary16: the sparse product takes the tokens as columns)."""
+    pruned weight for exactly as many tokens as X has (binary16: the sparse product takes the tokens as columns).  Either way the layer
+    has no gradient, and operands that want one are refused while gradients are recorded."""
 
     def __init__(self, W_gate, W_up, W_down, activation: str = "silu"):
         self.W_gate, self.W_up, self.W_down, self.activation = W_gate, W_up, W_down, activation
 
     def __call__(self, X):
         """X: [t, d]; result [t, d] of its type."""
+        _no_gradient(*(m for m in (X, self.W_gate, self.W_up) if isinstance(m, torch.Tensor)))
         H = gated(X, self.W_gate, self.W_up, self.activation)
         if isinstance(self.W_down, Mx4):
             return product(H, self.W_down)

@@ -22,6 +22,7 @@ from . import binding
 BLOCK = 32
 _TYPES = {torch.float32: binding.RSH_F32, torch.float16: binding.RSH_F16, torch.bfloat16: binding.RSH_BF16}
 _NOTHING = contextlib.nullcontext()
+_WHAT = "products and conversions in 4 bits, and layers as they are served, have"
 
 
 def _on(index: int):
@@ -60,9 +61,9 @@ def _tangent(*tensors) -> bool:
 
 def _no_gradient(*tensors) -> None:
     if any(t.requires_grad for t in tensors) and torch.is_grad_enabled():
-        raise ValueError("products and conversions in 4 bits have no gradient: call them under torch.no_grad() or on detached operands")
+        raise ValueError(f"{_WHAT} no gradient: call them under torch.no_grad() or on detached operands")
     if _tangent(*tensors):
-        raise ValueError("products and conversions in 4 bits have no forward-mode derivative: call them on detached operands")
+        raise ValueError(f"{_WHAT} no forward-mode derivative: call them on detached operands")
 
 
 class Mx4:

@@ -44,3 +44,29 @@ def test_a_tangent_of_the_incoming_gradient_is_refused():
         dual = forward_ad.make_dual(torch.ones_like(H), torch.ones_like(H))
         with pytest.raises(ValueError, match="forward-mode"):
             torch.autograd.grad(H, x, dual)
+
+
+@pytest.mark.parametrize("back", ["codes", "plan"])
+def test_a_served_layer_refuses_operands_that_want_a_gradient(back):
+    import os
+    import sys
+    import torch
+    from torch.autograd import forward_ad
+    from paper_2603_08734_amd import ffn, mx4
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    from feed_forward import prune
+    wg, wu = _weights(f=64, d=48)
+    wd = torch.randn((48, 64), device="cuda").half()
+    down = mx4.quantize(wd) if back == "codes" else prune(wd, 0.5, 8)
+    x = torch.randn((8, 48), device="cuda").half()
+    want = ffn.FeedForward(wg, wu, down)(x)
+    for operands in ((x.clone().requires_grad_(), wg, wu), (x, wg.clone().requires_grad_(), wu), (x, wg, wu.clone().requires_grad_())):
+        layer = ffn.FeedForward(*operands[1:], down)
+        with pytest.raises(ValueError, match="gradient"):
+            layer(operands[0])
+        with torch.no_grad():
+            assert torch.equal(layer(operands[0]), want)
+    with forward_ad.dual_level(), pytest.raises(ValueError, match="forward-mode"):
+        ffn.FeedForward(wg, wu, down)(forward_ad.make_dual(x, torch.ones_like(x)))
+    if back == "plan":
+        down.destroy()
