@@ -13,6 +13,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding
+from .binding import Plan
 from .mx4 import HALVES, Mx4, _no_gradient, _on, _rows, _tangent, product
 
 _FORWARD_MODE = "the gated block and its gradients have no forward-mode derivative: call them on detached operands"
@@ -117,16 +118,23 @@ class FeedForward:
     has no gradient, and operands that want one are refused while gradients are recorded."""
 
     def __init__(self, W_gate, W_up, W_down, activation: str = "silu"):
+        if not isinstance(W_down, (Mx4, Plan)):
+            raise TypeError(f"W_down: expected Mx4 or Plan, got {type(W_down)}")
+        shape = (W_down.n_rows, W_down.n_cols) if isinstance(W_down, Plan) else W_down.shape
+        if len(W_gate.shape) != 2 or shape[1] != W_gate.shape[0]:
+            raise ValueError(f"W_gate {tuple(W_gate.shape)} and W_down {shape}: expected [f, d] and [d, f]")
         self.W_gate, self.W_up, self.W_down, self.activation = W_gate, W_up, W_down, activation
 
     def __call__(self, X):
-        """X: [t, d]; result [t, d] of its type."""
+        """X: [t, d]; result [t, d] of its type, from a ``Plan`` the transposed view of a [d, t] matrix."""
+        if not isinstance(X, torch.Tensor) or X.dim() != 2:
+            raise ValueError(f"X: expected a matrix, got {tuple(X.shape) if isinstance(X, torch.Tensor) else type(X)}")
+        if isinstance(self.W_down, Plan) and (X.dtype != torch.float16 or X.shape[0] != self.W_down.N):
+            raise ValueError(f"the plan is for {self.W_down.N} tokens of binary16, got {X.shape[0]} of {X.dtype}")
         _no_gradient(*(m for m in (X, self.W_gate, self.W_up) if isinstance(m, torch.Tensor)))
         H = gated(X, self.W_gate, self.W_up, self.activation)
         if isinstance(self.W_down, Mx4):
             return product(H, self.W_down)
-        if H.dtype != torch.float16 or H.shape[0] != self.W_down.N:
-            raise ValueError(f"the plan is for {self.W_down.N} tokens of binary16, got {H.shape[0]} of {H.dtype}")
         Y = torch.empty((self.W_down.n_rows, self.W_down.N), dtype=torch.float16, device=H.device)
         with _on(H.get_device()):
             self.W_down.spmm_f16(H.t().contiguous(), Y)
