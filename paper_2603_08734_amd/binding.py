@@ -19,6 +19,7 @@ RSH_OK = 0
  RSH_ERR_HIP, RSH_ERR_NOT_UPLOADED, RSH_ERR_TOO_LARGE) = range(1, 9)
 
 RSH_F32, RSH_F16, RSH_BF16, RSH_MX4 = range(4)
+RSH_FFN_MAX_WIDTH = 1 << 21
 RSH_ACT_SILU, RSH_ACT_GELU, RSH_ACT_RELU = range(3)
 
 (RSH_ARR_WIN_ROW, RSH_ARR_WIN_TILE_OFF, RSH_ARR_TILE_COLID, RSH_ARR_TILE_MASK, RSH_ARR_TILE_VAL_OFF,

@@ -30,7 +30,7 @@ def _on(index: int):
     return _NOTHING if index == torch._C._cuda_getDevice() else torch.cuda.device(index)
 
 
-def _matrix(X, name: str, types):
+def _matrix(X, name: str, types, most: int):
     """X as (matrix whose rows are contiguous, elements from row to row)."""
     if not isinstance(X, torch.Tensor) or X.dtype not in types:
         raise TypeError(f"{name}: expected a tensor of {' or '.join(str(t) for t in types)}, got {getattr(X, 'dtype', type(X))}")
@@ -38,15 +38,16 @@ def _matrix(X, name: str, types):
         raise ValueError(f"{name}: expected a matrix, got shape {tuple(X.shape)}")
     if not X.is_cuda:
         raise ValueError(f"{name}: expected a tensor on the GPU, got {X.device}")
-    return _rows(X)
+    return _rows(X, most)
 
 
-def _rows(X):
-    """The same for a matrix that is known to be one."""
+def _rows(X, most: int = binding.RSH_FFN_MAX_WIDTH):
+    """The same for a matrix that is known to be one.  Rows further apart than `most` elements, which the library refuses, are copied
+    like columns with a stride."""
     k = X.shape[1]
     if X.is_contiguous():
         return X, k
-    if (k > 1 and X.stride(1) != 1) or (X.shape[0] > 1 and X.stride(0) < k):
+    if (k > 1 and X.stride(1) != 1) or (X.shape[0] > 1 and not k <= X.stride(0) <= most):
         return X.contiguous(), k
     return X, X.stride(0) if X.shape[0] > 1 else k
 
@@ -103,7 +104,7 @@ class Mx4:
 
 def quantize(X) -> Mx4:
     """X [rows, k] (fp32, binary16 or bfloat16; rows with a stride are read in place) in 4 bits."""
-    X, ld = _matrix(X, "X", _TYPES)
+    X, ld = _matrix(X, "X", _TYPES, (1 << 31) - 1)
     _no_gradient(X)
     rows, k = X.shape
     if rows == 0 or k == 0:
@@ -136,7 +137,7 @@ def product(X, W: Mx4, dtype=None):
             raise TypeError(f"dtype: expected one of {list(HALVES)} beside activations in 4 bits, got {dtype}")
         data, x_scales, x_type, ld = X.codes, X.scales, binding.RSH_MX4, 0
     else:
-        data, ld = _matrix(X, "X", HALVES)
+        data, ld = _matrix(X, "X", HALVES, binding.RSH_FFN_MAX_WIDTH)
         _no_gradient(data)
         if dtype not in (None, data.dtype):
             raise TypeError(f"dtype: the result has the activations' type {data.dtype}, asked for {dtype}")
