@@ -32,11 +32,13 @@ struct Result {
     int act;
 };
 
+// max(g, 0), of NaN NaN.  (g times a truth value would make NaN of minus infinity.)
+__device__ __forceinline__ float relu_of(float g) { return g < 0.f ? 0.f : g; }
 // act(g) and its derivative.  silu: g s with s = 1 / (1 + exp(-g)); gelu: g times the normal distribution function.
 __device__ __forceinline__ float act_of(int act, float g) {
     if (act == kSilu) return g / (1.f + __expf(-g));
     if (act == kGelu) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
-    return g * (g > 0.f ? 1.f : 0.f);
+    return relu_of(g);
 }
 __device__ __forceinline__ float act_of(int act, float g, float* slope) {
     if (act == kSilu) {
@@ -50,7 +52,7 @@ __device__ __forceinline__ float act_of(int act, float g, float* slope) {
         return g * c;
     }
     *slope = g > 0.f ? 1.f : 0.f;
-    return g * *slope;
+    return relu_of(g);
 }
 
 // What becomes of the sums of four columns of a row.
