@@ -155,17 +155,17 @@ struct Buffer {
     uint32_t size;     // bytes; reads past them come back as zero
 };
 
-// BYTES (16, 4 or 1) a lane from byte `at` of a buffer to LDS: lane by lane behind byte `lds` + PLUS of it, at least four bytes each.
+// BYTES (16 or 4) a lane from byte `at` of a buffer to LDS: lane by lane behind byte `lds` + PLUS of it.
 // Written as an instruction because the compiler, which does not see that reads of LDS are of other slices, has them wait for every
 // load that it knows to be on its way there.  What a wave has in flight is counted where it meets the others.
 template <int BYTES, int PLUS>
 __device__ __forceinline__ void load_to_lds([[maybe_unused]] Buffer buffer, [[maybe_unused]] uint32_t at, [[maybe_unused]] uint32_t lds) {
+    static_assert(BYTES == 16 || BYTES == 4);
 #ifdef __HIP_DEVICE_COMPILE__
     const uint4_t d = {(uint32_t)buffer.at, (uint32_t)(buffer.at >> 32), buffer.size, 0x00020000u};
 #define RSH_LOAD(name) asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\t" name " %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(d), "n"(PLUS) : "memory", "scc")
     if constexpr (BYTES == 16) RSH_LOAD("buffer_load_dwordx4");
-    else if constexpr (BYTES == 4) RSH_LOAD("buffer_load_dword");
-    else RSH_LOAD("buffer_load_ubyte");
+    else RSH_LOAD("buffer_load_dword");
 #undef RSH_LOAD
 #endif
 }
