@@ -273,7 +273,8 @@ int rsh_act_backward(const void *dY_dev, const void *Y_dev, void *dZ_dev, float 
  *   rsh_mx4_quantize    s brings the largest magnitude of a block into [4, 8): floor(log2 max) - 2 + 127, at least 0; elements go
  *                       to the nearest value, ties to the even code, above 6 to 6.  A block of zeros: s = 0.  A block with an
  *                       infinity or a NaN: s = 255, codes 0.
- *   rsh_mx4_dequantize  the values, rounded once (to RSH_F32 and RSH_BF16 they are exact)
+ *   rsh_mx4_dequantize  the values, rounded once (to RSH_F32 and RSH_BF16 they are exact; with scales of 253 and 254, which
+ *                       rsh_mx4_quantize does not make, those from 2^128 on are infinite there, and may be so in products)
  * type: RSH_F32, RSH_F16 or RSH_BF16, of X and Y, whose rows are ld elements apart (ld >= k); no alignment beyond the element's.
  *
  *   rsh_mx4_product     Y[i][j] = sum over k of X[i][k] w[j][k], fp32 sums, rounded once to y_type (RSH_F16 or RSH_BF16);
@@ -289,7 +290,9 @@ int rsh_act_backward(const void *dY_dev, const void *Y_dev, void *dZ_dev, float 
  * RSH_ACT_RELU.  fp32 sums, each result rounded once.
  *   rsh_gated_forward   g_scales and u_scales not NULL: Wg and Wu in 4 bits (ld_w unused).  G and U: NULL, or kept for the
  *                       gradients: fp32 [t][f rounded up to a multiple of 8], 16-byte aligned
- *   rsh_gated_backward  dX, dWg, dWu: NULL where not wanted.  dH: rows ld_h apart.  dG and dU are rounded to `type`.
+ *   rsh_gated_backward  dX, dWg, dWu: NULL where not wanted.  dH: rows ld_h apart.  dG and dU are rounded to `type`, as operands of
+ *                       the products: 2^-9 relative in bfloat16; in binary16 2^-12, zero below 2^-25 and infinite from 65520 on
+ *                       (scale dH where they could leave that range)
  * work: device, 16-byte aligned, of the bytes that the *_work function of the same sizes reports (0: may be NULL), rewritten by
  * every call.  t is positive and below 2^31; n, k, d, f and the distances between rows are at most RSH_FFN_MAX_WIDTH.  Results never depend on the order in which waves run.
  * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE

@@ -5,7 +5,8 @@
 
 Both projections, the activation and the product run as one kernel (``rsh_gated_forward``): sums are fp32 until H is rounded.
 A forward pass that will be differentiated keeps both projections in fp32; the backward pass
-(``rsh_gated_backward``) forms their gradients in one pass over them, rounds those to the inputs' type, and multiplies.
+(``rsh_gated_backward``) forms their gradients in one pass over them, rounds those to the inputs' type, and multiplies.  In binary16
+that rounding has the type's range: scale the loss, as for any gradients in binary16.
 """
 from __future__ import annotations
 
