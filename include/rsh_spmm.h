@@ -317,6 +317,15 @@ int rsh_gated_backward(const void *X_dev, int32_t type, int64_t ld_x, const void
                        int64_t d, int64_t f, void *work_dev, void *hip_stream);
 
 /*
+ * Which tiles a product above runs in (nothing is launched): tile[0] rows and tile[1] columns of the result, tile[2] parts of its sums,
+ * all 0 for the kernels of few rows.  aligned: whether the rows of the 16-bit operands are whole 16 bytes at 16-byte boundaries.
+ * RSH_TILES_PRODUCT, RSH_TILES_PRODUCT4 (X in 16 and in 4 bits): t, n, k.  The others: t, d, f; RSH_TILES_GATED4 with weights in 4
+ * bits, RSH_TILES_DW with both weights' gradients wanted, RSH_TILES_DW_ONE with one.
+ */
+enum { RSH_TILES_PRODUCT = 0, RSH_TILES_PRODUCT4 = 1, RSH_TILES_GATED = 2, RSH_TILES_GATED4 = 3, RSH_TILES_DX = 4, RSH_TILES_DW = 5, RSH_TILES_DW_ONE = 6 };
+int rsh_ffn_tiles(int32_t which, int32_t aligned, int64_t t, int64_t a, int64_t b, int32_t *tile);
+
+/*
  * Same work as rsh_spmm, but brackets each kernel with HIP events on hip_stream,
  * waits for the stream, and reports the elapsed milliseconds of the tile kernel,
  * the irregular kernel and the combine kernel (0 for a kernel that was not

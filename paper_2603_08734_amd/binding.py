@@ -21,6 +21,7 @@ RSH_OK = 0
 RSH_F32, RSH_F16, RSH_BF16, RSH_MX4 = range(4)
 RSH_FFN_MAX_WIDTH = 1 << 21
 RSH_ACT_SILU, RSH_ACT_GELU, RSH_ACT_RELU = range(3)
+(RSH_TILES_PRODUCT, RSH_TILES_PRODUCT4, RSH_TILES_GATED, RSH_TILES_GATED4, RSH_TILES_DX, RSH_TILES_DW, RSH_TILES_DW_ONE) = range(7)
 
 (RSH_ARR_WIN_ROW, RSH_ARR_WIN_TILE_OFF, RSH_ARR_TILE_COLID, RSH_ARR_TILE_MASK, RSH_ARR_TILE_VAL_OFF,
  RSH_ARR_TILE_VAL, RSH_ARR_TILE_ITEM, RSH_ARR_IRR_COL, RSH_ARR_IRR_VAL, RSH_ARR_IRR_WAVE, RSH_ARR_IRR_ROW,
@@ -42,6 +43,7 @@ EXPORTED_SYMBOLS = [
     "rsh_plan_opts_default", "rsh_plan_create", "rsh_spmm", "rsh_spmm_noalloc", "rsh_spmm_f16", "rsh_spmm_profile",
     "rsh_dense_forward", "rsh_dense_backward", "rsh_act_backward", "rsh_mx4_quantize", "rsh_mx4_dequantize",
     "rsh_mx4_product_work", "rsh_mx4_product", "rsh_gated_forward_work", "rsh_gated_forward", "rsh_gated_backward_work", "rsh_gated_backward",
+    "rsh_ffn_tiles",
     "rsh_copy_probe", "rsh_plan_destroy", "rsh_plan_stats",
     "rsh_plan_decode", "rsh_plan_row_order", "rsh_reorder_knn", "rsh_plan_array", "rsh_plan_teams_per_wave",
     "rsh_plan_kernels", "rsh_plan_strip", "rsh_plan_operand",
@@ -136,6 +138,7 @@ def lib() -> ctypes.CDLL:
         L.rsh_gated_forward.argtypes = [vp, i32, i64, vp, vp, i64, vp, vp, i32, vp, vp, vp, i64, i64, i64, vp, vp]
         L.rsh_gated_backward_work.argtypes = [i64, i64, i64, i64p]
         L.rsh_gated_backward.argtypes = [vp, i32, i64, vp, vp, i64, vp, vp, vp, i64, i32, vp, vp, vp, i64, i64, i64, vp, vp]
+        L.rsh_ffn_tiles.argtypes = [i32, i32, i64, i64, i64, ctypes.POINTER(i32)]
         L.rsh_copy_probe.argtypes = [vp, vp, ctypes.c_int64, vp]
         L.rsh_plan_destroy.argtypes = [vp]
         L.rsh_plan_stats.argtypes = [vp, ctypes.POINTER(rsh_plan_stats_t)]
@@ -303,6 +306,13 @@ def gated_backward(X, x_type: int, ld_x: int, Wg, Wu, ld_w: int, kept, dH, ld_h:
     _check(lib().rsh_gated_backward(X.data_ptr(), x_type, ld_x, Wg.data_ptr(), Wu.data_ptr(), ld_w, g, g + 2 * kept.numel(), dH.data_ptr(), ld_h, act,
                                     _address(dX), _address(dWg), _address(dWu), t, d, f, work.data_ptr(), current_stream()))
     return dX, dWg, dWu
+
+
+def ffn_tiles(which: int, aligned: bool, t: int, a: int, b: int):
+    """(rows, columns, parts of the sums) of the tiles that a feed-forward product runs in, zeros for few rows (rsh_ffn_tiles)."""
+    tile = (ctypes.c_int32 * 3)()
+    _check(lib().rsh_ffn_tiles(which, int(aligned), t, a, b, tile))
+    return tuple(tile)
 
 
 def rsh_copy_probe(src, dst, nbytes: int, stream=None) -> None:

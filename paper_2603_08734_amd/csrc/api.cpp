@@ -729,6 +729,14 @@ int rsh_gated_backward(const void* X, int32_t type, int64_t ld_x, const void* Wg
     return launch_status(rsh::launch_gated_backward(X, type, ld_x, Wg, Wu, ld_w, G, U, dH, ld_h, act, dX, dWg, dWu, t, d, f, work, hip_stream));
 }
 
+int rsh_ffn_tiles(int32_t which, int32_t aligned, int64_t t, int64_t a, int64_t b, int32_t* tile) {
+    if (!tile) return RSH_ERR_NULL;
+    if (which < RSH_TILES_PRODUCT || which > RSH_TILES_DW_ONE) return RSH_ERR_BAD_OPTION;
+    if (const int rc = sizes_ok(t, a, b)) return rc;
+    rsh::ffn_tiles(which, aligned != 0, t, a, b, tile);
+    return RSH_OK;
+}
+
 int rsh_copy_probe(const void* src_dev, void* dst_dev, int64_t bytes, void* hip_stream) {
     if (!src_dev || !dst_dev) return RSH_ERR_NULL;
     if (bytes < 0 || (bytes & 15) || ((uintptr_t)src_dev & 15u) || ((uintptr_t)dst_dev & 15u)) return RSH_ERR_BAD_OPTION;

@@ -823,17 +823,27 @@ void launch_tiles(int form, dim3 grid, const Operand& P, const Operand& Q, const
         hipLaunchKernelGGL((rsh_product_kernel<T, FP, FQ, GATED, SEGS, 64, 2, 2, 2, 1, DIRECT>), grid, dim3(256), 0, st, P, Q, res, sh, split);
 }
 
+// Of a product: the form, rows and columns of a tile's result, parts of k and the slices of each.
+struct Tiling {
+    int form;
+    int64_t tall, wide;
+    int parts, each;
+};
+Tiling tiling(Form p, int segs, bool pairs, int results, bool direct, int64_t rows, int64_t cols, int64_t k) {
+    const int64_t least = p == kFours ? 128 : 32;
+    const Choice c = choose(rows, cols, segs * ((k + least - 1) / least), pairs, results, p == kFours ? kFourBits : direct ? kStraight : kStaged);
+    const int64_t slice = c.form == 0 ? least * row_bytes(p, direct) / 64 : least, slices = segs * ((k + slice - 1) / slice);
+    const int64_t share = (slices + c.parts - 1) / c.parts, each = p == kCodes ? (share + 3) / 4 * 4 : share;      // parts begin where a word of scales does
+    return {c.form, kTall[c.form], kWide[c.form] / (pairs ? 2 : 1), (int)((slices + each - 1) / each), (int)each};
+}
+
 template <class T, Form FP, Form FQ, bool GATED, int SEGS>
 void product(const Operand& P, const Operand& Q, const Result& res, int64_t rows, int64_t cols, int64_t k, int results, void* work, hipStream_t st) {
-    constexpr int64_t kSlice = FP == kFours ? 128 : 32;
     const bool direct = FP == kFours || (whole_chunks(P, FP, FP == kAcross ? cols : k) && whole_chunks(Q, FQ, FQ == kAcross ? rows : k));
-    const Choice c = choose(rows, cols, SEGS * ((k + kSlice - 1) / kSlice), GATED, results, FP == kFours ? kFourBits : direct ? kStraight : kStaged);
-    const int64_t slice = c.form == 0 ? kSlice * row_bytes(FP, direct) / 64 : kSlice, slices = SEGS * ((k + slice - 1) / slice);
-    const int64_t wide = kWide[c.form] / (GATED ? 2 : 1), tall = kTall[c.form], share = (slices + c.parts - 1) / c.parts;
-    const int64_t each = FP == kCodes ? (share + 3) / 4 * 4 : share;      // parts begin where a word of scales does
-    const int parts = (int)((slices + each - 1) / each);
-    const Shape sh = {rows, cols, k, (int)((rows + tall - 1) / tall), (int)((cols + wide - 1) / wide)};
-    const Split split = {parts, (int)each, (float*)work};
+    const Tiling c = tiling(FP, SEGS, GATED, results, direct, rows, cols, k);
+    const int parts = c.parts;
+    const Shape sh = {rows, cols, k, (int)((rows + c.tall - 1) / c.tall), (int)((cols + c.wide - 1) / c.wide)};
+    const Split split = {parts, c.each, (float*)work};
     const int64_t tiles = (int64_t)sh.tiles_r * sh.tiles_c;
     const dim3 grid((unsigned)((tiles + 7) / 8 * 8), parts, results);
     if constexpr (FP != kFours)
@@ -883,6 +893,20 @@ int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k) {
 int64_t gated_forward_work(bool codes, int64_t t, int64_t d, int64_t f) {
     if (takes_few(t)) return 0;
     return (codes ? aligned_scales(2 * f, d) : 0) + partial_bytes(t, f, (d + 31) / 32, true, 1, false);
+}
+
+// tile: rows and columns of the result, parts of k; zeros for the kernels of few rows.  The same choice as the launches'.
+void ffn_tiles(int which, bool aligned, int64_t t, int64_t a, int64_t b, int32_t* tile) {
+    Tiling c = {0, 0, 0, 0, 0};
+    const bool backward = which == RSH_TILES_DX || which == RSH_TILES_DW || which == RSH_TILES_DW_ONE;
+    if (which == RSH_TILES_DX) c = tiling(kAcross, 2, false, 1, aligned, t, a, b);
+    else if (backward) c = tiling(kAcross, 1, false, which == RSH_TILES_DW ? 2 : 1, aligned, b, a, t);
+    else if (!takes_few(t) && which == RSH_TILES_PRODUCT) c = tiling(kCodes, 1, false, 1, aligned, t, a, b);
+    else if (!takes_few(t) && which == RSH_TILES_PRODUCT4) c = tiling(kFours, 1, false, 1, true, t, a, b);
+    else if (!takes_few(t)) c = tiling(which == RSH_TILES_GATED4 ? kCodes : kAlong, 1, true, 1, aligned, t, b, a);
+    tile[0] = (int32_t)c.tall;
+    tile[1] = (int32_t)c.wide;
+    tile[2] = c.parts;
 }
 
 // dG and dU, and behind them the larger of the sums of dX and of the weights' gradients (of both, or of one alone).

@@ -96,6 +96,7 @@ int launch_mx4_dequantize(const void* codes, const void* scales, int64_t rows, i
 int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k);
 int64_t gated_forward_work(bool codes, int64_t t, int64_t d, int64_t f);
 int64_t gated_backward_work(int64_t t, int64_t d, int64_t f);
+void ffn_tiles(int which, bool aligned, int64_t t, int64_t a, int64_t b, int32_t* tile);
 int launch_mx4_product(const void* X, const void* x_scales, int x_type, int64_t ld_x, const void* W, const void* w_scales, void* Y, int y_type,
                        int64_t t, int64_t n, int64_t k, void* work, void* stream);
 int launch_gated_forward(const void* X, int type, int64_t ld_x, const void* Wg, const void* Wu, int64_t ld_w, const void* g_scales,
