@@ -7,7 +7,7 @@
 // whose four words then make four operands.  Several groups of rows share the tokens' pieces.  The waves' sums meet in LDS and are
 // added in the waves' order.
 //
-// Measured: one token through the gated block of 8192 x 28672 in bfloat16 163 us (940 MB, 5.8 TB/s); through 28672 x 8192 in 4 bits
+// Measured: one token through the gated block of 8192 x 28672 in bfloat16 164 us (940 MB, 5.7 TB/s); through 28672 x 8192 in 4 bits
 // 27 us (125 MB, 4.6 TB/s; 39 on the matrix units); 16 tokens through the gated block of 4096 x 16384 in 4 bits 21 us (71 MB), bound
 // by the reads of the tokens, 4 KB for every 4 KB of codes.
 #include <algorithm>
@@ -363,8 +363,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rsh_one_row_kernel(Operand P, 
 }
 
 // Up to one tile of 16 tokens (two of eight beside codes in binary16).  Beyond, tiles of 128 x 64 read the tokens once for 128 weight
-// rows: 28672 x 8192 in 4 bits takes 16 tokens of bfloat16 46 us here, 17 to 64 of them 74 to 80 us there, and a second tile of
-// tokens would double the reads that these 46 us go into.
+// rows, and a second tile of tokens would double the reads here.  Measured with weights from memory, 16 tokens here and 17 there, us:
+// 28672 x 8192 in 4 bits beside bfloat16 45 and 62 (to 64 tokens 63), beside binary16 60 and 59, 4 bits on both sides 35 and 34;
+// 4096 x 4096 9 and 13, 12 and 13, 7 and 11; gated 8192 x 28672 in bfloat16 186 and 182, in 4 bits 90 and 104, beside binary16 120 and 109.
+// Rows of 28672 beside binary16 lose from 9 tokens on (68 to 76 against 58).
 bool takes_few(int64_t rows) { return rows <= 16; }
 
 template <class T, Form FP, bool GATED>

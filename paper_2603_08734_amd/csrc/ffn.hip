@@ -11,10 +11,10 @@
 // Tiles of 256 x 256 need 64 KB of operands for every 64 k, eight waves of 64 x 128 read 96 KB of them out of LDS in 2048 cycles of
 // products, and a compute unit holds one such workgroup; smaller products take tiles of 128 x 128 or 128 x 64, and k in parts.  What
 // bounds the large ones is power: with X all zeros the same launch runs a quarter faster, since the clock stays up.
-// Measured (bfloat16 unless said): 2048 tokens through a gated block of 8192 x 28672 1.46 ms, 1320 TFLOP/s where the library's product
-// of the same shape alone runs at 1490; a training step of 4096 tokens on 4096 x 16384 2.76 ms, 1200 TFLOP/s with dX at 1270 and the
-// weights' gradients at 1260 (the library's products: 1190 and 1000); 4096 tokens through 28672 x 8192, 4 bits on both sides 0.64 ms,
-// 3020 TFLOP/s; 128 tokens through 8192 x 28672 in 4 bits beside binary16 99 us, where four parts of k and a slice's latency count.
+// Measured (bfloat16 unless said): 2048 tokens through a gated block of 8192 x 28672 1.49 ms, 1290 TFLOP/s where the library's product
+// of the same shape alone runs at 1490; a training step of 4096 tokens on 4096 x 16384 2.85 ms, 1160 TFLOP/s with dX at 1290 and the
+// weights' gradients at 1260 (the library's products: 1190 and 1000); 4096 tokens through 28672 x 8192, 4 bits on both sides 0.65 ms,
+// 2950 TFLOP/s; 128 tokens through 8192 x 28672 in 4 bits beside binary16 99 us, where four parts of k and a slice's latency count.
 #include <algorithm>
 
 #include "../../include/rsh_spmm.h"
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(256) void rsh_join_parts_kernel(const float* __rest
 }
 
 // dU = dH act(G) and dG = dH U act'(G), eight elements a thread, rounded to the 16 bits that the matrix units take: the gradients'
-// one rounding besides that of their results.  A pass over five arrays: 110 us at 4096 x 16384, 6.1 TB/s.
+// one rounding besides that of their results.  A pass over five arrays: 187 us at 4096 x 16384, 5.0 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void rsh_gate_backward_kernel(const uint16_t* __restrict__ dH, const float* __restrict__ G,
                                                                 const float* __restrict__ U, uint16_t* __restrict__ dG,

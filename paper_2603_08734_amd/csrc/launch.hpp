@@ -90,9 +90,8 @@ int launch_mx4_quantize(const void* X, int type, int64_t rows, int64_t k, int64_
 int launch_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t k, void* Y, int type, int64_t ld, void* stream);
 
 // Products of the feed-forward block (ffn.hip).  x_type, y_type, type: RSH_F16 or RSH_BF16, x_type also RSH_MX4; scales null for
-// operands of 16 bits.  G and U are fp32; they, dG and dU have rows of f elements rounded up to a multiple
-// of eight.  work: the bytes that the
-// *_work function of the same sizes says.
+// operands of 16 bits.  G and U are fp32; they, dG and dU have rows of f elements rounded up to a multiple of eight.  work: the bytes
+// that the *_work function of the same sizes says.
 int64_t mx4_product_work(int x_type, int64_t t, int64_t n, int64_t k);
 int64_t gated_forward_work(bool codes, int64_t t, int64_t d, int64_t f);
 int64_t gated_backward_work(int64_t t, int64_t d, int64_t f);
