@@ -326,6 +326,99 @@ enum { RSH_TILES_PRODUCT = 0, RSH_TILES_PRODUCT4 = 1, RSH_TILES_GATED = 2, RSH_T
 int rsh_ffn_tiles(int32_t which, int32_t aligned, int64_t t, int64_t a, int64_t b, int32_t *tile);
 
 /*
+ * Dropout without a stored mask.  Element (row, column) of a matrix [t][d] has 16 random bits, a function of the seed, the offset, the
+ * row and the column alone: Philox4x32 of ten rounds with the counter (column / 8, row, low and high half of the offset) and the key
+ * (low, high half of the seed); of its four words, low half before high half, elements take theirs in order.  An element whose bits are
+ * below `share` becomes zero (an infinity or a NaN too), the others are multiplied by 65536 / (65536 - share).
+ *   rsh_dropout    Y = drop(X); its gradient is the same call on the gradient of Y.  Y without gaps, or X itself (ld = d)
+ * share: 0 .. 65536.  seed_dev: device, 8-byte aligned, read by the kernels in place of `seed`, or NULL.
+ */
+typedef struct {
+    uint64_t seed, offset;
+    const uint64_t *seed_dev;
+    uint32_t share;
+} rsh_drop_t;
+int rsh_dropout(const void *X_dev, int32_t type, int64_t t, int64_t d, int64_t ld, const rsh_drop_t *drop, void *Y_dev, void *hip_stream);
+
+/*
+ * The edges of a block, for every row of X and B [t][d]:
+ *   S = X + scale * gate * drop(after(B)),   Y = before(S)
+ * or, with B NULL, Y = before(X) alone.  A norm of a row x, of kind
+ *   RSH_NORM_NONE    x
+ *   RSH_NORM_RMS     x r weight + bias,        r = 1 / sqrt(mean of x^2 + eps)
+ *   RSH_NORM_LAYER   (x - m) r weight + bias,  m = mean of x, r = 1 / sqrt(mean of (x - m)^2 + eps)
+ * weight, bias: [d], NULL for ones and zeros.  stats: fp32 [t][2], m (0 with RSH_NORM_RMS) and r of every row; written by the forward
+ * call where it is not NULL, read by the backward call.
+ *   type         RSH_F32, RSH_F16 or RSH_BF16, of X, B, S, Y and their gradients; parameters and gate have types of their own
+ *   ld_x, ld_b   elements from row to row; no alignment beyond the element's
+ *   gate         [d] (ld_gate 0) or [t][d] with rows ld_gate apart; NULL for ones
+ *   S            [t][d] without gaps, not X or B; NULL if and only if B is
+ *   Y            [t][d] without gaps; NULL if and only if before.kind is RSH_NORM_NONE
+ * Everything is fp32 until it is stored: Y is the norm of the sum, not of the rounded S.  A row's differences from its mean are formed
+ * in fp32; squares may leave its range.
+ * rsh_join_backward: dS and dY (rows ld_ds and ld_dy apart; NULL for zeros) are the gradients of S and Y.  It reads S (with B NULL: X) as
+ * the forward call wrote it, and the statistics.  Results, each NULL where not wanted: dX and dB [t][d], dgate (gate's shape and type,
+ * without gaps), gradients of the parameters in their types.  work: 16-byte aligned, of the bytes that rsh_join_backward_work reports,
+ * rewritten by every call (0: may be NULL); vectors: how many results are [d].
+ * Results never depend on the order in which waves run.  RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride,
+ * alignment or number out of range (eps is positive and finite), RSH_ERR_TOO_LARGE for a d above RSH_FFN_MAX_WIDTH.
+ */
+enum { RSH_NORM_NONE = 0, RSH_NORM_RMS = 1, RSH_NORM_LAYER = 2 };
+typedef struct {
+    const void *weight, *bias;
+    float *stats;
+    int32_t weight_type, bias_type, kind;
+    float eps;
+} rsh_norm_t;
+typedef struct {
+    const void *X, *B, *gate;
+    void *S, *Y;
+    int64_t t, d, ld_x, ld_b, ld_gate;
+    rsh_norm_t after, before;
+    rsh_drop_t drop;
+    int32_t type, gate_type;
+    float scale;
+} rsh_join_t;
+typedef struct {
+    const void *dS, *dY;
+    void *dX, *dB, *dgate, *after_weight, *after_bias, *before_weight, *before_bias, *work;
+    int64_t ld_ds, ld_dy;
+} rsh_join_gradients_t;
+int rsh_join_forward(const rsh_join_t *join, void *hip_stream);
+int rsh_join_backward_work(int64_t t, int64_t d, int32_t vectors, int64_t *bytes);
+int rsh_join_backward(const rsh_join_t *join, const rsh_join_gradients_t *gradients, void *hip_stream);
+
+/*
+ * Low-rank adapters of many requests beside a projection that they share: for every token (row) with adapter i = index[token]
+ *   out = Y + scales[i] (X A_i^T) B_i,    H = X A_i^T
+ * and out = Y for a token whose index is not one of 0 .. n - 1.  X [t][k], Y and out [t][m] of `type` (RSH_F16 or RSH_BF16), rows ld_x
+ * and ld_y apart, out without gaps (it may be Y where that is); A [n][r][k] and B [n][r][m] without gaps, of the same type; index int32 or int64 (index_size
+ * 4 or 8); scales fp32 [n], NULL for ones.  No alignment beyond the element's.  Y NULL: zeros.
+ *   rsh_adapters_forward   H not NULL: kept for the gradients, fp32 [t][r rounded up to a multiple of 16], 16-byte aligned
+ *   rsh_adapters_backward  for dout (rows ld_dout apart): dX [t][k], dA and dB of A's and B's shapes, each NULL where not wanted; H as kept
+ *                          (NULL only where dB is).  The gradient of Y is dout.
+ * Sums are fp32 and so is H between the two products; each result is rounded once.  work: 16-byte aligned, of the bytes that the *_work function
+ * of the same sizes reports, rewritten by every call.  Results never depend on the order in which waves run.
+ * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE for widths
+ * above RSH_FFN_MAX_WIDTH, more than RSH_ADAPTERS_MAX adapters or a rank above RSH_ADAPTERS_MAX_RANK.
+ */
+#define RSH_ADAPTERS_MAX 4096
+#define RSH_ADAPTERS_MAX_RANK 512
+typedef struct {
+    const void *X, *Y, *A, *B, *index;
+    const float *scales;
+    void *out;
+    float *H;
+    int64_t t, k, m, ld_x, ld_y;
+    int32_t n, r, type, index_size;
+} rsh_adapters_t;
+int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t *bytes);
+int rsh_adapters_forward(const rsh_adapters_t *adapters, void *work_dev, void *hip_stream);
+int rsh_adapters_backward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t *bytes);
+int rsh_adapters_backward(const rsh_adapters_t *adapters, const void *dout_dev, int64_t ld_dout, void *dX_dev, void *dA_dev, void *dB_dev,
+                          void *work_dev, void *hip_stream);
+
+/*
  * Same work as rsh_spmm, but brackets each kernel with HIP events on hip_stream,
  * waits for the stream, and reports the elapsed milliseconds of the tile kernel,
  * the irregular kernel and the combine kernel (0 for a kernel that was not

@@ -21,6 +21,8 @@ RSH_OK = 0
 RSH_F32, RSH_F16, RSH_BF16, RSH_MX4 = range(4)
 RSH_FFN_MAX_WIDTH = 1 << 21
 RSH_ACT_SILU, RSH_ACT_GELU, RSH_ACT_RELU = range(3)
+RSH_NORM_NONE, RSH_NORM_RMS, RSH_NORM_LAYER = range(3)
+RSH_ADAPTERS_MAX, RSH_ADAPTERS_MAX_RANK = 4096, 512
 (RSH_TILES_PRODUCT, RSH_TILES_PRODUCT4, RSH_TILES_GATED, RSH_TILES_GATED4, RSH_TILES_DX, RSH_TILES_DW, RSH_TILES_DW_ONE) = range(7)
 
 (RSH_ARR_WIN_ROW, RSH_ARR_WIN_TILE_OFF, RSH_ARR_TILE_COLID, RSH_ARR_TILE_MASK, RSH_ARR_TILE_VAL_OFF,
@@ -44,6 +46,8 @@ EXPORTED_SYMBOLS = [
     "rsh_dense_forward", "rsh_dense_backward", "rsh_act_backward", "rsh_mx4_quantize", "rsh_mx4_dequantize",
     "rsh_mx4_product_work", "rsh_mx4_product", "rsh_gated_forward_work", "rsh_gated_forward", "rsh_gated_backward_work", "rsh_gated_backward",
     "rsh_ffn_tiles",
+    "rsh_dropout", "rsh_join_forward", "rsh_join_backward_work", "rsh_join_backward", "rsh_adapters_forward_work", "rsh_adapters_forward",
+    "rsh_adapters_backward_work", "rsh_adapters_backward",
     "rsh_copy_probe", "rsh_plan_destroy", "rsh_plan_stats",
     "rsh_plan_decode", "rsh_plan_row_order", "rsh_reorder_knn", "rsh_plan_array", "rsh_plan_teams_per_wave",
     "rsh_plan_kernels", "rsh_plan_strip", "rsh_plan_operand",
@@ -69,6 +73,31 @@ class rsh_plan_opts_t(ctypes.Structure):
 
 class rsh_kernel_times_t(ctypes.Structure):
     _fields_ = [("ms_tile", ctypes.c_float), ("ms_irregular", ctypes.c_float), ("ms_combine", ctypes.c_float)]
+
+
+class rsh_drop_t(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("seed_dev", ctypes.c_void_p), ("share", ctypes.c_uint32)]
+
+
+class rsh_norm_t(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("weight", "bias", "stats")] + [(n, ctypes.c_int32) for n in ("weight_type", "bias_type", "kind")] +
+                [("eps", ctypes.c_float)])
+
+
+class rsh_join_t(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("X", "B", "gate", "S", "Y")] + [(n, ctypes.c_int64) for n in ("t", "d", "ld_x", "ld_b", "ld_gate")] +
+                [("after", rsh_norm_t), ("before", rsh_norm_t), ("drop", rsh_drop_t), ("type", ctypes.c_int32), ("gate_type", ctypes.c_int32),
+                 ("scale", ctypes.c_float)])
+
+
+class rsh_join_gradients_t(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("dS", "dY", "dX", "dB", "dgate", "after_weight", "after_bias", "before_weight", "before_bias", "work")] +
+                [("ld_ds", ctypes.c_int64), ("ld_dy", ctypes.c_int64)])
+
+
+class rsh_adapters_t(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("X", "Y", "A", "B", "index", "scales", "out", "H")] +
+                [(n, ctypes.c_int64) for n in ("t", "k", "m", "ld_x", "ld_y")] + [(n, ctypes.c_int32) for n in ("n", "r", "type", "index_size")])
 
 
 class rsh_plan_stats_t(ctypes.Structure):
@@ -139,6 +168,14 @@ def lib() -> ctypes.CDLL:
         L.rsh_gated_backward_work.argtypes = [i64, i64, i64, i64p]
         L.rsh_gated_backward.argtypes = [vp, i32, i64, vp, vp, i64, vp, vp, vp, i64, i32, vp, vp, vp, i64, i64, i64, vp, vp]
         L.rsh_ffn_tiles.argtypes = [i32, i32, i64, i64, i64, ctypes.POINTER(i32)]
+        L.rsh_dropout.argtypes = [vp, i32, i64, i64, i64, ctypes.POINTER(rsh_drop_t), vp, vp]
+        L.rsh_join_forward.argtypes = [ctypes.POINTER(rsh_join_t), vp]
+        L.rsh_join_backward_work.argtypes = [i64, i64, i32, i64p]
+        L.rsh_join_backward.argtypes = [ctypes.POINTER(rsh_join_t), ctypes.POINTER(rsh_join_gradients_t), vp]
+        for f in (L.rsh_adapters_forward_work, L.rsh_adapters_backward_work):
+            f.argtypes = [i64, i64, i64, i32, i32, i64p]
+        L.rsh_adapters_forward.argtypes = [ctypes.POINTER(rsh_adapters_t), vp, vp]
+        L.rsh_adapters_backward.argtypes = [ctypes.POINTER(rsh_adapters_t), vp, i64, vp, vp, vp, vp, vp]
         L.rsh_copy_probe.argtypes = [vp, vp, ctypes.c_int64, vp]
         L.rsh_plan_destroy.argtypes = [vp]
         L.rsh_plan_stats.argtypes = [vp, ctypes.POINTER(rsh_plan_stats_t)]
@@ -313,6 +350,40 @@ def ffn_tiles(which: int, aligned: bool, t: int, a: int, b: int):
     tile = (ctypes.c_int32 * 3)()
     _check(lib().rsh_ffn_tiles(which, int(aligned), t, a, b, tile))
     return tuple(tile)
+
+
+def dropout(X, x_type: int, ld: int, drop: rsh_drop_t):
+    """drop(X) of a matrix whose rows are ld elements apart (rsh_dropout)."""
+    t, d = X.shape
+    Y = X.new_empty((t, d))
+    _check(lib().rsh_dropout(X.data_ptr(), x_type, t, d, ld, ctypes.byref(drop), Y.data_ptr(), current_stream()))
+    return Y
+
+
+def join_forward(join: rsh_join_t) -> None:
+    """Enqueue the join, or the norm alone, that `join` describes (rsh_join_forward)."""
+    _check(lib().rsh_join_forward(ctypes.byref(join), current_stream()))
+
+
+def join_backward(join: rsh_join_t, gradients: rsh_join_gradients_t, vectors: int, like) -> None:
+    """Enqueue its gradients, of which `vectors` are [d]; work memory beside the tensor `like` (rsh_join_backward)."""
+    bytes_ = _work_bytes("rsh_join_backward_work", join.t, join.d, vectors)
+    work = like.new_empty(bytes_ // like.element_size()) if bytes_ else None
+    gradients.work = _address(work)
+    _check(lib().rsh_join_backward(ctypes.byref(join), ctypes.byref(gradients), current_stream()))
+
+
+def adapters_forward(a: rsh_adapters_t, like) -> None:
+    """Enqueue out = Y + s_i (X A_i^T) B_i (rsh_adapters_forward); work memory beside the 16-bit tensor `like`."""
+    work = like.new_empty(_work_bytes("rsh_adapters_forward_work", a.t, a.k, a.m, a.n, a.r) // 2)
+    _check(lib().rsh_adapters_forward(ctypes.byref(a), work.data_ptr(), current_stream()))
+
+
+def adapters_backward(a: rsh_adapters_t, dout, ld_dout: int, dX, dA, dB) -> None:
+    """Enqueue its gradients, None where not wanted (rsh_adapters_backward)."""
+    work = dout.new_empty(_work_bytes("rsh_adapters_backward_work", a.t, a.k, a.m, a.n, a.r) // 2)
+    _check(lib().rsh_adapters_backward(ctypes.byref(a), dout.data_ptr(), ld_dout, _address(dX), _address(dA), _address(dB), work.data_ptr(),
+                                       current_stream()))
 
 
 def rsh_copy_probe(src, dst, nbytes: int, stream=None) -> None:

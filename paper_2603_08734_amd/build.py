@@ -10,7 +10,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librsh.so")
-SOURCES = ["kernels.hip", "dense.hip", "mx4.hip", "ffn.hip", "few.hip", "api.cpp", "planner.cpp", "reorder.cpp"]
+SOURCES = ["kernels.hip", "dense.hip", "mx4.hip", "ffn.hip", "few.hip", "join.hip", "adapters.hip", "api.cpp", "planner.cpp", "reorder.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          # packed-fp32 VALU forms are switched off for device code on the test machines
@@ -50,7 +50,7 @@ def needs_build() -> bool:
 def build(force: bool = True) -> str:
     """Compile every source for itself, side by side, and link."""
     if force or needs_build():
-        with tempfile.TemporaryDirectory() as tmp, concurrent.futures.ThreadPoolExecutor(4) as pool:
+        with tempfile.TemporaryDirectory() as tmp, concurrent.futures.ThreadPoolExecutor(8) as pool:
             objects = [os.path.join(tmp, name + ".o") for name in SOURCES]
             flags = [f for f in FLAGS if f != "-shared"]
             list(pool.map(lambda source, obj: subprocess.check_call([HIPCC, *flags, "-c", "-o", obj, source]), sources(), objects))

@@ -1,0 +1,562 @@
+// Low-rank adapters of many requests beside a shared projection: out = Y + s_i (X A_i^T) B_i, and its gradients.
+//
+// With both factors rank first, A_i [r][k] and B_i [r][m], three products make up both directions:
+//   shrink   H = X A_i^T, and dH = dout B_i^T      long rows against r short ones: matrix instructions of 16 bits
+//   expand   out = Y + s H B_i, and dX = s dH A_i   r terms for every element: H is fp32, so are the matrix instructions
+//   outer    dA_i = s dH^T X, and dB_i = s H^T dout    the tokens of an adapter summed up, in fp32 again
+// Tokens are taken in tiles that share an adapter.  A kernel of one workgroup deals them out; a few tokens are dealt out by every
+// workgroup for itself, which saves a launch.
+#include <algorithm>
+
+#include "rows.hpp"
+
+namespace rsh {
+
+namespace {
+
+constexpr int kFewTokens = 256, kFewTile = 16, kTile = 64;
+constexpr int kSortThreads = 1024, kSortWords = 8 * (RSH_ADAPTERS_MAX + 1);     // counters in LDS
+
+struct Tile {
+    int adapter, first, count, pad;        // adapter: -1 for none; first: in the order
+};
+
+// Of the tokens: int32 or int64, anything but 0 .. n - 1 for none.
+struct Index {
+    const void* data;
+    int wide, n;
+    __device__ __forceinline__ int at(int64_t i) const {      // n: none
+        const int64_t a = wide ? ((const int64_t*)data)[i] : ((const int32_t*)data)[i];
+        return a >= 0 && a < n ? (int)a : n;
+    }
+};
+
+// Where the tokens' order is.
+struct Order {
+    const int32_t* token;      // by adapter, those without one behind the others
+    const int32_t* starts;     // of every adapter, n + 2
+    const Tile* tiles;
+    const int32_t* n_tiles;
+};
+
+typedef int FewPlace[kFewTokens + 4 + kFewTile];
+
+// The tile of a workgroup whose tokens are few: its own token is the first of sixteen with the same adapter, or there is nothing to do.
+// Returns the adapter, n for none, or -1; the tokens are behind place[kFewTokens + 4].
+__device__ __forceinline__ int few_tile(const Index& index, int t, int mine, FewPlace& place, int* count) {
+    const int i = threadIdx.x, wave = threadIdx.x >> 6;
+    int a = -1;
+    if (i < t) a = index.at(i);
+    if (i < kFewTokens) place[i] = a;
+    __syncthreads();
+    const int own = place[mine];
+    const uint64_t same = __ballot(i < t && a == own);
+    if (i < kFewTokens && (i & 63) == 0) place[kFewTokens + wave] = __popcll(same);
+    __syncthreads();
+    int before = 0, all = 0, rank = 0;
+#pragma unroll
+    for (int w = 0; w < kFewTokens / 64; ++w) {
+        const int c = place[kFewTokens + w];
+        before += w < wave ? c : 0;
+        all += c;
+    }
+    before += (int)bits_below_lane(same);
+    if (i < t && a == own) place[i] = before;      // place in its adapter's order
+    __syncthreads();
+    rank = place[mine];
+    if (rank % kFewTile) return -1;
+    if (i < t && a == own && before >= rank && before < rank + kFewTile) place[kFewTokens + 4 + before - rank] = i;
+    __syncthreads();
+    *count = min(all - rank, kFewTile);
+    return own;
+}
+
+__device__ __forceinline__ float4_t mfma_f32(float a, float b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// Tokens of a tile.
+template <bool FEW>
+struct Members {
+    const int32_t* token;
+    int adapter, count;        // adapter: n for none
+    __device__ __forceinline__ int at(int i) const { return token[min(i, count - 1)]; }
+};
+template <bool FEW>
+__device__ __forceinline__ bool members(const Index& index, const Order& order, int64_t t, int* place, Members<FEW>* m) {
+    if constexpr (FEW) {
+        m->adapter = few_tile(index, (int)t, (int)blockIdx.x, *reinterpret_cast<FewPlace*>(place), &m->count);
+        m->token = place + kFewTokens + 4;
+        return m->adapter >= 0;
+    } else {
+        if ((int)blockIdx.x >= *order.n_tiles) return false;
+        const Tile tile = order.tiles[blockIdx.x];
+        m->adapter = tile.adapter;
+        m->count = tile.count;
+        m->token = order.token + tile.first;
+        return true;
+    }
+}
+
+}  // namespace
+
+// Tokens by adapter, in their own order, the tiles, and where every adapter's tokens begin.  A wave has a run of the tokens and its own
+// counters for all adapters.
+__global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index index, int64_t t, int waves, int tile, int32_t* token, int32_t* starts,
+                                                                         Tile* tiles, int32_t* n_tiles) {
+    __shared__ int32_t counts[kSortWords];     // [adapter][wave]
+    __shared__ int32_t tile_start[RSH_ADAPTERS_MAX + 2];
+    __shared__ int32_t sums[2][kSortThreads / 64];
+    __shared__ int32_t total[2];
+    const int n = index.n, groups = n + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i < groups * waves; i += kSortThreads) counts[i] = 0;
+    if (threadIdx.x < 2) total[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t share = ((t + waves - 1) / waves + 63) / 64 * 64, begin = wave * share, end = min(t, begin + share);
+    if (wave < waves)
+        for (int64_t i = begin + lane; i < end; i += 64) atomicAdd(&counts[index.at(i) * waves + wave], 1);
+    __syncthreads();
+    // Of every adapter: its tokens and tiles, added up over the adapters before it.
+    for (int a0 = 0; a0 < groups; a0 += kSortThreads) {
+        const int a = a0 + threadIdx.x;
+        int c = 0;
+        if (a < groups)
+            for (int w = 0; w < waves; ++w) c += counts[a * waves + w];
+        int before[2] = {c, (c + tile - 1) / tile};
+        const int own[2] = {before[0], before[1]};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int up = shfl_i32(before[s], lane - d < 0 ? lane : lane - d);
+                before[s] += lane >= d ? up : 0;
+            }
+            if (lane == 63) sums[s][wave] = before[s];
+        }
+        __syncthreads();
+        int start = total[0] + before[0] - own[0], first = total[1] + before[1] - own[1];
+        for (int w = 0; w < wave; ++w) start += sums[0][w], first += sums[1][w];
+        if (a < groups) {
+            starts[a] = start;
+            tile_start[a] = first;
+            for (int w = 0; w < waves; ++w) {
+                const int x = counts[a * waves + w];
+                counts[a * waves + w] = start;
+                start += x;
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x == kSortThreads - 1) total[0] = start, total[1] = first + own[1];
+        __syncthreads();
+    }
+    const int all = total[1];
+    if (threadIdx.x == 0) {
+        starts[groups] = (int32_t)t;
+        *n_tiles = all;
+    }
+    if (wave < waves) {
+        int bits = 0;
+        while (n >> bits) ++bits;
+        volatile int32_t* const next = counts;
+        for (int64_t i0 = begin; i0 < end; i0 += 64) {
+            const bool in = i0 + lane < end;
+            const int a = in ? index.at(i0 + lane) : 0;
+            uint64_t same = __ballot(in);
+            for (int b = 0; b < bits; ++b) {
+                const uint64_t set = __ballot(a >> b & 1);
+                same &= a >> b & 1 ? set : ~set;
+            }
+            const int rank = (int)bits_below_lane(same);
+            if (in) {
+                const int at = next[a * waves + wave];
+                token[at + rank] = (int32_t)(i0 + lane);
+                if (rank == 0) next[a * waves + wave] = at + __popcll(same);
+            }
+        }
+    }
+    // A tile's adapter: the last that begins at or before it (those without tiles share theirs with the next).
+    __syncthreads();
+    for (int b = threadIdx.x; b < all; b += kSortThreads) {
+        int lo = 0, hi = groups - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (tile_start[mid] <= b) lo = mid;
+            else hi = mid - 1;
+        }
+        // where it begins: what the adapter's first wave wrote is its end by now, so from the array
+        const int start = starts[lo] + (b - tile_start[lo]) * tile, stop = lo + 1 < groups ? starts[lo + 1] : (int)t;
+        tiles[b] = {lo, start, min(tile, stop - start), 0};
+    }
+}
+
+// H of a tile's tokens and 16 RT ranks, over a part of k.  WAVES waves share the part.
+template <class T, int RT, int TT, bool FEW, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const uint16_t* X, int64_t ld_x, const uint16_t* A, Index index, Order order,
+                                                                         float* H, int64_t t, int64_t k, int r, int steps) {
+    __shared__ int place[FEW ? sizeof(FewPlace) / sizeof(int) : 1];
+    __shared__ float4_t joined[WAVES][TT][64];
+    Members<FEW> tile;
+    if (!members<FEW>(index, order, t, place, &tile) || tile.adapter == index.n) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
+    const int r0 = 16 * RT * (int)blockIdx.y, r16 = (r + 15) / 16 * 16, tiles = (tile.count + 15) / 16;
+    const uint16_t* a[RT];
+    const uint16_t* x[TT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) a[i] = A + ((int64_t)tile.adapter * r + min(r0 + 16 * i + c, r - 1)) * k;
+#pragma unroll
+    for (int i = 0; i < TT; ++i) x[i] = X + (int64_t)tile.at(16 * i + c) * ld_x;
+    float4_t acc[RT][TT] = {};
+    const int64_t begin = (int64_t)blockIdx.z * steps, end = min((k + 63) / 64, begin + steps);
+    for (int64_t step = begin + wave; step < end; step += WAVES) {
+        const int64_t at = 64 * step + 16 * g;
+        uint4_t av[RT][2], xv[TT][2];
+        const int64_t left = 64 * step + 64 <= k ? 16 : k - at;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) av[i][h] = load8(a[i] + at + 8 * h, left - 8 * h);
+#pragma unroll
+            for (int i = 0; i < TT; ++i)
+                if (i < tiles) xv[i][h] = load8(x[i] + at + 8 * h, left - 8 * h);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < TT; ++j)
+                if (j < tiles)
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) acc[i][j] = T::mfma16(av[i][h], xv[j][h], acc[i][j]);
+    }
+    // The waves' sums, in their order.
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < TT; ++j) joined[wave][j][lane] = acc[i][j];
+        __syncthreads();
+        const int rank = r0 + 16 * i + 4 * g;
+        for (int j = wave; j < tiles; j += WAVES) {
+            float4_t s = joined[0][j][lane];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) s += joined[w][j][lane];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) s[v] = rank + v < r ? s[v] : 0.f;
+            if (rank < r16 && 16 * j + c < tile.count)
+                *reinterpret_cast<float4_t*>(H + ((int64_t)blockIdx.z * t + tile.at(16 * j + c)) * r16 + rank) = s;
+        }
+    }
+}
+
+// out = Y + s H B_i of a tile's tokens and 128 columns a wave.  A lane's loads of B are eight columns of a row, one for each of eight
+// results of 16 columns by 16 tokens; which eight is chosen so that lanes store pieces of a row that lie side by side.
+template <class T, int TT, bool FEW>
+__global__ __launch_bounds__(256) void rsh_adapters_expand_kernel(const uint16_t* Y, int64_t ld_y, const float* H, int parts, const uint16_t* B,
+                                                                  const float* scales, Index index, Order order, uint16_t* out, int64_t t, int64_t m,
+                                                                  int r) {
+    __shared__ int place[FEW ? sizeof(FewPlace) / sizeof(int) : 1];
+    Members<FEW> tile;
+    if (!members<FEW>(index, order, t, place, &tile)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15, r16 = (r + 15) / 16 * 16;
+    const int64_t col0 = 512 * (int64_t)blockIdx.y + 128 * wave;
+    if (col0 >= m) return;
+    const bool some = tile.adapter < index.n;
+    const float scale = some && scales ? scales[tile.adapter] : 1.f;
+    const int64_t col = col0 + 8 * (4 * (c & 3) + (c >> 2));
+    const uint16_t* const b = B + (int64_t)tile.adapter * r * m + col;
+    for (int first = 0; first < tile.count; first += 16 * TT) {
+        float4_t acc[TT][8] = {};
+        int64_t token[TT];
+#pragma unroll
+        for (int i = 0; i < TT; ++i) token[i] = tile.at(first + 16 * i + c);
+        if (some) {
+            for (int rank = 0; rank < r16; rank += 16) {
+                uint4_t bv[4];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int row = rank + 4 * g + s;
+                    bv[s] = load8(b + (int64_t)row * m, row < r ? m - col : 0);
+                }
+                float4_t h[TT];
+#pragma unroll
+                for (int i = 0; i < TT; ++i) {
+                    const float* p = H + token[i] * r16 + rank + 4 * g;
+                    h[i] = *reinterpret_cast<const float4_t*>(p);
+                    for (int q = 1; q < parts; ++q) h[i] += *reinterpret_cast<const float4_t*>(p += t * r16);
+                    h[i] *= scale;
+                }
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const Eight e = widen8<T>(bv[s]);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+#pragma unroll
+                        for (int i = 0; i < TT; ++i) acc[i][q] = mfma_f32(e.v[q], h[i][s], acc[i][q]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+            if (first + 16 * i + c >= tile.count) continue;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int64_t to = col0 + 32 * v + 8 * g;
+                Eight e = {};
+                if (Y) e = load_eight<T>(Y, token[i] * ld_y + to, (int)min(m - to, (int64_t)8));
+                if (some) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) e.v[q] += acc[i][q][v];
+                }
+                store_eight<T>(out, token[i] * m + to, e, (int)min(m - to, (int64_t)8));
+            }
+        }
+    }
+}
+
+// H of all tokens from its parts.
+__global__ __launch_bounds__(256) void rsh_adapters_join_kernel(const float4_t* from, float4_t* to, int64_t n, int parts) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        float4_t s = from[i];
+        for (int p = 1; p < parts; ++p) s += from[p * n + i];
+        to[i] = s;
+    }
+}
+
+// s H^T X over a part of the tokens of adapter blockIdx.y, 16 RT ranks by 128 columns: into `out` where there is one part, into `sums`
+// ([part][adapter][rank][column], fp32) where there are more.
+template <class T, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const uint16_t* X, int64_t ld_x, const float* H, const float* scales, Order order,
+                                                                        uint16_t* out, float* sums, int parts, int64_t k, int n, int r) {
+    __shared__ float4_t joined[WAVES][8][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15, r16 = (r + 15) / 16 * 16;
+    const int adapter = blockIdx.y, part = blockIdx.z % parts, r0 = 16 * RT * ((int)blockIdx.z / parts);
+    const int start = order.starts[adapter], tokens = order.starts[adapter + 1] - start, share = (tokens + parts - 1) / parts;
+    const int begin = start + (int)min((int64_t)tokens, (int64_t)part * share), end = start + (int)min((int64_t)tokens, (int64_t)(part + 1) * share);
+    const int64_t col = 128 * (int64_t)blockIdx.x + 8 * c;
+    float4_t acc[RT][8] = {};
+    for (int i0 = begin + 4 * wave; i0 < end; i0 += 4 * WAVES) {
+        const bool in = i0 + g < end;
+        const int64_t token = order.token[min(i0 + g, end - 1)];
+        const Eight x = load_eight<T>(X, token * ld_x + col, in ? (int)min(k - col, (int64_t)8) : 0);
+        float h[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) h[i] = in && r0 + 16 * i < r16 ? H[token * r16 + r0 + 16 * i + c] : 0.f;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) acc[i][q] = mfma_f32(h[i], x.v[q], acc[i][q]);
+    }
+    const float scale = scales ? scales[adapter] : 1.f;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) joined[wave][q][lane] = acc[i][q];
+        __syncthreads();
+        for (int v = wave; v < 4; v += WAVES) {
+            const int rank = r0 + 16 * i + 4 * g + v;
+            Eight e;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                float s = joined[0][q][lane][v];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) s += joined[w][q][lane][v];
+                e.v[q] = s * scale;
+            }
+            if (rank >= r || col >= k) continue;
+            const int64_t at = ((int64_t)adapter * r + rank) * k + col;
+            const int valid = (int)min(k - col, (int64_t)8);
+            if (parts == 1) store_eight<T>(out, at, e, valid);
+            else store_eight<F32>(sums, (int64_t)part * n * r * k + at, e, valid);
+        }
+    }
+}
+
+// The parts of a factor's gradient, added up in their order.
+template <class T>
+__global__ __launch_bounds__(256) void rsh_adapters_sum_kernel(const float* sums, uint16_t* out, int64_t n, int parts) {
+    for (int64_t i = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x); i < n; i += 8 * (int64_t)gridDim.x * 256) {
+        const int valid = (int)min(n - i, (int64_t)8);
+        Eight s = load_eight<F32>(sums, i, valid);
+        for (int p = 1; p < parts; ++p) {
+            const Eight e = load_eight<F32>(sums, p * n + i, valid);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s.v[q] += e.v[q];
+        }
+        store_eight<T>(out, i, s, valid);
+    }
+}
+
+namespace {
+int launched() { return hipGetLastError() == hipSuccess ? RSH_OK : RSH_ERR_HIP; }
+int64_t rounded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+int64_t wide_rank(int r) { return (r + 15) / 16 * 16; }
+
+template <class F>
+void by_half(int type, F f) {
+    if (type == RSH_F16) f(F16());
+    else f(BF16());
+}
+template <class F>
+void by_rank(int r, F f) {
+    if (r <= 16) f(std::integral_constant<int, 1>());
+    else if (r <= 32) f(std::integral_constant<int, 2>());
+    else f(std::integral_constant<int, 4>());
+}
+
+int64_t most_tiles(int64_t t, int n) { return t / kTile + std::min<int64_t>(t, n + 1); }
+
+// The order's place in the work memory.
+struct Sorted {
+    int64_t token, starts, tiles, n_tiles, bytes;
+    Sorted(int64_t t, int n) {
+        token = 0;
+        starts = rounded(4 * t);
+        tiles = starts + rounded(4 * (n + 2));
+        n_tiles = tiles + (int64_t)sizeof(Tile) * most_tiles(t, n);
+        bytes = n_tiles + 16;
+    }
+    Order at(void* work) const {
+        char* const w = (char*)work;
+        return {(const int32_t*)(w + token), (const int32_t*)(w + starts), (const Tile*)(w + tiles), (const int32_t*)(w + n_tiles)};
+    }
+};
+
+// Parts of the long axis of a shrinking product, and the steps of 64 in each.
+constexpr int kShrinkWaves = 8;
+struct Split {
+    int parts, steps;
+    Split(int64_t t, int64_t k, int r, bool few) {
+        const int64_t blocks = (few ? t : (t + kTile - 1) / kTile) * ((r + 63) / 64), all = (k + 63) / 64;
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? 16 : 4, 512 / std::max<int64_t>(1, blocks)));
+        const int64_t each = std::max<int64_t>(kShrinkWaves, (all + want - 1) / want);
+        steps = (int)each;
+        parts = (int)((all + each - 1) / each);
+    }
+};
+
+// Parts of the tokens in a factor's gradient.
+int outer_parts(int64_t t, int64_t k, int n, int r) {
+    const int64_t blocks = (k + 127) / 128 * n * ((r + 63) / 64);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({16, 512 / blocks, t / 64}));
+}
+
+void sort(const rsh_adapters_t& a, void* work, hipStream_t st) {
+    const Sorted s(a.t, a.n);
+    int waves = kSortThreads / 64;
+    while (waves * (a.n + 1) > kSortWords) waves /= 2;
+    char* const w = (char*)work;
+    hipLaunchKernelGGL(rsh_adapters_sort_kernel, dim3(1), dim3(kSortThreads), 0, st, Index{a.index, a.index_size == 8, a.n}, a.t, waves, kTile,
+                       (int32_t*)(w + s.token), (int32_t*)(w + s.starts), (Tile*)(w + s.tiles), (int32_t*)(w + s.n_tiles));
+}
+
+template <class T>
+void shrink(const rsh_adapters_t& a, bool few, const void* X, int64_t ld, int64_t k, const void* A, const Order& order, const Split& split, float* H,
+            hipStream_t st) {
+    const Index index = {a.index, a.index_size == 8, a.n};
+    by_rank(a.r, [&](auto rt) {
+        constexpr int RT = decltype(rt)::value;
+        const dim3 grid((unsigned)(few ? a.t : most_tiles(a.t, a.n)), (a.r + 16 * RT - 1) / (16 * RT), split.parts);
+        if (few)
+            hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 1, true, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, st, (const uint16_t*)X, ld,
+                               (const uint16_t*)A, index, order, H, a.t, k, a.r, split.steps);
+        else
+            hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 4, false, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, st, (const uint16_t*)X, ld,
+                               (const uint16_t*)A, index, order, H, a.t, k, a.r, split.steps);
+    });
+}
+
+template <class T>
+void expand(const rsh_adapters_t& a, bool few, const void* Y, int64_t ld, const float* H, int parts, const void* B, const Order& order, void* out,
+            int64_t m, hipStream_t st) {
+    const Index index = {a.index, a.index_size == 8, a.n};
+    const dim3 grid((unsigned)(few ? a.t : most_tiles(a.t, a.n)), (unsigned)((m + 511) / 512));
+    if (few)
+        hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, 1, true>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B, a.scales,
+                           index, order, (uint16_t*)out, a.t, m, a.r);
+    else
+        hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, 2, false>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B, a.scales,
+                           index, order, (uint16_t*)out, a.t, m, a.r);
+}
+
+void join(const float* from, float* to, int64_t t, int r, int parts, hipStream_t st) {
+    const int64_t n = t * wide_rank(r) / 4;
+    hipLaunchKernelGGL(rsh_adapters_join_kernel, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096)), dim3(256), 0, st, (const float4_t*)from,
+                       (float4_t*)to, n, parts);
+}
+
+template <class T>
+void outer(const rsh_adapters_t& a, const void* X, int64_t ld, int64_t k, const float* H, const Order& order, void* out, float* sums, hipStream_t st) {
+    const int parts = outer_parts(a.t, k, a.n, a.r);
+    by_rank(a.r, [&](auto rt) {
+        constexpr int RT = decltype(rt)::value;
+        const dim3 grid((unsigned)((k + 127) / 128), a.n, (a.r + 16 * RT - 1) / (16 * RT) * parts);
+        hipLaunchKernelGGL((rsh_adapters_outer_kernel<T, RT, 8>), grid, dim3(512), 0, st, (const uint16_t*)X, ld, H, a.scales, order, (uint16_t*)out, sums,
+                           parts, k, a.n, a.r);
+    });
+    if (parts > 1) {
+        const int64_t n = (int64_t)a.n * a.r * k;
+        hipLaunchKernelGGL(rsh_adapters_sum_kernel<T>, dim3((unsigned)std::min<int64_t>((n + 2047) / 2048, 4096)), dim3(256), 0, st, sums, (uint16_t*)out, n,
+                           parts);
+    }
+}
+}  // namespace
+
+int64_t adapters_forward_work(int64_t t, int64_t k, int64_t, int n, int r) {
+    const bool few = t <= kFewTokens;
+    return (few ? 0 : Sorted(t, n).bytes) + (Split(t, k, r, few).parts + 1) * t * wide_rank(r) * 4;
+}
+
+int64_t adapters_backward_work(int64_t t, int64_t k, int64_t m, int n, int r) {
+    int64_t sums = 0;
+    for (int64_t w : {k, m}) {
+        const int parts = outer_parts(t, w, n, r);
+        if (parts > 1) sums = std::max(sums, parts * w * n * r * 4);
+    }
+    return Sorted(t, n).bytes + (Split(t, m, r, false).parts + 1) * t * wide_rank(r) * 4 + sums;
+}
+
+int launch_adapters_forward(const rsh_adapters_t& a, void* work, void* stream) {
+    const hipStream_t st = (hipStream_t)stream;
+    const bool few = a.t <= kFewTokens;
+    const Split split(a.t, a.k, a.r, few);
+    const Sorted s(a.t, a.n);
+    float* H = (float*)((char*)work + (few ? 0 : s.bytes));
+    if (!few) sort(a, work, st);
+    by_half(a.type, [&](auto half) {
+        using T = decltype(half);
+        float* const direct = split.parts == 1 && a.H ? a.H : H;
+        shrink<T>(a, few, a.X, a.ld_x, a.k, a.A, s.at(work), split, direct, st);
+        int parts = split.parts;
+        const float* all = direct;
+        if (parts > 1 && (a.H || !few)) {
+            float* const to = a.H ? a.H : H + parts * a.t * wide_rank(a.r);
+            join(H, to, a.t, a.r, parts, st);
+            all = to;
+            parts = 1;
+        }
+        expand<T>(a, few, a.Y, a.ld_y, all, parts, a.B, s.at(work), a.out, a.m, st);
+    });
+    return launched();
+}
+
+int launch_adapters_backward(const rsh_adapters_t& a, const void* dout, int64_t ld_dout, void* dX, void* dA, void* dB, void* work, void* stream) {
+    const hipStream_t st = (hipStream_t)stream;
+    const Split split(a.t, a.m, a.r, false);
+    const Sorted s(a.t, a.n);
+    float* const parts = (float*)((char*)work + s.bytes);
+    float* const dH = parts + (split.parts > 1 ? split.parts * a.t * wide_rank(a.r) : 0);
+    float* const sums = parts + (split.parts + 1) * a.t * wide_rank(a.r);
+    const Order order = s.at(work);
+    sort(a, work, st);
+    by_half(a.type, [&](auto half) {
+        using T = decltype(half);
+        if (dX || dA) {
+            shrink<T>(a, false, dout, ld_dout, a.m, a.B, order, split, parts, st);
+            if (split.parts > 1) join(parts, dH, a.t, a.r, split.parts, st);
+        }
+        if (dX) expand<T>(a, false, nullptr, 0, dH, 1, a.A, order, dX, a.k, st);
+        if (dA) outer<T>(a, a.X, a.ld_x, a.k, dH, order, dA, sums, st);
+        if (dB) outer<T>(a, dout, ld_dout, a.m, a.H, order, dB, sums, st);
+    });
+    return launched();
+}
+
+}  // namespace rsh

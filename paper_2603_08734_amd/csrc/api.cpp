@@ -729,6 +729,124 @@ int rsh_gated_backward(const void* X, int32_t type, int64_t ld_x, const void* Wg
     return launch_status(rsh::launch_gated_backward(X, type, ld_x, Wg, Wu, ld_w, G, U, dH, ld_h, act, dX, dWg, dWu, t, d, f, work, hip_stream));
 }
 
+namespace {
+bool any_type(int32_t type) { return type == RSH_F32 || half_type(type); }
+uintptr_t type_bytes(int32_t type) { return type == RSH_F32 ? 4 : 2; }
+int rows_ok(int64_t t, int64_t d) {
+    if (t <= 0 || d <= 0 || t >= kMaxSize) return RSH_ERR_BAD_OPTION;
+    return d > kMaxWidth ? RSH_ERR_TOO_LARGE : RSH_OK;
+}
+bool stride_ok(int64_t ld, int64_t d) { return ld >= d && ld < kMaxSize; }
+bool drop_ok(const rsh_drop_t& drop) { return drop.share <= 65536 && aligned_to({drop.seed_dev}, 8); }
+bool norm_ok(const rsh_norm_t& n) {
+    if (n.kind == RSH_NORM_NONE) return true;
+    return (n.kind == RSH_NORM_RMS || n.kind == RSH_NORM_LAYER) && n.eps > 0 && n.eps < INFINITY && aligned_to({n.stats}, 8) &&
+           (!n.weight || (any_type(n.weight_type) && aligned_to({n.weight}, type_bytes(n.weight_type)))) &&
+           (!n.bias || (any_type(n.bias_type) && aligned_to({n.bias}, type_bytes(n.bias_type))));
+}
+int join_ok(const rsh_join_t* j, bool forward) {
+    if (!j) return RSH_ERR_NULL;
+    if (!any_type(j->type)) return RSH_ERR_BAD_OPTION;
+    if (const int rc = rows_ok(j->t, j->d)) return rc;
+    const bool norm = j->before.kind != RSH_NORM_NONE;
+    if ((forward || !j->B) && !j->X) return RSH_ERR_NULL;
+    if ((forward && (!j->S != !j->B || !j->Y != !norm)) || (!j->B && !norm)) return RSH_ERR_NULL;
+    if (!norm_ok(j->after) || !norm_ok(j->before) || !aligned_to({j->X, j->B, j->S, j->Y}, type_bytes(j->type)) || (j->X && !stride_ok(j->ld_x, j->d)) ||
+        (j->B && !stride_ok(j->ld_b, j->d)) || !drop_ok(j->drop) || !(j->scale - j->scale == 0))
+        return RSH_ERR_BAD_OPTION;
+    if (j->gate && (!any_type(j->gate_type) || !aligned_to({j->gate}, type_bytes(j->gate_type)) || (j->ld_gate && !stride_ok(j->ld_gate, j->d))))
+        return RSH_ERR_BAD_OPTION;
+    if (forward && j->B && (j->S == j->X || j->S == j->B)) return RSH_ERR_BAD_OPTION;
+    return RSH_OK;
+}
+}  // namespace
+
+int rsh_dropout(const void* X, int32_t type, int64_t t, int64_t d, int64_t ld, const rsh_drop_t* drop, void* Y, void* hip_stream) {
+    if (!X || !Y || !drop) return RSH_ERR_NULL;
+    if (!any_type(type)) return RSH_ERR_BAD_OPTION;
+    if (const int rc = rows_ok(t, d)) return rc;
+    if (!stride_ok(ld, d) || !drop_ok(*drop) || !aligned_to({X, Y}, type_bytes(type)) || (X == Y && ld != d && t > 1)) return RSH_ERR_BAD_OPTION;
+    return launch_status(rsh::launch_dropout(X, type, t, d, ld, *drop, Y, hip_stream));
+}
+
+int rsh_join_forward(const rsh_join_t* join, void* hip_stream) {
+    const int rc = join_ok(join, true);
+    return rc ? rc : launch_status(rsh::launch_join_forward(*join, hip_stream));
+}
+
+int rsh_join_backward_work(int64_t t, int64_t d, int32_t vectors, int64_t* bytes) {
+    if (!bytes) return RSH_ERR_NULL;
+    *bytes = 0;
+    if (vectors < 0 || vectors > 5) return RSH_ERR_BAD_OPTION;
+    if (const int rc = rows_ok(t, d)) return rc;
+    *bytes = rsh::join_backward_work(t, d, vectors);
+    return RSH_OK;
+}
+
+int rsh_join_backward(const rsh_join_t* join, const rsh_join_gradients_t* g, void* hip_stream) {
+    if (const int rc = join_ok(join, false)) return rc;
+    if (!g) return RSH_ERR_NULL;
+    const rsh_join_t& j = *join;
+    const bool before = j.before.kind != RSH_NORM_NONE, after = j.B && j.after.kind != RSH_NORM_NONE;
+    const int vectors = !!g->after_weight + !!g->after_bias + !!g->before_weight + !!g->before_bias + (g->dgate && !j.ld_gate);
+    if (!g->dX && !g->dB && !g->dgate && !vectors) return RSH_ERR_NULL;
+    if ((!g->dS && !g->dY) || (vectors && !g->work) || (g->dY && before && (!j.before.stats || (j.B && !j.S))) || (after && !j.after.stats)) return RSH_ERR_NULL;
+    if ((g->dB && !j.B) || (g->dgate && !j.gate) || (g->dS && !j.B) || (g->dY && !before) ||
+        ((g->before_weight || g->before_bias) && !(before && g->dY)) || (g->before_weight && !j.before.weight) || (g->before_bias && !j.before.bias) ||
+        ((g->after_weight || g->after_bias) && !after) || (g->after_weight && !j.after.weight) || (g->after_bias && !j.after.bias) ||
+        (g->dS && !stride_ok(g->ld_ds, j.d)) || (g->dY && !stride_ok(g->ld_dy, j.d)) || !aligned_to({g->dS, g->dY, g->dX, g->dB}, type_bytes(j.type)) ||
+        !aligned_to({g->dgate}, type_bytes(j.gate_type)) || !aligned_to({g->after_weight}, type_bytes(j.after.weight_type)) ||
+        !aligned_to({g->after_bias}, type_bytes(j.after.bias_type)) || !aligned_to({g->before_weight}, type_bytes(j.before.weight_type)) ||
+        !aligned_to({g->before_bias}, type_bytes(j.before.bias_type)) || !aligned_to({g->work}, 16))
+        return RSH_ERR_BAD_OPTION;
+    return launch_status(rsh::launch_join_backward(j, *g, hip_stream));
+}
+
+namespace {
+int adapter_sizes_ok(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r) {
+    if (t <= 0 || k <= 0 || m <= 0 || n <= 0 || r <= 0 || t >= kMaxSize) return RSH_ERR_BAD_OPTION;
+    return k > kMaxWidth || m > kMaxWidth || n > RSH_ADAPTERS_MAX || r > RSH_ADAPTERS_MAX_RANK ? RSH_ERR_TOO_LARGE : RSH_OK;
+}
+int adapters_ok(const rsh_adapters_t* a, const void* work) {
+    if (!a) return RSH_ERR_NULL;
+    if (const int rc = adapter_sizes_ok(a->t, a->k, a->m, a->n, a->r)) return rc;
+    if (!a->A || !a->B || !a->index || !work) return RSH_ERR_NULL;
+    if (!half_type(a->type) || (a->index_size != 4 && a->index_size != 8) || !aligned_to({a->X, a->Y, a->A, a->B, a->out}, 2) ||
+        !aligned_to({a->index}, (uintptr_t)a->index_size) || !aligned_to({a->scales}, 4) || !aligned_to({a->H, work}, 16) ||
+        (a->X && !stride_ok(a->ld_x, a->k)) || (a->Y && !stride_ok(a->ld_y, a->m)))
+        return RSH_ERR_BAD_OPTION;
+    return RSH_OK;
+}
+}  // namespace
+
+int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t* bytes) {
+    if (!bytes) return RSH_ERR_NULL;
+    const int rc = adapter_sizes_ok(t, k, m, n, r);
+    *bytes = rc ? 0 : rsh::adapters_forward_work(t, k, m, n, r);
+    return rc;
+}
+
+int rsh_adapters_forward(const rsh_adapters_t* a, void* work, void* hip_stream) {
+    if (const int rc = adapters_ok(a, work)) return rc;
+    if (!a->X || !a->out) return RSH_ERR_NULL;
+    if (a->out == a->Y && a->ld_y != a->m && a->t > 1) return RSH_ERR_BAD_OPTION;
+    return launch_status(rsh::launch_adapters_forward(*a, work, hip_stream));
+}
+
+int rsh_adapters_backward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t* bytes) {
+    if (!bytes) return RSH_ERR_NULL;
+    const int rc = adapter_sizes_ok(t, k, m, n, r);
+    *bytes = rc ? 0 : rsh::adapters_backward_work(t, k, m, n, r);
+    return rc;
+}
+
+int rsh_adapters_backward(const rsh_adapters_t* a, const void* dout, int64_t ld_dout, void* dX, void* dA, void* dB, void* work, void* hip_stream) {
+    if (const int rc = adapters_ok(a, work)) return rc;
+    if (!dout || (!dX && !dA && !dB) || (dA && !a->X) || (dB && !a->H)) return RSH_ERR_NULL;
+    if (!stride_ok(ld_dout, a->m) || !aligned_to({dout, dX, dA, dB}, 2)) return RSH_ERR_BAD_OPTION;
+    return launch_status(rsh::launch_adapters_backward(*a, dout, ld_dout, dX, dA, dB, work, hip_stream));
+}
+
 int rsh_ffn_tiles(int32_t which, int32_t aligned, int64_t t, int64_t a, int64_t b, int32_t* tile) {
     if (!tile) return RSH_ERR_NULL;
     if (which < RSH_TILES_PRODUCT || which > RSH_TILES_DW_ONE) return RSH_ERR_BAD_OPTION;

@@ -105,6 +105,18 @@ int launch_gated_backward(const void* X, int type, int64_t ld_x, const void* Wg,
                           const void* dH, int64_t ld_h, int act, void* dX, void* dWg, void* dWu, int64_t t, int64_t d, int64_t f, void* work,
                           void* stream);
 
+// Norms, joins and dropout (join.hip): the C entry points' structures, already checked.
+int64_t join_backward_work(int64_t t, int64_t d, int vectors);
+int launch_join_forward(const rsh_join_t& join, void* stream);
+int launch_join_backward(const rsh_join_t& join, const rsh_join_gradients_t& gradients, void* stream);
+int launch_dropout(const void* X, int type, int64_t t, int64_t d, int64_t ld, const rsh_drop_t& drop, void* Y, void* stream);
+
+// Low-rank adapters (adapters.hip): the same.
+int64_t adapters_forward_work(int64_t t, int64_t k, int64_t m, int n, int r);
+int64_t adapters_backward_work(int64_t t, int64_t k, int64_t m, int n, int r);
+int launch_adapters_forward(const rsh_adapters_t& a, void* work, void* stream);
+int launch_adapters_backward(const rsh_adapters_t& a, const void* dout, int64_t ld_dout, void* dX, void* dA, void* dB, void* work, void* stream);
+
 // Plain device-to-device copy of `bytes` (multiple of 16) used to calibrate traffic counters.
 int launch_copy_probe(const void* src_dev, void* dst_dev, size_t bytes, void* stream);
 
