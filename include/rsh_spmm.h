@@ -349,15 +349,15 @@ int rsh_dropout(const void *X_dev, int32_t type, int64_t t, int64_t d, int64_t l
  *   RSH_NORM_LAYER   (x - m) r weight + bias,  m = mean of x, r = 1 / sqrt(mean of (x - m)^2 + eps)
  * weight, bias: [d], NULL for ones and zeros.  stats: fp32 [t][2], m (0 with RSH_NORM_RMS) and r of every row; written by the forward
  * call where it is not NULL, read by the backward call.
- *   type         RSH_F32, RSH_F16 or RSH_BF16, of X, B, S, Y and their gradients; parameters and gate have types of their own
+ *   type         RSH_F32, RSH_F16 or RSH_BF16, of X, B, S, Y and their gradients; parameters and gate have it or are RSH_F32
  *   ld_x, ld_b   elements from row to row; no alignment beyond the element's
- *   gate         [d] (ld_gate 0) or [t][d] with rows ld_gate apart; NULL for ones
+ *   gate         [d] (ld_gate 0) or [t][d] with rows ld_gate apart; NULL (ld_gate 0) for ones
  *   S            [t][d] without gaps, not X or B; NULL if and only if B is
  *   Y            [t][d] without gaps; NULL if and only if before.kind is RSH_NORM_NONE
  * Everything is fp32 until it is stored: Y is the norm of the sum, not of the rounded S.  A row's differences from its mean are formed
  * in fp32; squares may leave its range.
- * rsh_join_backward: dS and dY (rows ld_ds and ld_dy apart; NULL for zeros) are the gradients of S and Y.  It reads S (with B NULL: X) as
- * the forward call wrote it, and the statistics.  Results, each NULL where not wanted: dX and dB [t][d], dgate (gate's shape and type,
+ * rsh_join_backward: dS and dY (rows ld_ds and ld_dy apart; NULL for zeros) are the gradients of S and Y.  It reads X (where dY is there), B,
+ * the parameters and the statistics as the forward call had them, not S and Y.  Results, each NULL where not wanted: dX and dB [t][d], dgate (gate's shape and type,
  * without gaps), gradients of the parameters in their types.  work: 16-byte aligned, of the bytes that rsh_join_backward_work reports,
  * rewritten by every call (0: may be NULL); vectors: how many results are [d].
  * Results never depend on the order in which waves run.  RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride,

@@ -10,7 +10,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librsh.so")
-SOURCES = ["kernels.hip", "dense.hip", "mx4.hip", "ffn.hip", "few.hip", "join.hip", "adapters.hip", "api.cpp", "planner.cpp", "reorder.cpp"]
+SOURCES = ["kernels.hip", "dense.hip", "mx4.hip", "ffn.hip", "few.hip", "join.hip", "join_f32.hip", "join_f16.hip", "join_bf16.hip", "adapters.hip", "api.cpp", "planner.cpp", "reorder.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          # packed-fp32 VALU forms are switched off for device code on the test machines

@@ -738,24 +738,26 @@ int rows_ok(int64_t t, int64_t d) {
 }
 bool stride_ok(int64_t ld, int64_t d) { return ld >= d && ld < kMaxSize; }
 bool drop_ok(const rsh_drop_t& drop) { return drop.share <= 65536 && aligned_to({drop.seed_dev}, 8); }
-bool norm_ok(const rsh_norm_t& n) {
+// Parameters: in fp32 or in the rows' type.
+bool parameter_ok(const void* p, int32_t p_type, int32_t type) {
+    return !p || ((p_type == RSH_F32 || p_type == type) && aligned_to({p}, type_bytes(p_type)));
+}
+bool norm_ok(const rsh_norm_t& n, int32_t type) {
     if (n.kind == RSH_NORM_NONE) return true;
     return (n.kind == RSH_NORM_RMS || n.kind == RSH_NORM_LAYER) && n.eps > 0 && n.eps < INFINITY && aligned_to({n.stats}, 8) &&
-           (!n.weight || (any_type(n.weight_type) && aligned_to({n.weight}, type_bytes(n.weight_type)))) &&
-           (!n.bias || (any_type(n.bias_type) && aligned_to({n.bias}, type_bytes(n.bias_type))));
+           parameter_ok(n.weight, n.weight_type, type) && parameter_ok(n.bias, n.bias_type, type);
 }
 int join_ok(const rsh_join_t* j, bool forward) {
     if (!j) return RSH_ERR_NULL;
     if (!any_type(j->type)) return RSH_ERR_BAD_OPTION;
     if (const int rc = rows_ok(j->t, j->d)) return rc;
     const bool norm = j->before.kind != RSH_NORM_NONE;
-    if ((forward || !j->B) && !j->X) return RSH_ERR_NULL;
+    if (forward && !j->X) return RSH_ERR_NULL;
     if ((forward && (!j->S != !j->B || !j->Y != !norm)) || (!j->B && !norm)) return RSH_ERR_NULL;
-    if (!norm_ok(j->after) || !norm_ok(j->before) || !aligned_to({j->X, j->B, j->S, j->Y}, type_bytes(j->type)) || (j->X && !stride_ok(j->ld_x, j->d)) ||
+    if (!norm_ok(j->after, j->type) || !norm_ok(j->before, j->type) || !aligned_to({j->X, j->B, j->S, j->Y}, type_bytes(j->type)) || (j->X && !stride_ok(j->ld_x, j->d)) ||
         (j->B && !stride_ok(j->ld_b, j->d)) || !drop_ok(j->drop) || !(j->scale - j->scale == 0))
         return RSH_ERR_BAD_OPTION;
-    if (j->gate && (!any_type(j->gate_type) || !aligned_to({j->gate}, type_bytes(j->gate_type)) || (j->ld_gate && !stride_ok(j->ld_gate, j->d))))
-        return RSH_ERR_BAD_OPTION;
+    if (!parameter_ok(j->gate, j->gate_type, j->type) || (j->gate ? j->ld_gate && !stride_ok(j->ld_gate, j->d) : j->ld_gate != 0)) return RSH_ERR_BAD_OPTION;
     if (forward && j->B && (j->S == j->X || j->S == j->B)) return RSH_ERR_BAD_OPTION;
     return RSH_OK;
 }
@@ -790,7 +792,7 @@ int rsh_join_backward(const rsh_join_t* join, const rsh_join_gradients_t* g, voi
     const bool before = j.before.kind != RSH_NORM_NONE, after = j.B && j.after.kind != RSH_NORM_NONE;
     const int vectors = !!g->after_weight + !!g->after_bias + !!g->before_weight + !!g->before_bias + (g->dgate && !j.ld_gate);
     if (!g->dX && !g->dB && !g->dgate && !vectors) return RSH_ERR_NULL;
-    if ((!g->dS && !g->dY) || (vectors && !g->work) || (g->dY && before && (!j.before.stats || (j.B && !j.S))) || (after && !j.after.stats)) return RSH_ERR_NULL;
+    if ((!g->dS && !g->dY) || (vectors && !g->work) || (g->dY && before && (!j.before.stats || !j.X)) || (after && !j.after.stats)) return RSH_ERR_NULL;
     if ((g->dB && !j.B) || (g->dgate && !j.gate) || (g->dS && !j.B) || (g->dY && !before) ||
         ((g->before_weight || g->before_bias) && !(before && g->dY)) || (g->before_weight && !j.before.weight) || (g->before_bias && !j.before.bias) ||
         ((g->after_weight || g->after_bias) && !after) || (g->after_weight && !j.after.weight) || (g->after_bias && !j.after.bias) ||

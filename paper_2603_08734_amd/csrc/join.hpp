@@ -1,0 +1,746 @@
+// Kernels of norms and joins: S = X + scale * gate * drop(N1(B)) and Y = N2(S), and their gradients; a source file for each type.
+#pragma once
+#include <algorithm>
+
+#include "rows.hpp"
+
+namespace rsh {
+
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+
+// Sums over the LANES lanes that share a row; every lane gets them, always added in the same order.  Waves meet in LDS, in two places
+// by turns: a wave that writes a place again has passed the barrier that all come to after having read it.
+template <int LANES>
+struct Team {
+    static constexpr int kWaves = LANES > 64 ? LANES / 64 : 1;
+    typedef float2_t Meeting[2][kWaves];
+    Meeting& place;
+    int turn = 0;
+    __device__ __forceinline__ explicit Team(Meeting& p) : place(p) {}
+    static __device__ __forceinline__ float in_wave(float v) {
+        v = add_dpp<0xb1>(v);       // lanes 1 0 3 2
+        v = add_dpp<0x4e>(v);       // lanes 2 3 0 1
+        v = add_dpp<0x141>(v);      // eight lanes mirrored
+        if constexpr (LANES >= 16) v = add_dpp<0x140>(v);      // sixteen
+        const int lane = threadIdx.x & 63;
+        if constexpr (LANES >= 32) v += shfl_f32(v, lane ^ 16);
+        if constexpr (LANES >= 64) v += shfl_f32(v, lane ^ 32);
+        return v;
+    }
+    __device__ __forceinline__ float2_t sum(float a, float b) {
+        a = in_wave(a);
+        b = in_wave(b);
+        if constexpr (LANES > 64) {
+            if ((threadIdx.x & 63) == 0) place[turn][threadIdx.x >> 6] = (float2_t){a, b};
+            __syncthreads();
+            a = b = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float2_t p = place[turn][w];
+                a += p[0];
+                b += p[1];
+            }
+            turn ^= 1;
+        }
+        return (float2_t){a, b};
+    }
+};
+
+// What is widened from it before is not kept for after: it is widened again, an instruction an element in place of a register.
+template <class T>
+__device__ __forceinline__ void renew(Raw<T>& r) {
+#pragma unroll
+    for (auto& v : r.v) asm volatile("" : "+v"(v));
+}
+
+// f(c, column) for the runs of eight columns that a lane has: C of them, kept in registers, or (C = 0) as many as there are.
+template <int LANES, int C, class F>
+__device__ __forceinline__ void each_run(int d, F f) {
+    const int lane = threadIdx.x % LANES;
+    if constexpr (C > 0) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) f(c, 8 * (lane + LANES * c));
+    } else {
+        for (int col = 8 * lane; col < d; col += 8 * LANES) f(0, col);
+    }
+}
+
+__device__ __forceinline__ void clear_from(Eight& e, int valid) {
+    if (valid < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = i < valid ? e.v[i] : 0.f;
+    }
+}
+
+// A run of a row of parameters or of the gate, in fp32 or in the rows' type.
+template <class T, bool SHORT>
+__device__ __forceinline__ Eight load_vector(const void* p, int type, int col, int d) {
+    if (std::is_same<T, F32>::value || type == RSH_F32) return widen(load_raw<F32, SHORT>(p, col, d));
+    return widen(load_raw<T, SHORT>(p, col, d));
+}
+// Parameters of a run: ones or zeros where there are none.
+template <class T, bool SHORT>
+__device__ __forceinline__ Eight parameters(const void* p, int type, int col, int d, float otherwise) {
+    if (p) return load_vector<T, SHORT>(p, type, col, d);
+    Eight e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e.v[i] = otherwise;
+    return e;
+}
+__device__ __forceinline__ const void* element(const void* base, int64_t at, int size) { return base ? (const uint8_t*)base + at * size : nullptr; }
+
+// Into a row of d at column col.
+template <class T>
+__device__ __forceinline__ void store_run(void* base, int64_t row, int col, int d, const Eight& e) {
+    store_eight<T>((void*)byte_of(element(base, row * d, size_of<T>()), (uint32_t)col * (uint32_t)size_of<T>()), 0, e, d - col);
+}
+
+// The row of a team, alike in all lanes of a wave where a team is no smaller.
+template <int LANES>
+__device__ __forceinline__ int64_t row_of(int64_t first) {
+    if constexpr (LANES >= 64) {
+        const int64_t r = first + threadIdx.x / LANES;
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(r >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)r));
+    }
+    return first + threadIdx.x / LANES;
+}
+
+// m and r of a row whose runs are get(c, column), zeros behind the row's end.  Where a sum leaves the range of fp32, once more with the
+// row scaled by a power of two.
+template <int LANES, int C, class GET>
+__device__ __forceinline__ float2_t statistics(const rsh_norm_t& norm, int d, Team<LANES>& team, GET get) {
+    float m = 0.f, q = 0.f;
+    auto attempt = [&](float c) {
+        if (norm.kind == RSH_NORM_LAYER) {
+            float a = 0.f;
+            each_run<LANES, C>(d, [&](int i, int col) {
+                const Eight e = get(i, col);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) a += e.v[j] * c;
+            });
+            m = team.sum(a, 0.f)[0] / (float)d;
+        }
+        q = 0.f;
+        each_run<LANES, C>(d, [&](int i, int col) {
+            Eight e = get(i, col);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e.v[j] = e.v[j] * c - m;
+            clear_from(e, d - col);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q += e.v[j] * e.v[j];
+        });
+        q = team.sum(q, 0.f)[0] / (float)d;
+    };
+    attempt(1.f);
+    if (m - m + q < INFINITY) return (float2_t){m, 1.f / sqrtf(q + norm.eps)};
+    const float c = 0x1p-70f;
+    attempt(c);
+    return (float2_t){m / c, c / sqrtf(q + fmaxf(norm.eps * c * c, 0x1p-149f))};
+}
+
+template <int LANES> constexpr int kThreadsOf = LANES <= 64 ? 256 : LANES;
+template <int LANES> constexpr int kRowsOf = kThreadsOf<LANES> / LANES;
+
+// Parameters of the run of columns that a lane has in every row: kept in fp32 registers while the workgroup goes through its rows.  Loaded anew
+// for every row they took as many instructions as the row itself, and their latency showed.
+template <class T, bool SHORT>
+struct Affine {
+    Eight w, b;
+    __device__ __forceinline__ Affine(const rsh_norm_t& n, int col, int d)
+        : w(parameters<T, SHORT>(n.kind == RSH_NORM_NONE ? nullptr : n.weight, n.weight_type, col, d, 1.f)),
+          b(parameters<T, SHORT>(n.kind == RSH_NORM_NONE ? nullptr : n.bias, n.bias_type, col, d, 0.f)) {}
+    __device__ __forceinline__ void apply(Eight& e, float2_t s) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = (e.v[i] - s[0]) * s[1] * w.v[i] + b.v[i];
+    }
+};
+
+// Rows of up to 8 LANES columns, a run a lane.  JOIN: whether there is a B.  The next row's loads go out when this one's have been used.
+template <class T, int LANES, bool JOIN>
+__global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(4))) void rsh_join_forward_kernel(rsh_join_t j) {
+    constexpr bool kShort = LANES == 8;        // rows may be shorter than a run
+    constexpr int kSize = size_of<T>(), kRows = kRowsOf<LANES>;
+    __shared__ typename Team<LANES>::Meeting meeting;
+    Team<LANES> team(meeting);
+    const Random random(j.drop);
+    const int d = (int)j.d, col = 8 * (threadIdx.x % LANES);
+    const Affine<T, kShort> first(j.after, col, d), second(j.before, col, d);
+    const float factor = j.drop.share ? j.scale * random.keep : j.scale;
+    Eight gate = parameters<T, kShort>(j.ld_gate ? nullptr : j.gate, j.gate_type, col, d, 1.f);
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    Raw<T> x, b;
+    auto load = [&](int64_t head) {
+        const int64_t row = min(row_of<LANES>(head), j.t - 1);
+        if constexpr (JOIN) b = load_raw<T, kShort>(element(j.B, row * j.ld_b, kSize), col, d);
+        x = load_raw<T, kShort>(element(j.X, row * j.ld_x, kSize), col, d);
+    };
+    load((int64_t)blockIdx.x * kRows);
+    for (int64_t head = (int64_t)blockIdx.x * kRows; head < j.t; head += step) {
+        const int64_t mine = row_of<LANES>(head), row = min(mine, j.t - 1);
+        const bool live = mine < j.t, leads = live && threadIdx.x % LANES == 0;
+        Eight s;
+        if constexpr (JOIN) {
+            Eight n = widen(b);
+            if (j.after.kind != RSH_NORM_NONE) {
+                const float2_t at = statistics<LANES, 1>(j.after, d, team, [&](int, int) { return n; });
+                if (leads && j.after.stats) *reinterpret_cast<float2_t*>(j.after.stats + 2 * row) = at;
+                first.apply(n, at);
+            }
+            if (j.ld_gate) gate = load_vector<T, kShort>(element(j.gate, row * j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d);
+            if (j.drop.share) random.drop(n, col, row, factor);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) n.v[i] *= factor;
+            s = widen(x);
+            if (head + step < j.t) load(head + step);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s.v[i] += gate.v[i] * n.v[i];
+            clear_from(s, d - col);
+            if (live) store_run<T>(j.S, row, col, d, s);
+        } else {
+            s = widen(x);
+            if (head + step < j.t) load(head + step);
+        }
+        if (j.before.kind == RSH_NORM_NONE) continue;
+        const float2_t at = statistics<LANES, 1>(j.before, d, team, [&](int, int) { return s; });
+        if (leads && j.before.stats) *reinterpret_cast<float2_t*>(j.before.stats + 2 * row) = at;
+        second.apply(s, at);
+        if (live) store_run<T>(j.Y, row, col, d, s);
+    }
+}
+
+// Longer rows: C runs a lane in registers, or (C = 0) as many as there are, read again at every pass.
+template <class T, int LANES, int C, bool JOIN>
+__global__ __launch_bounds__(LANES) __attribute__((amdgpu_waves_per_eu(4))) void rsh_join_forward_long_kernel(rsh_join_t j) {
+    constexpr int kSize = size_of<T>();
+    __shared__ typename Team<LANES>::Meeting meeting;
+    Team<LANES> team(meeting);
+    const Random random(j.drop);
+    const int d = (int)j.d;
+    const float factor = j.drop.share ? j.scale * random.keep : j.scale;
+    for (int64_t row = blockIdx.x; row < j.t; row += gridDim.x) {
+        const void* const x_row = element(j.X, row * j.ld_x, kSize);
+        const void* const b_row = element(j.B, row * j.ld_b, kSize);
+        Raw<T> x[C ? C : 1], b[JOIN && C ? C : 1];
+        Eight kept[C ? C : 1];
+        if constexpr (C > 0) {
+            if constexpr (JOIN) each_run<LANES, C>(d, [&](int c, int col) { b[c] = load_raw<T, false>(b_row, col, d); });
+            each_run<LANES, C>(d, [&](int c, int col) { x[c] = load_raw<T, false>(x_row, col, d); });
+        }
+        float2_t after = {0.f, 1.f};
+        auto loaded = [&](int c, int col) { return widen(C ? b[c] : load_raw<T, false>(b_row, col, d)); };
+        if (JOIN && j.after.kind != RSH_NORM_NONE) {
+            after = statistics<LANES, C>(j.after, d, team, loaded);
+            if (threadIdx.x == 0 && j.after.stats) *reinterpret_cast<float2_t*>(j.after.stats + 2 * row) = after;
+        }
+        auto sum = [&](int c, int col) {
+            Eight s = widen(C ? x[c] : load_raw<T, false>(x_row, col, d));
+            if constexpr (JOIN) {
+                Eight n = loaded(c, col);
+                if (j.after.kind != RSH_NORM_NONE) Affine<T, false>(j.after, col, d).apply(n, after);
+                if (j.drop.share) random.drop(n, col, row, factor);
+                else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) n.v[i] *= factor;
+                const Eight gate = parameters<T, false>(element(j.gate, row * j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d, 1.f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s.v[i] += gate.v[i] * n.v[i];
+                clear_from(s, d - col);
+            }
+            return s;
+        };
+        if constexpr (JOIN || C > 0) {
+            each_run<LANES, C>(d, [&](int c, int col) {
+                if constexpr (C > 0 && JOIN) renew(b[c]);
+                const Eight s = sum(c, col);
+                if (C) kept[c] = s;
+                if (JOIN) store_run<T>(j.S, row, col, d, s);
+            });
+        }
+        if (j.before.kind == RSH_NORM_NONE) continue;
+        auto summed = [&](int c, int col) { return C ? kept[c] : sum(c, col); };
+        const float2_t before = statistics<LANES, C>(j.before, d, team, summed);
+        if (threadIdx.x == 0 && j.before.stats) *reinterpret_cast<float2_t*>(j.before.stats + 2 * row) = before;
+        each_run<LANES, C>(d, [&](int c, int col) {
+            Eight y = summed(c, col);
+            Affine<T, false>(j.before, col, d).apply(y, before);
+            store_run<T>(j.Y, row, col, d, y);
+        });
+    }
+}
+
+// The vectors among the gradients, in the order of their sums.
+enum Slot { kBeforeWeight, kBeforeBias, kAfterWeight, kAfterBias, kGate, kSlots };
+struct Vectors {
+    void* out[kSlots];
+    int type[kSlots];
+    int at[kSlots];        // place among the wanted ones, or -1
+    int count;
+};
+
+// A run's share of the vectors, which add(slot, terms) takes.  In registers, or, where a row's gradients need those, in LDS, 16 bytes a thread
+// and turn that it alone reads and writes: weights and gate, or with the biases all but the gate (five would be all of the LDS).
+struct NoSums {
+    __device__ __forceinline__ void add(Slot, const Eight&) {}
+};
+struct RegisterSums {
+    Eight of[kSlots] = {};
+    __device__ __forceinline__ void add(Slot k, const Eight& e) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) of[k].v[i] += e.v[i];
+    }
+    __device__ __forceinline__ Eight get(int k) const { return of[k]; }
+};
+template <int THREADS, bool BIAS>
+struct LdsSums {
+    static constexpr int SLOTS = BIAS ? 4 : 3;
+    typedef float4_t Place[SLOTS][2][THREADS];
+    Place& place;
+    const Vectors& vectors;
+    Eight gate = {};
+    __device__ __forceinline__ LdsSums(Place& p, const Vectors& v) : place(p), vectors(v) {
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) place[k][0][threadIdx.x] = place[k][1][threadIdx.x] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    }
+    static __device__ __forceinline__ constexpr int at(int k) {      // SLOTS: not there
+        return k == kBeforeWeight ? 0 : k == kAfterWeight ? 1 : k == kGate ? (BIAS ? SLOTS : 2) : BIAS ? (k == kBeforeBias ? 2 : 3) : SLOTS;
+    }
+    __device__ __forceinline__ void add(Slot k, const Eight& e) {
+        if (BIAS && k == kGate) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gate.v[i] += e.v[i];
+        } else if (at(k) < SLOTS && vectors.at[k] >= 0) {
+            float4_t* const lo = &place[at(k)][0][threadIdx.x];
+            float4_t* const hi = &place[at(k)][1][threadIdx.x];
+            *lo += (float4_t){e.v[0], e.v[1], e.v[2], e.v[3]};
+            *hi += (float4_t){e.v[4], e.v[5], e.v[6], e.v[7]};
+        }
+    }
+    __device__ __forceinline__ Eight get(int k) const {
+        if (at(k) >= SLOTS) return gate;
+        const float4_t a = place[at(k)][0][threadIdx.x], b = place[at(k)][1][threadIdx.x];
+        return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+    }
+};
+
+template <class T>
+struct Inputs {
+    Raw<T> x, b, ds, dy;
+    float2_t before, after;        // m and r of S and of B
+};
+
+// Gradients of a run of a row.
+struct Run {
+    Eight g, xh;           // of Y times N2's weight; S without mean and size
+    Eight ds;              // of S
+    Eight xb;              // B without mean and size
+    Eight gb;              // gradient of N1's result times its weight
+    uint32_t kept;         // of dropout
+};
+
+// The parameters of a run: of every row the same run, so kept, or loaded anew.
+template <class T, bool SHORT>
+struct KeptParameters {
+    Affine<T, SHORT> after, before;
+    Eight gate;
+    __device__ __forceinline__ KeptParameters(const rsh_join_t& j, int col, int d)
+        : after(j.after, col, d), before(j.before, col, d),
+          gate(parameters<T, SHORT>(j.ld_gate ? nullptr : j.gate, j.gate_type, col, d, 1.f)) {}
+    __device__ __forceinline__ Eight after_weight(int) const { return after.w; }
+    __device__ __forceinline__ Eight after_bias(int) const { return after.b; }
+    __device__ __forceinline__ Eight before_weight(int) const { return before.w; }
+    __device__ __forceinline__ Eight gate_of(int) const { return gate; }
+};
+template <class T>
+struct LoadedParameters {
+    const rsh_join_t& j;
+    int d;
+    __device__ __forceinline__ Eight after_weight(int col) const { return parameters<T, false>(j.after.weight, j.after.weight_type, col, d, 1.f); }
+    __device__ __forceinline__ Eight after_bias(int col) const { return parameters<T, false>(j.after.bias, j.after.bias_type, col, d, 0.f); }
+    __device__ __forceinline__ Eight before_weight(int col) const { return parameters<T, false>(j.before.weight, j.before.weight_type, col, d, 1.f); }
+    __device__ __forceinline__ Eight gate_of(int col) const { return parameters<T, false>(j.ld_gate ? nullptr : j.gate, j.gate_type, col, d, 1.f); }
+};
+
+// JOIN as above; SUMS: where the vectors are added up, PARAMETERS: where the parameters come from.
+template <class T, bool JOIN, bool SHORT, class SUMS, class PARAMETERS>
+struct Backward {
+    static constexpr int kSize = size_of<T>();
+    const rsh_join_t& j;
+    const rsh_join_gradients_t& g;
+    const Random& random;
+    const PARAMETERS& given;
+    int d;
+    bool first, second;        // whether N2 and its gradient, and whether N1 are there
+
+    __device__ __forceinline__ Backward(const rsh_join_t& join, const rsh_join_gradients_t& grad, const Random& r, const PARAMETERS& p)
+        : j(join), g(grad), random(r), given(p), d((int)join.d), first(join.before.kind != RSH_NORM_NONE && grad.dY),
+          second(JOIN && join.after.kind != RSH_NORM_NONE) {}
+
+    // Of a row.  live: it is one, else all of it counts as zero.
+    __device__ __forceinline__ Inputs<T> load(int64_t row, bool live, int col) const {
+        Inputs<T> in = {};
+        const int end = live ? d : 0;      // what is loaded is zero from here on
+        auto run = [&](const void* p, int64_t ld) {
+            Raw<T> r = load_raw<T, SHORT>(element(p, row * ld, kSize), col, d);
+#pragma unroll
+            for (auto& v : r.v)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v[w] = end ? v[w] : 0u;
+            return r;
+        };
+        if (first) {
+            in.dy = run(g.dY, g.ld_dy);
+            in.x = run(j.X, j.ld_x);
+            if (live) in.before = *reinterpret_cast<const float2_t*>(j.before.stats + 2 * row);
+        }
+        if constexpr (JOIN) {
+            in.b = run(j.B, j.ld_b);
+            if (second && live) in.after = *reinterpret_cast<const float2_t*>(j.after.stats + 2 * row);
+            if (g.dS) in.ds = run(g.dS, g.ld_ds);
+        }
+        return in;
+    }
+    // N1's result, after dropout but for its factor.
+    __device__ __forceinline__ Eight inner(const Run& x, int col) const {
+        Eight n = x.xb;
+        if (second) {
+            const Eight w = given.after_weight(col), b = given.after_bias(col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n.v[i] = n.v[i] * w.v[i] + b.v[i];
+        }
+        if (j.drop.share) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n.v[i] = x.kept >> i & 1 ? n.v[i] : 0.f;
+        }
+        return n;
+    }
+    __device__ __forceinline__ float factor() const { return j.drop.share ? j.scale * random.keep : j.scale; }
+    // scale * gate, zero where dropped, times dropout's factor.
+    __device__ __forceinline__ Eight factors(const Run& x, int64_t row, int col) const {
+        Eight f;
+        if (j.ld_gate) f = load_vector<T, SHORT>(element(j.gate, row * j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d);
+        else f = given.gate_of(col);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.v[i] *= factor();
+        if (j.drop.share) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f.v[i] = x.kept >> i & 1 ? f.v[i] : 0.f;
+        }
+        return f;
+    }
+    __device__ __forceinline__ void store_gate(int64_t row, int col, const Eight& gate) const {
+        if (std::is_same<T, F32>::value || j.gate_type == RSH_F32) store_run<F32>(g.dgate, row, col, d, gate);
+        else store_run<T>(g.dgate, row, col, d, gate);
+    }
+    // Up to the gradient of N2 and what its two means are of.
+    __device__ __forceinline__ void before(const Inputs<T>& in, int64_t row, int col, Run& x, SUMS& sums) const {
+        if constexpr (JOIN) {
+            x.xb = widen(in.b);
+            if (second) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x.xb.v[i] = (x.xb.v[i] - in.after[0]) * in.after[1];
+            }
+            if (j.drop.share) x.kept = random.kept(col, row);
+        }
+        if (!first) return;
+        x.xh = widen(in.x);
+        if constexpr (JOIN) {
+            const Eight n = inner(x, col), f = factors(x, row, col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.xh.v[i] += f.v[i] * n.v[i];
+        }
+        x.g = widen(in.dy);
+        const Eight w = given.before_weight(col);
+        Eight term;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x.xh.v[i] = (x.xh.v[i] - in.before[0]) * in.before[1];
+            term.v[i] = x.g.v[i] * x.xh.v[i];
+        }
+        sums.add(kBeforeWeight, term);
+        sums.add(kBeforeBias, x.g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x.g.v[i] *= w.v[i];
+    }
+    // The gradient of S, from the means of g and g xh.
+    __device__ __forceinline__ void sum(const Inputs<T>& in, float2_t mean, int valid, Run& x) const {
+        x.ds = widen(in.ds);
+        if (first) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.ds.v[i] += in.before[1] * (x.g.v[i] - mean[0] - x.xh.v[i] * mean[1]);
+        }
+        clear_from(x.ds, valid);
+    }
+    // From there to the gradient of N1's result; returns what the gate's gradient gets.
+    __device__ __forceinline__ Eight through(const Inputs<T>&, int64_t row, int col, Run& x, SUMS& sums) const {
+        const Eight f = factors(x, row, col);
+        Eight gate = {};
+        if (g.dgate) {
+            gate = inner(x, col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gate.v[i] *= x.ds.v[i] * factor();
+            sums.add(kGate, gate);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x.gb.v[i] = x.ds.v[i] * f.v[i];
+        if (second) {
+            const Eight w = given.after_weight(col);
+            Eight term;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) term.v[i] = x.gb.v[i] * x.xb.v[i];
+            sums.add(kAfterWeight, term);
+            sums.add(kAfterBias, x.gb);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.gb.v[i] *= w.v[i];
+        }
+        return gate;
+    }
+};
+
+// One pass over the rows, each in its lanes' registers, and the vectors' sums with it, a part of them from every workgroup.  The next
+// row is on its way while one is computed.
+template <class T, int LANES, bool JOIN, bool BIAS>
+__global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(4))) void rsh_join_backward_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts) {
+    constexpr int kThreads = kThreadsOf<LANES>, kRows = kRowsOf<LANES>;
+    __shared__ typename Team<LANES>::Meeting meeting;
+    using Sums = std::conditional_t<JOIN, LdsSums<kThreads, BIAS>, RegisterSums>;
+    __shared__ std::conditional_t<JOIN, typename LdsSums<kThreads, BIAS>::Place, float> place;
+    __shared__ float joined[kRows > 1 ? kThreads * 8 : 1];
+    Team<LANES> team(meeting);
+    const Random random(j.drop);
+    const int d = (int)j.d, col = 8 * (threadIdx.x % LANES);
+    const KeptParameters<T, LANES == 8> given(j, col, d);
+    const Backward<T, JOIN, LANES == 8, Sums, KeptParameters<T, LANES == 8>> back(j, g, random, given);
+    Sums sums = [&] {
+        if constexpr (JOIN) return Sums(place, vectors);
+        else return Sums();
+    }();
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    auto load = [&](int64_t head) {
+        const int64_t mine = row_of<LANES>(head);
+        return back.load(min(mine, j.t - 1), mine < j.t, col);
+    };
+    Inputs<T> next = load((int64_t)blockIdx.x * kRows);
+    for (int64_t head = (int64_t)blockIdx.x * kRows; head < j.t; head += step) {
+        const int64_t mine = row_of<LANES>(head), row = min(mine, j.t - 1);
+        const bool live = mine < j.t;
+        Inputs<T> in = next;
+        Run x;
+        float2_t mean = {0.f, 0.f};
+        back.before(in, row, col, x, sums);
+        if (head + step < j.t) next = load(head + step);
+        if (back.first) {
+            float a = 0.f, b = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a += x.g.v[i], b += x.g.v[i] * x.xh.v[i];
+            mean = team.sum(a, b) / (float)d;
+            if (j.before.kind != RSH_NORM_LAYER) mean[0] = 0.f;
+        }
+        back.sum(in, mean, live ? d - col : 0, x);
+        if (g.dX && live) store_run<T>(g.dX, row, col, d, x.ds);
+        if constexpr (JOIN) {
+            const Eight gate = back.through(in, row, col, x, sums);
+            if (g.dgate && j.ld_gate && live) back.store_gate(row, col, gate);
+            if (!g.dB) continue;
+            if (back.second) {
+                float a = 0.f, b = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a += x.gb.v[i], b += x.gb.v[i] * x.xb.v[i];
+                mean = team.sum(a, b) / (float)d;
+                if (j.after.kind != RSH_NORM_LAYER) mean[0] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x.gb.v[i] = in.after[1] * (x.gb.v[i] - mean[0] - x.xb.v[i] * mean[1]);
+            }
+            if (live) store_run<T>(g.dB, row, col, d, x.gb);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) {
+        if ((!JOIN && k >= kAfterWeight) || (!BIAS && (k == kBeforeBias || k == kAfterBias))) continue;
+        if (vectors.at[k] >= 0) {
+            float* const out = parts + ((int64_t)blockIdx.x * vectors.count + vectors.at[k]) * d;
+            if constexpr (kRows == 1) {
+                store_eight<F32>(out, col, sums.get(k), d - col);
+            } else {
+                const Eight e = sums.get(k);
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) joined[threadIdx.x * 8 + i] = e.v[i];
+                __syncthreads();
+                for (int c = threadIdx.x; c < d; c += kThreads) {
+                    float a = 0.f;
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) a += joined[r * LANES * 8 + c];
+                    out[c] = a;
+                }
+            }
+        }
+    }
+}
+
+// Rows of any length, read again at each of three passes; the means of g and g xh go to `means`, and the next kernel adds up the vectors.
+template <class T, bool JOIN>
+__global__ __launch_bounds__(1024) void rsh_join_backward_long_kernel(rsh_join_t j, rsh_join_gradients_t g, float* means) {
+    __shared__ Team<1024>::Meeting meeting;
+    Team<1024> team(meeting);
+    const Random random(j.drop);
+    const LoadedParameters<T> given{j, (int)j.d};
+    const Backward<T, JOIN, false, NoSums, LoadedParameters<T>> back(j, g, random, given);
+    const int d = back.d;
+    NoSums none;
+    for (int64_t row = blockIdx.x; row < j.t; row += gridDim.x) {
+        float2_t mean = {0.f, 0.f};
+        Run x;
+        if (back.first) {
+            float a = 0.f, b = 0.f;
+            each_run<1024, 0>(d, [&](int, int col) {
+                back.before(back.load(row, true, col), row, col, x, none);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a += x.g.v[i], b += x.g.v[i] * x.xh.v[i];
+            });
+            mean = team.sum(a, b) / (float)d;
+            if (j.before.kind != RSH_NORM_LAYER) mean[0] = 0.f;
+            if (means && threadIdx.x == 0) *reinterpret_cast<float2_t*>(means + 2 * row) = mean;
+        }
+        float a = 0.f, b = 0.f;
+        each_run<1024, 0>(d, [&](int, int col) {
+            const Inputs<T> in = back.load(row, true, col);
+            back.before(in, row, col, x, none);
+            back.sum(in, mean, d - col, x);
+            if (g.dX) store_run<T>(g.dX, row, col, d, x.ds);
+            if constexpr (JOIN) {
+                const Eight gate = back.through(in, row, col, x, none);
+                if (g.dgate && j.ld_gate) back.store_gate(row, col, gate);
+                if (!back.second && g.dB) store_run<T>(g.dB, row, col, d, x.gb);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a += x.gb.v[i], b += x.gb.v[i] * x.xb.v[i];
+            }
+        });
+        if (!JOIN || !back.second || !g.dB) continue;
+        float2_t inner = team.sum(a, b) / (float)d;
+        if (j.after.kind != RSH_NORM_LAYER) inner[0] = 0.f;
+        each_run<1024, 0>(d, [&](int, int col) {
+            const Inputs<T> in = back.load(row, true, col);
+            back.before(in, row, col, x, none);
+            back.sum(in, mean, d - col, x);
+            (void)back.through(in, row, col, x, none);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.gb.v[i] = in.after[1] * (x.gb.v[i] - inner[0] - x.xb.v[i] * inner[1]);
+            store_run<T>(g.dB, row, col, d, x.gb);
+        });
+    }
+}
+
+// The vectors' sums of such rows: a thread has eight columns of the rows of a part.
+template <class T, bool JOIN>
+__global__ __launch_bounds__(256) void rsh_join_columns_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts,
+                                                               const float* means) {
+    const Random random(j.drop);
+    const LoadedParameters<T> given{j, (int)j.d};
+    const Backward<T, JOIN, false, RegisterSums, LoadedParameters<T>> back(j, g, random, given);
+    const int col = 8 * (int)(blockIdx.x * 256 + threadIdx.x);
+    if (col >= back.d) return;
+    RegisterSums sums;
+    for (int64_t row = blockIdx.y; row < j.t; row += gridDim.y) {
+        Run x;
+        const Inputs<T> in = back.load(row, true, col);
+        back.before(in, row, col, x, sums);
+        if constexpr (JOIN) {
+            back.sum(in, back.first ? *reinterpret_cast<const float2_t*>(means + 2 * row) : (float2_t){0.f, 0.f}, back.d - col, x);
+            (void)back.through(in, row, col, x, sums);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k)
+        if (vectors.at[k] >= 0)
+            store_eight<F32>(parts + ((int64_t)blockIdx.y * vectors.count + vectors.at[k]) * back.d, col, sums.get(k), back.d - col);
+}
+
+// f(lanes) of the kernels that have a row in registers, a run a lane: the fewest that do.
+constexpr int64_t kRegisterWidth = 8192, kColumnParts = 64;
+template <class F>
+void by_width(int64_t d, F f) {
+    using std::integral_constant;
+    const int64_t runs = (d + 7) / 8;
+    if (runs <= 8) f(integral_constant<int, 8>());
+    else if (runs <= 16) f(integral_constant<int, 16>());
+    else if (runs <= 32) f(integral_constant<int, 32>());
+    else if (runs <= 64) f(integral_constant<int, 64>());
+    else if (runs <= 128) f(integral_constant<int, 128>());
+    else if (runs <= 256) f(integral_constant<int, 256>());
+    else if (runs <= 512) f(integral_constant<int, 512>());
+    else if (runs <= 1024) f(integral_constant<int, 1024>());
+}
+int64_t backward_parts(int64_t t, int64_t d);
+int64_t vector_bytes(int64_t t, int64_t d, int vectors);
+
+// Launches of one type, in a source file of its own.
+template <class T>
+void join_forward_of(const rsh_join_t& j, hipStream_t st);
+template <class T>
+void join_backward_of(const rsh_join_t& j, const rsh_join_gradients_t& g, const Vectors& v, float* parts, int64_t n, hipStream_t st);
+
+#define RSH_JOIN_OF(T)                                                                                                                              \
+    template <>                                                                                                                                     \
+    void join_forward_of<T>(const rsh_join_t& j, hipStream_t st) {                                                                                   \
+        join_forward_launch<T>(j, st);                                                                                    \
+    }                                                                                                                   \
+    template <>                                                                                                                                     \
+    void join_backward_of<T>(const rsh_join_t& j, const rsh_join_gradients_t& g, const Vectors& v, float* parts, int64_t n, hipStream_t st) {        \
+        join_backward_launch<T>(j, g, v, parts, n, st);                                                                                              \
+    }
+
+template <class T>
+void join_forward_launch(const rsh_join_t& j, hipStream_t st) {
+    if (j.d > kRegisterWidth) {
+        const dim3 rows((unsigned)std::min<int64_t>(j.t, 1 << 16));
+        if (j.d <= 2 * kRegisterWidth) {
+            if (j.B) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 512, 4, true>), rows, dim3(512), 0, st, j);
+            else hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 512, 4, false>), rows, dim3(512), 0, st, j);
+        } else {
+            if (j.B) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 0, true>), rows, dim3(1024), 0, st, j);
+            else hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 0, false>), rows, dim3(1024), 0, st, j);
+        }
+        return;
+    }
+    by_width(j.d, [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        const unsigned blocks = (unsigned)std::min<int64_t>((j.t + kRowsOf<L> - 1) / kRowsOf<L>, 256 * (2048 / kThreadsOf<L>));
+        if (j.B) hipLaunchKernelGGL((rsh_join_forward_kernel<T, L, true>), dim3(blocks), dim3(kThreadsOf<L>), 0, st, j);
+        else hipLaunchKernelGGL((rsh_join_forward_kernel<T, L, false>), dim3(blocks), dim3(kThreadsOf<L>), 0, st, j);
+    });
+}
+
+template <class T>
+void join_backward_launch(const rsh_join_t& j, const rsh_join_gradients_t& g, const Vectors& v, float* parts, int64_t n, hipStream_t st) {
+    if (j.d > kRegisterWidth) {
+        float* const means = v.count ? (float*)((char*)g.work + vector_bytes(j.t, j.d, v.count)) : nullptr;
+        const dim3 rows((unsigned)std::min<int64_t>(j.t, 1 << 16)), columns((unsigned)((j.d + 2047) / 2048), (unsigned)n);
+        if (j.B) hipLaunchKernelGGL((rsh_join_backward_long_kernel<T, true>), rows, dim3(1024), 0, st, j, g, means);
+        else hipLaunchKernelGGL((rsh_join_backward_long_kernel<T, false>), rows, dim3(1024), 0, st, j, g, means);
+        if (!v.count) return;
+        if (j.B) hipLaunchKernelGGL((rsh_join_columns_kernel<T, true>), columns, dim3(256), 0, st, j, g, v, parts, means);
+        else hipLaunchKernelGGL((rsh_join_columns_kernel<T, false>), columns, dim3(256), 0, st, j, g, v, parts, means);
+        return;
+    }
+    const bool bias = v.at[kBeforeBias] >= 0 || v.at[kAfterBias] >= 0;
+    by_width(j.d, [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        const dim3 grid((unsigned)n), block(kThreadsOf<L>);
+        auto launch = [&](auto b) {
+            if (j.B) hipLaunchKernelGGL((rsh_join_backward_kernel<T, L, true, decltype(b)::value>), grid, block, 0, st, j, g, v, parts);
+            else hipLaunchKernelGGL((rsh_join_backward_kernel<T, L, false, decltype(b)::value>), grid, block, 0, st, j, g, v, parts);
+        };
+        if constexpr (L >= 512) {
+            if (bias) launch(std::true_type());
+            else launch(std::false_type());
+        } else {
+            launch(std::true_type());
+        }
+    });
+}
+
+}  // namespace rsh

@@ -23,6 +23,80 @@ __device__ __forceinline__ Eight widen8(uint4_t x) {
     return e;
 }
 
+// Eight elements as they lie in memory.
+template <class T>
+struct Raw {
+    uint4_t v[size_of<T>() / 2];
+};
+template <class T>
+__device__ __forceinline__ Eight widen(const Raw<T>& r) {
+    if constexpr (std::is_same<T, F32>::value) {
+        Eight e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t w = r.v[i / 4][i % 4];
+            e.v[i] = __uint_as_float(w);
+        }
+        return e;
+    } else {
+        return widen8<T>(r.v[0]);
+    }
+}
+
+// Byte `at` of a row whose address is alike in all lanes.  Loops over rows would otherwise have the sums ready, two registers for every
+// vector and run, and an access would no longer have its address in scalar registers and an offset.
+__device__ __forceinline__ const uint8_t* byte_of(const void* row, uint32_t at) {
+    asm volatile("" : "+v"(at));
+    return (const uint8_t*)row + at;
+}
+
+// Elements col .. col + 7 of a row of d that begins at `row`, zeros from d on.  Every lane makes the same whole loads, the last of a row that
+// is no multiple of eight from where the row's last eight lie: a load under a condition of its own would have to arrive before the two
+// ways meet again, and no two would be under way at once.  SHORT: the row may have less than eight.
+template <class T, bool SHORT>
+__device__ __forceinline__ Raw<T> load_raw(const void* row, int col, int d) {
+    constexpr int N = size_of<T>() / 2;
+    Raw<T> r = {};
+    if (SHORT && d < 8) {
+        if constexpr (std::is_same<T, F32>::value) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (col + i < d) r.v[i / 4][i % 4] = ((const uint32_t*)row)[col + i];
+        } else {
+            r.v[0] = load8((const uint16_t*)row + col, d - col);
+        }
+        return r;
+    }
+    const int at = min(col, d - 8);
+    const uint8_t* const p = byte_of(row, (uint32_t)at * (uint32_t)size_of<T>());
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (std::is_same<T, F32>::value) r.v[i] = *reinterpret_cast<const uint4_a4*>(p + 16 * i);
+        else r.v[i] = *reinterpret_cast<const uint4_a2*>(p);
+    }
+    if (d & 7) {
+        const int past = min(col - at, 8);
+        if (past) {
+            if constexpr (std::is_same<T, F32>::value) {
+                if (past & 4) r.v[0] = r.v[1], r.v[1] = (uint4_t){0, 0, 0, 0};
+                if (past & 2) r.v[0] = (uint4_t){r.v[0][2], r.v[0][3], r.v[1][0], r.v[1][1]}, r.v[1] = (uint4_t){r.v[1][2], r.v[1][3], 0, 0};
+                if (past & 1) r.v[0] = (uint4_t){r.v[0][1], r.v[0][2], r.v[0][3], r.v[1][0]}, r.v[1] = (uint4_t){r.v[1][1], r.v[1][2], r.v[1][3], 0};
+            } else {
+                uint4_t x = r.v[0];
+                if (past & 4) x = (uint4_t){x[2], x[3], 0, 0};
+                if (past & 2) x = (uint4_t){x[1], x[2], x[3], 0};
+                if (past & 1) x = (uint4_t){x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16};
+                r.v[0] = x;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) r.v[i][w] = col < d ? r.v[i][w] : 0u;
+    return r;
+}
+
 // Eight elements from element `at` on, of which `valid` exist (any number); the others are zero.  Any alignment of the element's.
 template <class T>
 __device__ __forceinline__ Eight load_eight(const void* base, int64_t at, int valid) {
@@ -68,17 +142,6 @@ __device__ __forceinline__ void store_eight(void* base, int64_t at, const Eight&
     }
 }
 
-// The same where the type is known at run time only, alike for the launch: parameters.
-__device__ __forceinline__ Eight load_eight(int type, const void* base, int64_t at, int valid) {
-    if (type == RSH_F32) return load_eight<F32>(base, at, valid);
-    return type == RSH_F16 ? load_eight<F16>(base, at, valid) : load_eight<BF16>(base, at, valid);
-}
-__device__ __forceinline__ void store_eight(int type, void* base, int64_t at, const Eight& e, int valid) {
-    if (type == RSH_F32) store_eight<F32>(base, at, e, valid);
-    else if (type == RSH_F16) store_eight<F16>(base, at, e, valid);
-    else store_eight<BF16>(base, at, e, valid);
-}
-
 // Dropout's random numbers: Philox4x32 of ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3",
 // 2011).  Eight elements of a row share a block: 16 bits each, the low half of a word before its high half.  The counter is (place of
 // the eight in the row, row, both halves of the offset), the key the seed's halves: an element's bits depend on nothing else, so the
@@ -93,6 +156,7 @@ struct Random {
         keep = 65536.f / (float)(share < 65536u ? 65536u - share : 1u);
     }
     __device__ __forceinline__ uint4_t bits(uint32_t place, uint32_t row) const {
+        asm volatile("" : "+v"(place));       // its first product is not kept from row to row
         uint32_t a = place, b = row, c = c2, d = c3, x = k0, y = k1;
 #pragma unroll
         for (int i = 0; i < 10; ++i) {
@@ -106,11 +170,21 @@ struct Random {
         }
         return (uint4_t){a, b, c, d};
     }
+    // Whether element i of a block is kept.  share << 16 fits 32 bits but for its last value, so less one; share 0 is nothing to drop.
+    __device__ __forceinline__ bool keeps(const uint4_t& r, int i) const { return (i & 1 ? r[i / 2] : r[i / 2] << 16) > (share << 16) - 1u; }
+    // Bit i: element col + i is kept.
+    __device__ __forceinline__ uint32_t kept(int col, int64_t row) const {
+        const uint4_t r = bits((uint32_t)col / 8, (uint32_t)row);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m |= keeps(r, i) ? 1u << i : 0u;
+        return m;
+    }
     // What is dropped becomes zero, infinities and NaN too; what is kept is multiplied by `factor`.
     __device__ __forceinline__ void drop(Eight& e, int col, int64_t row, float factor) const {
         const uint4_t r = bits((uint32_t)col / 8, (uint32_t)row);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e.v[i] = (i & 1 ? r[i / 2] >> 16 : r[i / 2] & 0xffffu) >= share ? e.v[i] * factor : 0.f;
+        for (int i = 0; i < 8; ++i) e.v[i] = keeps(r, i) ? e.v[i] * factor : 0.f;
     }
 };
 

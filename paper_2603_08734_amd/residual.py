@@ -6,7 +6,8 @@
 
 All of a row's steps run in one kernel (``rsh_join_forward``) in fp32; S and Y are each rounded once, Y being the norm of the sum as it was
 before its rounding.  Autograd-aware (reverse mode, first derivatives) in X, B, the gate and the norms' parameters; one pass over the
-rows (``rsh_join_backward``) forms all gradients, from S, B and two numbers a row.
+rows (``rsh_join_backward``) forms all gradients, from X, B and two numbers a row and norm: S is added up again,
+since the rounded one would bring its error into them.
 """
 from __future__ import annotations
 
@@ -21,8 +22,8 @@ KINDS = {"rms": binding.RSH_NORM_RMS, "layer": binding.RSH_NORM_LAYER}
 
 
 class Norm:
-    """x r weight + bias with r = 1 / sqrt(mean of x^2 + eps) ("rms"), or the same of x - mean of x ("layer").  weight, bias: [d] of
-    fp32, binary16 or bfloat16, None for ones and zeros."""
+    """x r weight + bias with r = 1 / sqrt(mean of x^2 + eps) ("rms"), or the same of x - mean of x ("layer").  weight, bias: [d] in
+    fp32 or in the rows' type, None for ones and zeros."""
 
     __slots__ = ("kind", "weight", "bias", "eps")
 
@@ -88,7 +89,7 @@ def _forward(plan, X, B, gate, aw, ab, bw, bb, keep):
 
 def _backward(ctx, *grads):
     plan, want = ctx.plan, ctx.needs_input_grad
-    X, B, gate, aw, ab, bw, bb, S, stats, seed = ctx.saved_tensors
+    X, B, gate, aw, ab, bw, bb, stats, seed = ctx.saved_tensors
     grads = list(grads)
     dS = grads.pop(0) if B is not None else None
     dY = grads.pop(0) if plan.before else None
@@ -113,7 +114,7 @@ def _backward(ctx, *grads):
     dy, ld_dy = _rows(dY, MOST) if dY is not None else (None, 0)
     a = binding._address
     with _on(like.get_device()):
-        join, alive = _describe(plan, X, B, gate, aw, ab, bw, bb, S, None, stats, t, d, like.get_device())
+        join, alive = _describe(plan, X, B, gate, aw, ab, bw, bb, None, None, stats, t, d, like.get_device())
         gradients = binding.rsh_join_gradients_t(a(ds), a(dy), a(dX), a(dB), a(dgate), *(a(v) for v in vectors.values()), None, ld_ds, ld_dy)
         binding.join_backward(join, gradients, count, like)
     return tuple(none)
@@ -128,7 +129,7 @@ class _Join(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         S, Y, stats = _forward(plan, X, B, gate, aw, ab, bw, bb, True)
         ctx.plan = plan
-        ctx.save_for_backward(X if B is None else None, B, gate, aw, ab, bw, bb, S if plan.before else None, stats, seed)
+        ctx.save_for_backward(X if plan.before else None, B, gate, aw, ab, bw, bb, stats, seed)
         return Y if S is None else S if Y is None else (S, Y)
 
     @staticmethod
@@ -154,8 +155,8 @@ def _refuse(X, B, after, gate, drop, before):
                          f"{getattr(B, 'dtype', type(B))} {tuple(getattr(B, 'shape', ()))} on {getattr(B, 'device', None)}")
     for name, v, shapes in (("gate", gate, (X.shape, (d,))), ("after.weight", after and after.weight, ((d,),)), ("after.bias", after and after.bias, ((d,),)),
                             ("before.weight", before and before.weight, ((d,),)), ("before.bias", before and before.bias, ((d,),))):
-        if v is not None and (not isinstance(v, torch.Tensor) or v.dtype not in _TYPES or v.device != X.device or tuple(v.shape) not in map(tuple, shapes)):
-            raise ValueError(f"{name}: expected {' or '.join(str(tuple(s)) for s in shapes)} of {list(_TYPES)} on {X.device}, got "
+        if v is not None and (not isinstance(v, torch.Tensor) or v.dtype not in (X.dtype, torch.float32) or v.device != X.device or tuple(v.shape) not in map(tuple, shapes)):
+            raise ValueError(f"{name}: expected {' or '.join(str(tuple(s)) for s in shapes)} of {X.dtype} or fp32 on {X.device}, got "
                              f"{getattr(v, 'dtype', type(v))} {tuple(getattr(v, 'shape', ()))} on {getattr(v, 'device', None)}")
 
 
@@ -199,7 +200,7 @@ def norm(X, norm: Norm):
 
 def join(X, B, after: Norm | None = None, gate=None, scale: float = 1.0, drop: Drop | None = None, before: Norm | None = None):
     """S = X + scale * gate * drop(after(B)), and with ``before`` the pair (S, before(S)).  X, B [..., d] of one type; gate: [d] or of X's
-    shape; scale: a number."""
+    shape, in fp32 or X's type; scale: a number."""
     if B is None:
         raise TypeError("B: expected a tensor; the norm alone is residual.norm")
     if not abs(scale) < 2.0 ** 127:

@@ -40,7 +40,8 @@ def _join(**change):
 JOINS = [
     (b.RSH_ERR_BAD_OPTION, dict(type=b.RSH_MX4)), (b.RSH_ERR_BAD_OPTION, dict(t=0)), (b.RSH_ERR_BAD_OPTION, dict(d=-1)),
     (b.RSH_ERR_TOO_LARGE, dict(d=(1 << 21) + 1)), (b.RSH_ERR_BAD_OPTION, dict(ld_b=63)), (b.RSH_ERR_BAD_OPTION, dict(ld_b=1 << 31)),
-    (b.RSH_ERR_BAD_OPTION, dict(ld_gate=63)), (b.RSH_ERR_BAD_OPTION, dict(gate_type=b.RSH_MX4)), (b.RSH_ERR_BAD_OPTION, dict(gate=P + 1)),
+    (b.RSH_ERR_BAD_OPTION, dict(ld_gate=63)), (b.RSH_ERR_BAD_OPTION, dict(gate_type=b.RSH_MX4)), (b.RSH_ERR_BAD_OPTION, dict(gate_type=b.RSH_BF16)),
+    (b.RSH_ERR_BAD_OPTION, dict(gate=None, ld_gate=64)), (b.RSH_ERR_BAD_OPTION, dict(after=_norm(weight_type=b.RSH_BF16))), (b.RSH_ERR_BAD_OPTION, dict(gate=P + 1)),
     (b.RSH_ERR_BAD_OPTION, dict(scale=INF)), (b.RSH_ERR_BAD_OPTION, dict(scale=float("nan"))), (b.RSH_ERR_BAD_OPTION, dict(drop=_drop(1 << 17))),
     (b.RSH_ERR_BAD_OPTION, dict(after=_norm(kind=3))), (b.RSH_ERR_BAD_OPTION, dict(before=_norm(eps=0))), (b.RSH_ERR_BAD_OPTION, dict(before=_norm(eps=INF))),
     (b.RSH_ERR_BAD_OPTION, dict(after=_norm(eps=float("nan")))), (b.RSH_ERR_BAD_OPTION, dict(after=_norm(weight_type=b.RSH_MX4))),
@@ -70,7 +71,7 @@ def _gradients(**change):
 
 
 @pytest.mark.parametrize("status,join,gradients", [(s, c, {}) for s, c in JOINS] + [
-    (b.RSH_ERR_NULL, {}, dict(dS=None, dY=None)), (b.RSH_ERR_NULL, {}, dict(work=None)), (b.RSH_ERR_NULL, dict(S=None), {}),
+    (b.RSH_ERR_NULL, {}, dict(dS=None, dY=None)), (b.RSH_ERR_NULL, {}, dict(work=None)), (b.RSH_ERR_NULL, dict(X=None), {}),
     (b.RSH_ERR_NULL, dict(before=_norm(stats=None)), {}), (b.RSH_ERR_NULL, dict(after=_norm(stats=None)), {}),
     (b.RSH_ERR_NULL, {}, dict(dX=None, dB=None, dgate=None, after_weight=None, before_weight=None)),
     (b.RSH_ERR_BAD_OPTION, dict(B=None), {}), (b.RSH_ERR_BAD_OPTION, dict(gate=None), {}), (b.RSH_ERR_BAD_OPTION, {}, dict(after_bias=P)),
