@@ -95,10 +95,28 @@ def _refuse(Y, X, A, B, index, scales):
         raise ValueError(_FORWARD_MODE)
 
 
+def _fits(Y, X, A, B, index, scales) -> bool:
+    """The ordinary case of what is refused otherwise: matrices on one GPU."""
+    for v in (Y, X, A, B, index):
+        if not isinstance(v, torch.Tensor):
+            return False
+    dtype, device = X.dtype, X.get_device()
+    if X.dim() != 2 or Y.dim() != 2 or A.dim() != 3 or B.dim() != 3 or dtype not in HALVES or index.dtype not in (torch.int32, torch.int64) or device < 0:
+        return False
+    (t, k), (n, r, ka), m = X.shape, A.shape, Y.shape[1]
+    if Y.shape[0] != t or ka != k or B.shape != (n, r, m) or index.shape != (t,) or not Y.dtype == A.dtype == B.dtype == dtype:
+        return False
+    if not Y.get_device() == A.get_device() == B.get_device() == index.get_device() == device:
+        return False
+    return scales is None or (isinstance(scales, torch.Tensor) and scales.dtype == torch.float32 and scales.shape == (n,) and
+                              scales.get_device() == device and not scales.requires_grad and not _tangent(scales))
+
+
 def add(Y, X, A, B, index, scales=None):
     """Y + scales[i] (X A[i]^T) B[i] for every token, i its index: X [..., k], Y [..., m], index [...] int32 or int64, scales fp32 [n] or None for
     ones."""
-    _refuse(Y, X, A, B, index, scales)
+    if not _fits(Y, X, A, B, index, scales) or _tangent(Y, X, A, B):
+        _refuse(Y, X, A, B, index, scales)
     k, m = X.shape[-1], Y.shape[-1]
     grads = torch.is_grad_enabled() and any(v.requires_grad for v in (Y, X, A, B))
     if 0 in (Y.numel(), X.numel(), A.numel(), B.numel()):

@@ -14,7 +14,7 @@ namespace rsh {
 
 namespace {
 
-constexpr int kFewTokens = 256, kFewTile = 16, kTile = 64;
+constexpr int kFewTokens = 256, kFewTile = 16, kFewParts = 8, kTile = 64;
 constexpr int kSortThreads = 1024, kSortWords = 8 * (RSH_ADAPTERS_MAX + 1);     // counters in LDS
 
 struct Tile {
@@ -71,8 +71,6 @@ __device__ __forceinline__ int few_tile(const Index& index, int t, int mine, Few
     return own;
 }
 
-__device__ __forceinline__ float4_t mfma_f32(float a, float b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
-
 // Tokens of a tile.
 template <bool FEW>
 struct Members {
@@ -111,8 +109,35 @@ __global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index i
     if (threadIdx.x < 2) total[threadIdx.x] = 0;
     __syncthreads();
     const int64_t share = ((t + waves - 1) / waves + 63) / 64 * 64, begin = wave * share, end = min(t, begin + share);
-    if (wave < waves)
-        for (int64_t i = begin + lane; i < end; i += 64) atomicAdd(&counts[index.at(i) * waves + wave], 1);
+    int bits = 0;
+    while (n >> bits) ++bits;
+    // Lanes whose token has the same adapter as this one's; a run of tokens of one request needs no look at the bits.
+    auto peers = [&](int a, bool in) {
+        uint64_t same = __ballot(in);
+        if (same == __ballot(in && a == __builtin_amdgcn_readfirstlane(a))) return same;      // lane 0 is always in
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot(a >> b & 1);
+            same &= a >> b & 1 ? set : ~set;
+        }
+        return same;
+    };
+    // The adapters of the wave's first tokens stay in registers for the second look.
+    constexpr int kHeld = 8;
+    int held[kHeld];
+    volatile int32_t* const count = counts;
+    if (wave < waves) {
+#pragma unroll
+        for (int c = 0; c < kHeld; ++c) held[c] = begin + 64 * c + lane < end ? index.at(begin + 64 * c + lane) : 0;
+        auto add = [&](int64_t i0, int a) {
+            const bool in = i0 + lane < end;
+            const uint64_t same = peers(a, in);
+            if (in && bits_below_lane(same) == 0) count[a * waves + wave] = count[a * waves + wave] + __popcll(same);
+        };
+#pragma unroll
+        for (int c = 0; c < kHeld; ++c)
+            if (begin + 64 * c < end) add(begin + 64 * c, held[c]);
+        for (int64_t i0 = begin + 64 * kHeld; i0 < end; i0 += 64) add(i0, i0 + lane < end ? index.at(i0 + lane) : 0);
+    }
     __syncthreads();
     // Of every adapter: its tokens and tiles, added up over the adapters before it.
     for (int a0 = 0; a0 < groups; a0 += kSortThreads) {
@@ -153,24 +178,20 @@ __global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index i
         *n_tiles = all;
     }
     if (wave < waves) {
-        int bits = 0;
-        while (n >> bits) ++bits;
-        volatile int32_t* const next = counts;
-        for (int64_t i0 = begin; i0 < end; i0 += 64) {
+        auto place = [&](int64_t i0, int a) {
             const bool in = i0 + lane < end;
-            const int a = in ? index.at(i0 + lane) : 0;
-            uint64_t same = __ballot(in);
-            for (int b = 0; b < bits; ++b) {
-                const uint64_t set = __ballot(a >> b & 1);
-                same &= a >> b & 1 ? set : ~set;
-            }
+            const uint64_t same = peers(a, in);
             const int rank = (int)bits_below_lane(same);
             if (in) {
-                const int at = next[a * waves + wave];
+                const int at = count[a * waves + wave];
                 token[at + rank] = (int32_t)(i0 + lane);
-                if (rank == 0) next[a * waves + wave] = at + __popcll(same);
+                if (rank == 0) count[a * waves + wave] = at + __popcll(same);
             }
-        }
+        };
+#pragma unroll
+        for (int c = 0; c < kHeld; ++c)
+            if (begin + 64 * c < end) place(begin + 64 * c, held[c]);
+        for (int64_t i0 = begin + 64 * kHeld; i0 < end; i0 += 64) place(i0, i0 + lane < end ? index.at(i0 + lane) : 0);
     }
     // A tile's adapter: the last that begins at or before it (those without tiles share theirs with the next).
     __syncthreads();
@@ -205,25 +226,49 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const u
     for (int i = 0; i < TT; ++i) x[i] = X + (int64_t)tile.at(16 * i + c) * ld_x;
     float4_t acc[RT][TT] = {};
     const int64_t begin = (int64_t)blockIdx.z * steps, end = min((k + 63) / 64, begin + steps);
-    for (int64_t step = begin + wave; step < end; step += WAVES) {
+    struct Slab {
+        uint4_t a[RT][2], x[TT][2];
+    };
+    auto load = [&](int64_t step) {        // a whole one
+        Slab v;
         const int64_t at = 64 * step + 16 * g;
-        uint4_t av[RT][2], xv[TT][2];
-        const int64_t left = 64 * step + 64 <= k ? 16 : k - at;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i) av[i][h] = load8(a[i] + at + 8 * h, left - 8 * h);
+            for (int i = 0; i < RT; ++i) v.a[i][h] = *reinterpret_cast<const uint4_a2*>(a[i] + at + 8 * h);
 #pragma unroll
-            for (int i = 0; i < TT; ++i)
-                if (i < tiles) xv[i][h] = load8(x[i] + at + 8 * h, left - 8 * h);
+            for (int i = 0; i < TT; ++i) v.x[i][h] = *reinterpret_cast<const uint4_a2*>(x[i] + at + 8 * h);
         }
+        return v;
+    };
+    auto multiply = [&](const Slab& v) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < TT; ++j)
-                if (j < tiles)
 #pragma unroll
-                    for (int i = 0; i < RT; ++i) acc[i][j] = T::mfma16(av[i][h], xv[j][h], acc[i][j]);
+                for (int i = 0; i < RT; ++i) acc[i][j] = T::mfma16(v.a[i][h], v.x[j][h], acc[i][j]);
+    };
+    const int64_t whole = min(end, k / 64);
+    if (begin + wave < whole) {
+        Slab next = load(begin + wave);
+        for (int64_t step = begin + wave; step < whole; step += WAVES) {
+            const Slab v = next;
+            if (step + WAVES < whole) next = load(step + WAVES);
+            multiply(v);
+        }
+    }
+    if (whole < end && (whole - begin) % WAVES == wave) {      // what is left of k
+        const int64_t at = 64 * whole + 16 * g;
+        Slab v;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) v.a[i][h] = load8(a[i] + at + 8 * h, k - at - 8 * h);
+#pragma unroll
+            for (int i = 0; i < TT; ++i) v.x[i][h] = load8(x[i] + at + 8 * h, k - at - 8 * h);
+        }
+        multiply(v);
     }
     // The waves' sums, in their order.
 #pragma unroll
@@ -245,9 +290,53 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const u
     }
 }
 
-// out = Y + s H B_i of a tile's tokens and 128 columns a wave.  A lane's loads of B are eight columns of a row, one for each of eight
+// An fp32 number as two of bfloat16, hi + lo, 2^-17 of it off at most; of an infinity or a NaN lo is zero.  Sums of r or t products of one of
+// them with 16-bit numbers are formed in the matrix unit's 16-bit form with both halves side by side in k: eight times the rate of its fp32
+// form, which took 55 of the 100 us of 4096 tokens at rank 64 by 16384 columns.  Rounding H to 16 bits alone would put as much error into the
+// result as the result's own rounding.
+__device__ __forceinline__ uint4_t halves(const float* h) {
+    float hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        hi[i] = __uint_as_float((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)h[i]) << 16);
+        const float rest = h[i] - hi[i];
+        lo[i] = rest - rest == 0.f ? rest : 0.f;
+    }
+    return (uint4_t){BF16::pair(hi[0], hi[1]), BF16::pair(hi[2], hi[3]), BF16::pair(lo[0], lo[1]), BF16::pair(lo[2], lo[3])};
+}
+
+// Four rows of eight 16-bit numbers as the eight operands that have a column's four beside themselves (for hi and for lo).  bfloat16 goes as it
+// is; a number of binary16 is two of bfloat16 exactly, of which `rest` is the second.
+template <class T>
+struct Fours {
+    uint2_t main[8], rest[std::is_same<T, F16>::value ? 8 : 1];
+    __device__ __forceinline__ void from(const uint4_t* rows) {
+        auto pick = [](uint32_t a, uint32_t b, int odd) { return __builtin_amdgcn_perm(b, a, odd ? 0x07060302u : 0x05040100u); };
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            if constexpr (std::is_same<T, BF16>::value) {
+                main[q] = (uint2_t){pick(rows[0][q / 2], rows[1][q / 2], q & 1), pick(rows[2][q / 2], rows[3][q / 2], q & 1)};
+            } else {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = F16::widen((uint16_t)(rows[i][q / 2] >> (16 * (q & 1))));
+                    hi[i] = __float_as_uint(x);
+                    const float r = x - __uint_as_float(hi[i] & 0xffff0000u);
+                    lo[i] = __float_as_uint(r - r == 0.f ? r : 0.f);
+                }
+                main[q] = (uint2_t){pick(hi[0], hi[1], 1), pick(hi[2], hi[3], 1)};
+                rest[q] = (uint2_t){pick(lo[0], lo[1], 1), pick(lo[2], lo[3], 1)};
+            }
+        }
+    }
+};
+__device__ __forceinline__ uint4_t twice(uint2_t v) { return (uint4_t){v[0], v[1], v[0], v[1]}; }
+
+// out = Y + s H B_i of a tile's tokens and 128 columns a wave.  A lane's loads of B are eight columns of four rows, four for each of eight
 // results of 16 columns by 16 tokens; which eight is chosen so that lanes store pieces of a row that lie side by side.
-template <class T, int TT, bool FEW>
+// RT: rows of B in registers, in sixteens; more of them are loaded anew for every 16 tokens.
+template <class T, int RT, bool FEW>
 __global__ __launch_bounds__(256) void rsh_adapters_expand_kernel(const uint16_t* Y, int64_t ld_y, const float* H, int parts, const uint16_t* B,
                                                                   const float* scales, Index index, Order order, uint16_t* out, int64_t t, int64_t m,
                                                                   int r) {
@@ -261,51 +350,75 @@ __global__ __launch_bounds__(256) void rsh_adapters_expand_kernel(const uint16_t
     const float scale = some && scales ? scales[tile.adapter] : 1.f;
     const int64_t col = col0 + 8 * (4 * (c & 3) + (c >> 2));
     const uint16_t* const b = B + (int64_t)tile.adapter * r * m + col;
-    for (int first = 0; first < tile.count; first += 16 * TT) {
-        float4_t acc[TT][8] = {};
-        int64_t token[TT];
+    Fours<T> f[RT];
+    auto load_b = [&](int rank) {
 #pragma unroll
-        for (int i = 0; i < TT; ++i) token[i] = tile.at(first + 16 * i + c);
+        for (int i = 0; i < RT; ++i) {
+            uint4_t rows[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int row = rank + 16 * i + 4 * g + s;
+                rows[s] = load8(b + (int64_t)row * m, row < r ? m - col : 0);
+            }
+            f[i].from(rows);
+        }
+    };
+    if (some && r16 <= 16 * RT) load_b(0);
+    for (int first = 0; first < tile.count; first += 16) {
+        const int64_t token = tile.at(first + c);
+        const bool in = first + c < tile.count;
+        uint4_t y[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int64_t to = col0 + 32 * v + 8 * g;
+            y[v] = load8(Y + token * ld_y + to, Y && in ? m - to : 0);
+        }
+        float4_t acc[8] = {};
         if (some) {
-            for (int rank = 0; rank < r16; rank += 16) {
-                uint4_t bv[4];
+            for (int rank = 0; rank < r16; rank += 16 * RT) {
+                if (r16 > 16 * RT) load_b(rank);
+                float4_t h[RT];
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int row = rank + 4 * g + s;
-                    bv[s] = load8(b + (int64_t)row * m, row < r ? m - col : 0);
+                for (int i = 0; i < RT; ++i) {
+                    const int at = rank + 16 * i + 4 * g;
+                    h[i] = (float4_t){0.f, 0.f, 0.f, 0.f};
+                    if (at < r16) {
+                        const float* const p = H + token * r16 + at;
+                        if constexpr (FEW) {
+                            float4_t part[kFewParts];
+#pragma unroll
+                            for (int q = 0; q < kFewParts; ++q) part[q] = *reinterpret_cast<const float4_t*>(p + (int64_t)min(q, parts - 1) * t * r16);
+#pragma unroll
+                            for (int q = 0; q < kFewParts; ++q)
+                                if (q < parts) h[i] += part[q];
+                        } else {
+                            h[i] = *reinterpret_cast<const float4_t*>(p);
+                        }
+                    }
                 }
-                float4_t h[TT];
 #pragma unroll
-                for (int i = 0; i < TT; ++i) {
-                    const float* p = H + token[i] * r16 + rank + 4 * g;
-                    h[i] = *reinterpret_cast<const float4_t*>(p);
-                    for (int q = 1; q < parts; ++q) h[i] += *reinterpret_cast<const float4_t*>(p += t * r16);
+                for (int i = 0; i < RT; ++i) {
                     h[i] *= scale;
-                }
+                    const float hv[4] = {h[i][0], h[i][1], h[i][2], h[i][3]};
+                    const uint4_t k = halves(hv);
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const Eight e = widen8<T>(bv[s]);
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-#pragma unroll
-                        for (int i = 0; i < TT; ++i) acc[i][q] = mfma_f32(e.v[q], h[i][s], acc[i][q]);
+                    for (int q = 0; q < 8; ++q) {
+                        acc[q] = BF16::mfma16(twice(f[i].main[q]), k, acc[q]);
+                        if constexpr (std::is_same<T, F16>::value) acc[q] = BF16::mfma16(twice(f[i].rest[q]), k, acc[q]);
+                    }
                 }
             }
         }
+        if (!in) continue;
 #pragma unroll
-        for (int i = 0; i < TT; ++i) {
-            if (first + 16 * i + c >= tile.count) continue;
+        for (int v = 0; v < 4; ++v) {
+            const int64_t to = col0 + 32 * v + 8 * g;
+            Eight e = widen8<T>(y[v]);
+            if (some) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int64_t to = col0 + 32 * v + 8 * g;
-                Eight e = {};
-                if (Y) e = load_eight<T>(Y, token[i] * ld_y + to, (int)min(m - to, (int64_t)8));
-                if (some) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) e.v[q] += acc[i][q][v];
-                }
-                store_eight<T>(out, token[i] * m + to, e, (int)min(m - to, (int64_t)8));
+                for (int q = 0; q < 8; ++q) e.v[q] += acc[q][v];
             }
+            store_eight<T>(out, token * m + to, e, (int)min(m - to, (int64_t)8));
         }
     }
 }
@@ -331,17 +444,55 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
     const int begin = start + (int)min((int64_t)tokens, (int64_t)part * share), end = start + (int)min((int64_t)tokens, (int64_t)(part + 1) * share);
     const int64_t col = 128 * (int64_t)blockIdx.x + 8 * c;
     float4_t acc[RT][8] = {};
-    for (int i0 = begin + 4 * wave; i0 < end; i0 += 4 * WAVES) {
-        const bool in = i0 + g < end;
-        const int64_t token = order.token[min(i0 + g, end - 1)];
-        const Eight x = load_eight<T>(X, token * ld_x + col, in ? (int)min(k - col, (int64_t)8) : 0);
-        float h[RT];
+    // 16 tokens a turn and wave, four of them a lane's.
+    struct Slab {
+        uint4_t x[4];
+        float h[RT][4];
+    };
+    const int valid = (int)min(k - col, (int64_t)8);
+    struct Four {
+        int token[4];
+    };
+    auto find = [&](int i0) {
+        Four f;
 #pragma unroll
-        for (int i = 0; i < RT; ++i) h[i] = in && r0 + 16 * i < r16 ? H[token * r16 + r0 + 16 * i + c] : 0.f;
+        for (int i = 0; i < 4; ++i) f.token[i] = order.token[min(i0 + 4 * g + i, end - 1)];
+        return f;
+    };
+    auto load = [&](const Four& f, int i0) {
+        Slab s;
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+        for (int i = 0; i < 4; ++i) {
+            const bool in = i0 + 4 * g + i < end;
+            const int64_t token = f.token[i];
+            s.x[i] = load8(X + token * ld_x + col, in ? valid : 0);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) acc[i][q] = mfma_f32(h[i], x.v[q], acc[i][q]);
+            for (int j = 0; j < RT; ++j) s.h[j][i] = in && r0 + 16 * j < r16 ? H[token * r16 + r0 + 16 * j + c] : 0.f;
+        }
+        return s;
+    };
+    const int first = begin + 16 * wave;
+    if (first < end) {
+        Slab next = load(find(first), first);
+        Four after = find(first + 16 * WAVES);
+        for (int i0 = first; i0 < end; i0 += 16 * WAVES) {
+            const Slab s = next;
+            if (i0 + 16 * WAVES < end) {
+                next = load(after, i0 + 16 * WAVES);
+                after = find(i0 + 32 * WAVES);
+            }
+            Fours<T> f;
+            f.from(s.x);
+#pragma unroll
+            for (int j = 0; j < RT; ++j) {
+                const uint4_t h = halves(s.h[j]);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    acc[j][q] = BF16::mfma16(h, twice(f.main[q]), acc[j][q]);
+                    if constexpr (std::is_same<T, F16>::value) acc[j][q] = BF16::mfma16(h, twice(f.rest[q]), acc[j][q]);
+                }
+            }
+        }
     }
     const float scale = scales ? scales[adapter] : 1.f;
 #pragma unroll
@@ -362,7 +513,6 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
             }
             if (rank >= r || col >= k) continue;
             const int64_t at = ((int64_t)adapter * r + rank) * k + col;
-            const int valid = (int)min(k - col, (int64_t)8);
             if (parts == 1) store_eight<T>(out, at, e, valid);
             else store_eight<F32>(sums, (int64_t)part * n * r * k + at, e, valid);
         }
@@ -425,7 +575,7 @@ struct Split {
     int parts, steps;
     Split(int64_t t, int64_t k, int r, bool few) {
         const int64_t blocks = (few ? t : (t + kTile - 1) / kTile) * ((r + 63) / 64), all = (k + 63) / 64;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? 16 : 4, 512 / std::max<int64_t>(1, blocks)));
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? kFewParts : 4, 512 / std::max<int64_t>(1, blocks)));
         const int64_t each = std::max<int64_t>(kShrinkWaves, (all + want - 1) / want);
         steps = (int)each;
         parts = (int)((all + each - 1) / each);
@@ -468,12 +618,15 @@ void expand(const rsh_adapters_t& a, bool few, const void* Y, int64_t ld, const 
             int64_t m, hipStream_t st) {
     const Index index = {a.index, a.index_size == 8, a.n};
     const dim3 grid((unsigned)(few ? a.t : most_tiles(a.t, a.n)), (unsigned)((m + 511) / 512));
-    if (few)
-        hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, 1, true>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B, a.scales,
-                           index, order, (uint16_t*)out, a.t, m, a.r);
-    else
-        hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, 2, false>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B, a.scales,
-                           index, order, (uint16_t*)out, a.t, m, a.r);
+    by_rank(a.r, [&](auto rt) {
+        constexpr int RT = decltype(rt)::value;
+        if (few)
+            hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, RT, true>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B,
+                               a.scales, index, order, (uint16_t*)out, a.t, m, a.r);
+        else
+            hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, RT, false>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, 1, (const uint16_t*)B,
+                               a.scales, index, order, (uint16_t*)out, a.t, m, a.r);
+    });
 }
 
 void join(const float* from, float* to, int64_t t, int r, int parts, hipStream_t st) {

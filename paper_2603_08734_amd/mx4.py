@@ -54,6 +54,8 @@ def _rows(X, most: int = binding.RSH_FFN_MAX_WIDTH):
 
 def _tangent(*tensors) -> bool:
     """Whether one of them carries a tangent (forward-mode derivatives, which torch.no_grad() does not stop)."""
+    if forward_ad._current_level < 0:      # no such derivative is being formed anywhere
+        return False
     for t in tensors:
         if forward_ad.unpack_dual(t).tangent is not None:
             return True

@@ -18,6 +18,7 @@ from . import binding
 from .dropout import _FORWARD_MODE, MOST, Drop, _struct
 from .mx4 import _TYPES, _on, _rows, _tangent
 
+_DROPS = (type(None), Drop)
 KINDS = {"rms": binding.RSH_NORM_RMS, "layer": binding.RSH_NORM_LAYER}
 
 
@@ -33,6 +34,9 @@ class Norm:
         if not 2.0 ** -126 <= eps < float("inf"):
             raise ValueError(f"eps: expected a positive normal number of fp32, got {eps}")
         self.kind, self.weight, self.bias, self.eps = kind, weight, bias, eps
+
+
+_NORMS = (type(None), Norm)
 
 
 def _vector(v):
@@ -160,13 +164,31 @@ def _refuse(X, B, after, gate, drop, before):
                              f"{getattr(v, 'dtype', type(v))} {tuple(getattr(v, 'shape', ()))} on {getattr(v, 'device', None)}")
 
 
+def _fits(X, B, gate, params) -> bool:
+    """The ordinary case of what is refused otherwise: matrices, vectors as parameters."""
+    if X.dim() != 2 or not X.is_cuda or X.dtype not in _TYPES:
+        return False
+    dtype, shape, device = X.dtype, X.shape, X.get_device()
+    if B is not None and (type(B) is not torch.Tensor or B.dtype != dtype or B.shape != shape or B.get_device() != device):
+        return False
+    d = shape[1:]
+    for v in params:
+        if v is not None and (v.dtype not in (dtype, torch.float32) or v.shape != d or v.get_device() != device):
+            return False
+    return gate is None or (gate.dtype in (dtype, torch.float32) and (gate.shape == d or gate.shape == shape) and gate.get_device() == device)
+
+
 def _run(X, B, after, gate, scale, drop, before):
     """S, Y or both, in X's shape."""
-    _refuse(X, B, after, gate, drop, before)
-    aw, ab = (after.weight, after.bias) if after else (None, None)
-    bw, bb = (before.weight, before.bias) if before else (None, None)
+    if not (type(X) is torch.Tensor and type(after) in _NORMS and type(before) in _NORMS and type(drop) in _DROPS):
+        _refuse(X, B, after, gate, drop, before)
+    aw, ab = (after.weight, after.bias) if after is not None else (None, None)
+    bw, bb = (before.weight, before.bias) if before is not None else (None, None)
+    params = (aw, ab, bw, bb)
+    tensors = [v for v in (X, B, gate, *params) if v is not None]
+    if not (all(isinstance(v, torch.Tensor) for v in tensors) and _fits(X, B, gate, params)):
+        _refuse(X, B, after, gate, drop, before)
     d = X.shape[-1]
-    tensors = [v for v in (X, B, gate, aw, ab, bw, bb) if v is not None]
     if _tangent(*tensors):
         raise ValueError(_FORWARD_MODE)
     if X.numel() == 0:
@@ -178,7 +200,7 @@ def _run(X, B, after, gate, scale, drop, before):
     rows = [v if v is None or flat else v.reshape(-1, d) for v in (X, B)]
     if gate is not None:
         gate = gate.contiguous() if gate.dim() == 1 else gate if flat else gate.reshape(-1, d)
-    params = [v if v is None else v.contiguous() for v in (aw, ab, bw, bb)]
+    params = [v if v is None or v.is_contiguous() else v.contiguous() for v in params]
     plan = _Plan(after, before, scale, drop)
     if torch.is_grad_enabled() and any(v.requires_grad for v in tensors):
         out = _Join.apply(plan, *rows, gate, *params, drop.tensor if drop else None)

@@ -2,9 +2,10 @@
 
 Bounds.  E = 2^-24 is half a step of fp32, u half a step of the result's type.  H = X A^T: products of 16-bit numbers are exact in fp32, and a
 sum of k of them is at most k / 8 + 40 additions one after the other (eight waves of a workgroup, then the waves, then the parts):
-e(H) <= E (k / 8 + 40) |X| |A|^T.  The second product has r terms: e <= E (r + 8) s |H| |B| + s e(H) |B|, Y is added (E of the sum), and the
-result rounded once: + u |value|.  A factor's gradient is a sum over the tokens of an adapter, t at most, one after the other:
-e <= s e(dH)^T |X| + E (t + 64) s |dH|^T |X|.  Results in binary16 may be subnormal: + 2^-25.
+e(H) <= E (k / 8 + 40) |X| |A|^T.  The second product takes H as two numbers of bfloat16, P = 2^-17 of it off, and numbers of binary16 as two
+exact ones: at most 4 r terms, e <= (P + E (4 r + 40)) s |H| |B| + s e(H) |B|, Y is added (E of the sum), and the result rounded once: + u |value|.
+A factor's gradient is a sum over the tokens of an adapter in the same form, at most 4 t terms one after the other:
+e <= s e(dH)^T |X| + (P + E (4 t + 64)) s |dH|^T |X|.  Results in binary16 may be subnormal: + 2^-25.
 """
 import pytest
 import torch
@@ -13,7 +14,7 @@ from oracle import edges
 
 pytestmark = pytest.mark.gpu
 
-E = 2.0 ** -24
+E, P = 2.0 ** -24, 2.0 ** -17
 TYPES = {"fp16": torch.float16, "bf16": torch.bfloat16}
 
 
@@ -54,11 +55,11 @@ def reference(c, device):
         h, dh = xi @ a[i].t(), gi @ b[i].t()
         eh, edh = E * (k / 8 + 40) * (xi.abs() @ a[i].abs().t()), E * (m / 8 + 40) * (gi.abs() @ b[i].abs().t())
         out[rows] += s * (h @ b[i])
-        eout[rows] += S * (eh @ b[i].abs()) + E * (r + 8) * S * (h.abs() @ b[i].abs()) + 2 * E * out[rows].abs()
+        eout[rows] += S * (eh @ b[i].abs()) + (P + E * (4 * r + 40)) * S * (h.abs() @ b[i].abs()) + 2 * E * out[rows].abs()
         dx[rows] = s * (dh @ a[i])
-        edx[rows] = S * (edh @ a[i].abs()) + E * (r + 8) * S * (dh.abs() @ a[i].abs())
+        edx[rows] = S * (edh @ a[i].abs()) + (P + E * (4 * r + 40)) * S * (dh.abs() @ a[i].abs())
         da[i], db[i] = s * (dh.t() @ xi), s * (h.t() @ gi)
-        chain = E * (len(rows) + 64)
+        chain = P + E * (4 * len(rows) + 64)
         eda[i] = S * (edh.t() @ xi.abs()) + chain * S * (dh.abs().t() @ xi.abs())
         edb[i] = S * (eh.t() @ gi.abs()) + chain * S * (h.abs().t() @ gi.abs())
     return [(out, eout), (dout, torch.zeros_like(dout)), (dx, edx), (da, eda), (db, edb)]
@@ -219,6 +220,23 @@ def test_large_and_infinite_values_stay_with_their_tokens():
         small = torch.full_like(c["b"], 2.0 ** -16)
         got = adapters.add(torch.zeros_like(c["y"]), torch.full_like(c["x"], 1024.0), big, small, c["index"])
         assert torch.equal(got, torch.full_like(got, 16 * 64 * 16 * 1024 * 2.0 ** -16))
+
+
+def test_subnormal_numbers():
+    """Products of numbers of binary16 below its normal range: exact in fp32, H = 64 2^-24 2^-2 and so on."""
+    from paper_2603_08734_amd import adapters
+    for t in (20, 300):
+        x, a, b = torch.full((t, 64), 2.0 ** -24), torch.full((1, 4, 64), 0.25), torch.full((1, 4, 48), 2.0 ** -20 * 3)
+        x, a, b = (v.half().cuda().requires_grad_() for v in (x, a, b))
+        y = torch.zeros(t, 48, device="cuda").half()
+        i = torch.zeros(t, dtype=torch.int32, device="cuda")
+        scales = torch.tensor([2.0 ** 24], device="cuda")
+        out = adapters.add(y, x, a, b, i, scales)
+        assert torch.equal(out, torch.full_like(out, 4 * 64 * 2.0 ** -24 * 0.25 * 3 * 2.0 ** -20 * 2 ** 24))
+        dx, da, db = torch.autograd.grad(out, (x, a, b), torch.full_like(out, 2.0 ** -10))
+        assert torch.equal(dx, torch.full_like(dx, 4 * 48 * 3 * 2.0 ** -20 * 2.0 ** -10 * 0.25 * 2 ** 24))
+        assert torch.equal(da, torch.full_like(da, t * 48 * 3 * 2.0 ** -20 * 2.0 ** -10 * 2.0 ** -24 * 2 ** 24))
+        assert torch.equal(db, torch.full_like(db, t * 64 * 2.0 ** -24 * 0.25 * 2.0 ** -10 * 2 ** 24))
 
 
 def test_captured_and_replayed():
