@@ -15,7 +15,7 @@ namespace rsh {
 namespace {
 
 constexpr int kFewTokens = 256, kFewTile = 16, kFewParts = 8, kTile = 64;
-constexpr int kSortThreads = 1024, kSortWords = 8 * (RSH_ADAPTERS_MAX + 1);     // counters in LDS
+constexpr int kSortThreads = 1024, kSortWords = 7 * (RSH_ADAPTERS_MAX + 1);     // counters in LDS
 
 struct Tile {
     int adapter, first, count, pad;        // adapter: -1 for none; first: in the order
@@ -101,7 +101,7 @@ __device__ __forceinline__ bool members(const Index& index, const Order& order, 
 __global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index index, int64_t t, int waves, int tile, int32_t* token, int32_t* starts,
                                                                          Tile* tiles, int32_t* n_tiles) {
     __shared__ int32_t counts[kSortWords];     // [adapter][wave]
-    __shared__ int32_t tile_start[RSH_ADAPTERS_MAX + 2];
+    __shared__ int32_t tile_start[RSH_ADAPTERS_MAX + 2], token_start[RSH_ADAPTERS_MAX + 2];
     __shared__ int32_t sums[2][kSortThreads / 64];
     __shared__ int32_t total[2];
     const int n = index.n, groups = n + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index i
         int start = total[0] + before[0] - own[0], first = total[1] + before[1] - own[1];
         for (int w = 0; w < wave; ++w) start += sums[0][w], first += sums[1][w];
         if (a < groups) {
-            starts[a] = start;
+            starts[a] = token_start[a] = start;
             tile_start[a] = first;
             for (int w = 0; w < waves; ++w) {
                 const int x = counts[a * waves + w];
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index i
     }
     const int all = total[1];
     if (threadIdx.x == 0) {
-        starts[groups] = (int32_t)t;
+        starts[groups] = token_start[groups] = (int32_t)t;
         *n_tiles = all;
     }
     if (wave < waves) {
@@ -202,9 +202,8 @@ __global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index i
             if (tile_start[mid] <= b) lo = mid;
             else hi = mid - 1;
         }
-        // where it begins: what the adapter's first wave wrote is its end by now, so from the array
-        const int start = starts[lo] + (b - tile_start[lo]) * tile, stop = lo + 1 < groups ? starts[lo + 1] : (int)t;
-        tiles[b] = {lo, start, min(tile, stop - start), 0};
+        const int start = token_start[lo] + (b - tile_start[lo]) * tile;
+        tiles[b] = {lo, start, min(tile, token_start[lo + 1] - start), 0};
     }
 }
 
@@ -290,11 +289,14 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const u
     }
 }
 
-// An fp32 number as two of bfloat16, hi + lo, 2^-17 of it off at most; of an infinity or a NaN lo is zero.  Sums of r or t products of one of
-// them with 16-bit numbers are formed in the matrix unit's 16-bit form with both halves side by side in k: eight times the rate of its fp32
-// form, which took 55 of the 100 us of 4096 tokens at rank 64 by 16384 columns.  Rounding H to 16 bits alone would put as much error into the
-// result as the result's own rounding.
-__device__ __forceinline__ uint4_t halves(const float* h) {
+// Four fp32 numbers as two of bfloat16 each, hi + lo, 2^-17 of them off at most; of an infinity or a NaN lo is zero.  Sums of r or t products of
+// one of them with 16-bit numbers are formed by the matrix unit's 16-bit instructions, one for hi and one for lo: four times the rate of its
+// fp32 form, which took 55 of the 100 us of 4096 tokens at rank 64 by 16384 columns.  Rounding H to 16 bits alone would put as much error into
+// the result as the result's own rounding.
+struct Halves {
+    uint2_t hi, lo;
+};
+__device__ __forceinline__ Halves halves(const float* h) {
     float hi[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -302,11 +304,15 @@ __device__ __forceinline__ uint4_t halves(const float* h) {
         const float rest = h[i] - hi[i];
         lo[i] = rest - rest == 0.f ? rest : 0.f;
     }
-    return (uint4_t){BF16::pair(hi[0], hi[1]), BF16::pair(hi[2], hi[3]), BF16::pair(lo[0], lo[1]), BF16::pair(lo[2], lo[3])};
+    return {{BF16::pair(hi[0], hi[1]), BF16::pair(hi[2], hi[3])}, {BF16::pair(lo[0], lo[1]), BF16::pair(lo[2], lo[3])}};
+}
+// 16 by 16 results, 16 terms: lane l has terms 4 (l / 16) .. + 3 of row l % 16 of either operand.
+__device__ __forceinline__ float4_t multiply(uint2_t a, uint2_t b, float4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
 }
 
-// Four rows of eight 16-bit numbers as the eight operands that have a column's four beside themselves (for hi and for lo).  bfloat16 goes as it
-// is; a number of binary16 is two of bfloat16 exactly, of which `rest` is the second.
+// Four rows of eight 16-bit numbers as eight operands of a column's four.  bfloat16 goes as it is; a number of binary16 is two of bfloat16
+// exactly, of which `rest` is the second.
 template <class T>
 struct Fours {
     uint2_t main[8], rest[std::is_same<T, F16>::value ? 8 : 1];
@@ -331,15 +337,15 @@ struct Fours {
         }
     }
 };
-__device__ __forceinline__ uint4_t twice(uint2_t v) { return (uint4_t){v[0], v[1], v[0], v[1]}; }
-
 // out = Y + s H B_i of a tile's tokens and 128 columns a wave.  A lane's loads of B are eight columns of four rows, four for each of eight
-// results of 16 columns by 16 tokens; which eight is chosen so that lanes store pieces of a row that lie side by side.
-// RT: rows of B in registers, in sixteens; more of them are loaded anew for every 16 tokens.
-template <class T, int RT, bool FEW>
-__global__ __launch_bounds__(256) void rsh_adapters_expand_kernel(const uint16_t* Y, int64_t ld_y, const float* H, int parts, const uint16_t* B,
-                                                                  const float* scales, Index index, Order order, uint16_t* out, int64_t t, int64_t m,
-                                                                  int r) {
+// results of 16 columns by 16 tokens; which eight is chosen so that lanes store pieces of a row that lie side by side.  The sums of all tokens
+// of a tile stay in registers while B goes by once, 16 rows at a time and the next 16 on their way.
+template <class T, bool FEW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void rsh_adapters_expand_kernel(const uint16_t* Y, int64_t ld_y, const float* H,
+                                                                                                         int parts, const uint16_t* B, const float* scales,
+                                                                                                         Index index, Order order, uint16_t* out, int64_t t,
+                                                                                                         int64_t m, int r) {
+    constexpr int kGroups = (FEW ? kFewTile : kTile) / 16;
     __shared__ int place[FEW ? sizeof(FewPlace) / sizeof(int) : 1];
     Members<FEW> tile;
     if (!members<FEW>(index, order, t, place, &tile)) return;
@@ -347,78 +353,101 @@ __global__ __launch_bounds__(256) void rsh_adapters_expand_kernel(const uint16_t
     const int64_t col0 = 512 * (int64_t)blockIdx.y + 128 * wave;
     if (col0 >= m) return;
     const bool some = tile.adapter < index.n;
-    const float scale = some && scales ? scales[tile.adapter] : 1.f;
     const int64_t col = col0 + 8 * (4 * (c & 3) + (c >> 2));
-    const uint16_t* const b = B + (int64_t)tile.adapter * r * m + col;
-    Fours<T> f[RT];
-    auto load_b = [&](int rank) {
+    // Whole pieces of eight columns where m has them: a load under a condition of its own would have to arrive before the next goes out.
+    const bool whole = col0 + 128 <= m;
+    int64_t token[kGroups];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
+    for (int i = 0; i < kGroups; ++i) token[i] = tile.at(16 * i + c);
+    float4_t acc[kGroups][8] = {};
+    if (some) {
+        const float scale = scales ? scales[tile.adapter] : 1.f;
+        const uint16_t* const b = B + (int64_t)tile.adapter * r * m + col;
+        struct Slab {
             uint4_t rows[4];
+            float4_t h[kGroups];
+        };
+        auto load = [&](int rank) {
+            Slab v;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const int row = rank + 16 * i + 4 * g + s;
-                rows[s] = load8(b + (int64_t)row * m, row < r ? m - col : 0);
+                const int row = rank + 4 * g + s;
+                if (whole) v.rows[s] = *reinterpret_cast<const uint4_a2*>(b + (int64_t)min(row, r - 1) * m);
+                else v.rows[s] = load8(b + (int64_t)min(row, r - 1) * m, m - col);
             }
-            f[i].from(rows);
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                const float* const p = H + token[i] * r16 + rank + 4 * g;
+                if constexpr (FEW) {
+                    float4_t part[kFewParts];
+#pragma unroll
+                    for (int q = 0; q < kFewParts; ++q) part[q] = *reinterpret_cast<const float4_t*>(p + (int64_t)min(q, parts - 1) * t * r16);
+                    v.h[i] = part[0];
+#pragma unroll
+                    for (int q = 1; q < kFewParts; ++q)
+                        if (q < parts) v.h[i] += part[q];
+                } else {
+                    v.h[i] = *reinterpret_cast<const float4_t*>(p);
+                }
+            }
+            return v;
+        };
+        Slab next = load(0);
+        for (int rank = 0; rank < r16; rank += 16) {
+            Slab v = next;
+            if (rank + 16 < r16) next = load(rank + 16);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v.rows[s][w] = rank + 4 * g + s < r ? v.rows[s][w] : 0u;
+            Fours<T> f;
+            f.from(v.rows);
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                if (16 * i >= tile.count) break;
+                const float hv[4] = {v.h[i][0] * scale, v.h[i][1] * scale, v.h[i][2] * scale, v.h[i][3] * scale};
+                const Halves k = halves(hv);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    acc[i][q] = multiply(f.main[q], k.hi, acc[i][q]);
+                    acc[i][q] = multiply(f.main[q], k.lo, acc[i][q]);
+                    if constexpr (std::is_same<T, F16>::value) {
+                        acc[i][q] = multiply(f.rest[q], k.hi, acc[i][q]);
+                        acc[i][q] = multiply(f.rest[q], k.lo, acc[i][q]);
+                    }
+                }
+            }
         }
-    };
-    if (some && r16 <= 16 * RT) load_b(0);
-    for (int first = 0; first < tile.count; first += 16) {
-        const int64_t token = tile.at(first + c);
-        const bool in = first + c < tile.count;
+    }
+    struct Four {
         uint4_t y[4];
+    };
+    auto read = [&](int64_t row) {
+        Four v;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int64_t to = col0 + 32 * v + 8 * g;
-            y[v] = load8(Y + token * ld_y + to, Y && in ? m - to : 0);
+        for (int u = 0; u < 4; ++u) {
+            const int64_t to = col0 + 32 * u + 8 * g;
+            if (Y && whole) v.y[u] = *reinterpret_cast<const uint4_a2*>(Y + row * ld_y + to);
+            else v.y[u] = load8(Y + row * ld_y + to, Y ? m - to : 0);
         }
-        float4_t acc[8] = {};
-        if (some) {
-            for (int rank = 0; rank < r16; rank += 16 * RT) {
-                if (r16 > 16 * RT) load_b(rank);
-                float4_t h[RT];
+        return v;
+    };
+    Four next = read(token[0]);
 #pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    const int at = rank + 16 * i + 4 * g;
-                    h[i] = (float4_t){0.f, 0.f, 0.f, 0.f};
-                    if (at < r16) {
-                        const float* const p = H + token * r16 + at;
-                        if constexpr (FEW) {
-                            float4_t part[kFewParts];
+    for (int i = 0; i < kGroups; ++i) {
+        if (16 * i >= tile.count) break;
+        const Four v = next;
+        if (i + 1 < kGroups && 16 * (i + 1) < tile.count) next = read(token[i + 1 < kGroups ? i + 1 : i]);
+        if (16 * i + c >= tile.count) continue;
 #pragma unroll
-                            for (int q = 0; q < kFewParts; ++q) part[q] = *reinterpret_cast<const float4_t*>(p + (int64_t)min(q, parts - 1) * t * r16);
-#pragma unroll
-                            for (int q = 0; q < kFewParts; ++q)
-                                if (q < parts) h[i] += part[q];
-                        } else {
-                            h[i] = *reinterpret_cast<const float4_t*>(p);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    h[i] *= scale;
-                    const float hv[4] = {h[i][0], h[i][1], h[i][2], h[i][3]};
-                    const uint4_t k = halves(hv);
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        acc[q] = BF16::mfma16(twice(f[i].main[q]), k, acc[q]);
-                        if constexpr (std::is_same<T, F16>::value) acc[q] = BF16::mfma16(twice(f[i].rest[q]), k, acc[q]);
-                    }
-                }
-            }
-        }
-        if (!in) continue;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int64_t to = col0 + 32 * v + 8 * g;
-            Eight e = widen8<T>(y[v]);
+        for (int u = 0; u < 4; ++u) {
+            const int64_t to = col0 + 32 * u + 8 * g;
+            Eight e = widen8<T>(v.y[u]);
             if (some) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) e.v[q] += acc[q][v];
+                for (int q = 0; q < 8; ++q) e.v[q] += acc[i][q][u];
             }
-            store_eight<T>(out, token * m + to, e, (int)min(m - to, (int64_t)8));
+            store_eight<T>(out, token[i] * m + to, e, (int)min(m - to, (int64_t)8));
         }
     }
 }
@@ -485,11 +514,15 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
             f.from(s.x);
 #pragma unroll
             for (int j = 0; j < RT; ++j) {
-                const uint4_t h = halves(s.h[j]);
+                const Halves h = halves(s.h[j]);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    acc[j][q] = BF16::mfma16(h, twice(f.main[q]), acc[j][q]);
-                    if constexpr (std::is_same<T, F16>::value) acc[j][q] = BF16::mfma16(h, twice(f.rest[q]), acc[j][q]);
+                    acc[j][q] = multiply(h.hi, f.main[q], acc[j][q]);
+                    acc[j][q] = multiply(h.lo, f.main[q], acc[j][q]);
+                    if constexpr (std::is_same<T, F16>::value) {
+                        acc[j][q] = multiply(h.hi, f.rest[q], acc[j][q]);
+                        acc[j][q] = multiply(h.lo, f.rest[q], acc[j][q]);
+                    }
                 }
             }
         }
@@ -575,8 +608,8 @@ struct Split {
     int parts, steps;
     Split(int64_t t, int64_t k, int r, bool few) {
         const int64_t blocks = (few ? t : (t + kTile - 1) / kTile) * ((r + 63) / 64), all = (k + 63) / 64;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? kFewParts : 4, 512 / std::max<int64_t>(1, blocks)));
-        const int64_t each = std::max<int64_t>(kShrinkWaves, (all + want - 1) / want);
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? kFewParts : 16, (few ? 512 : 1024) / std::max<int64_t>(1, blocks)));
+        const int64_t each = std::max<int64_t>(1, (all + want * kShrinkWaves - 1) / (want * kShrinkWaves)) * kShrinkWaves;
         steps = (int)each;
         parts = (int)((all + each - 1) / each);
     }
@@ -590,8 +623,7 @@ int outer_parts(int64_t t, int64_t k, int n, int r) {
 
 void sort(const rsh_adapters_t& a, void* work, hipStream_t st) {
     const Sorted s(a.t, a.n);
-    int waves = kSortThreads / 64;
-    while (waves * (a.n + 1) > kSortWords) waves /= 2;
+    const int waves = std::min(kSortThreads / 64, kSortWords / (a.n + 1));
     char* const w = (char*)work;
     hipLaunchKernelGGL(rsh_adapters_sort_kernel, dim3(1), dim3(kSortThreads), 0, st, Index{a.index, a.index_size == 8, a.n}, a.t, waves, kTile,
                        (int32_t*)(w + s.token), (int32_t*)(w + s.starts), (Tile*)(w + s.tiles), (int32_t*)(w + s.n_tiles));
@@ -618,15 +650,12 @@ void expand(const rsh_adapters_t& a, bool few, const void* Y, int64_t ld, const 
             int64_t m, hipStream_t st) {
     const Index index = {a.index, a.index_size == 8, a.n};
     const dim3 grid((unsigned)(few ? a.t : most_tiles(a.t, a.n)), (unsigned)((m + 511) / 512));
-    by_rank(a.r, [&](auto rt) {
-        constexpr int RT = decltype(rt)::value;
-        if (few)
-            hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, RT, true>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B,
-                               a.scales, index, order, (uint16_t*)out, a.t, m, a.r);
-        else
-            hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, RT, false>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, 1, (const uint16_t*)B,
-                               a.scales, index, order, (uint16_t*)out, a.t, m, a.r);
-    });
+    if (few)
+        hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, true>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B, a.scales,
+                           index, order, (uint16_t*)out, a.t, m, a.r);
+    else
+        hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, false>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, 1, (const uint16_t*)B, a.scales, index,
+                           order, (uint16_t*)out, a.t, m, a.r);
 }
 
 void join(const float* from, float* to, int64_t t, int r, int parts, hipStream_t st) {
