@@ -394,10 +394,11 @@ int rsh_join_backward(const rsh_join_t *join, const rsh_join_gradients_t *gradie
  * and out = Y for a token whose index is not one of 0 .. n - 1.  X [t][k], Y and out [t][m] of `type` (RSH_F16 or RSH_BF16), rows ld_x
  * and ld_y apart, out without gaps (it may be Y where that is); A [n][r][k] and B [n][r][m] without gaps, of the same type; index int32 or int64 (index_size
  * 4 or 8); scales fp32 [n], NULL for ones.  No alignment beyond the element's.  Y NULL: zeros.
- *   rsh_adapters_forward   H not NULL: kept for the gradients, fp32 [t][r rounded up to a multiple of 16], 16-byte aligned
- *   rsh_adapters_backward  for dout (rows ld_dout apart): dX [t][k], dA and dB of A's and B's shapes, each NULL where not wanted; H as kept
- *                          (NULL only where dB is).  The gradient of Y is dout.
- * Sums are fp32 and so is H between the two products; each result is rounded once.  work: 16-byte aligned, of the bytes that the *_work function
+ *   rsh_adapters_forward   kept not NULL: what the gradients need of H and of the tokens' order, 16-byte aligned, rsh_adapters_kept bytes
+ *   rsh_adapters_backward  for dout (rows ld_dout apart): dX [t][k], dA and dB of A's and B's shapes, each NULL where not wanted, from what
+ *                          was kept for these tokens and indexes.  The gradient of Y is dout.
+ * Sums are fp32.  Between the products H is held in fp32 and multiplied to 2^-17 of itself; each result is rounded once.  An infinite
+ * element of B, or of dout or X in a factor's gradient, may make NaN of what would be infinite.  work: 16-byte aligned, of the bytes that the *_work function
  * of the same sizes reports, rewritten by every call.  Results never depend on the order in which waves run.
  * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE for widths
  * above RSH_FFN_MAX_WIDTH, more than RSH_ADAPTERS_MAX adapters or a rank above RSH_ADAPTERS_MAX_RANK.
@@ -407,11 +408,11 @@ int rsh_join_backward(const rsh_join_t *join, const rsh_join_gradients_t *gradie
 typedef struct {
     const void *X, *Y, *A, *B, *index;
     const float *scales;
-    void *out;
-    float *H;
+    void *out, *kept;
     int64_t t, k, m, ld_x, ld_y;
     int32_t n, r, type, index_size;
 } rsh_adapters_t;
+int rsh_adapters_kept(int64_t t, int32_t n, int32_t r, int64_t *bytes);
 int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t *bytes);
 int rsh_adapters_forward(const rsh_adapters_t *adapters, void *work_dev, void *hip_stream);
 int rsh_adapters_backward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t *bytes);

@@ -20,9 +20,9 @@ from .mx4 import HALVES, _on, _rows, _tangent
 _FORWARD_MODE = "adapters have no forward-mode derivative: call them on detached operands"
 
 
-def _struct(X, ld_x, Y, ld_y, A, B, index, scales, out, H, t, k, m):
+def _struct(X, ld_x, Y, ld_y, A, B, index, scales, out, kept, t, k, m):
     a = binding._address
-    return binding.rsh_adapters_t(a(X), a(Y), A.data_ptr(), B.data_ptr(), index.data_ptr(), a(scales), a(out), a(H), t, k, m, ld_x, ld_y, A.shape[0],
+    return binding.rsh_adapters_t(a(X), a(Y), A.data_ptr(), B.data_ptr(), index.data_ptr(), a(scales), a(out), a(kept), t, k, m, ld_x, ld_y, A.shape[0],
                                   A.shape[1], HALVES[A.dtype], index.element_size())
 
 
@@ -31,16 +31,16 @@ def _forward(Y, X, A, B, index, scales, keep):
     x, ld_x = _rows(X, MOST)
     y, ld_y = _rows(Y, MOST)
     out = Y.new_empty((t, m))
-    H = X.new_empty((t, (A.shape[1] + 15) // 16 * 16), dtype=torch.float32) if keep else None
+    kept = binding.adapters_kept(X, t, A.shape[0], A.shape[1]) if keep else None
     with _on(x.get_device()):
-        binding.adapters_forward(_struct(x, ld_x, y, ld_y, A, B, index, scales, out, H, t, k, m), x)
-    return out, H
+        binding.adapters_forward(_struct(x, ld_x, y, ld_y, A, B, index, scales, out, kept, t, k, m), x)
+    return out, kept
 
 
 def _backward(ctx, dout):
     if _tangent(dout):
         raise ValueError(_FORWARD_MODE)
-    X, A, B, index, scales, H = ctx.saved_tensors
+    X, A, B, index, scales, kept = ctx.saved_tensors
     t, m, k = dout.shape[0], B.shape[2], A.shape[2]
     want_y, want_x, want_a, want_b = ctx.needs_input_grad[:4]
     dX = dout.new_empty((t, k)) if want_x else None
@@ -50,7 +50,7 @@ def _backward(ctx, dout):
         g, ld_g = _rows(dout, MOST)
         x, ld_x = _rows(X, MOST) if want_a else (None, 0)
         with _on(g.get_device()):
-            binding.adapters_backward(_struct(x, ld_x, None, 0, A, B, index, scales, None, H, t, k, m), g, ld_g, dX, dA, dB)
+            binding.adapters_backward(_struct(x, ld_x, None, 0, A, B, index, scales, None, kept, t, k, m), g, ld_g, dX, dA, dB)
     return dout if want_y else None, dX, dA, dB, None, None
 
 
@@ -60,9 +60,8 @@ _backward_once = once_differentiable(_backward)
 class _Adapt(torch.autograd.Function):
     @staticmethod
     def forward(ctx, Y, X, A, B, index, scales):
-        keep = ctx.needs_input_grad[3]
-        out, H = _forward(Y, X, A, B, index, scales, keep)
-        ctx.save_for_backward(X if ctx.needs_input_grad[2] else None, A, B, index, scales, H)
+        out, kept = _forward(Y, X, A, B, index, scales, any(ctx.needs_input_grad[1:4]))
+        ctx.save_for_backward(X if ctx.needs_input_grad[2] else None, A, B, index, scales, kept)
         return out
 
     @staticmethod

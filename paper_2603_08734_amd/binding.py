@@ -46,7 +46,7 @@ EXPORTED_SYMBOLS = [
     "rsh_dense_forward", "rsh_dense_backward", "rsh_act_backward", "rsh_mx4_quantize", "rsh_mx4_dequantize",
     "rsh_mx4_product_work", "rsh_mx4_product", "rsh_gated_forward_work", "rsh_gated_forward", "rsh_gated_backward_work", "rsh_gated_backward",
     "rsh_ffn_tiles",
-    "rsh_dropout", "rsh_join_forward", "rsh_join_backward_work", "rsh_join_backward", "rsh_adapters_forward_work", "rsh_adapters_forward",
+    "rsh_dropout", "rsh_join_forward", "rsh_join_backward_work", "rsh_join_backward", "rsh_adapters_kept", "rsh_adapters_forward_work", "rsh_adapters_forward",
     "rsh_adapters_backward_work", "rsh_adapters_backward",
     "rsh_copy_probe", "rsh_plan_destroy", "rsh_plan_stats",
     "rsh_plan_decode", "rsh_plan_row_order", "rsh_reorder_knn", "rsh_plan_array", "rsh_plan_teams_per_wave",
@@ -96,7 +96,7 @@ class rsh_join_gradients_t(ctypes.Structure):
 
 
 class rsh_adapters_t(ctypes.Structure):
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("X", "Y", "A", "B", "index", "scales", "out", "H")] +
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("X", "Y", "A", "B", "index", "scales", "out", "kept")] +
                 [(n, ctypes.c_int64) for n in ("t", "k", "m", "ld_x", "ld_y")] + [(n, ctypes.c_int32) for n in ("n", "r", "type", "index_size")])
 
 
@@ -172,6 +172,7 @@ def lib() -> ctypes.CDLL:
         L.rsh_join_forward.argtypes = [ctypes.POINTER(rsh_join_t), vp]
         L.rsh_join_backward_work.argtypes = [i64, i64, i32, i64p]
         L.rsh_join_backward.argtypes = [ctypes.POINTER(rsh_join_t), ctypes.POINTER(rsh_join_gradients_t), vp]
+        L.rsh_adapters_kept.argtypes = [i64, i32, i32, i64p]
         for f in (L.rsh_adapters_forward_work, L.rsh_adapters_backward_work):
             f.argtypes = [i64, i64, i64, i32, i32, i64p]
         L.rsh_adapters_forward.argtypes = [ctypes.POINTER(rsh_adapters_t), vp, vp]
@@ -371,6 +372,11 @@ def join_backward(join: rsh_join_t, gradients: rsh_join_gradients_t, vectors: in
     work = like.new_empty(bytes_ // like.element_size()) if bytes_ else None
     gradients.work = _address(work)
     _check(lib().rsh_join_backward(ctypes.byref(join), ctypes.byref(gradients), current_stream()))
+
+
+def adapters_kept(like, t: int, n: int, r: int):
+    """Memory beside the 16-bit tensor `like` for what a forward pass leaves for the gradients (rsh_adapters_kept)."""
+    return like.new_empty(_work_bytes("rsh_adapters_kept", t, n, r) // 2)
 
 
 def adapters_forward(a: rsh_adapters_t, like) -> None:

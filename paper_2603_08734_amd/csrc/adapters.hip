@@ -359,6 +359,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
     int64_t token[kGroups];
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) token[i] = tile.at(16 * i + c);
+    struct Four {
+        uint4_t y[4];
+    };
+    auto read = [&](int64_t row) {
+        Four v;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t to = col0 + 32 * u + 8 * g;
+            if (Y && whole) v.y[u] = *reinterpret_cast<const uint4_a2*>(Y + row * ld_y + to);
+            else v.y[u] = load8(Y + row * ld_y + to, Y ? m - to : 0);
+        }
+        return v;
+    };
+    const Four head = read(token[0]);
     float4_t acc[kGroups][8] = {};
     if (some) {
         const float scale = scales ? scales[tile.adapter] : 1.f;
@@ -419,30 +433,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
             }
         }
     }
-    struct Four {
-        uint4_t y[4];
-    };
-    auto read = [&](int64_t row) {
-        Four v;
+    // the others all at once, in registers that B no longer needs
+    Four y[kGroups];
+    y[0] = head;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t to = col0 + 32 * u + 8 * g;
-            if (Y && whole) v.y[u] = *reinterpret_cast<const uint4_a2*>(Y + row * ld_y + to);
-            else v.y[u] = load8(Y + row * ld_y + to, Y ? m - to : 0);
-        }
-        return v;
-    };
-    Four next = read(token[0]);
+    for (int i = 1; i < kGroups; ++i)
+        if (16 * i < tile.count) y[i] = read(token[i]);
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
         if (16 * i >= tile.count) break;
-        const Four v = next;
-        if (i + 1 < kGroups && 16 * (i + 1) < tile.count) next = read(token[i + 1 < kGroups ? i + 1 : i]);
         if (16 * i + c >= tile.count) continue;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t to = col0 + 32 * u + 8 * g;
-            Eight e = widen8<T>(v.y[u]);
+            Eight e = widen8<T>(y[i].y[u]);
             if (some) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q) e.v[q] += acc[i][q][u];
@@ -602,14 +606,17 @@ struct Sorted {
     }
 };
 
-// Parts of the long axis of a shrinking product, and the steps of 64 in each.
-constexpr int kShrinkWaves = 8;
+// Parts of the long axis of a shrinking product, and the steps of 64 in each: as many as bring all compute units their fill of workgroups at
+// once, since a second round costs as much as the first (4096 tokens at rank 64 by 16384 columns in 16 parts and four rounds 63 us).
+constexpr int kFewWaves = 8, kShrinkWaves = 4, kOuterWaves = 4;
+int slots_of(int r) { return r <= 16 ? 1024 : r <= 32 ? 768 : 512; }     // workgroups of four waves that fit the chip, by their registers
 struct Split {
     int parts, steps;
-    Split(int64_t t, int64_t k, int r, bool few) {
-        const int64_t blocks = (few ? t : (t + kTile - 1) / kTile) * ((r + 63) / 64), all = (k + 63) / 64;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? kFewParts : 16, (few ? 512 : 1024) / std::max<int64_t>(1, blocks)));
-        const int64_t each = std::max<int64_t>(1, (all + want * kShrinkWaves - 1) / (want * kShrinkWaves)) * kShrinkWaves;
+    Split(int64_t t, int64_t k, int n, int r, bool few) {
+        const int64_t all = (k + 63) / 64, waves = few ? kFewWaves : kShrinkWaves;
+        const int64_t blocks = (few ? t : most_tiles(t, n)) * ((r + 63) / 64), slots = few ? 512 : slots_of(r);
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? kFewParts : 16, slots / blocks));
+        const int64_t each = (all + want * waves - 1) / (want * waves) * waves;
         steps = (int)each;
         parts = (int)((all + each - 1) / each);
     }
@@ -618,7 +625,7 @@ struct Split {
 // Parts of the tokens in a factor's gradient.
 int outer_parts(int64_t t, int64_t k, int n, int r) {
     const int64_t blocks = (k + 127) / 128 * n * ((r + 63) / 64);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({16, 512 / blocks, t / 64}));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({16, slots_of(r) / blocks, t / 64}));
 }
 
 void sort(const rsh_adapters_t& a, void* work, hipStream_t st) {
@@ -637,7 +644,7 @@ void shrink(const rsh_adapters_t& a, bool few, const void* X, int64_t ld, int64_
         constexpr int RT = decltype(rt)::value;
         const dim3 grid((unsigned)(few ? a.t : most_tiles(a.t, a.n)), (a.r + 16 * RT - 1) / (16 * RT), split.parts);
         if (few)
-            hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 1, true, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, st, (const uint16_t*)X, ld,
+            hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 1, true, kFewWaves>), grid, dim3(64 * kFewWaves), 0, st, (const uint16_t*)X, ld,
                                (const uint16_t*)A, index, order, H, a.t, k, a.r, split.steps);
         else
             hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 4, false, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, st, (const uint16_t*)X, ld,
@@ -670,7 +677,7 @@ void outer(const rsh_adapters_t& a, const void* X, int64_t ld, int64_t k, const 
     by_rank(a.r, [&](auto rt) {
         constexpr int RT = decltype(rt)::value;
         const dim3 grid((unsigned)((k + 127) / 128), a.n, (a.r + 16 * RT - 1) / (16 * RT) * parts);
-        hipLaunchKernelGGL((rsh_adapters_outer_kernel<T, RT, 8>), grid, dim3(512), 0, st, (const uint16_t*)X, ld, H, a.scales, order, (uint16_t*)out, sums,
+        hipLaunchKernelGGL((rsh_adapters_outer_kernel<T, RT, kOuterWaves>), grid, dim3(64 * kOuterWaves), 0, st, (const uint16_t*)X, ld, H, a.scales, order, (uint16_t*)out, sums,
                            parts, k, a.n, a.r);
     });
     if (parts > 1) {
@@ -681,9 +688,12 @@ void outer(const rsh_adapters_t& a, const void* X, int64_t ld, int64_t k, const 
 }
 }  // namespace
 
+// What a forward pass leaves for the gradients: H, and behind it the order of the tokens where it has made one.
+int64_t adapters_kept(int64_t t, int n, int r) { return t * wide_rank(r) * 4 + (t <= kFewTokens ? 0 : Sorted(t, n).bytes); }
+
 int64_t adapters_forward_work(int64_t t, int64_t k, int64_t, int n, int r) {
     const bool few = t <= kFewTokens;
-    return (few ? 0 : Sorted(t, n).bytes) + (Split(t, k, r, few).parts + 1) * t * wide_rank(r) * 4;
+    return (few ? 0 : Sorted(t, n).bytes) + (Split(t, k, n, r, few).parts + 1) * t * wide_rank(r) * 4;
 }
 
 int64_t adapters_backward_work(int64_t t, int64_t k, int64_t m, int n, int r) {
@@ -692,42 +702,44 @@ int64_t adapters_backward_work(int64_t t, int64_t k, int64_t m, int n, int r) {
         const int parts = outer_parts(t, w, n, r);
         if (parts > 1) sums = std::max(sums, parts * w * n * r * 4);
     }
-    return Sorted(t, n).bytes + (Split(t, m, r, false).parts + 1) * t * wide_rank(r) * 4 + sums;
+    return Sorted(t, n).bytes + (Split(t, m, n, r, false).parts + 1) * t * wide_rank(r) * 4 + sums;
 }
 
 int launch_adapters_forward(const rsh_adapters_t& a, void* work, void* stream) {
     const hipStream_t st = (hipStream_t)stream;
     const bool few = a.t <= kFewTokens;
-    const Split split(a.t, a.k, a.r, few);
+    const Split split(a.t, a.k, a.n, a.r, few);
     const Sorted s(a.t, a.n);
-    float* H = (float*)((char*)work + (few ? 0 : s.bytes));
-    if (!few) sort(a, work, st);
+    float* const H = (float*)((char*)work + (few ? 0 : s.bytes));
+    void* const order = a.kept ? (char*)a.kept + a.t * wide_rank(a.r) * 4 : work;
+    if (!few) sort(a, order, st);
     by_half(a.type, [&](auto half) {
         using T = decltype(half);
-        float* const direct = split.parts == 1 && a.H ? a.H : H;
-        shrink<T>(a, few, a.X, a.ld_x, a.k, a.A, s.at(work), split, direct, st);
+        float* const direct = split.parts == 1 && a.kept ? (float*)a.kept : H;
+        shrink<T>(a, few, a.X, a.ld_x, a.k, a.A, s.at(order), split, direct, st);
         int parts = split.parts;
         const float* all = direct;
-        if (parts > 1 && (a.H || !few)) {
-            float* const to = a.H ? a.H : H + parts * a.t * wide_rank(a.r);
+        if (parts > 1 && (a.kept || !few)) {
+            float* const to = a.kept ? (float*)a.kept : H + parts * a.t * wide_rank(a.r);
             join(H, to, a.t, a.r, parts, st);
             all = to;
             parts = 1;
         }
-        expand<T>(a, few, a.Y, a.ld_y, all, parts, a.B, s.at(work), a.out, a.m, st);
+        expand<T>(a, few, a.Y, a.ld_y, all, parts, a.B, s.at(order), a.out, a.m, st);
     });
     return launched();
 }
 
 int launch_adapters_backward(const rsh_adapters_t& a, const void* dout, int64_t ld_dout, void* dX, void* dA, void* dB, void* work, void* stream) {
     const hipStream_t st = (hipStream_t)stream;
-    const Split split(a.t, a.m, a.r, false);
+    const Split split(a.t, a.m, a.n, a.r, false);
     const Sorted s(a.t, a.n);
     float* const parts = (float*)((char*)work + s.bytes);
     float* const dH = parts + (split.parts > 1 ? split.parts * a.t * wide_rank(a.r) : 0);
     float* const sums = parts + (split.parts + 1) * a.t * wide_rank(a.r);
-    const Order order = s.at(work);
-    sort(a, work, st);
+    const bool sorted = a.t > kFewTokens;
+    const Order order = s.at(sorted ? (char*)a.kept + a.t * wide_rank(a.r) * 4 : work);
+    if (!sorted) sort(a, work, st);
     by_half(a.type, [&](auto half) {
         using T = decltype(half);
         if (dX || dA) {
@@ -736,7 +748,7 @@ int launch_adapters_backward(const rsh_adapters_t& a, const void* dout, int64_t 
         }
         if (dX) expand<T>(a, false, nullptr, 0, dH, 1, a.A, order, dX, a.k, st);
         if (dA) outer<T>(a, a.X, a.ld_x, a.k, dH, order, dA, sums, st);
-        if (dB) outer<T>(a, dout, ld_dout, a.m, a.H, order, dB, sums, st);
+        if (dB) outer<T>(a, dout, ld_dout, a.m, (const float*)a.kept, order, dB, sums, st);
     });
     return launched();
 }

@@ -814,12 +814,19 @@ int adapters_ok(const rsh_adapters_t* a, const void* work) {
     if (const int rc = adapter_sizes_ok(a->t, a->k, a->m, a->n, a->r)) return rc;
     if (!a->A || !a->B || !a->index || !work) return RSH_ERR_NULL;
     if (!half_type(a->type) || (a->index_size != 4 && a->index_size != 8) || !aligned_to({a->X, a->Y, a->A, a->B, a->out}, 2) ||
-        !aligned_to({a->index}, (uintptr_t)a->index_size) || !aligned_to({a->scales}, 4) || !aligned_to({a->H, work}, 16) ||
+        !aligned_to({a->index}, (uintptr_t)a->index_size) || !aligned_to({a->scales}, 4) || !aligned_to({a->kept, work}, 16) ||
         (a->X && !stride_ok(a->ld_x, a->k)) || (a->Y && !stride_ok(a->ld_y, a->m)))
         return RSH_ERR_BAD_OPTION;
     return RSH_OK;
 }
 }  // namespace
+
+int rsh_adapters_kept(int64_t t, int32_t n, int32_t r, int64_t* bytes) {
+    if (!bytes) return RSH_ERR_NULL;
+    const int rc = adapter_sizes_ok(t, 1, 1, n, r);
+    *bytes = rc ? 0 : rsh::adapters_kept(t, n, r);
+    return rc;
+}
 
 int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t* bytes) {
     if (!bytes) return RSH_ERR_NULL;
@@ -844,7 +851,7 @@ int rsh_adapters_backward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32
 
 int rsh_adapters_backward(const rsh_adapters_t* a, const void* dout, int64_t ld_dout, void* dX, void* dA, void* dB, void* work, void* hip_stream) {
     if (const int rc = adapters_ok(a, work)) return rc;
-    if (!dout || (!dX && !dA && !dB) || (dA && !a->X) || (dB && !a->H)) return RSH_ERR_NULL;
+    if (!dout || (!dX && !dA && !dB) || (dA && !a->X) || !a->kept) return RSH_ERR_NULL;
     if (!stride_ok(ld_dout, a->m) || !aligned_to({dout, dX, dA, dB}, 2)) return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_adapters_backward(*a, dout, ld_dout, dX, dA, dB, work, hip_stream));
 }

@@ -112,6 +112,7 @@ int launch_join_backward(const rsh_join_t& join, const rsh_join_gradients_t& gra
 int launch_dropout(const void* X, int type, int64_t t, int64_t d, int64_t ld, const rsh_drop_t& drop, void* Y, void* stream);
 
 // Low-rank adapters (adapters.hip): the same.
+int64_t adapters_kept(int64_t t, int n, int r);
 int64_t adapters_forward_work(int64_t t, int64_t k, int64_t m, int n, int r);
 int64_t adapters_backward_work(int64_t t, int64_t k, int64_t m, int n, int r);
 int launch_adapters_forward(const rsh_adapters_t& a, void* work, void* stream);

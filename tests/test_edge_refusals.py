@@ -84,7 +84,7 @@ def test_gradients_of_joins_refuse(status, join, gradients):
 
 
 def _adapters(**change):
-    a = dict(X=P, Y=P, A=P, B=P, index=P, scales=P, out=2 * P, H=P, t=4, k=64, m=32, ld_x=64, ld_y=32, n=3, r=8, type=b.RSH_F16, index_size=4)
+    a = dict(X=P, Y=P, A=P, B=P, index=P, scales=P, out=2 * P, kept=P, t=4, k=64, m=32, ld_x=64, ld_y=32, n=3, r=8, type=b.RSH_F16, index_size=4)
     a.update(change)
     return b.rsh_adapters_t(**a)
 
@@ -95,7 +95,7 @@ ADAPTERS = [
     (b.RSH_ERR_BAD_OPTION, dict(t=1 << 31)), (b.RSH_ERR_TOO_LARGE, dict(n=4097)), (b.RSH_ERR_TOO_LARGE, dict(r=513)),
     (b.RSH_ERR_TOO_LARGE, dict(k=(1 << 21) + 1)), (b.RSH_ERR_TOO_LARGE, dict(m=(1 << 21) + 1)), (b.RSH_ERR_BAD_OPTION, dict(type=b.RSH_F32)),
     (b.RSH_ERR_BAD_OPTION, dict(index_size=2)), (b.RSH_ERR_BAD_OPTION, dict(index=P + 4, index_size=8)), (b.RSH_ERR_BAD_OPTION, dict(scales=P + 2)),
-    (b.RSH_ERR_BAD_OPTION, dict(H=P + 8)), (b.RSH_ERR_BAD_OPTION, dict(A=P + 1)), (b.RSH_ERR_BAD_OPTION, dict(ld_x=63)),
+    (b.RSH_ERR_BAD_OPTION, dict(kept=P + 8)), (b.RSH_ERR_BAD_OPTION, dict(A=P + 1)), (b.RSH_ERR_BAD_OPTION, dict(ld_x=63)),
     (b.RSH_ERR_BAD_OPTION, dict(ld_y=31))]
 
 
@@ -107,7 +107,7 @@ def test_adapters_refuse(status, change):
 
 @pytest.mark.parametrize("status,change,call", [(s, c, {}) for s, c in ADAPTERS] + [
     (b.RSH_ERR_NULL, {}, dict(dout=None)), (b.RSH_ERR_NULL, {}, dict(dX=None, dA=None, dB=None)), (b.RSH_ERR_NULL, dict(X=None), {}),
-    (b.RSH_ERR_NULL, dict(H=None), {}), (b.RSH_ERR_NULL, {}, dict(work=None)), (b.RSH_ERR_BAD_OPTION, {}, dict(work=P + 8)),
+    (b.RSH_ERR_NULL, dict(kept=None), {}), (b.RSH_ERR_NULL, {}, dict(work=None)), (b.RSH_ERR_BAD_OPTION, {}, dict(work=P + 8)),
     (b.RSH_ERR_BAD_OPTION, {}, dict(ld=31)), (b.RSH_ERR_BAD_OPTION, {}, dict(dA=P + 1))])
 def test_gradients_of_adapters_refuse(status, change, call):
     a = dict(dout=P, ld=32, dX=P, dA=P, dB=P, work=P)
@@ -122,6 +122,8 @@ def test_work_sizes():
         for t in (1, 256, 257, 100000):
             assert f(t, 64, 32, 3, 8, ctypes.byref(n)) == 0 and n.value >= 4 * t * 16
         assert f(4, 64, 32, 3, 8, None) == b.RSH_ERR_NULL and f(4, 64, 32, 0, 8, ctypes.byref(n)) == b.RSH_ERR_BAD_OPTION and n.value == 0
+    assert L.rsh_adapters_kept(300, 3, 20, ctypes.byref(n)) == 0 and n.value >= 4 * 300 * 32 and L.rsh_adapters_kept(300, 3, 20, None) == b.RSH_ERR_NULL
+    assert L.rsh_adapters_kept(300, 4097, 20, ctypes.byref(n)) == b.RSH_ERR_TOO_LARGE and n.value == 0
     for d in (64, 8192, 8193):
         assert L.rsh_join_backward_work(100, d, 3, ctypes.byref(n)) == 0 and n.value >= 4 * 3 * d
         assert L.rsh_join_backward_work(100, d, 0, ctypes.byref(n)) == 0 and n.value == 0
