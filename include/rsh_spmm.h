@@ -399,7 +399,7 @@ int rsh_join_backward(const rsh_join_t *join, const rsh_join_gradients_t *gradie
  *                          was kept for these tokens and indexes.  The gradient of Y is dout.
  * Sums are fp32.  Between the products H is held in fp32 and multiplied to 2^-17 of itself; each result is rounded once.  An infinite
  * element of B, or of dout or X in a factor's gradient, may make NaN of what would be infinite.  work: 16-byte aligned, of the bytes that the *_work function
- * of the same sizes reports, rewritten by every call.  Results never depend on the order in which waves run.
+ * of the same sizes reports (keep: whether `kept` is there; 0 bytes: may be NULL), rewritten by every call.  Results never depend on the order in which waves run.
  * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE for widths
  * above RSH_FFN_MAX_WIDTH, more than RSH_ADAPTERS_MAX adapters or a rank above RSH_ADAPTERS_MAX_RANK.
  */
@@ -413,7 +413,7 @@ typedef struct {
     int32_t n, r, type, index_size;
 } rsh_adapters_t;
 int rsh_adapters_kept(int64_t t, int32_t n, int32_t r, int64_t *bytes);
-int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t *bytes);
+int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int32_t keep, int64_t *bytes);
 int rsh_adapters_forward(const rsh_adapters_t *adapters, void *work_dev, void *hip_stream);
 int rsh_adapters_backward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t *bytes);
 int rsh_adapters_backward(const rsh_adapters_t *adapters, const void *dout_dev, int64_t ld_dout, void *dX_dev, void *dA_dev, void *dB_dev,

@@ -173,8 +173,8 @@ def lib() -> ctypes.CDLL:
         L.rsh_join_backward_work.argtypes = [i64, i64, i32, i64p]
         L.rsh_join_backward.argtypes = [ctypes.POINTER(rsh_join_t), ctypes.POINTER(rsh_join_gradients_t), vp]
         L.rsh_adapters_kept.argtypes = [i64, i32, i32, i64p]
-        for f in (L.rsh_adapters_forward_work, L.rsh_adapters_backward_work):
-            f.argtypes = [i64, i64, i64, i32, i32, i64p]
+        L.rsh_adapters_forward_work.argtypes = [i64, i64, i64, i32, i32, i32, i64p]
+        L.rsh_adapters_backward_work.argtypes = [i64, i64, i64, i32, i32, i64p]
         L.rsh_adapters_forward.argtypes = [ctypes.POINTER(rsh_adapters_t), vp, vp]
         L.rsh_adapters_backward.argtypes = [ctypes.POINTER(rsh_adapters_t), vp, i64, vp, vp, vp, vp, vp]
         L.rsh_copy_probe.argtypes = [vp, vp, ctypes.c_int64, vp]
@@ -381,8 +381,9 @@ def adapters_kept(like, t: int, n: int, r: int):
 
 def adapters_forward(a: rsh_adapters_t, like) -> None:
     """Enqueue out = Y + s_i (X A_i^T) B_i (rsh_adapters_forward); work memory beside the 16-bit tensor `like`."""
-    work = like.new_empty(_work_bytes("rsh_adapters_forward_work", a.t, a.k, a.m, a.n, a.r) // 2)
-    _check(lib().rsh_adapters_forward(ctypes.byref(a), work.data_ptr(), current_stream()))
+    bytes_ = _work_bytes("rsh_adapters_forward_work", a.t, a.k, a.m, a.n, a.r, a.kept is not None)
+    work = like.new_empty(bytes_ // 2) if bytes_ else None
+    _check(lib().rsh_adapters_forward(ctypes.byref(a), None if work is None else work.data_ptr(), current_stream()))
 
 
 def adapters_backward(a: rsh_adapters_t, dout, ld_dout: int, dX, dA, dB) -> None:

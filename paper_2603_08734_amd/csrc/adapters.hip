@@ -14,7 +14,7 @@ namespace rsh {
 
 namespace {
 
-constexpr int kFewTokens = 256, kFewTile = 16, kFewParts = 8, kTile = 64;
+constexpr int kFewTokens = 256, kFewTile = 16, kFewParts = 8, kFewColumns = 1024, kTile = 64;
 constexpr int kSortThreads = 1024, kSortWords = 7 * (RSH_ADAPTERS_MAX + 1);     // counters in LDS
 
 struct Tile {
@@ -69,6 +69,14 @@ __device__ __forceinline__ int few_tile(const Index& index, int t, int mine, Few
     __syncthreads();
     *count = min(all - rank, kFewTile);
     return own;
+}
+
+// Eight elements of a row of d, zeros behind its end and in a lane that is not `in`.
+__device__ __forceinline__ uint4_t run_of(const uint16_t* row, int64_t col, int64_t d, bool in = true) {
+    uint4_t v = load_raw<F16, true>(row, (int)col, (int)d).v[0];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v[w] = in ? v[w] : 0u;
+    return v;
 }
 
 // Tokens of a tile.
@@ -230,13 +238,13 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const u
     };
     auto load = [&](int64_t step) {        // a whole one
         Slab v;
-        const int64_t at = 64 * step + 16 * g;
+        const int64_t at = 64 * step + 8 * g;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i) v.a[i][h] = *reinterpret_cast<const uint4_a2*>(a[i] + at + 8 * h);
+            for (int i = 0; i < RT; ++i) v.a[i][h] = *reinterpret_cast<const uint4_a2*>(a[i] + at + 32 * h);
 #pragma unroll
-            for (int i = 0; i < TT; ++i) v.x[i][h] = *reinterpret_cast<const uint4_a2*>(x[i] + at + 8 * h);
+            for (int i = 0; i < TT; ++i) v.x[i][h] = *reinterpret_cast<const uint4_a2*>(x[i] + at + 32 * h);
         }
         return v;
     };
@@ -258,14 +266,14 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const u
         }
     }
     if (whole < end && (whole - begin) % WAVES == wave) {      // what is left of k
-        const int64_t at = 64 * whole + 16 * g;
+        const int64_t at = 64 * whole + 8 * g;
         Slab v;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i) v.a[i][h] = load8(a[i] + at + 8 * h, k - at - 8 * h);
+            for (int i = 0; i < RT; ++i) v.a[i][h] = run_of(a[i], at + 32 * h, k);
 #pragma unroll
-            for (int i = 0; i < TT; ++i) v.x[i][h] = load8(x[i] + at + 8 * h, k - at - 8 * h);
+            for (int i = 0; i < TT; ++i) v.x[i][h] = run_of(x[i], at + 32 * h, k);
         }
         multiply(v);
     }
@@ -367,8 +375,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t to = col0 + 32 * u + 8 * g;
-            if (Y && whole) v.y[u] = *reinterpret_cast<const uint4_a2*>(Y + row * ld_y + to);
-            else v.y[u] = load8(Y + row * ld_y + to, Y ? m - to : 0);
+            if (!Y) v.y[u] = (uint4_t){0, 0, 0, 0};
+            else if (whole) v.y[u] = *reinterpret_cast<const uint4_a2*>(Y + row * ld_y + to);
+            else v.y[u] = run_of(Y + row * ld_y, to, m);
         }
         return v;
     };
@@ -376,7 +385,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
     float4_t acc[kGroups][8] = {};
     if (some) {
         const float scale = scales ? scales[tile.adapter] : 1.f;
-        const uint16_t* const b = B + (int64_t)tile.adapter * r * m + col;
+        const uint16_t* const b = B + (int64_t)tile.adapter * r * m;
         struct Slab {
             uint4_t rows[4];
             float4_t h[kGroups];
@@ -386,8 +395,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int row = rank + 4 * g + s;
-                if (whole) v.rows[s] = *reinterpret_cast<const uint4_a2*>(b + (int64_t)min(row, r - 1) * m);
-                else v.rows[s] = load8(b + (int64_t)min(row, r - 1) * m, m - col);
+                if (whole) v.rows[s] = *reinterpret_cast<const uint4_a2*>(b + (int64_t)min(row, r - 1) * m + col);
+                else v.rows[s] = run_of(b + (int64_t)min(row, r - 1) * m, col, m);
             }
 #pragma unroll
             for (int i = 0; i < kGroups; ++i) {
@@ -456,6 +465,130 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
     }
 }
 
+// A few tokens in one launch: every workgroup forms H of its tile for itself, sixteen waves over k, and eight of them go on to 128 columns each.
+template <class T, int RT>
+__global__ __launch_bounds__(1024) void rsh_adapters_few_kernel(const uint16_t* X, int64_t ld_x, const uint16_t* A, const uint16_t* Y, int64_t ld_y,
+                                                                const uint16_t* B, const float* scales, Index index, uint16_t* out, int64_t t, int64_t k,
+                                                                int64_t m, int r) {
+    constexpr int kWaves = 16, kAhead = RT == 1 ? 4 : 2;
+    __shared__ int place[sizeof(FewPlace) / sizeof(int)];
+    __shared__ float4_t joined[RT][kWaves][64];
+    __shared__ float4_t sums[RT][64];      // as a lane of the matrix unit has them: token lane % 16, ranks 4 (lane / 16) .. + 3
+    Members<true> tile;
+    if (!members<true>(index, Order{}, t, place, &tile)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
+    const bool some = tile.adapter < index.n;
+    const int64_t col0 = kFewColumns * (int64_t)blockIdx.y + 128 * wave, col = col0 + 8 * (4 * (c & 3) + (c >> 2)), token = tile.at(c);
+    const bool columns = 128 * wave < kFewColumns && col0 < m, all = col0 + 128 <= m;
+    uint4_t rows[RT][4], y[4];
+    if (columns) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t to = col0 + 32 * u + 8 * g;
+            if (!Y) y[u] = (uint4_t){0, 0, 0, 0};
+            else if (all) y[u] = *reinterpret_cast<const uint4_a2*>(Y + token * ld_y + to);
+            else y[u] = run_of(Y + token * ld_y, to, m);
+        }
+        if (some) {
+            const uint16_t* const b = B + (int64_t)tile.adapter * r * m;
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int row = 16 * i + 4 * g + s;
+                    if (all) rows[i][s] = *reinterpret_cast<const uint4_a2*>(b + (int64_t)min(row, r - 1) * m + col);
+                    else rows[i][s] = run_of(b + (int64_t)min(row, r - 1) * m, col, m);
+                }
+        }
+    }
+    if (some) {
+        const uint16_t* a[RT];
+        const uint16_t* const x = X + token * ld_x;
+#pragma unroll
+        for (int i = 0; i < RT; ++i) a[i] = A + ((int64_t)tile.adapter * r + min(16 * i + c, r - 1)) * k;
+        float4_t acc[RT] = {};
+        const int64_t whole = k / 64;
+        for (int64_t step = wave; step < whole; step += kWaves * kAhead) {
+            uint4_t av[kAhead][RT][2], xv[kAhead][2];
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) {
+                const int64_t at = 64 * min(step + kWaves * s, whole - 1) + 8 * g;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    xv[s][h] = *reinterpret_cast<const uint4_a2*>(x + at + 32 * h);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) av[s][i][h] = *reinterpret_cast<const uint4_a2*>(a[i] + at + 32 * h);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s)
+                if (step + kWaves * s < whole)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) acc[i] = T::mfma16(av[s][i][h], xv[s][h], acc[i]);
+        }
+        if (k % 64 && whole % kWaves == wave) {
+            const int64_t at = 64 * whole + 8 * g;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint4_t xv = run_of(x, at + 32 * h, k);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) acc[i] = T::mfma16(run_of(a[i], at + 32 * h, k), xv, acc[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) joined[i][wave][lane] = acc[i];
+        __syncthreads();
+        if (wave < RT) {
+            float4_t s = joined[wave][0][lane];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) s += joined[wave][w][lane];
+            const float scale = scales ? scales[tile.adapter] : 1.f;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) s[v] = 16 * wave + 4 * g + v < r ? s[v] * scale : 0.f;
+            sums[wave][lane] = s;
+        }
+        __syncthreads();
+    }
+    if (!columns) return;
+    float4_t acc[8] = {};
+    if (some) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const float4_t h = sums[i][lane];
+            const float hv[4] = {h[0], h[1], h[2], h[3]};
+            const Halves two = halves(hv);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) rows[i][s][w] = 16 * i + 4 * g + s < r ? rows[i][s][w] : 0u;
+            Fours<T> f;
+            f.from(rows[i]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                acc[q] = multiply(f.main[q], two.hi, acc[q]);
+                acc[q] = multiply(f.main[q], two.lo, acc[q]);
+                if constexpr (std::is_same<T, F16>::value) {
+                    acc[q] = multiply(f.rest[q], two.hi, acc[q]);
+                    acc[q] = multiply(f.rest[q], two.lo, acc[q]);
+                }
+            }
+        }
+    }
+    if (c >= tile.count) return;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int64_t to = col0 + 32 * u + 8 * g;
+        Eight e = widen8<T>(y[u]);
+        if (some) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) e.v[q] += acc[q][u];
+        }
+        store_eight<T>(out, token * m + to, e, (int)min(m - to, (int64_t)8));
+    }
+}
+
 // H of all tokens from its parts.
 __global__ __launch_bounds__(256) void rsh_adapters_join_kernel(const float4_t* from, float4_t* to, int64_t n, int parts) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
@@ -483,6 +616,7 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
         float h[RT][4];
     };
     const int valid = (int)min(k - col, (int64_t)8);
+    const bool whole = 128 * (int64_t)blockIdx.x + 128 <= k;
     struct Four {
         int token[4];
     };
@@ -498,7 +632,10 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
         for (int i = 0; i < 4; ++i) {
             const bool in = i0 + 4 * g + i < end;
             const int64_t token = f.token[i];
-            s.x[i] = load8(X + token * ld_x + col, in ? valid : 0);
+            if (whole) s.x[i] = *reinterpret_cast<const uint4_a2*>(X + token * ld_x + col);
+            else s.x[i] = run_of(X + token * ld_x, col, k);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) s.x[i][w] = in ? s.x[i][w] : 0u;
 #pragma unroll
             for (int j = 0; j < RT; ++j) s.h[j][i] = in && r0 + 16 * j < r16 ? H[token * r16 + r0 + 16 * j + c] : 0.f;
         }
@@ -606,6 +743,13 @@ struct Sorted {
     }
 };
 
+// Whether a few tokens go in one launch: all workgroups read A once more for every 1024 columns, from caches.  One launch takes 6 us where two take
+// 12 until that is some tens of megabytes, or more than a compute unit reads in the time of the second launch.
+bool in_one(int64_t t, int64_t k, int64_t m, int r) {
+    const int64_t factor = 2 * k * wide_rank(r), columns = (m + kFewColumns - 1) / kFewColumns;
+    return t <= kFewTokens && r <= 32 && factor <= (1 << 18) && factor * columns * t <= (1 << 26);
+}
+
 // Parts of the long axis of a shrinking product, and the steps of 64 in each: as many as bring all compute units their fill of workgroups at
 // once, since a second round costs as much as the first (4096 tokens at rank 64 by 16384 columns in 16 parts and four rounds 63 us).
 constexpr int kFewWaves = 8, kShrinkWaves = 4, kOuterWaves = 4;
@@ -691,7 +835,8 @@ void outer(const rsh_adapters_t& a, const void* X, int64_t ld, int64_t k, const 
 // What a forward pass leaves for the gradients: H, and behind it the order of the tokens where it has made one.
 int64_t adapters_kept(int64_t t, int n, int r) { return t * wide_rank(r) * 4 + (t <= kFewTokens ? 0 : Sorted(t, n).bytes); }
 
-int64_t adapters_forward_work(int64_t t, int64_t k, int64_t, int n, int r) {
+int64_t adapters_forward_work(int64_t t, int64_t k, int64_t m, int n, int r, bool keep) {
+    if (!keep && in_one(t, k, m, r)) return 0;
     const bool few = t <= kFewTokens;
     return (few ? 0 : Sorted(t, n).bytes) + (Split(t, k, n, r, few).parts + 1) * t * wide_rank(r) * 4;
 }
@@ -708,6 +853,20 @@ int64_t adapters_backward_work(int64_t t, int64_t k, int64_t m, int n, int r) {
 int launch_adapters_forward(const rsh_adapters_t& a, void* work, void* stream) {
     const hipStream_t st = (hipStream_t)stream;
     const bool few = a.t <= kFewTokens;
+    if (!a.kept && in_one(a.t, a.k, a.m, a.r)) {
+        const dim3 grid((unsigned)a.t, (unsigned)((a.m + kFewColumns - 1) / kFewColumns));
+        by_half(a.type, [&](auto half) {
+            using T = decltype(half);
+            auto launch = [&](auto rt) {
+                hipLaunchKernelGGL((rsh_adapters_few_kernel<T, decltype(rt)::value>), grid, dim3(1024), 0, st, (const uint16_t*)a.X, a.ld_x,
+                                   (const uint16_t*)a.A, (const uint16_t*)a.Y, a.ld_y, (const uint16_t*)a.B, a.scales,
+                                   Index{a.index, a.index_size == 8, a.n}, (uint16_t*)a.out, a.t, a.k, a.m, a.r);
+            };
+            if (a.r <= 16) launch(std::integral_constant<int, 1>());
+            else launch(std::integral_constant<int, 2>());
+        });
+        return launched();
+    }
     const Split split(a.t, a.k, a.n, a.r, few);
     const Sorted s(a.t, a.n);
     float* const H = (float*)((char*)work + (few ? 0 : s.bytes));

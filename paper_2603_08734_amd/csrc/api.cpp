@@ -809,10 +809,11 @@ int adapter_sizes_ok(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r) {
     if (t <= 0 || k <= 0 || m <= 0 || n <= 0 || r <= 0 || t >= kMaxSize) return RSH_ERR_BAD_OPTION;
     return k > kMaxWidth || m > kMaxWidth || n > RSH_ADAPTERS_MAX || r > RSH_ADAPTERS_MAX_RANK ? RSH_ERR_TOO_LARGE : RSH_OK;
 }
-int adapters_ok(const rsh_adapters_t* a, const void* work) {
+int adapters_ok(const rsh_adapters_t* a, const void* work, bool forward) {
     if (!a) return RSH_ERR_NULL;
     if (const int rc = adapter_sizes_ok(a->t, a->k, a->m, a->n, a->r)) return rc;
-    if (!a->A || !a->B || !a->index || !work) return RSH_ERR_NULL;
+    const bool needs = !forward || rsh::adapters_forward_work(a->t, a->k, a->m, a->n, a->r, a->kept) > 0;
+    if (!a->A || !a->B || !a->index || (needs && !work)) return RSH_ERR_NULL;
     if (!half_type(a->type) || (a->index_size != 4 && a->index_size != 8) || !aligned_to({a->X, a->Y, a->A, a->B, a->out}, 2) ||
         !aligned_to({a->index}, (uintptr_t)a->index_size) || !aligned_to({a->scales}, 4) || !aligned_to({a->kept, work}, 16) ||
         (a->X && !stride_ok(a->ld_x, a->k)) || (a->Y && !stride_ok(a->ld_y, a->m)))
@@ -828,15 +829,15 @@ int rsh_adapters_kept(int64_t t, int32_t n, int32_t r, int64_t* bytes) {
     return rc;
 }
 
-int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int64_t* bytes) {
+int rsh_adapters_forward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r, int32_t keep, int64_t* bytes) {
     if (!bytes) return RSH_ERR_NULL;
     const int rc = adapter_sizes_ok(t, k, m, n, r);
-    *bytes = rc ? 0 : rsh::adapters_forward_work(t, k, m, n, r);
+    *bytes = rc ? 0 : rsh::adapters_forward_work(t, k, m, n, r, keep != 0);
     return rc;
 }
 
 int rsh_adapters_forward(const rsh_adapters_t* a, void* work, void* hip_stream) {
-    if (const int rc = adapters_ok(a, work)) return rc;
+    if (const int rc = adapters_ok(a, work, true)) return rc;
     if (!a->X || !a->out) return RSH_ERR_NULL;
     if (a->out == a->Y && a->ld_y != a->m && a->t > 1) return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_adapters_forward(*a, work, hip_stream));
@@ -850,7 +851,7 @@ int rsh_adapters_backward_work(int64_t t, int64_t k, int64_t m, int32_t n, int32
 }
 
 int rsh_adapters_backward(const rsh_adapters_t* a, const void* dout, int64_t ld_dout, void* dX, void* dA, void* dB, void* work, void* hip_stream) {
-    if (const int rc = adapters_ok(a, work)) return rc;
+    if (const int rc = adapters_ok(a, work, false)) return rc;
     if (!dout || (!dX && !dA && !dB) || (dA && !a->X) || !a->kept) return RSH_ERR_NULL;
     if (!stride_ok(ld_dout, a->m) || !aligned_to({dout, dX, dA, dB}, 2)) return RSH_ERR_BAD_OPTION;
     return launch_status(rsh::launch_adapters_backward(*a, dout, ld_dout, dX, dA, dB, work, hip_stream));

@@ -158,7 +158,8 @@ struct Affine {
     }
 };
 
-// Rows of up to 8 LANES columns, a run a lane.  JOIN: whether there is a B.  The next row's loads go out when this one's have been used.
+// Rows of up to 8 LANES columns, a run a lane.  JOIN: whether there is a B.  The next row's loads go out before
+// this one is begun: a row takes as long as they do.
 template <class T, int LANES, bool JOIN>
 __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(4))) void rsh_join_forward_kernel(rsh_join_t j) {
     constexpr bool kShort = LANES == 8;        // rows may be shorter than a run
@@ -171,16 +172,19 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
     const float factor = j.drop.share ? j.scale * random.keep : j.scale;
     Eight gate = parameters<T, kShort>(j.ld_gate ? nullptr : j.gate, j.gate_type, col, d, 1.f);
     const int64_t step = (int64_t)gridDim.x * kRows;
-    Raw<T> x, b;
+    Raw<T> x, b, next_x, next_b;
     auto load = [&](int64_t head) {
         const int64_t row = min(row_of<LANES>(head), j.t - 1);
-        if constexpr (JOIN) b = load_raw<T, kShort>(element(j.B, row * j.ld_b, kSize), col, d);
-        x = load_raw<T, kShort>(element(j.X, row * j.ld_x, kSize), col, d);
+        if constexpr (JOIN) next_b = load_raw<T, kShort>(element(j.B, row * j.ld_b, kSize), col, d);
+        next_x = load_raw<T, kShort>(element(j.X, row * j.ld_x, kSize), col, d);
     };
     load((int64_t)blockIdx.x * kRows);
     for (int64_t head = (int64_t)blockIdx.x * kRows; head < j.t; head += step) {
         const int64_t mine = row_of<LANES>(head), row = min(mine, j.t - 1);
         const bool live = mine < j.t, leads = live && threadIdx.x % LANES == 0;
+        x = next_x;
+        if constexpr (JOIN) b = next_b;
+        if (head + step < j.t) load(head + step);
         Eight s;
         if constexpr (JOIN) {
             Eight n = widen(b);
@@ -195,14 +199,12 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
 #pragma unroll
                 for (int i = 0; i < 8; ++i) n.v[i] *= factor;
             s = widen(x);
-            if (head + step < j.t) load(head + step);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s.v[i] += gate.v[i] * n.v[i];
             clear_from(s, d - col);
             if (live) store_run<T>(j.S, row, col, d, s);
         } else {
             s = widen(x);
-            if (head + step < j.t) load(head + step);
         }
         if (j.before.kind == RSH_NORM_NONE) continue;
         const float2_t at = statistics<LANES, 1>(j.before, d, team, [&](int, int) { return s; });
@@ -342,7 +344,7 @@ struct Run {
 };
 
 // The parameters of a run: of every row the same run, so kept, or loaded anew.
-template <class T, bool SHORT>
+template <class T, bool SHORT, bool BIAS>
 struct KeptParameters {
     Affine<T, SHORT> after, before;
     Eight gate;
@@ -350,7 +352,7 @@ struct KeptParameters {
         : after(j.after, col, d), before(j.before, col, d),
           gate(parameters<T, SHORT>(j.ld_gate ? nullptr : j.gate, j.gate_type, col, d, 1.f)) {}
     __device__ __forceinline__ Eight after_weight(int) const { return after.w; }
-    __device__ __forceinline__ Eight after_bias(int) const { return after.b; }
+    __device__ __forceinline__ Eight after_bias(int) const { return BIAS ? after.b : Eight{}; }
     __device__ __forceinline__ Eight before_weight(int) const { return before.w; }
     __device__ __forceinline__ Eight gate_of(int) const { return gate; }
 };
@@ -505,6 +507,8 @@ struct Backward {
 template <class T, int LANES, bool JOIN, bool BIAS>
 __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(4))) void rsh_join_backward_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts) {
     constexpr int kThreads = kThreadsOf<LANES>, kRows = kRowsOf<LANES>;
+    // Whether the registers hold the next row beside this one: a row takes about as long as its loads.
+    constexpr bool kEarly = !JOIN || (size_of<T>() == 2 && !BIAS);
     __shared__ typename Team<LANES>::Meeting meeting;
     using Sums = std::conditional_t<JOIN, LdsSums<kThreads, BIAS>, RegisterSums>;
     __shared__ std::conditional_t<JOIN, typename LdsSums<kThreads, BIAS>::Place, float> place;
@@ -512,8 +516,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
     Team<LANES> team(meeting);
     const Random random(j.drop);
     const int d = (int)j.d, col = 8 * (threadIdx.x % LANES);
-    const KeptParameters<T, LANES == 8> given(j, col, d);
-    const Backward<T, JOIN, LANES == 8, Sums, KeptParameters<T, LANES == 8>> back(j, g, random, given);
+    const KeptParameters<T, LANES == 8, BIAS> given(j, col, d);
+    const Backward<T, JOIN, LANES == 8, Sums, KeptParameters<T, LANES == 8, BIAS>> back(j, g, random, given);
     Sums sums = [&] {
         if constexpr (JOIN) return Sums(place, vectors);
         else return Sums();
@@ -528,10 +532,11 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
         const int64_t mine = row_of<LANES>(head), row = min(mine, j.t - 1);
         const bool live = mine < j.t;
         Inputs<T> in = next;
+        if (kEarly && head + step < j.t) next = load(head + step);
         Run x;
         float2_t mean = {0.f, 0.f};
         back.before(in, row, col, x, sums);
-        if (head + step < j.t) next = load(head + step);
+        if (!kEarly && head + step < j.t) next = load(head + step);
         if (back.first) {
             float a = 0.f, b = 0.f;
 #pragma unroll
@@ -726,7 +731,7 @@ void join_backward_launch(const rsh_join_t& j, const rsh_join_gradients_t& g, co
         else hipLaunchKernelGGL((rsh_join_columns_kernel<T, false>), columns, dim3(256), 0, st, j, g, v, parts, means);
         return;
     }
-    const bool bias = v.at[kBeforeBias] >= 0 || v.at[kAfterBias] >= 0;
+    const bool bias = v.at[kBeforeBias] >= 0 || v.at[kAfterBias] >= 0 || j.after.bias;
     by_width(j.d, [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
         const dim3 grid((unsigned)n), block(kThreadsOf<L>);
@@ -734,7 +739,7 @@ void join_backward_launch(const rsh_join_t& j, const rsh_join_gradients_t& g, co
             if (j.B) hipLaunchKernelGGL((rsh_join_backward_kernel<T, L, true, decltype(b)::value>), grid, block, 0, st, j, g, v, parts);
             else hipLaunchKernelGGL((rsh_join_backward_kernel<T, L, false, decltype(b)::value>), grid, block, 0, st, j, g, v, parts);
         };
-        if constexpr (L >= 512) {
+        if constexpr (L >= 256) {
             if (bias) launch(std::true_type());
             else launch(std::false_type());
         } else {

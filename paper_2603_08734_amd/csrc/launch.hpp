@@ -113,7 +113,7 @@ int launch_dropout(const void* X, int type, int64_t t, int64_t d, int64_t ld, co
 
 // Low-rank adapters (adapters.hip): the same.
 int64_t adapters_kept(int64_t t, int n, int r);
-int64_t adapters_forward_work(int64_t t, int64_t k, int64_t m, int n, int r);
+int64_t adapters_forward_work(int64_t t, int64_t k, int64_t m, int n, int r, bool keep);
 int64_t adapters_backward_work(int64_t t, int64_t k, int64_t m, int n, int r);
 int launch_adapters_forward(const rsh_adapters_t& a, void* work, void* stream);
 int launch_adapters_backward(const rsh_adapters_t& a, const void* dout, int64_t ld_dout, void* dX, void* dA, void* dB, void* work, void* stream);

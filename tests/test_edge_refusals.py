@@ -117,8 +117,10 @@ def test_gradients_of_adapters_refuse(status, change, call):
 
 def test_work_sizes():
     L, n = b.lib(), ctypes.c_int64(-1)
-    assert L.rsh_adapters_forward(ctypes.byref(_adapters()), None, None) == b.RSH_ERR_NULL
-    for f in (L.rsh_adapters_forward_work, L.rsh_adapters_backward_work):
+    assert L.rsh_adapters_forward(ctypes.byref(_adapters()), None, None) == b.RSH_ERR_NULL      # something is kept
+    assert L.rsh_adapters_forward(ctypes.byref(_adapters(t=257, kept=None)), None, None) == b.RSH_ERR_NULL
+    assert L.rsh_adapters_forward_work(4, 64, 32, 3, 8, 0, ctypes.byref(n)) == 0 and n.value == 0      # one launch, nothing between
+    for f in (lambda *a: L.rsh_adapters_forward_work(*a[:5], 1, a[5]), L.rsh_adapters_backward_work):
         for t in (1, 256, 257, 100000):
             assert f(t, 64, 32, 3, 8, ctypes.byref(n)) == 0 and n.value >= 4 * t * 16
         assert f(4, 64, 32, 3, 8, None) == b.RSH_ERR_NULL and f(4, 64, 32, 0, 8, ctypes.byref(n)) == b.RSH_ERR_BAD_OPTION and n.value == 0

@@ -66,6 +66,9 @@ def reference(c, device):
 
 
 def check(c, grads=True):
+    """With gradients, and without: few tokens then go in one launch."""
+    if grads:
+        check(c, False)
     got, want = library(c, grads), reference(c, "cuda" if c["x"].numel() > 1 << 18 else "cpu")
     dtype = c["x"].dtype
     u, least = torch.finfo(dtype).eps / 2, 2.0 ** -25 if dtype == torch.float16 else 2.0 ** -134
@@ -120,6 +123,12 @@ def test_indexes_of_64_bits_that_look_small():
     c["index"] = torch.where(torch.arange(20) % 2 == 0, (1 << 32) + 1, 1)
     got = check(c)
     assert torch.equal(got[0].cpu()[::2], c["y"][::2])
+
+
+@pytest.mark.parametrize("k,m,r", [(8192, 2100, 16), (8200, 1024, 20), (16384, 64, 16), (16400, 64, 16), (1024, 3000, 32), (1000, 5000, 33)])
+def test_few_tokens_around_what_one_launch_takes(k, m, r):
+    for t in (1, 3, 40):
+        check(make(t, k, m, 5, r, "bf16", "random" if t > 1 else "one"))
 
 
 @pytest.mark.parametrize("scaled", [False, True])
