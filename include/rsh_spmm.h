@@ -331,8 +331,9 @@ int rsh_ffn_tiles(int32_t which, int32_t aligned, int64_t t, int64_t a, int64_t 
  * (low, high half of the seed); of its four words, low half before high half, elements take theirs in order.  An element whose bits are
  * below `share` becomes zero (an infinity or a NaN too), the others are multiplied by 65536 / (65536 - share).
  *   rsh_dropout    Y = drop(X); its gradient is the same call on the gradient of Y.  Y without gaps, or X itself (ld = d)
- * share: 0 .. 65536.  seed_dev: device, 8-byte aligned, read by the kernels in place of `seed`, or NULL.
+ * ld: elements from row to row, d .. RSH_ROWS_MAX_STRIDE.  share: 0 .. 65536.  seed_dev: device, 8-byte aligned, read by the kernels in place of `seed`, or NULL.
  */
+#define RSH_ROWS_MAX_STRIDE (1 << 29)
 typedef struct {
     uint64_t seed, offset;
     const uint64_t *seed_dev;
@@ -350,7 +351,7 @@ int rsh_dropout(const void *X_dev, int32_t type, int64_t t, int64_t d, int64_t l
  * weight, bias: [d], NULL for ones and zeros.  stats: fp32 [t][2], m (0 with RSH_NORM_RMS) and r of every row; written by the forward
  * call where it is not NULL, read by the backward call.
  *   type         RSH_F32, RSH_F16 or RSH_BF16, of X, B, S, Y and their gradients; parameters and gate have it or are RSH_F32
- *   ld_x, ld_b   elements from row to row; no alignment beyond the element's
+ *   ld_x, ld_b   elements from row to row, at most RSH_ROWS_MAX_STRIDE like all such here; no alignment beyond the element's
  *   gate         [d] (ld_gate 0) or [t][d] with rows ld_gate apart; NULL (ld_gate 0) for ones
  *   S            [t][d] without gaps, not X or B; NULL if and only if B is
  *   Y            [t][d] without gaps; NULL if and only if before.kind is RSH_NORM_NONE
@@ -392,7 +393,7 @@ int rsh_join_backward(const rsh_join_t *join, const rsh_join_gradients_t *gradie
  * Low-rank adapters of many requests beside a projection that they share: for every token (row) with adapter i = index[token]
  *   out = Y + scales[i] (X A_i^T) B_i,    H = X A_i^T
  * and out = Y for a token whose index is not one of 0 .. n - 1.  X [t][k], Y and out [t][m] of `type` (RSH_F16 or RSH_BF16), rows ld_x
- * and ld_y apart, out without gaps (it may be Y where that is); A [n][r][k] and B [n][r][m] without gaps, of the same type; index int32 or int64 (index_size
+ * and ld_y apart (at most RSH_ROWS_MAX_STRIDE), out without gaps (it may be Y where that is); A [n][r][k] and B [n][r][m] without gaps, of the same type; index int32 or int64 (index_size
  * 4 or 8); scales fp32 [n], NULL for ones.  No alignment beyond the element's.  Y NULL: zeros.
  *   rsh_adapters_forward   kept not NULL: what the gradients need of H and of the tokens' order, 16-byte aligned, rsh_adapters_kept bytes
  *   rsh_adapters_backward  for dout (rows ld_dout apart): dX [t][k], dA and dB of A's and B's shapes, each NULL where not wanted, from what

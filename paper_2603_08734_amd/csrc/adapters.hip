@@ -73,10 +73,7 @@ __device__ __forceinline__ int few_tile(const Index& index, int t, int mine, Few
 
 // Eight elements of a row of d, zeros behind its end and in a lane that is not `in`.
 __device__ __forceinline__ uint4_t run_of(const uint16_t* row, int64_t col, int64_t d, bool in = true) {
-    uint4_t v = load_raw<F16, true>(row, (int)col, (int)d).v[0];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) v[w] = in ? v[w] : 0u;
-    return v;
+    return settle<F16, true>(load_raw<F16, true>(row, (int)col, (int)d), (int)col, (int)d, in).v[0];
 }
 
 // Tokens of a tile.

@@ -736,7 +736,7 @@ int rows_ok(int64_t t, int64_t d) {
     if (t <= 0 || d <= 0 || t >= kMaxSize) return RSH_ERR_BAD_OPTION;
     return d > kMaxWidth ? RSH_ERR_TOO_LARGE : RSH_OK;
 }
-bool stride_ok(int64_t ld, int64_t d) { return ld >= d && ld < kMaxSize; }
+bool stride_ok(int64_t ld, int64_t d) { return ld >= d && ld <= RSH_ROWS_MAX_STRIDE; }
 bool drop_ok(const rsh_drop_t& drop) { return drop.share <= 65536 && aligned_to({drop.seed_dev}, 8); }
 // Parameters: in fp32 or in the rows' type.
 bool parameter_ok(const void* p, int32_t p_type, int32_t type) {

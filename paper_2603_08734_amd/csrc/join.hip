@@ -61,7 +61,7 @@ int64_t backward_parts(int64_t t, int64_t d) {
     int64_t parts = 0;
     by_width(d, [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
-        parts = std::min<int64_t>((t + kRowsOf<L> - 1) / kRowsOf<L>, 256 * (1024 / kThreadsOf<L>));
+        parts = std::min<int64_t>((t + kRowsOf<L> - 1) / kRowsOf<L>, 256 * ((L <= 64 ? 2048 : 1024) / kThreadsOf<L>));
     });
     return parts;
 }

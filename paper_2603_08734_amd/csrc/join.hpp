@@ -96,8 +96,8 @@ __device__ __forceinline__ void clear_from(Eight& e, int valid) {
 // A run of a row of parameters or of the gate, in fp32 or in the rows' type.
 template <class T, bool SHORT>
 __device__ __forceinline__ Eight load_vector(const void* p, int type, int col, int d) {
-    if (std::is_same<T, F32>::value || type == RSH_F32) return widen(load_raw<F32, SHORT>(p, col, d));
-    return widen(load_raw<T, SHORT>(p, col, d));
+    if (std::is_same<T, F32>::value || type == RSH_F32) return widen(settle<F32, SHORT>(load_raw<F32, SHORT>(p, col, d), col, d));
+    return widen(settle<T, SHORT>(load_raw<T, SHORT>(p, col, d), col, d));
 }
 // Parameters of a run: ones or zeros where there are none.
 template <class T, bool SHORT>
@@ -108,22 +108,35 @@ __device__ __forceinline__ Eight parameters(const void* p, int type, int col, in
     for (int i = 0; i < 8; ++i) e.v[i] = otherwise;
     return e;
 }
-__device__ __forceinline__ const void* element(const void* base, int64_t at, int size) { return base ? (const uint8_t*)base + at * size : nullptr; }
+// The row of a team: `head`, alike in all lanes of a wave, and the lane's distance from it, which is zero where a team is no smaller than a wave.
+// A row's address is then a scalar product and one addition; with teams of a few lanes it was a 64-bit product of vectors for every tensor.
+struct Place {
+    int64_t head;
+    int mine;
+    __device__ __forceinline__ int64_t row() const { return head + mine; }
+    // What lies row() * ld elements of `size` behind `base`, which may be null; ld * size is below 2^32.
+    __device__ __forceinline__ const void* of(const void* base, int64_t ld, int size) const {
+        return base ? (const uint8_t*)base + head * ld * size + (uint64_t)(uint32_t)mine * (uint32_t)(ld * size) : nullptr;
+    }
+};
+template <int LANES>
+__device__ __forceinline__ Place place_of(int64_t first, int64_t t, bool* live) {
+    if constexpr (LANES >= 64) {
+        const int64_t r = first + threadIdx.x / LANES;
+        const int64_t head = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(r >> 32)) << 32 |
+                                       (uint32_t)__builtin_amdgcn_readfirstlane((int)r));
+        *live = head < t;
+        return {min(head, t - 1), 0};
+    }
+    const int mine = threadIdx.x / LANES;
+    *live = first + mine < t;
+    return {first, (int)min((int64_t)mine, t - 1 - first)};
+}
 
 // Into a row of d at column col.
 template <class T>
-__device__ __forceinline__ void store_run(void* base, int64_t row, int col, int d, const Eight& e) {
-    store_eight<T>((void*)byte_of(element(base, row * d, size_of<T>()), (uint32_t)col * (uint32_t)size_of<T>()), 0, e, d - col);
-}
-
-// The row of a team, alike in all lanes of a wave where a team is no smaller.
-template <int LANES>
-__device__ __forceinline__ int64_t row_of(int64_t first) {
-    if constexpr (LANES >= 64) {
-        const int64_t r = first + threadIdx.x / LANES;
-        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(r >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)r));
-    }
-    return first + threadIdx.x / LANES;
+__device__ __forceinline__ void store_run(void* base, const Place& row, int col, int d, const Eight& e) {
+    store_eight<T>((void*)byte_of(row.of(base, d, size_of<T>()), (uint32_t)col * (uint32_t)size_of<T>()), 0, e, d - col);
 }
 
 // m and r of a row whose runs are get(c, column), zeros behind the row's end.  Where a sum leaves the range of fp32, once more with the
@@ -193,41 +206,43 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
     const int64_t step = (int64_t)gridDim.x * kRows;
     Raw<T> x, b, next_x, next_b;
     auto load = [&](int64_t head) {
-        const int64_t row = min(row_of<LANES>(head), j.t - 1);
-        if constexpr (JOIN) next_b = load_raw<T, kShort>(element(j.B, row * j.ld_b, kSize), col, d);
-        next_x = load_raw<T, kShort>(element(j.X, row * j.ld_x, kSize), col, d);
+        bool is;
+        const Place row = place_of<LANES>(head, j.t, &is);
+        if constexpr (JOIN) next_b = load_raw<T, kShort>(row.of(j.B, j.ld_b, kSize), col, d);
+        next_x = load_raw<T, kShort>(row.of(j.X, j.ld_x, kSize), col, d);
     };
     load((int64_t)blockIdx.x * kRows);
     for (int64_t head = (int64_t)blockIdx.x * kRows; head < j.t; head += step) {
-        const int64_t mine = row_of<LANES>(head), row = min(mine, j.t - 1);
-        const bool live = mine < j.t, leads = live && threadIdx.x % LANES == 0;
+        bool live;
+        const Place row = place_of<LANES>(head, j.t, &live);
+        const bool leads = live && threadIdx.x % LANES == 0;
         x = next_x;
         if constexpr (JOIN) b = next_b;
         if (head + step < j.t) load(head + step);
         Eight s;
         if constexpr (JOIN) {
-            Eight n = widen(b);
+            Eight n = widen(settle<T, kShort>(b, col, d));
             if (j.after.kind != RSH_NORM_NONE) {
                 const float2_t at = statistics<LANES, 1>(j.after, d, team, [&](int, int) { return n; });
-                if (leads && j.after.stats) *reinterpret_cast<float2_t*>(j.after.stats + 2 * row) = at;
+                if (leads && j.after.stats) *reinterpret_cast<float2_t*>(j.after.stats + 2 * row.row()) = at;
                 first.apply(n, at);
             }
-            if (j.ld_gate) gate = load_vector<T, kShort>(element(j.gate, row * j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d);
-            if (j.drop.share) random.drop(n, col, row, factor);
+            if (j.ld_gate) gate = load_vector<T, kShort>(row.of(j.gate, j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d);
+            if (j.drop.share) random.drop(n, col, row.row(), factor);
             else
 #pragma unroll
                 for (int i = 0; i < 8; ++i) n.v[i] *= factor;
-            s = widen(x);
+            s = widen(settle<T, kShort>(x, col, d));
 #pragma unroll
             for (int i = 0; i < 8; ++i) s.v[i] += gate.v[i] * n.v[i];
             clear_from(s, d - col);
             if (live) store_run<T>(j.S, row, col, d, s);
         } else {
-            s = widen(x);
+            s = widen(settle<T, kShort>(x, col, d));
         }
         if (j.before.kind == RSH_NORM_NONE) continue;
         const float2_t at = statistics<LANES, 1>(j.before, d, team, [&](int, int) { return s; });
-        if (leads && j.before.stats) *reinterpret_cast<float2_t*>(j.before.stats + 2 * row) = at;
+        if (leads && j.before.stats) *reinterpret_cast<float2_t*>(j.before.stats + 2 * row.row()) = at;
         second.apply(s, at);
         if (live) store_run<T>(j.Y, row, col, d, s);
     }
@@ -242,9 +257,10 @@ __global__ __launch_bounds__(LANES) __attribute__((amdgpu_waves_per_eu(4))) void
     const Random random(j.drop);
     const int d = (int)j.d;
     const float factor = j.drop.share ? j.scale * random.keep : j.scale;
-    for (int64_t row = blockIdx.x; row < j.t; row += gridDim.x) {
-        const void* const x_row = element(j.X, row * j.ld_x, kSize);
-        const void* const b_row = element(j.B, row * j.ld_b, kSize);
+    for (int64_t at = blockIdx.x; at < j.t; at += gridDim.x) {
+        const Place row = {at, 0};
+        const void* const x_row = row.of(j.X, j.ld_x, kSize);
+        const void* const b_row = row.of(j.B, j.ld_b, kSize);
         Raw<T> x[C ? C : 1], b[JOIN && C ? C : 1];
         Eight kept[C ? C : 1];
         if constexpr (C > 0) {
@@ -252,21 +268,21 @@ __global__ __launch_bounds__(LANES) __attribute__((amdgpu_waves_per_eu(4))) void
             each_run<LANES, C>(d, [&](int c, int col) { x[c] = load_raw<T, false>(x_row, col, d); });
         }
         float2_t after = {0.f, 1.f};
-        auto loaded = [&](int c, int col) { return widen(C ? b[c] : load_raw<T, false>(b_row, col, d)); };
+        auto loaded = [&](int c, int col) { return widen(settle<T, false>(C ? b[c] : load_raw<T, false>(b_row, col, d), col, d)); };
         if (JOIN && j.after.kind != RSH_NORM_NONE) {
             after = statistics<LANES, C>(j.after, d, team, loaded);
-            if (threadIdx.x == 0 && j.after.stats) *reinterpret_cast<float2_t*>(j.after.stats + 2 * row) = after;
+            if (threadIdx.x == 0 && j.after.stats) *reinterpret_cast<float2_t*>(j.after.stats + 2 * row.row()) = after;
         }
         auto sum = [&](int c, int col) {
-            Eight s = widen(C ? x[c] : load_raw<T, false>(x_row, col, d));
+            Eight s = widen(settle<T, false>(C ? x[c] : load_raw<T, false>(x_row, col, d), col, d));
             if constexpr (JOIN) {
                 Eight n = loaded(c, col);
                 if (j.after.kind != RSH_NORM_NONE) Affine<T, false>(j.after, col, d).apply(n, after);
-                if (j.drop.share) random.drop(n, col, row, factor);
+                if (j.drop.share) random.drop(n, col, row.row(), factor);
                 else
 #pragma unroll
                     for (int i = 0; i < 8; ++i) n.v[i] *= factor;
-                const Eight gate = parameters<T, false>(element(j.gate, row * j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d, 1.f);
+                const Eight gate = parameters<T, false>(row.of(j.gate, j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d, 1.f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s.v[i] += gate.v[i] * n.v[i];
                 clear_from(s, d - col);
@@ -284,7 +300,7 @@ __global__ __launch_bounds__(LANES) __attribute__((amdgpu_waves_per_eu(4))) void
         if (j.before.kind == RSH_NORM_NONE) continue;
         auto summed = [&](int c, int col) { return C ? kept[c] : sum(c, col); };
         const float2_t before = statistics<LANES, C>(j.before, d, team, summed);
-        if (threadIdx.x == 0 && j.before.stats) *reinterpret_cast<float2_t*>(j.before.stats + 2 * row) = before;
+        if (threadIdx.x == 0 && j.before.stats) *reinterpret_cast<float2_t*>(j.before.stats + 2 * row.row()) = before;
         each_run<LANES, C>(d, [&](int c, int col) {
             Eight y = summed(c, col);
             Affine<T, false>(j.before, col, d).apply(y, before);
@@ -351,6 +367,7 @@ template <class T>
 struct Inputs {
     Raw<T> x, b, ds, dy;
     float2_t before, after;        // m and r of S and of B
+    bool live;
 };
 
 // Gradients of a run of a row.
@@ -401,28 +418,24 @@ struct Backward {
           second(JOIN && join.after.kind != RSH_NORM_NONE) {}
 
     // Of a row.  live: it is one, else all of it counts as zero.
-    __device__ __forceinline__ Inputs<T> load(int64_t row, bool live, int col) const {
+    __device__ __forceinline__ Inputs<T> load(const Place& row, bool live, int col) const {
         Inputs<T> in = {};
-        const int end = live ? d : 0;      // what is loaded is zero from here on
-        auto run = [&](const void* p, int64_t ld) {
-            Raw<T> r = load_raw<T, SHORT>(element(p, row * ld, kSize), col, d);
-#pragma unroll
-            for (auto& v : r.v)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) v[w] = end ? v[w] : 0u;
-            return r;
-        };
+        in.live = live;
+        auto run = [&](const void* p, int64_t ld) { return load_raw<T, SHORT>(row.of(p, ld, kSize), col, d); };
         if (first) {
             in.dy = run(g.dY, g.ld_dy);
             in.x = run(j.X, j.ld_x);
-            if (live) in.before = *reinterpret_cast<const float2_t*>(j.before.stats + 2 * row);
+            in.before = *reinterpret_cast<const float2_t*>(j.before.stats + 2 * row.row());
         }
         if constexpr (JOIN) {
             in.b = run(j.B, j.ld_b);
-            if (second && live) in.after = *reinterpret_cast<const float2_t*>(j.after.stats + 2 * row);
+            if (second) in.after = *reinterpret_cast<const float2_t*>(j.after.stats + 2 * row.row());
             if (g.dS) in.ds = run(g.dS, g.ld_ds);
         }
         return in;
+    }
+    __device__ __forceinline__ Eight value(const Inputs<T>& in, const Raw<T>& r, int col) const {
+        return widen(settle<T, SHORT>(r, col, d, in.live));
     }
     // N1's result, after dropout but for its factor.
     __device__ __forceinline__ Eight inner(const Run& x, int col) const {
@@ -440,9 +453,9 @@ struct Backward {
     }
     __device__ __forceinline__ float factor() const { return j.drop.share ? j.scale * random.keep : j.scale; }
     // scale * gate, zero where dropped, times dropout's factor.
-    __device__ __forceinline__ Eight factors(const Run& x, int64_t row, int col) const {
+    __device__ __forceinline__ Eight factors(const Run& x, const Place& row, int col) const {
         Eight f;
-        if (j.ld_gate) f = load_vector<T, SHORT>(element(j.gate, row * j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d);
+        if (j.ld_gate) f = load_vector<T, SHORT>(row.of(j.gate, j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d);
         else f = given.gate_of(col);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f.v[i] *= factor();
@@ -452,28 +465,28 @@ struct Backward {
         }
         return f;
     }
-    __device__ __forceinline__ void store_gate(int64_t row, int col, const Eight& gate) const {
+    __device__ __forceinline__ void store_gate(const Place& row, int col, const Eight& gate) const {
         if (std::is_same<T, F32>::value || j.gate_type == RSH_F32) store_run<F32>(g.dgate, row, col, d, gate);
         else store_run<T>(g.dgate, row, col, d, gate);
     }
     // Up to the gradient of N2 and what its two means are of.
-    __device__ __forceinline__ void before(const Inputs<T>& in, int64_t row, int col, Run& x, SUMS& sums) const {
+    __device__ __forceinline__ void before(const Inputs<T>& in, const Place& row, int col, Run& x, SUMS& sums) const {
         if constexpr (JOIN) {
-            x.xb = widen(in.b);
+            x.xb = value(in, in.b, col);
             if (second) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x.xb.v[i] = (x.xb.v[i] - in.after[0]) * in.after[1];
             }
-            if (j.drop.share) x.kept = random.kept(col, row);
+            if (j.drop.share) x.kept = random.kept(col, row.row());
         }
         if (!first) return;
-        x.xh = widen(in.x);
+        x.xh = value(in, in.x, col);
         if constexpr (JOIN) {
             const Eight n = inner(x, col), f = factors(x, row, col);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x.xh.v[i] += f.v[i] * n.v[i];
         }
-        x.g = widen(in.dy);
+        x.g = value(in, in.dy, col);
         const Eight w = given.before_weight(col);
         Eight term;
 #pragma unroll
@@ -487,16 +500,16 @@ struct Backward {
         for (int i = 0; i < 8; ++i) x.g.v[i] *= w.v[i];
     }
     // The gradient of S, from the means of g and g xh.
-    __device__ __forceinline__ void sum(const Inputs<T>& in, float2_t mean, int valid, Run& x) const {
-        x.ds = widen(in.ds);
+    __device__ __forceinline__ void sum(const Inputs<T>& in, float2_t mean, int col, Run& x) const {
+        x.ds = g.dS ? value(in, in.ds, col) : Eight{};
         if (first) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x.ds.v[i] += in.before[1] * (x.g.v[i] - mean[0] - x.xh.v[i] * mean[1]);
         }
-        clear_from(x.ds, valid);
+        clear_from(x.ds, in.live ? d - col : 0);
     }
     // From there to the gradient of N1's result; returns what the gate's gradient gets.
-    __device__ __forceinline__ Eight through(const Inputs<T>&, int64_t row, int col, Run& x, SUMS& sums) const {
+    __device__ __forceinline__ Eight through(const Inputs<T>&, const Place& row, int col, Run& x, SUMS& sums) const {
         const Eight f = factors(x, row, col);
         Eight gate = {};
         if (g.dgate) {
@@ -524,7 +537,7 @@ struct Backward {
 // One pass over the rows, each in its lanes' registers, and the vectors' sums with it, a part of them from every workgroup.  The next
 // row is on its way while one is computed.
 template <class T, int LANES, bool JOIN, bool BIAS>
-__global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(4))) void rsh_join_backward_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts) {
+__global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(JOIN && LANES <= 64 ? 2 : 4))) void rsh_join_backward_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts) {
     constexpr int kThreads = kThreadsOf<LANES>, kRows = kRowsOf<LANES>;
     // Whether the registers hold the next row beside this one: a row takes about as long as its loads.
     constexpr bool kEarly = !JOIN || (size_of<T>() == 2 && !BIAS);
@@ -543,13 +556,14 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
     }();
     const int64_t step = (int64_t)gridDim.x * kRows;
     auto load = [&](int64_t head) {
-        const int64_t mine = row_of<LANES>(head);
-        return back.load(min(mine, j.t - 1), mine < j.t, col);
+        bool live;
+        const Place row = place_of<LANES>(head, j.t, &live);
+        return back.load(row, live, col);
     };
     Inputs<T> next = load((int64_t)blockIdx.x * kRows);
     for (int64_t head = (int64_t)blockIdx.x * kRows; head < j.t; head += step) {
-        const int64_t mine = row_of<LANES>(head), row = min(mine, j.t - 1);
-        const bool live = mine < j.t;
+        bool live;
+        const Place row = place_of<LANES>(head, j.t, &live);
         Inputs<T> in = next;
         if (kEarly && head + step < j.t) next = load(head + step);
         Run x;
@@ -563,7 +577,7 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
             mean = team.sum(a, b) * (1.f / (float)d);
             if (j.before.kind != RSH_NORM_LAYER) mean[0] = 0.f;
         }
-        back.sum(in, mean, live ? d - col : 0, x);
+        back.sum(in, mean, col, x);
         if (g.dX && live) store_run<T>(g.dX, row, col, d, x.ds);
         if constexpr (JOIN) {
             const Eight gate = back.through(in, row, col, x, sums);
@@ -615,7 +629,8 @@ __global__ __launch_bounds__(1024) void rsh_join_backward_long_kernel(rsh_join_t
     const Backward<T, JOIN, false, NoSums, LoadedParameters<T>> back(j, g, random, given);
     const int d = back.d;
     NoSums none;
-    for (int64_t row = blockIdx.x; row < j.t; row += gridDim.x) {
+    for (int64_t at = blockIdx.x; at < j.t; at += gridDim.x) {
+        const Place row = {at, 0};
         float2_t mean = {0.f, 0.f};
         Run x;
         if (back.first) {
@@ -627,13 +642,13 @@ __global__ __launch_bounds__(1024) void rsh_join_backward_long_kernel(rsh_join_t
             });
             mean = team.sum(a, b) * (1.f / (float)d);
             if (j.before.kind != RSH_NORM_LAYER) mean[0] = 0.f;
-            if (means && threadIdx.x == 0) *reinterpret_cast<float2_t*>(means + 2 * row) = mean;
+            if (means && threadIdx.x == 0) *reinterpret_cast<float2_t*>(means + 2 * at) = mean;
         }
         float a = 0.f, b = 0.f;
         each_run<1024, 0>(d, [&](int, int col) {
             const Inputs<T> in = back.load(row, true, col);
             back.before(in, row, col, x, none);
-            back.sum(in, mean, d - col, x);
+            back.sum(in, mean, col, x);
             if (g.dX) store_run<T>(g.dX, row, col, d, x.ds);
             if constexpr (JOIN) {
                 const Eight gate = back.through(in, row, col, x, none);
@@ -649,7 +664,7 @@ __global__ __launch_bounds__(1024) void rsh_join_backward_long_kernel(rsh_join_t
         each_run<1024, 0>(d, [&](int, int col) {
             const Inputs<T> in = back.load(row, true, col);
             back.before(in, row, col, x, none);
-            back.sum(in, mean, d - col, x);
+            back.sum(in, mean, col, x);
             (void)back.through(in, row, col, x, none);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x.gb.v[i] = in.after[1] * (x.gb.v[i] - inner[0] - x.xb.v[i] * inner[1]);
@@ -668,12 +683,13 @@ __global__ __launch_bounds__(256) void rsh_join_columns_kernel(rsh_join_t j, rsh
     const int col = 8 * (int)(blockIdx.x * 256 + threadIdx.x);
     if (col >= back.d) return;
     RegisterSums sums;
-    for (int64_t row = blockIdx.y; row < j.t; row += gridDim.y) {
+    for (int64_t at = blockIdx.y; at < j.t; at += gridDim.y) {
+        const Place row = {at, 0};
         Run x;
         const Inputs<T> in = back.load(row, true, col);
         back.before(in, row, col, x, sums);
         if constexpr (JOIN) {
-            back.sum(in, back.first ? *reinterpret_cast<const float2_t*>(means + 2 * row) : (float2_t){0.f, 0.f}, back.d - col, x);
+            back.sum(in, back.first ? *reinterpret_cast<const float2_t*>(means + 2 * at) : (float2_t){0.f, 0.f}, col, x);
             (void)back.through(in, row, col, x, sums);
         }
     }

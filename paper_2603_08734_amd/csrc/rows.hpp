@@ -50,9 +50,9 @@ __device__ __forceinline__ const uint8_t* byte_of(const void* row, uint32_t at) 
     return (const uint8_t*)row + at;
 }
 
-// Elements col .. col + 7 of a row of d that begins at `row`, zeros from d on.  Every lane makes the same whole loads, the last of a row that
+// Elements col .. col + 7 of a row of d, to be settled before they are used.  Every lane makes the same whole loads, the last of a row that
 // is no multiple of eight from where the row's last eight lie: a load under a condition of its own would have to arrive before the two
-// ways meet again, and no two would be under way at once.  SHORT: the row may have less than eight.
+// ways meet again, and one whose result is looked at here before the next goes out.  SHORT: the row may have less than eight.
 template <class T, bool SHORT>
 __device__ __forceinline__ Raw<T> load_raw(const void* row, int col, int d) {
     constexpr int N = size_of<T>() / 2;
@@ -67,15 +67,20 @@ __device__ __forceinline__ Raw<T> load_raw(const void* row, int col, int d) {
         }
         return r;
     }
-    const int at = min(col, d - 8);
-    const uint8_t* const p = byte_of(row, (uint32_t)at * (uint32_t)size_of<T>());
+    const uint8_t* const p = byte_of(row, (uint32_t)min(col, d - 8) * (uint32_t)size_of<T>());
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if constexpr (std::is_same<T, F32>::value) r.v[i] = *reinterpret_cast<const uint4_a4*>(p + 16 * i);
         else r.v[i] = *reinterpret_cast<const uint4_a2*>(p);
     }
-    if (d & 7) {
-        const int past = min(col - at, 8);
+    return r;
+}
+// The same in their places, zeros from d on, and nothing but zeros in a lane that is not `live`.
+template <class T, bool SHORT>
+__device__ __forceinline__ Raw<T> settle(Raw<T> r, int col, int d, bool live = true) {
+    constexpr int N = size_of<T>() / 2;
+    if ((d & 7) && !(SHORT && d < 8)) {
+        const int past = min(max(col - (d - 8), 0), 8);
         if (past) {
             if constexpr (std::is_same<T, F32>::value) {
                 if (past & 4) r.v[0] = r.v[1], r.v[1] = (uint4_t){0, 0, 0, 0};
@@ -90,10 +95,11 @@ __device__ __forceinline__ Raw<T> load_raw(const void* row, int col, int d) {
             }
         }
     }
+    const bool in = live && col < d;
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) r.v[i][w] = col < d ? r.v[i][w] : 0u;
+        for (int w = 0; w < 4; ++w) r.v[i][w] = in ? r.v[i][w] : 0u;
     return r;
 }
 

@@ -15,7 +15,7 @@ from . import binding
 from .mx4 import _TYPES, _on, _rows, _tangent
 
 _FORWARD_MODE = "dropout and joins have no forward-mode derivative: call them on detached operands"
-MOST = (1 << 31) - 1       # elements from row to row
+MOST = binding.RSH_ROWS_MAX_STRIDE       # elements from row to row; rows further apart are copied
 
 
 class Drop:
