@@ -623,30 +623,37 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
         for (int i = 0; i < 4; ++i) f.token[i] = order.token[min(i0 + 4 * g + i, end - 1)];
         return f;
     };
-    auto load = [&](const Four& f, int i0) {
+    auto load = [&](const Four& f) {       // of tokens behind the last: the last, which counts as zeros when it is used
         Slab s;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bool in = i0 + 4 * g + i < end;
             const int64_t token = f.token[i];
             if (whole) s.x[i] = *reinterpret_cast<const uint4_a2*>(X + token * ld_x + col);
             else s.x[i] = run_of(X + token * ld_x, col, k);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) s.x[i][w] = in ? s.x[i][w] : 0u;
-#pragma unroll
-            for (int j = 0; j < RT; ++j) s.h[j][i] = in && r0 + 16 * j < r16 ? H[token * r16 + r0 + 16 * j + c] : 0.f;
+            for (int j = 0; j < RT; ++j) s.h[j][i] = H[token * r16 + min(r0 + 16 * j, r16 - 16) + c];
         }
         return s;
     };
     const int first = begin + 16 * wave;
     if (first < end) {
-        Slab next = load(find(first), first);
+        Slab next = load(find(first));
         Four after = find(first + 16 * WAVES);
         for (int i0 = first; i0 < end; i0 += 16 * WAVES) {
-            const Slab s = next;
+            Slab s = next;
             if (i0 + 16 * WAVES < end) {
-                next = load(after, i0 + 16 * WAVES);
+                next = load(after);
                 after = find(i0 + 32 * WAVES);
+            }
+            if (i0 + 16 > end) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool in = i0 + 4 * g + i < end;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) s.x[i][w] = in ? s.x[i][w] : 0u;
+#pragma unroll
+                    for (int j = 0; j < RT; ++j) s.h[j][i] = in ? s.h[j][i] : 0.f;
+                }
             }
             Fours<T> f;
             f.from(s.x);
