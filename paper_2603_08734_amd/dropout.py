@@ -18,6 +18,9 @@ _FORWARD_MODE = "dropout and joins have no forward-mode derivative: call them on
 MOST = binding.RSH_ROWS_MAX_STRIDE       # elements from row to row; rows further apart are copied
 
 
+NOTHING = binding.rsh_drop_t()      # no dropout, as part of other structures
+
+
 class Drop:
     """p: share that is dropped, 0 .. 1.  seed: an integer, or an int64 tensor of one element on the operands' GPU, read when the kernels
     run (a captured graph draws new numbers when the program changes it between replays; changing it between a forward pass and its
@@ -44,7 +47,7 @@ class Drop:
 def _struct(drop, device: int):
     """The library's description; no dropout where there is none."""
     if drop is None:
-        return binding.rsh_drop_t()
+        return NOTHING
     seed = drop.tensor
     if seed is None:
         return binding.rsh_drop_t(drop.seed, drop.offset, None, drop.share)

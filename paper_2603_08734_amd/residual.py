@@ -15,7 +15,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding
-from .dropout import _FORWARD_MODE, MOST, Drop, _struct
+from .dropout import _FORWARD_MODE, MOST, NOTHING, Drop, _struct
 from .mx4 import _TYPES, _on, _rows, _tangent
 
 _DROPS = (type(None), Drop)
@@ -39,16 +39,13 @@ class Norm:
 _NORMS = (type(None), Norm)
 
 
-def _vector(v):
-    """(address, type) of a parameter, which is contiguous or None."""
-    return (None, 0) if v is None else (v.data_ptr(), _TYPES[v.dtype])
+_NO_NORM = binding.rsh_norm_t()
 
 
 def _norm_struct(kind: int, eps: float, weight, bias, stats):
-    if not kind:
-        return binding.rsh_norm_t()
-    (w, wt), (b, bt) = _vector(weight), _vector(bias)
-    return binding.rsh_norm_t(w, b, stats, wt, bt, kind, eps)
+    """Of a norm whose parameters are contiguous or None."""
+    return binding.rsh_norm_t(None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), stats,
+                              0 if weight is None else _TYPES[weight.dtype], 0 if bias is None else _TYPES[bias.dtype], kind, eps)
 
 
 class _Plan:
@@ -64,16 +61,24 @@ class _Plan:
 
 def _describe(plan, X, B, gate, aw, ab, bw, bb, S, Y, stats, t, d, device):
     """The library's structure, and what has to live until the launch.  X may be None in a backward pass."""
-    x, ld_x = _rows(X, MOST) if X is not None else (None, 0)
-    b, ld_b = _rows(B, MOST) if B is not None else (None, 0)
-    g, ld_g = (None, 0) if gate is None else (gate, 0) if gate.dim() == 1 else _rows(gate, MOST)
-    first = second = None
+    x = b = g = first = second = at_x = at_b = at_g = None
+    ld_x = ld_b = ld_g = g_type = 0
+    if X is not None:
+        x, ld_x = _rows(X, MOST)
+        at_x = x.data_ptr()
+    if B is not None:
+        b, ld_b = _rows(B, MOST)
+        at_b = b.data_ptr()
+    if gate is not None:
+        g, ld_g = (gate, 0) if gate.dim() == 1 else _rows(gate, MOST)
+        at_g, g_type = g.data_ptr(), _TYPES[g.dtype]
     if stats is not None:
         first = stats.data_ptr()
         second = first + 8 * t if plan.after and plan.before else first
-    join = binding.rsh_join_t(binding._address(x), binding._address(b), binding._address(g), binding._address(S), binding._address(Y), t, d, ld_x, ld_b,
-                              ld_g, _norm_struct(plan.after, plan.after_eps, aw, ab, first), _norm_struct(plan.before, plan.before_eps, bw, bb, second),
-                              _struct(plan.drop, device), _TYPES[(X if B is None else B).dtype], 0 if g is None else _TYPES[g.dtype], plan.scale)
+    join = binding.rsh_join_t(at_x, at_b, at_g, None if S is None else S.data_ptr(), None if Y is None else Y.data_ptr(), t, d, ld_x, ld_b, ld_g,
+                              _norm_struct(plan.after, plan.after_eps, aw, ab, first) if plan.after else _NO_NORM,
+                              _norm_struct(plan.before, plan.before_eps, bw, bb, second) if plan.before else _NO_NORM,
+                              NOTHING if plan.drop is None else _struct(plan.drop, device), _TYPES[(X if B is None else B).dtype], g_type, plan.scale)
     return join, (x, b, g)
 
 
@@ -94,34 +99,33 @@ def _forward(plan, X, B, gate, aw, ab, bw, bb, keep):
 def _backward(ctx, *grads):
     plan, want = ctx.plan, ctx.needs_input_grad
     X, B, gate, aw, ab, bw, bb, stats, seed = ctx.saved_tensors
-    grads = list(grads)
-    dS = grads.pop(0) if B is not None else None
-    dY = grads.pop(0) if plan.before else None
-    if dS is None and dY is None:
+    dS = grads[0] if B is not None else None
+    dY = grads[-1] if plan.before else None
+    like = dY if dS is None else dS
+    if like is None:
         return (None,) * 9
     if _tangent(*(g for g in (dS, dY) if g is not None)):
         raise ValueError(_FORWARD_MODE)
-    like = dS if dS is not None else dY
     t, d = like.shape
-    none = [None] * 9
-    wanted = dict(zip(("X", "B", "gate", "aw", "ab", "bw", "bb"), want[1:8]))
-    dX = like.new_empty((t, d)) if wanted["X"] else None
-    dB = like.new_empty((t, d)) if wanted["B"] else None
-    dgate = torch.empty(gate.shape, dtype=gate.dtype, device=gate.device) if wanted["gate"] else None
-    vectors = {n: torch.empty_like(v) if wanted[n] and (n in ("aw", "ab") or dY is not None) else None
-               for n, v in (("aw", aw), ("ab", ab), ("bw", bw), ("bb", bb))}
-    count = sum(v is not None for v in vectors.values()) + (dgate is not None and gate.dim() == 1)
-    none[1:8] = [dX, dB, dgate, *vectors.values()]
-    if all(g is None for g in none):
-        return tuple(none)
+    dX = like.new_empty((t, d)) if want[1] else None
+    dB = like.new_empty((t, d)) if want[2] else None
+    dgate = torch.empty(gate.shape, dtype=gate.dtype, device=gate.device) if want[3] else None
+    daw = torch.empty_like(aw) if want[4] else None
+    dab = torch.empty_like(ab) if want[5] else None
+    dbw = torch.empty_like(bw) if want[6] and dY is not None else None
+    dbb = torch.empty_like(bb) if want[7] and dY is not None else None
+    vectors = (daw is not None) + (dab is not None) + (dbw is not None) + (dbb is not None) + (dgate is not None and gate.dim() == 1)
+    out = (None, dX, dB, dgate, daw, dab, dbw, dbb, None)
+    if not vectors and dX is None and dB is None and dgate is None:
+        return out
     ds, ld_ds = _rows(dS, MOST) if dS is not None else (None, 0)
     dy, ld_dy = _rows(dY, MOST) if dY is not None else (None, 0)
-    a = binding._address
-    with _on(like.get_device()):
-        join, alive = _describe(plan, X, B, gate, aw, ab, bw, bb, None, None, stats, t, d, like.get_device())
-        gradients = binding.rsh_join_gradients_t(a(ds), a(dy), a(dX), a(dB), a(dgate), *(a(v) for v in vectors.values()), None, ld_ds, ld_dy)
-        binding.join_backward(join, gradients, count, like)
-    return tuple(none)
+    at, device = binding._address, like.get_device()
+    with _on(device):
+        join, alive = _describe(plan, X, B, gate, aw, ab, bw, bb, None, None, stats, t, d, device)
+        gradients = binding.rsh_join_gradients_t(at(ds), at(dy), at(dX), at(dB), at(dgate), at(daw), at(dab), at(dbw), at(dbb), None, ld_ds, ld_dy)
+        binding.join_backward(join, gradients, vectors, like)
+    return out
 
 
 _backward_once = once_differentiable(_backward)
