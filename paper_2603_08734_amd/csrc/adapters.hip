@@ -14,7 +14,7 @@ namespace rsh {
 
 namespace {
 
-constexpr int kFewTokens = 256, kFewTile = 16, kFewParts = 8, kFewColumns = 1024, kTile = 64;
+constexpr int kFewTokens = 256, kFewTile = 16, kFewParts = 8, kFewColumns = 1024, kTile = 64, kShares = 2;     // kShares: workgroups of the second product that share a tile
 constexpr int kSortThreads = 1024, kSortWords = 7 * (RSH_ADAPTERS_MAX + 1);     // counters in LDS
 
 struct Tile {
@@ -84,14 +84,14 @@ struct Members {
     __device__ __forceinline__ int at(int i) const { return token[min(i, count - 1)]; }
 };
 template <bool FEW>
-__device__ __forceinline__ bool members(const Index& index, const Order& order, int64_t t, int* place, Members<FEW>* m) {
+__device__ __forceinline__ bool members(const Index& index, const Order& order, int64_t t, int at, int* place, Members<FEW>* m) {
     if constexpr (FEW) {
-        m->adapter = few_tile(index, (int)t, (int)blockIdx.x, *reinterpret_cast<FewPlace*>(place), &m->count);
+        m->adapter = few_tile(index, (int)t, at, *reinterpret_cast<FewPlace*>(place), &m->count);
         m->token = place + kFewTokens + 4;
         return m->adapter >= 0;
     } else {
-        if ((int)blockIdx.x >= *order.n_tiles) return false;
-        const Tile tile = order.tiles[blockIdx.x];
+        if (at >= *order.n_tiles) return false;
+        const Tile tile = order.tiles[at];
         m->adapter = tile.adapter;
         m->count = tile.count;
         m->token = order.token + tile.first;
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const u
     __shared__ int place[FEW ? sizeof(FewPlace) / sizeof(int) : 1];
     __shared__ float4_t joined[WAVES][TT][64];
     Members<FEW> tile;
-    if (!members<FEW>(index, order, t, place, &tile) || tile.adapter == index.n) return;
+    if (!members<FEW>(index, order, t, (int)blockIdx.x, place, &tile) || tile.adapter == index.n) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
     const int r0 = 16 * RT * (int)blockIdx.y, r16 = (r + 15) / 16 * 16, tiles = (tile.count + 15) / 16;
     const uint16_t* a[RT];
@@ -346,17 +346,30 @@ struct Fours {
 // results of 16 columns by 16 tokens; which eight is chosen so that lanes store pieces of a row that lie side by side.  The sums of all tokens
 // of a tile stay in registers while B goes by once, 16 rows at a time and the next 16 on their way.
 template <class T, bool FEW>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void rsh_adapters_expand_kernel(const uint16_t* Y, int64_t ld_y, const float* H,
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void rsh_adapters_expand_kernel(const uint16_t* Y, int64_t ld_y, const float* H,
                                                                                                          int parts, const uint16_t* B, const float* scales,
                                                                                                          Index index, Order order, uint16_t* out, int64_t t,
                                                                                                          int64_t m, int r) {
-    constexpr int kGroups = (FEW ? kFewTile : kTile) / 16;
+    constexpr int kGroups = (FEW ? kFewTile : kTile / kShares) / 16;
+    constexpr int kBlocks = FEW ? 1 : 8;       // of 16 ranks, whose H is in LDS at once
+    struct Pair {
+        uint2_t hi, lo;
+    };
     __shared__ int place[FEW ? sizeof(FewPlace) / sizeof(int) : 1];
+    // H of the tile as the matrix unit takes it, which the four waves share: read by each for itself it was as many requests as Y.
+    __shared__ __attribute__((aligned(16))) Pair shared[FEW ? 1 : kBlocks][FEW ? 1 : kGroups][64];
     Members<FEW> tile;
-    if (!members<FEW>(index, order, t, place, &tile)) return;
+    if (!members<FEW>(index, order, t, (int)(FEW ? blockIdx.x : blockIdx.x / kShares), place, &tile)) return;
+    if constexpr (!FEW) {
+        const int first = 16 * kGroups * ((int)blockIdx.x % kShares);
+        if (first >= tile.count) return;
+        tile.token += first;
+        tile.count = min(tile.count - first, 16 * kGroups);
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15, r16 = (r + 15) / 16 * 16;
     const int64_t col0 = 512 * (int64_t)blockIdx.y + 128 * wave;
-    if (col0 >= m) return;
+    if (FEW && col0 >= m) return;
+    const bool active = col0 < m;
     const bool some = tile.adapter < index.n;
     const int64_t col = col0 + 8 * (4 * (c & 3) + (c >> 2));
     // Whole pieces of eight columns where m has them: a load under a condition of its own would have to arrive before the next goes out.
@@ -378,14 +391,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
         }
         return v;
     };
-    const Four head = read(token[0]);
+    Four head = {};
+    if (active) head = read(token[0]);
     float4_t acc[kGroups][8] = {};
     if (some) {
         const float scale = scales ? scales[tile.adapter] : 1.f;
         const uint16_t* const b = B + (int64_t)tile.adapter * r * m;
         struct Slab {
             uint4_t rows[4];
-            float4_t h[kGroups];
         };
         auto load = [&](int rank) {
             Slab v;
@@ -395,50 +408,66 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void r
                 if (whole) v.rows[s] = *reinterpret_cast<const uint4_a2*>(b + (int64_t)min(row, r - 1) * m + col);
                 else v.rows[s] = run_of(b + (int64_t)min(row, r - 1) * m, col, m);
             }
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i) {
-                const float* const p = H + token[i] * r16 + rank + 4 * g;
-                if constexpr (FEW) {
-                    float4_t part[kFewParts];
-#pragma unroll
-                    for (int q = 0; q < kFewParts; ++q) part[q] = *reinterpret_cast<const float4_t*>(p + (int64_t)min(q, parts - 1) * t * r16);
-                    v.h[i] = part[0];
-#pragma unroll
-                    for (int q = 1; q < kFewParts; ++q)
-                        if (q < parts) v.h[i] += part[q];
-                } else {
-                    v.h[i] = *reinterpret_cast<const float4_t*>(p);
-                }
-            }
             return v;
         };
-        Slab next = load(0);
-        for (int rank = 0; rank < r16; rank += 16) {
-            Slab v = next;
-            if (rank + 16 < r16) next = load(rank + 16);
+        // H of four ranks of a token, from its parts where there are any.
+        auto pair_of = [&](int64_t row, int rank) {
+            const float* const p = H + row * r16 + rank + 4 * g;
+            float4_t h = *reinterpret_cast<const float4_t*>(p);
+            if constexpr (FEW) {
+                float4_t part[kFewParts];
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+                for (int q = 1; q < kFewParts; ++q) part[q] = *reinterpret_cast<const float4_t*>(p + (int64_t)min(q, parts - 1) * t * r16);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v.rows[s][w] = rank + 4 * g + s < r ? v.rows[s][w] : 0u;
-            Fours<T> f;
-            f.from(v.rows);
+                for (int q = 1; q < kFewParts; ++q)
+                    if (q < parts) h += part[q];
+            }
+            const float hv[4] = {h[0] * scale, h[1] * scale, h[2] * scale, h[3] * scale};
+            const Halves two = halves(hv);
+            return Pair{two.hi, two.lo};
+        };
+        Slab next = {};
+        if (active) next = load(0);
+        for (int rank0 = 0; rank0 < r16; rank0 += 16 * kBlocks) {
+            const int last = min(r16, rank0 + 16 * kBlocks);
+            if constexpr (!FEW) {
+                if (rank0) __syncthreads();
+                const int group = wave % kGroups;
+                const int64_t row = tile.at(16 * group + c);
+                for (int rank = rank0 + 16 * (wave / kGroups); rank < last; rank += 16 * (4 / kGroups))
+                    shared[(rank - rank0) / 16][group][lane] = pair_of(row, rank);
+                __syncthreads();
+            }
+            if (!active) continue;
+            for (int rank = rank0; rank < last; rank += 16) {
+                Slab v = next;
+                if (rank + 16 < r16) next = load(rank + 16);
 #pragma unroll
-            for (int i = 0; i < kGroups; ++i) {
-                if (16 * i >= tile.count) break;
-                const float hv[4] = {v.h[i][0] * scale, v.h[i][1] * scale, v.h[i][2] * scale, v.h[i][3] * scale};
-                const Halves k = halves(hv);
+                for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    acc[i][q] = multiply(f.main[q], k.hi, acc[i][q]);
-                    acc[i][q] = multiply(f.main[q], k.lo, acc[i][q]);
-                    if constexpr (std::is_same<T, F16>::value) {
-                        acc[i][q] = multiply(f.rest[q], k.hi, acc[i][q]);
-                        acc[i][q] = multiply(f.rest[q], k.lo, acc[i][q]);
+                    for (int w = 0; w < 4; ++w) v.rows[s][w] = rank + 4 * g + s < r ? v.rows[s][w] : 0u;
+                Fours<T> f;
+                f.from(v.rows);
+#pragma unroll
+                for (int i = 0; i < kGroups; ++i) {
+                    if (16 * i >= tile.count) break;
+                    Pair k;
+                    if constexpr (FEW) k = pair_of(token[i], rank);
+                    else k = shared[(rank - rank0) / 16][i][lane];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        acc[i][q] = multiply(f.main[q], k.hi, acc[i][q]);
+                        acc[i][q] = multiply(f.main[q], k.lo, acc[i][q]);
+                        if constexpr (std::is_same<T, F16>::value) {
+                            acc[i][q] = multiply(f.rest[q], k.hi, acc[i][q]);
+                            acc[i][q] = multiply(f.rest[q], k.lo, acc[i][q]);
+                        }
                     }
                 }
             }
         }
     }
+    if (!active) return;
     // the others all at once, in registers that B no longer needs
     Four y[kGroups];
     y[0] = head;
@@ -472,7 +501,7 @@ __global__ __launch_bounds__(1024) void rsh_adapters_few_kernel(const uint16_t* 
     __shared__ float4_t joined[RT][kWaves][64];
     __shared__ float4_t sums[RT][64];      // as a lane of the matrix unit has them: token lane % 16, ranks 4 (lane / 16) .. + 3
     Members<true> tile;
-    if (!members<true>(index, Order{}, t, place, &tile)) return;
+    if (!members<true>(index, Order{}, t, (int)blockIdx.x, place, &tile)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
     const bool some = tile.adapter < index.n;
     const int64_t col0 = kFewColumns * (int64_t)blockIdx.y + 128 * wave, col = col0 + 8 * (4 * (c & 3) + (c >> 2)), token = tile.at(c);
@@ -804,7 +833,7 @@ template <class T>
 void expand(const rsh_adapters_t& a, bool few, const void* Y, int64_t ld, const float* H, int parts, const void* B, const Order& order, void* out,
             int64_t m, hipStream_t st) {
     const Index index = {a.index, a.index_size == 8, a.n};
-    const dim3 grid((unsigned)(few ? a.t : most_tiles(a.t, a.n)), (unsigned)((m + 511) / 512));
+    const dim3 grid((unsigned)(few ? a.t : kShares * most_tiles(a.t, a.n)), (unsigned)((m + 511) / 512));
     if (few)
         hipLaunchKernelGGL((rsh_adapters_expand_kernel<T, true>), grid, dim3(256), 0, st, (const uint16_t*)Y, ld, H, parts, (const uint16_t*)B, a.scales,
                            index, order, (uint16_t*)out, a.t, m, a.r);
