@@ -2,6 +2,8 @@
 
     H = ffn.gated(X, W_gate, W_up, "silu")     # binary16 or bfloat16, X [..., d], weights [f, d]; autograd-aware (reverse mode)
     H = ffn.gated(X, Wg4, Wu4, "silu")         # the weights in 4 bits (mx4.quantize), for serving
+    Y = ffn.FeedForward(Wg4, Wu4, Wd4)(X)      # the layer as it is served, with adapters beside its projection back if wanted
+    S = ffn.Block(layer, norm)(X)              # and between its norm and its residual
 
 Both projections, the activation and the product run as one kernel (``rsh_gated_forward``): sums are fp32 until H is rounded.
 A forward pass that will be differentiated keeps both projections in fp32; the backward pass
@@ -13,7 +15,7 @@ from __future__ import annotations
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import binding
+from . import adapters, binding, residual
 from .binding import Plan
 from .mx4 import HALVES, Mx4, _no_gradient, _on, _rows, _tangent, product
 
@@ -116,27 +118,57 @@ class FeedForward:
 
     W_gate, W_up: [f, d] of the activations' type, or in 4 bits (``mx4.quantize``).  W_down: [d, f] in 4 bits, or a ``Plan`` of the
     pruned weight for exactly as many tokens as X has (binary16: the sparse product takes the tokens as columns).  Either way the layer
-    has no gradient, and operands that want one are refused while gradients are recorded."""
+    has no gradient, and operands that want one are refused while gradients are recorded.
 
-    def __init__(self, W_gate, W_up, W_down, activation: str = "silu"):
+    adapters: (A [n, r, f], B [n, r, d], scales or None), low-rank adapters beside the projection back (``adapters.add``); a call then says
+    which of them every token has."""
+
+    def __init__(self, W_gate, W_up, W_down, activation: str = "silu", adapters=None):
         if not isinstance(W_down, (Mx4, Plan)):
             raise TypeError(f"W_down: expected Mx4 or Plan, got {type(W_down)}")
         shape = (W_down.n_rows, W_down.n_cols) if isinstance(W_down, Plan) else W_down.shape
         if len(W_gate.shape) != 2 or shape[1] != W_gate.shape[0]:
             raise ValueError(f"W_gate {tuple(W_gate.shape)} and W_down {shape}: expected [f, d] and [d, f]")
-        self.W_gate, self.W_up, self.W_down, self.activation = W_gate, W_up, W_down, activation
+        if adapters is not None:
+            A, B, _ = adapters
+            if A.dim() != 3 or B.dim() != 3 or A.shape[:2] != B.shape[:2] or A.shape[2] != shape[1] or B.shape[2] != shape[0]:
+                raise ValueError(f"adapters: A {tuple(A.shape)} and B {tuple(B.shape)} beside W_down {shape}: expected [n, r, f] and [n, r, d]")
+        self.W_gate, self.W_up, self.W_down, self.activation, self.adapters = W_gate, W_up, W_down, activation, adapters
 
-    def __call__(self, X):
-        """X: [t, d]; result [t, d] of its type, from a ``Plan`` the transposed view of a [d, t] matrix."""
+    def __call__(self, X, index=None):
+        """X: [t, d]; index: [t], the adapter of every token (another number for none), where the layer has adapters.  Result [t, d] of X's
+        type, from a ``Plan`` without adapters the transposed view of a [d, t] matrix."""
         if not isinstance(X, torch.Tensor) or X.dim() != 2:
             raise ValueError(f"X: expected a matrix, got {tuple(X.shape) if isinstance(X, torch.Tensor) else type(X)}")
         if isinstance(self.W_down, Plan) and (X.dtype != torch.float16 or X.shape[0] != self.W_down.N):
             raise ValueError(f"the plan is for {self.W_down.N} tokens of binary16, got {X.shape[0]} of {X.dtype}")
-        _no_gradient(*(m for m in (X, self.W_gate, self.W_up) if isinstance(m, torch.Tensor)))
+        if (index is None) != (self.adapters is None):
+            raise ValueError("index: expected one with a layer that has adapters, and none with another")
+        _no_gradient(*(m for m in (X, self.W_gate, self.W_up, *(self.adapters or ())) if isinstance(m, torch.Tensor)))
         H = gated(X, self.W_gate, self.W_up, self.activation)
         if isinstance(self.W_down, Mx4):
-            return product(H, self.W_down)
-        Y = torch.empty((self.W_down.n_rows, self.W_down.N), dtype=torch.float16, device=H.device)
-        with _on(H.get_device()):
-            self.W_down.spmm_f16(H.t().contiguous(), Y)
-        return Y.t()
+            Y = product(H, self.W_down)
+        else:
+            Y = torch.empty((self.W_down.n_rows, self.W_down.N), dtype=torch.float16, device=H.device)
+            with _on(H.get_device()):
+                self.W_down.spmm_f16(H.t().contiguous(), Y)
+            Y = Y.t()
+        return Y if index is None else adapters.add(Y, H, self.adapters[0], self.adapters[1], index, self.adapters[2])
+
+
+class Block:
+    """A layer between the edges of its residual block, as it is served: S = X + scale * gate * after(layer(before(X))).
+
+    layer: a ``FeedForward``, or anything else that is called with a matrix [t, d] (and the adapters' index, where one is given) and returns one.
+    before, after: ``residual.Norm`` or None; gate: [d] or [t, d], None for ones."""
+
+    def __init__(self, layer, before=None, after=None, gate=None, scale: float = 1.0):
+        self.layer, self.before, self.after, self.gate, self.scale = layer, before, after, gate, scale
+
+    def __call__(self, X, index=None, following=None, normed=None):
+        """S, or with ``following`` (the next block's norm before it) the pair (S, following(S)), one kernel for both.  normed: before(X),
+        where the block before has formed it that way."""
+        if normed is None:
+            normed = X if self.before is None else residual.norm(X, self.before)
+        B = self.layer(normed) if index is None else self.layer(normed, index)
+        return residual.join(X, B, after=self.after, gate=self.gate, scale=self.scale, before=following)
