@@ -354,7 +354,7 @@ int rsh_dropout(const void *X_dev, int32_t type, int64_t t, int64_t d, int64_t l
  *   ld_x, ld_b   elements from row to row, at most RSH_ROWS_MAX_STRIDE like all such here; no alignment beyond the element's
  *   gate         [d] (ld_gate 0) or [t][d] with rows ld_gate apart; NULL (ld_gate 0) for ones
  *   S            [t][d] without gaps, not X or B; NULL if and only if B is
- *   Y            [t][d] without gaps; NULL if and only if before.kind is RSH_NORM_NONE
+ *   Y            [t][d] without gaps, none of the others; NULL if and only if before.kind is RSH_NORM_NONE
  * Everything is fp32 until it is stored: Y is the norm of the sum, not of the rounded S.  A row's differences from its mean are formed
  * in fp32; squares may leave its range.
  * rsh_join_backward: dS and dY (rows ld_ds and ld_dy apart; NULL for zeros) are the gradients of S and Y.  It reads X (where dY is there), B,
@@ -362,7 +362,7 @@ int rsh_dropout(const void *X_dev, int32_t type, int64_t t, int64_t d, int64_t l
  * without gaps), gradients of the parameters in their types.  work: 16-byte aligned, of the bytes that rsh_join_backward_work reports,
  * rewritten by every call (0: may be NULL); vectors: how many results are [d].
  * Results never depend on the order in which waves run.  RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride,
- * alignment or number out of range (eps is positive and finite), RSH_ERR_TOO_LARGE for a d above RSH_FFN_MAX_WIDTH.
+ * alignment or number out of range (eps is a finite normal number above 0), RSH_ERR_TOO_LARGE for a d above RSH_FFN_MAX_WIDTH.
  */
 enum { RSH_NORM_NONE = 0, RSH_NORM_RMS = 1, RSH_NORM_LAYER = 2 };
 typedef struct {

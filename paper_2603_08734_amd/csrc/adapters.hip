@@ -4,8 +4,15 @@
 //   shrink   H = X A_i^T, and dH = dout B_i^T      long rows against r short ones: matrix instructions of 16 bits
 //   expand   out = Y + s H B_i, and dX = s dH A_i   r terms for every element: H is fp32, so are the matrix instructions
 //   outer    dA_i = s dH^T X, and dB_i = s H^T dout    the tokens of an adapter summed up, in fp32 again
-// Tokens are taken in tiles that share an adapter.  A kernel of one workgroup deals them out; a few tokens are dealt out by every
-// workgroup for itself, which saves a launch.
+// Tokens are taken in tiles that share an adapter.  A kernel of one workgroup deals them out (8 to 9 us for 4096 tokens, all of it latency; it is
+// kept for the gradients); a few tokens are dealt out by every workgroup for itself, which saves a launch.
+//
+// Ranks are small, so all three are passes over X, Y and dout, bound by memory; operands go from memory to the matrix unit through registers
+// alone, a step ahead of their use.  Measured (bfloat16): 4096 tokens of 28672 features at rank 16, shrink 59 us (235 MB, 4.0 TB/s),
+// expand to 8192 columns 33 us (134 MB, 4.1); 4096 tokens at rank 64 between 4096 and 16384 features: shrink 16.5 and 48 us, expand 20.5
+// and 80, outer 24 and 46 (a copy of the bytes would take 7, 26, 7, 53, 7 and 26): what counts there is the time until a workgroup's first
+// loads have come, since all of them fit the chip at once or nearly so.  One token at rank 16 between 8192 and 28672 features 13.6 us in one
+// launch, 7.0 at 1024 features: one compute unit's reading of A, 35 KB a us; 77 tokens of 61 adapters at 4100 by 1003 11.1 us.
 #include <algorithm>
 
 #include "rows.hpp"
@@ -214,7 +221,7 @@ __global__ __launch_bounds__(kSortThreads) void rsh_adapters_sort_kernel(Index i
 
 // H of a tile's tokens and 16 RT ranks, over a part of k.  WAVES waves share the part.
 template <class T, int RT, int TT, bool FEW, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void rsh_adapters_shrink_kernel(const uint16_t* X, int64_t ld_x, const uint16_t* A, Index index, Order order,
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4 : RT == 2 ? 3 : 2))) void rsh_adapters_shrink_kernel(const uint16_t* X, int64_t ld_x, const uint16_t* A, Index index, Order order,
                                                                          float* H, int64_t t, int64_t k, int r, int steps) {
     __shared__ int place[FEW ? sizeof(FewPlace) / sizeof(int) : 1];
     __shared__ float4_t joined[WAVES][TT][64];
@@ -776,8 +783,9 @@ struct Sorted {
     }
 };
 
-// Whether a few tokens go in one launch: all workgroups read A once more for every 1024 columns, from caches.  One launch takes 6 us where two take
-// 12 until that is some tens of megabytes, or more than a compute unit reads in the time of the second launch.
+// Whether a few tokens go in one launch, in which every workgroup reads its A for itself.  It takes 4.4 us and 1 us for every 30 KB of A (7.0 us at
+// k = 1024 and rank 16, 13.6 at 8192); two launches take 10.1 us at 8192 and, called one by one, 4 us more on the host.  So up to 256 KB, and
+// while what all workgroups read together stays below 64 MB.
 bool in_one(int64_t t, int64_t k, int64_t m, int r) {
     const int64_t factor = 2 * k * wide_rank(r), columns = (m + kFewColumns - 1) / kFewColumns;
     return t <= kFewTokens && r <= 32 && factor <= (1 << 18) && factor * columns * t <= (1 << 26);

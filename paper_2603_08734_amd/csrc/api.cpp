@@ -744,7 +744,7 @@ bool parameter_ok(const void* p, int32_t p_type, int32_t type) {
 }
 bool norm_ok(const rsh_norm_t& n, int32_t type) {
     if (n.kind == RSH_NORM_NONE) return true;
-    return (n.kind == RSH_NORM_RMS || n.kind == RSH_NORM_LAYER) && n.eps > 0 && n.eps < INFINITY && aligned_to({n.stats}, 8) &&
+    return (n.kind == RSH_NORM_RMS || n.kind == RSH_NORM_LAYER) && n.eps >= 0x1p-126f && n.eps < INFINITY && aligned_to({n.stats}, 8) &&
            parameter_ok(n.weight, n.weight_type, type) && parameter_ok(n.bias, n.bias_type, type);
 }
 int join_ok(const rsh_join_t* j, bool forward) {
@@ -758,7 +758,7 @@ int join_ok(const rsh_join_t* j, bool forward) {
         (j->B && !stride_ok(j->ld_b, j->d)) || !drop_ok(j->drop) || !(j->scale - j->scale == 0))
         return RSH_ERR_BAD_OPTION;
     if (!parameter_ok(j->gate, j->gate_type, j->type) || (j->gate ? j->ld_gate && !stride_ok(j->ld_gate, j->d) : j->ld_gate != 0)) return RSH_ERR_BAD_OPTION;
-    if (forward && j->B && (j->S == j->X || j->S == j->B)) return RSH_ERR_BAD_OPTION;
+    if (forward && ((j->B && (j->S == j->X || j->S == j->B)) || (j->Y && (j->Y == j->X || j->Y == j->B || j->Y == j->S)))) return RSH_ERR_BAD_OPTION;
     return RSH_OK;
 }
 }  // namespace

@@ -39,7 +39,7 @@ def _join(**change):
 
 JOINS = [
     (b.RSH_ERR_BAD_OPTION, dict(type=b.RSH_MX4)), (b.RSH_ERR_BAD_OPTION, dict(t=0)), (b.RSH_ERR_BAD_OPTION, dict(d=-1)),
-    (b.RSH_ERR_TOO_LARGE, dict(d=(1 << 21) + 1)), (b.RSH_ERR_BAD_OPTION, dict(ld_b=63)), (b.RSH_ERR_BAD_OPTION, dict(ld_b=1 << 31)),
+    (b.RSH_ERR_TOO_LARGE, dict(d=(1 << 21) + 1)), (b.RSH_ERR_BAD_OPTION, dict(ld_b=63)), (b.RSH_ERR_BAD_OPTION, dict(ld_b=(1 << 29) + 1)),
     (b.RSH_ERR_BAD_OPTION, dict(ld_gate=63)), (b.RSH_ERR_BAD_OPTION, dict(gate_type=b.RSH_MX4)), (b.RSH_ERR_BAD_OPTION, dict(gate_type=b.RSH_BF16)),
     (b.RSH_ERR_BAD_OPTION, dict(gate=None, ld_gate=64)), (b.RSH_ERR_BAD_OPTION, dict(after=_norm(weight_type=b.RSH_BF16))), (b.RSH_ERR_BAD_OPTION, dict(gate=P + 1)),
     (b.RSH_ERR_BAD_OPTION, dict(scale=INF)), (b.RSH_ERR_BAD_OPTION, dict(scale=float("nan"))), (b.RSH_ERR_BAD_OPTION, dict(drop=_drop(1 << 17))),
@@ -52,7 +52,9 @@ JOINS = [
 @pytest.mark.parametrize("status,change", JOINS + [
     (b.RSH_ERR_NULL, dict(X=None)), (b.RSH_ERR_NULL, dict(B=None)), (b.RSH_ERR_NULL, dict(S=None)), (b.RSH_ERR_NULL, dict(Y=None)),
     (b.RSH_ERR_NULL, dict(before=_norm(kind=b.RSH_NORM_NONE))), (b.RSH_ERR_NULL, dict(B=None, S=None, Y=None, before=_norm(kind=b.RSH_NORM_NONE))),
-    (b.RSH_ERR_BAD_OPTION, dict(ld_x=63)), (b.RSH_ERR_BAD_OPTION, dict(S=P)), (b.RSH_ERR_BAD_OPTION, dict(S=2 * P))])
+    (b.RSH_ERR_BAD_OPTION, dict(ld_x=63)), (b.RSH_ERR_BAD_OPTION, dict(S=P)), (b.RSH_ERR_BAD_OPTION, dict(S=2 * P)),
+    (b.RSH_ERR_BAD_OPTION, dict(Y=P)), (b.RSH_ERR_BAD_OPTION, dict(Y=2 * P)), (b.RSH_ERR_BAD_OPTION, dict(Y=3 * P)),
+    (b.RSH_ERR_BAD_OPTION, dict(B=None, S=None, Y=P)), (b.RSH_ERR_BAD_OPTION, dict(before=_norm(eps=1e-45)))])
 def test_joins_refuse(status, change):
     assert b.lib().rsh_join_forward(ctypes.byref(_join(**change)), None) == status
 
