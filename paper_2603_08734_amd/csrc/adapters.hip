@@ -793,13 +793,14 @@ bool in_one(int64_t t, int64_t k, int64_t m, int r) {
 
 // Parts of the long axis of a shrinking product, and the steps of 64 in each: as many as bring all compute units their fill of workgroups at
 // once, since a second round costs as much as the first (4096 tokens at rank 64 by 16384 columns in 16 parts and four rounds 63 us).
-constexpr int kFewWaves = 8, kShrinkWaves = 4, kOuterWaves = 4;
+constexpr int kFewWaves = 8, kOuterWaves = 4;
+constexpr int shrink_waves(int r) { return r <= 16 ? 8 : 4; }      // fewer parts to add up where the registers leave room (63 -> 60 us)
 int slots_of(int r) { return r <= 16 ? 1024 : r <= 32 ? 768 : 512; }     // workgroups of four waves that fit the chip, by their registers
 struct Split {
     int parts, steps;
     Split(int64_t t, int64_t k, int n, int r, bool few) {
-        const int64_t all = (k + 63) / 64, waves = few ? kFewWaves : kShrinkWaves;
-        const int64_t blocks = (few ? t : most_tiles(t, n)) * ((r + 63) / 64), slots = few ? 512 : slots_of(r);
+        const int64_t all = (k + 63) / 64, waves = few ? kFewWaves : shrink_waves(r);
+        const int64_t blocks = (few ? t : most_tiles(t, n)) * ((r + 63) / 64), slots = few ? 512 : slots_of(r) * 4 / shrink_waves(r);
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>(few ? kFewParts : 16, slots / blocks));
         const int64_t each = (all + want * waves - 1) / (want * waves) * waves;
         steps = (int)each;
@@ -832,7 +833,7 @@ void shrink(const rsh_adapters_t& a, bool few, const void* X, int64_t ld, int64_
             hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 1, true, kFewWaves>), grid, dim3(64 * kFewWaves), 0, st, (const uint16_t*)X, ld,
                                (const uint16_t*)A, index, order, H, a.t, k, a.r, split.steps);
         else
-            hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 4, false, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, st, (const uint16_t*)X, ld,
+            hipLaunchKernelGGL((rsh_adapters_shrink_kernel<T, RT, 4, false, shrink_waves(16 * RT)>), grid, dim3(64 * shrink_waves(16 * RT)), 0, st, (const uint16_t*)X, ld,
                                (const uint16_t*)A, index, order, H, a.t, k, a.r, split.steps);
     });
 }

@@ -331,3 +331,25 @@ def test_refusals_on_the_gpu():
         torch.autograd.grad(g.float().sum(), v)
     with forward_ad.dual_level(), pytest.raises(ValueError, match="forward-mode"):
         adapters.add(forward_ad.make_dual(y, y), x, a, b, i, s)
+
+
+def test_offsets_beyond_32_bits():
+    """Adapters whose factors lie more than 2^31 elements from the first, and tokens far apart."""
+    from paper_2603_08734_amd import adapters
+    n, r, k, m = 4096, 16, 33000, 64
+    a = torch.empty(n, r, k, dtype=torch.bfloat16, device="cuda")
+    b = torch.empty(n, r, m, dtype=torch.bfloat16, device="cuda")
+    a[4090:], b[4090:] = torch.randn(6, r, k, device="cuda").bfloat16(), torch.randn(6, r, m, device="cuda").bfloat16()
+    for t in (7, 300):
+        x, y = torch.randn(t, k, device="cuda").bfloat16(), torch.randn(t, m, device="cuda").bfloat16()
+        i = torch.randint(4090, 4096, (t,), device="cuda")
+        # the parts of k go by how many adapters there may be, so by the bounds
+        value, bound = reference(dict(y=y, x=x, a=a[4090:], b=b[4090:], dout=y, index=i - 4090, scales=None), "cuda")[0]
+        off = (adapters.add(y, x, a, b, i).double() - value).abs() - (bound + 2.0 ** -8 * (value.abs() + bound))
+        assert bool((off <= 0).all())
+    base = torch.empty(6 << 28, dtype=torch.bfloat16, device="cuda")
+    far = base.as_strided((6, 200), (1 << 28, 1))
+    far[:] = torch.randn(6, 200, device="cuda").bfloat16()
+    i = torch.arange(6, device="cuda") % 3
+    a, b, y = torch.randn(3, 8, 200, device="cuda").bfloat16(), torch.randn(3, 8, 72, device="cuda").bfloat16(), torch.randn(6, 72, device="cuda").bfloat16()
+    assert torch.equal(adapters.add(y, far, a, b, i), adapters.add(y, far.contiguous(), a, b, i))

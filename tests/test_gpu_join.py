@@ -474,3 +474,33 @@ def test_refusals_on_the_gpu():
     v.detach().add_(1)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         torch.autograd.grad(Y, v, torch.ones_like(Y))
+
+
+def test_offsets_beyond_32_bits():
+    """Rows whose elements lie more than 2^31 from the first, by their number or by their distance: the same results as by themselves."""
+    from paper_2603_08734_amd import dropout, residual
+    n = residual.Norm("layer", torch.rand(32768, device="cuda") + 0.5, None, EPS)
+    t = 70000
+    x = torch.empty(t, 32768, dtype=torch.float16, device="cuda")
+    x[:] = torch.randn(1, 32768, device="cuda").half()
+    x[-5:] = torch.randn(5, 32768, device="cuda").half()
+    drop = dropout.Drop(0.5, 1)
+    y = residual.norm(x, n)
+    assert torch.equal(y[-5:], residual.norm(x[-5:], n)) and torch.equal(y[:2], residual.norm(x[:2], n))
+    del y
+    z = dropout.dropout(x, drop)
+    kept, factor = edges.kept(1, 8, 0.5, 1, 0)
+    assert torch.equal(z[0, :8].cpu() != 0, kept[0] & (x[0, :8].cpu() != 0)) and torch.equal(z[-1][z[-1] != 0], 2 * x[-1][z[-1] != 0])
+    del z, x
+    for d, ld in ((40, 1 << 28), (40, (1 << 28) + 3), (600, 1 << 28)):
+        base = torch.empty(9 * ld, dtype=torch.float16, device="cuda")
+        far = base.as_strided((9, d), (ld, 1))
+        far[:] = torch.randn(9, d, device="cuda").half()
+        near = far.contiguous()
+        n = residual.Norm("rms", None, None, EPS)
+        leaves = [v.detach().requires_grad_() for v in (far, near)]
+        outs = [residual.join(v, near, before=n) for v in leaves]
+        grads = [torch.autograd.grad(list(o), v, [near, near])[0] for o, v in zip(outs, leaves)]
+        assert all(torch.equal(p, q) for p, q in zip(*outs)) and torch.equal(*grads)
+        assert torch.equal(dropout.dropout(far, drop), dropout.dropout(near, drop))
+        del base, far, leaves
