@@ -792,7 +792,7 @@ int rsh_join_backward(const rsh_join_t* join, const rsh_join_gradients_t* g, voi
     const bool before = j.before.kind != RSH_NORM_NONE, after = j.B && j.after.kind != RSH_NORM_NONE;
     const int vectors = !!g->after_weight + !!g->after_bias + !!g->before_weight + !!g->before_bias + (g->dgate && !j.ld_gate);
     if (!g->dX && !g->dB && !g->dgate && !vectors) return RSH_ERR_NULL;
-    if ((!g->dS && !g->dY) || (vectors && !g->work) || (g->dY && before && (!j.before.stats || !j.X)) || (after && !j.after.stats)) return RSH_ERR_NULL;
+    if ((!g->dS && !g->dY) || (rsh::join_backward_work(j.t, j.d, vectors) && !g->work) || (g->dY && before && (!j.before.stats || !j.X)) || (after && !j.after.stats)) return RSH_ERR_NULL;
     if ((g->dB && !j.B) || (g->dgate && !j.gate) || (g->dS && !j.B) || (g->dY && !before) ||
         ((g->before_weight || g->before_bias) && !(before && g->dY)) || (g->before_weight && !j.before.weight) || (g->before_bias && !j.before.bias) ||
         ((g->after_weight || g->after_bias) && !after) || (g->after_weight && !j.after.weight) || (g->after_bias && !j.after.bias) ||

@@ -60,7 +60,7 @@ template <> void join_backward_of<BF16>(const rsh_join_t&, const rsh_join_gradie
 
 // Workgroups of the backward pass, each with a part of the vectors' sums, or parts of the columns' kernel.
 int64_t backward_parts(int64_t t, int64_t d) {
-    if (d > kRegisterWidth) return std::min(t, kColumnParts);
+    if (d > kRegisterWidth) return std::min<int64_t>(t, std::max<int64_t>(1, kColumnBlocks / ((d + 2047) / 2048)));
     int64_t parts = 0;
     by_width(d, [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
@@ -71,7 +71,7 @@ int64_t backward_parts(int64_t t, int64_t d) {
 int64_t vector_bytes(int64_t t, int64_t d, int vectors) { return (backward_parts(t, d) * vectors * d * 4 + 15) / 16 * 16; }
 
 int64_t join_backward_work(int64_t t, int64_t d, int vectors) {
-    return vector_bytes(t, d, vectors) + (d > kRegisterWidth && vectors ? (8 * t + 15) / 16 * 16 : 0);
+    return vector_bytes(t, d, vectors) + (d > kRegisterWidth ? 16 * t : 0);
 }
 
 int launch_join_forward(const rsh_join_t& join, void* stream) {

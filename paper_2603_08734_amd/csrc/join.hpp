@@ -631,88 +631,103 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
     }
 }
 
-// Rows of any length, read again at each of three passes; the means of g and g xh go to `means`, and the next kernel adds up the vectors.
+// Longer rows: this kernel forms the four means of a row, means[4 row] = those of g and g xh and those of N1's, and the next one goes through the
+// columns.  N1's means are of gb = (dS + r g - r mean(g) - r xh mean(g xh)) fw with fw = w1 scale gate drop, so of (dS + r g) fw, fw and xh fw,
+// which need no other mean: one pass has them all.  (Three passes over the rows, and a fourth for the vectors, took twice as long.)
 template <class T, bool JOIN>
-__global__ __launch_bounds__(1024) void rsh_join_backward_long_kernel(rsh_join_t j, rsh_join_gradients_t g, float* means) {
+__global__ __launch_bounds__(1024) void rsh_join_means_kernel(rsh_join_t j, rsh_join_gradients_t g, float* means) {
     __shared__ Team<1024>::Meeting meeting;
     Team<1024> team(meeting);
     const Random random(j.drop);
     const LoadedParameters<T> given{j, (int)j.d};
     const Backward<T, JOIN, false, NoSums, LoadedParameters<T>> back(j, g, random, given);
     const int d = back.d;
+    const float share = 1.f / (float)d;
     NoSums none;
     for (int64_t at = blockIdx.x; at < j.t; at += gridDim.x) {
         const Place row = {at, 0};
-        float2_t mean = {0.f, 0.f};
-        Run x;
-        if (back.first) {
-            float a = 0.f, b = 0.f;
-            each_run<1024, 0>(d, [&](int, int col) {
-                back.before(back.load(row, true, col), row, col, x, none);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) a += x.g.v[i], b += x.g.v[i] * x.xh.v[i];
-            });
-            mean = team.sum(a, b) * (1.f / (float)d);
-            if (j.before.kind != RSH_NORM_LAYER) mean[0] = 0.f;
-            if (means && threadIdx.x == 0) *reinterpret_cast<float2_t*>(means + 2 * at) = mean;
-        }
-        float a = 0.f, b = 0.f;
+        float a1 = 0.f, a2 = 0.f, b1 = 0.f, b2 = 0.f, c1 = 0.f, c2 = 0.f, d1 = 0.f, d2 = 0.f;
+        Inputs<T> in;
         each_run<1024, 0>(d, [&](int, int col) {
-            const Inputs<T> in = back.load(row, true, col);
+            in = back.load(row, true, col);
+            Run x;
             back.before(in, row, col, x, none);
-            back.sum(in, mean, col, x);
-            if (g.dX) store_run<T>(g.dX, row, col, d, x.ds);
-            if constexpr (JOIN) {
-                const Eight gate = back.through(in, row, col, x, none);
-                if (g.dgate && j.ld_gate) back.store_gate(row, col, gate);
-                if (!back.second && g.dB) store_run<T>(g.dB, row, col, d, x.gb);
+            if (back.first) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) a += x.gb.v[i], b += x.gb.v[i] * x.xb.v[i];
+                for (int i = 0; i < 8; ++i) a1 += x.g.v[i], a2 += x.g.v[i] * x.xh.v[i];
+            }
+            if (JOIN && back.second && g.dB) {
+                Eight fw = back.factors(x, row, col), ds = g.dS ? back.value(in, in.ds, col) : Eight{};
+                const Eight w = given.after_weight(col);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) fw.v[i] *= w.v[i];
+                clear_from(fw, d - col);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float f = fw.v[i], xb = x.xb.v[i], p = (back.first ? ds.v[i] + in.before[1] * x.g.v[i] : ds.v[i]) * f;
+                    b1 += p, b2 += p * xb;
+                    if (back.first) {
+                        const float h = x.xh.v[i] * f;
+                        c1 += f, c2 += f * xb, d1 += h, d2 += h * xb;
+                    }
+                }
             }
         });
-        if (!JOIN || !back.second || !g.dB) continue;
-        float2_t inner = team.sum(a, b) * (1.f / (float)d);
-        if (j.after.kind != RSH_NORM_LAYER) inner[0] = 0.f;
-        each_run<1024, 0>(d, [&](int, int col) {
-            const Inputs<T> in = back.load(row, true, col);
-            back.before(in, row, col, x, none);
-            back.sum(in, mean, col, x);
-            (void)back.through(in, row, col, x, none);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x.gb.v[i] = in.after[1] * (x.gb.v[i] - inner[0] - x.xb.v[i] * inner[1]);
-            store_run<T>(g.dB, row, col, d, x.gb);
-        });
+        float2_t outer = {0.f, 0.f}, inner = {0.f, 0.f};
+        if (back.first) {
+            in.before = *reinterpret_cast<const float2_t*>(j.before.stats + 2 * at);
+            outer = team.sum(a1, a2) * share;
+            if (j.before.kind != RSH_NORM_LAYER) outer[0] = 0.f;
+        }
+        if (JOIN && back.second && g.dB) {
+            inner = team.sum(b1, b2);
+            if (back.first) inner -= in.before[1] * (outer[0] * team.sum(c1, c2) + outer[1] * team.sum(d1, d2));
+            inner *= share;
+            if (j.after.kind != RSH_NORM_LAYER) inner[0] = 0.f;
+        }
+        if (threadIdx.x == 0) *reinterpret_cast<float4_t*>(means + 4 * at) = (float4_t){outer[0], outer[1], inner[0], inner[1]};
     }
 }
 
-// The vectors' sums of such rows: a thread has eight columns of the rows of a part.
+// A thread has eight columns of the rows of a part: their gradients, and their share of the vectors.  Nothing is waited for between rows.
 template <class T, bool JOIN>
 __global__ __launch_bounds__(256) void rsh_join_columns_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts,
                                                                const float* means) {
     const Random random(j.drop);
-    const LoadedParameters<T> given{j, (int)j.d};
-    const Backward<T, JOIN, false, RegisterSums, LoadedParameters<T>> back(j, g, random, given);
-    const int col = 8 * (int)(blockIdx.x * 256 + threadIdx.x);
-    if (col >= back.d) return;
+    const int d = (int)j.d, col = 8 * (int)(blockIdx.x * 256 + threadIdx.x);
+    if (col >= d) return;
+    const KeptParameters<T, false, true> given(j, col, d);
+    const Backward<T, JOIN, false, RegisterSums, KeptParameters<T, false, true>> back(j, g, random, given);
     RegisterSums sums;
+    Inputs<T> next = back.load({blockIdx.y, 0}, true, col);
     for (int64_t at = blockIdx.y; at < j.t; at += gridDim.y) {
         const Place row = {at, 0};
+        const Inputs<T> in = next;
+        if (at + gridDim.y < j.t) next = back.load({at + gridDim.y, 0}, true, col);
+        const float4_t mean = *reinterpret_cast<const float4_t*>(means + 4 * at);
         Run x;
-        const Inputs<T> in = back.load(row, true, col);
         back.before(in, row, col, x, sums);
+        back.sum(in, (float2_t){mean[0], mean[1]}, col, x);
+        if (g.dX) store_run<T>(g.dX, row, col, d, x.ds);
         if constexpr (JOIN) {
-            back.sum(in, back.first ? *reinterpret_cast<const float2_t*>(means + 2 * at) : (float2_t){0.f, 0.f}, col, x);
-            (void)back.through(in, row, col, x, sums);
+            const Eight gate = back.through(in, row, col, x, sums);
+            if (g.dgate && j.ld_gate) back.store_gate(row, col, gate);
+            if (!g.dB) continue;
+            if (back.second) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x.gb.v[i] = in.after[1] * (x.gb.v[i] - mean[2] - x.xb.v[i] * mean[3]);
+            }
+            store_run<T>(g.dB, row, col, d, x.gb);
         }
     }
 #pragma unroll
     for (int k = 0; k < kSlots; ++k)
         if (vectors.at[k] >= 0)
-            store_eight<F32>(parts + ((int64_t)blockIdx.y * vectors.count + vectors.at[k]) * back.d, col, sums.get(k), back.d - col);
+            store_eight<F32>(parts + ((int64_t)blockIdx.y * vectors.count + vectors.at[k]) * d, col, sums.get(k), d - col);
 }
 
 // f(lanes) of the kernels that have a row in registers, a run a lane: the fewest that do.
-constexpr int64_t kRegisterWidth = 8192, kColumnParts = 64;
+constexpr int64_t kRegisterWidth = 8192, kColumnBlocks = 512;      // workgroups of the columns' kernel that fit the chip at once
 template <class F>
 void by_width(int64_t d, F f) {
     using std::integral_constant;
@@ -769,11 +784,10 @@ void join_forward_launch(const rsh_join_t& j, hipStream_t st) {
 template <class T>
 void join_backward_launch(const rsh_join_t& j, const rsh_join_gradients_t& g, const Vectors& v, float* parts, int64_t n, hipStream_t st) {
     if (j.d > kRegisterWidth) {
-        float* const means = v.count ? (float*)((char*)g.work + vector_bytes(j.t, j.d, v.count)) : nullptr;
+        float* const means = (float*)((char*)g.work + vector_bytes(j.t, j.d, v.count));
         const dim3 rows((unsigned)std::min<int64_t>(j.t, 1 << 16)), columns((unsigned)((j.d + 2047) / 2048), (unsigned)n);
-        if (j.B) hipLaunchKernelGGL((rsh_join_backward_long_kernel<T, true>), rows, dim3(1024), 0, st, j, g, means);
-        else hipLaunchKernelGGL((rsh_join_backward_long_kernel<T, false>), rows, dim3(1024), 0, st, j, g, means);
-        if (!v.count) return;
+        if (j.B) hipLaunchKernelGGL((rsh_join_means_kernel<T, true>), rows, dim3(1024), 0, st, j, g, means);
+        else hipLaunchKernelGGL((rsh_join_means_kernel<T, false>), rows, dim3(1024), 0, st, j, g, means);
         if (j.B) hipLaunchKernelGGL((rsh_join_columns_kernel<T, true>), columns, dim3(256), 0, st, j, g, v, parts, means);
         else hipLaunchKernelGGL((rsh_join_columns_kernel<T, false>), columns, dim3(256), 0, st, j, g, v, parts, means);
         return;
