@@ -549,7 +549,7 @@ struct Backward {
 // One pass over the rows, each in its lanes' registers, and the vectors' sums with it, a part of them from every workgroup.  The next
 // row is on its way while one is computed.
 template <class T, int LANES, bool JOIN, bool BIAS>
-__global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(JOIN && LANES <= 64 ? 2 : 4))) void rsh_join_backward_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts) {
+__global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(!JOIN || LANES > 256 ? 4 : LANES > 64 ? 3 : 2))) void rsh_join_backward_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts) {
     constexpr int kThreads = kThreadsOf<LANES>, kRows = kRowsOf<LANES>;
     // Whether the registers hold the next row beside this one: a row takes about as long as its loads.
     constexpr bool kEarly = !JOIN || (size_of<T>() == 2 && !BIAS);
@@ -763,14 +763,13 @@ void join_backward_of(const rsh_join_t& j, const rsh_join_gradients_t& g, const 
 template <class T>
 void join_forward_launch(const rsh_join_t& j, hipStream_t st) {
     if (j.d > kRegisterWidth) {
+        // Joins keep a row in registers while it fits (1170 x 28672 bfloat16 79 us, 104 read again at every pass, 1677 x 20000 106 and 97); a norm alone is
+        // faster read again, from the caches (28 and 32 us, 26 and 43; 3276 x 10240 27.5 and 37).
         const dim3 rows((unsigned)std::min<int64_t>(j.t, 1 << 16));
-        if (j.d <= 2 * kRegisterWidth) {
-            if (j.B) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 512, 4, true>), rows, dim3(512), 0, st, j);
-            else hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 512, 4, false>), rows, dim3(512), 0, st, j);
-        } else {
-            if (j.B) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 0, true>), rows, dim3(1024), 0, st, j);
-            else hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 0, false>), rows, dim3(1024), 0, st, j);
-        }
+        if (!j.B) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 0, false>), rows, dim3(1024), 0, st, j);
+        else if (j.d <= 2 * kRegisterWidth) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 512, 4, true>), rows, dim3(512), 0, st, j);
+        else if (j.d <= 4 * kRegisterWidth) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 4, true>), rows, dim3(1024), 0, st, j);
+        else hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 0, true>), rows, dim3(1024), 0, st, j);
         return;
     }
     by_width(j.d, [&](auto lanes) {
