@@ -119,8 +119,8 @@ def add(Y, X, A, B, index, scales=None):
     k, m = X.shape[-1], Y.shape[-1]
     grads = torch.is_grad_enabled() and any(v.requires_grad for v in (Y, X, A, B))
     if 0 in (Y.numel(), X.numel(), A.numel(), B.numel()):
-        # no sums: Y, and zeros as the others' gradients
-        return Y + sum(v.sum() for v in (X, A, B)) * 0 if grads else Y.clone()
+        # no sums: Y, and zeros as the others' gradients, whatever the operands hold
+        return Y + sum(v.reshape(-1)[:0].sum() for v in (X, A, B)) if grads else Y.clone()
     flat = X.dim() == 2
     rows = [Y, X, index] if flat else [Y.reshape(-1, m), X.reshape(-1, k), index.reshape(-1)]
     A, B, index = A.contiguous(), B.contiguous(), rows[2].contiguous()

@@ -24,7 +24,7 @@ NOTHING = binding.rsh_drop_t()      # no dropout, as part of other structures
 class Drop:
     """p: share that is dropped, 0 .. 1.  seed: an integer, or an int64 tensor of one element on the operands' GPU, read when the kernels
     run (a captured graph draws new numbers when the program changes it between replays; changing it between a forward pass and its
-    backward pass is an error).  offset: an integer; both are taken modulo 2^64."""
+    backward pass is an error).  offset: an integer; both are taken modulo 2^64.  It does not change afterwards."""
 
     __slots__ = ("share", "seed", "offset")
 
@@ -36,7 +36,15 @@ class Drop:
                 raise ValueError(f"seed: expected an integer or one int64 on the GPU, got {seed.dtype} {tuple(seed.shape)} on {seed.device}")
         else:
             seed = int(seed) % (1 << 64)
-        self.share, self.seed, self.offset = round(p * 65536), seed, int(offset) % (1 << 64)
+        for name, v in zip(self.__slots__, (round(p * 65536), seed, int(offset) % (1 << 64))):
+            object.__setattr__(self, name, v)
+
+    def __setattr__(self, name, value):
+        # a backward pass draws the forward pass's numbers again
+        raise AttributeError(f"{name}: a Drop does not change; make another")
+
+    def __reduce__(self):
+        return Drop, (self.share / 65536, self.seed, self.offset)
 
     @property
     def tensor(self):

@@ -147,3 +147,16 @@ def test_calls_without_a_gpu_refuse():
                         (lambda: adapters.add(x, x, x[:, None], x[:, None], torch.zeros(2, dtype=torch.int64)), "one GPU")):
         with pytest.raises(ValueError, match=match):
             call()
+
+
+def test_a_drop_does_not_change():
+    """A backward pass draws the forward pass's numbers from it again."""
+    import copy
+    import pickle
+    from paper_2603_08734_amd.dropout import Drop
+    drop = Drop(0.3, -5, 7)
+    for name in ("share", "seed", "offset"):
+        with pytest.raises(AttributeError):
+            setattr(drop, name, 1)
+    for other in (drop, copy.deepcopy(drop), pickle.loads(pickle.dumps(drop))):
+        assert (other.share, other.seed, other.offset) == (round(0.3 * 65536), (1 << 64) - 5, 7)

@@ -198,6 +198,19 @@ def test_empty_sizes():
             assert torch.equal(out, y) and (out.numel() == 0 or out.data_ptr() != y.data_ptr())
 
 
+@pytest.mark.parametrize("value", [60000.0, float("inf"), float("nan")])
+def test_empty_sizes_leave_out_what_the_operands_hold(value):
+    """Nothing is multiplied, so nothing of X (whose sum overflows, or is no number), A, B or dout reaches the others."""
+    from paper_2603_08734_amd import adapters
+    for t, k, m, n, r in ((3, 0, 8, 2, 4), (3, 8, 8, 0, 4), (3, 8, 8, 2, 0)):
+        y = torch.ones((t, m), device="cuda", dtype=torch.float16, requires_grad=True)
+        x, a, b = (torch.full(s, value, device="cuda", dtype=torch.float16, requires_grad=True) for s in ((t, k), (n, r, k), (n, r, m)))
+        out = adapters.add(y, x, a, b, torch.zeros(t, dtype=torch.int64, device="cuda"))
+        assert torch.equal(out, y)
+        grads = torch.autograd.grad(out, (y, x, a, b), torch.full_like(out, value))
+        assert all(torch.equal(g, torch.zeros_like(v)) for g, v in zip(grads[1:], (x, a, b)))
+
+
 @pytest.mark.parametrize("want", [(0,), (1,), (2,), (3,), (0, 2), (1, 3)])
 def test_some_gradients(want):
     from paper_2603_08734_amd import adapters
