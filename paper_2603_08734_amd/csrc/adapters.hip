@@ -8,7 +8,7 @@
 // kept for the gradients); a few tokens are dealt out by every workgroup for itself, which saves a launch.
 //
 // Ranks are small, so all three are passes over X, Y and dout, bound by memory; operands go from memory to the matrix unit through registers
-// alone, a step ahead of their use.  Measured (bfloat16): 4096 tokens of 28672 features at rank 16, shrink 59 us (235 MB, 4.0 TB/s),
+// alone, a step ahead of their use.  Measured (bfloat16): 4096 tokens of 28672 features at rank 16, shrink 57 us (235 MB, 4.1 TB/s),
 // expand to 8192 columns 33 us (134 MB, 4.1); 4096 tokens at rank 64 between 4096 and 16384 features: shrink 16.5 and 48 us, expand 20.5
 // and 80, outer 24 and 46 (a copy of the bytes would take 7, 26, 7, 53, 7 and 26): what counts there is the time until a workgroup's first
 // loads have come, since all of them fit the chip at once or nearly so.  One token at rank 16 between 8192 and 28672 features 13.6 us in one

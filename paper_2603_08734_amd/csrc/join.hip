@@ -1,7 +1,7 @@
 // The edges of a block: launches of norms and joins, the sums of their vectors' gradients, and dropout alone.
 //
 // Dropout reads and writes each element once; ten rounds for eight elements are about 20 instructions' time an element, below what memory takes:
-// 4096 x 16384 bfloat16 46.4 us, 1999 x 4999 fp32 12.6 us (5.8 and 6.3 TB/s; part of it stays in the last-level cache).
+// 4096 x 16384 bfloat16 46.4 us, 1999 x 4999 fp32 14.0 us (5.8 and 5.7 TB/s; part of it stays in the last-level cache).
 #include "join.hpp"
 
 namespace rsh {

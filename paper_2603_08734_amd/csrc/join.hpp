@@ -633,7 +633,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
 
 // Longer rows: this kernel forms the four means of a row, means[4 row] = those of g and g xh and those of N1's, and the next one goes through the
 // columns.  N1's means are of gb = (dS + r g - r mean(g) - r xh mean(g xh)) fw with fw = w1 scale gate drop, so of (dS + r g) fw, fw and xh fw,
-// which need no other mean: one pass has them all.  (Three passes over the rows, and a fourth for the vectors, took twice as long.)
+// which need no other mean: one pass has them all.  (With three passes over
+// the rows, and a fourth for the vectors, a step of 1677 x 20000 bfloat16 took 448 us, with these two 353.)
 template <class T, bool JOIN>
 __global__ __launch_bounds__(1024) void rsh_join_means_kernel(rsh_join_t j, rsh_join_gradients_t g, float* means) {
     __shared__ Team<1024>::Meeting meeting;
