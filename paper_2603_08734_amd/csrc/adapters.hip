@@ -2,8 +2,8 @@
 //
 // With both factors rank first, A_i [r][k] and B_i [r][m], three products make up both directions:
 //   shrink   H = X A_i^T, and dH = dout B_i^T      long rows against r short ones: matrix instructions of 16 bits
-//   expand   out = Y + s H B_i, and dX = s dH A_i   r terms for every element: H is fp32, so are the matrix instructions
-//   outer    dA_i = s dH^T X, and dB_i = s H^T dout    the tokens of an adapter summed up, in fp32 again
+//   expand   out = Y + s H B_i, and dX = s dH A_i   r terms for every element: H is fp32, and enters as three numbers of bfloat16
+//   outer    dA_i = s dH^T X, and dB_i = s H^T dout    the tokens of an adapter summed up, H in the same way
 // Tokens are taken in tiles that share an adapter.  A kernel of one workgroup deals them out (8 to 9 us for 4096 tokens, all of it latency; it is
 // kept for the gradients); a few tokens are dealt out by every workgroup for itself, which saves a launch.
 //
@@ -301,51 +301,65 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(RT =
     }
 }
 
-// Four fp32 numbers as two of bfloat16 each, hi + lo, 2^-17 of them off at most; of an infinity or a NaN lo is zero.  Sums of r or t products of
-// one of them with 16-bit numbers are formed by the matrix unit's 16-bit instructions, one for hi and one for lo: four times the rate of its
-// fp32 form, which took 55 of the 100 us of 4096 tokens at rank 64 by 16384 columns.  Rounding H to 16 bits alone would put as much error into
-// the result as the result's own rounding.
-struct Halves {
-    uint2_t hi, lo;
+// Four fp32 numbers as three of bfloat16 each, hi + mid + lo: cut into eight bits at a time, so the three are the number itself (its last bits
+// may be lost below 2^-110, where lo is subnormal); of an infinity or a NaN mid and lo are zero.  Sums of r or t products of one of them with 16-bit
+// numbers are formed by the matrix unit's 16-bit instructions, whose products and sums are fp32: two instructions for bfloat16, three for binary16, of which
+// one takes 32 terms.  Its fp32 form, at an eighth of the rate, took 55 of the 100 us of 4096 tokens at rank 64 by 16384 columns.
+struct Thirds {
+    uint2_t hi, mid, lo;
 };
-__device__ __forceinline__ Halves halves(const float* h) {
-    float hi[4], lo[4];
+__device__ __forceinline__ uint2_t upper(const uint32_t* v) {
+    return {__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
+}
+__device__ __forceinline__ Thirds thirds(const float* h) {
+    uint32_t hi[4], mid[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        hi[i] = __uint_as_float((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)h[i]) << 16);
-        const float rest = h[i] - hi[i];
-        lo[i] = rest - rest == 0.f ? rest : 0.f;
+        hi[i] = __float_as_uint(h[i]) & 0xffff0000u;
+        const float rest = h[i] - __uint_as_float(hi[i]);
+        mid[i] = rest - rest == 0.f ? __float_as_uint(rest) & 0xffff0000u : 0u;
+        lo[i] = rest - rest == 0.f ? __float_as_uint(rest - __uint_as_float(mid[i])) : 0u;
     }
-    return {{BF16::pair(hi[0], hi[1]), BF16::pair(hi[2], hi[3])}, {BF16::pair(lo[0], lo[1]), BF16::pair(lo[2], lo[3])}};
+    return {upper(hi), upper(mid), upper(lo)};
 }
-// 16 by 16 results, 16 terms: lane l has terms 4 (l / 16) .. + 3 of row l % 16 of either operand.
-__device__ __forceinline__ float4_t multiply(uint2_t a, uint2_t b, float4_t c) {
-    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
+// 16 by 16 results of 16 terms in two forms at once, a0 b0 + a1 b1: lane l has terms 4 (l / 16) .. + 3 of row l % 16 of either operand.  Every sum is
+// made of this instruction alone: one of 16 terms that takes up its result at once, as the compiler orders them, finds it unfinished.
+__device__ __forceinline__ float4_t multiply(uint2_t a0, uint2_t a1, uint2_t b0, uint2_t b1, float4_t c) {
+    return BF16::mfma16((uint4_t){a0[0], a0[1], a1[0], a1[1]}, (uint4_t){b0[0], b0[1], b1[0], b1[1]}, c);
 }
 
-// Four rows of eight 16-bit numbers as eight operands of a column's four.  bfloat16 goes as it is; a number of binary16 is two of bfloat16
-// exactly, of which `rest` is the second.
+// Column q of four rows of eight 16-bit numbers, as an operand.  bfloat16 goes as it is; a number of binary16 is two of bfloat16 exactly, of which
+// `rest` is the second.
 template <class T>
-struct Fours {
-    uint2_t main[8], rest[std::is_same<T, F16>::value ? 8 : 1];
-    __device__ __forceinline__ void from(const uint4_t* rows) {
+struct Column {
+    uint2_t main, rest;
+    __device__ __forceinline__ Column(const uint4_t* rows, int q) : rest{0, 0} {
         auto pick = [](uint32_t a, uint32_t b, int odd) { return __builtin_amdgcn_perm(b, a, odd ? 0x07060302u : 0x05040100u); };
+        if constexpr (std::is_same<T, BF16>::value) {
+            main = (uint2_t){pick(rows[0][q / 2], rows[1][q / 2], q & 1), pick(rows[2][q / 2], rows[3][q / 2], q & 1)};
+        } else {
+            uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            if constexpr (std::is_same<T, BF16>::value) {
-                main[q] = (uint2_t){pick(rows[0][q / 2], rows[1][q / 2], q & 1), pick(rows[2][q / 2], rows[3][q / 2], q & 1)};
-            } else {
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float x = F16::widen((uint16_t)(rows[i][q / 2] >> (16 * (q & 1))));
-                    hi[i] = __float_as_uint(x);
-                    const float r = x - __uint_as_float(hi[i] & 0xffff0000u);
-                    lo[i] = __float_as_uint(r - r == 0.f ? r : 0.f);
-                }
-                main[q] = (uint2_t){pick(hi[0], hi[1], 1), pick(hi[2], hi[3], 1)};
-                rest[q] = (uint2_t){pick(lo[0], lo[1], 1), pick(lo[2], lo[3], 1)};
+            for (int i = 0; i < 4; ++i) {
+                const float x = F16::widen((uint16_t)(rows[i][q / 2] >> (16 * (q & 1))));
+                hi[i] = __float_as_uint(x);
+                const float r = x - __uint_as_float(hi[i] & 0xffff0000u);
+                lo[i] = __float_as_uint(r - r == 0.f ? r : 0.f);
             }
+            main = upper(hi), rest = upper(lo);
+        }
+    }
+    // c and the products with H, whose numbers are the rows' terms.  FIRST: the column is the first operand, its place the results' row.
+    template <bool FIRST>
+    __device__ __forceinline__ float4_t times(const Thirds& h, float4_t c) const {
+        if constexpr (std::is_same<T, BF16>::value) {
+            const uint2_t none = {0, 0};
+            c = FIRST ? multiply(main, main, h.hi, h.mid, c) : multiply(h.hi, h.mid, main, main, c);
+            return FIRST ? multiply(main, main, h.lo, none, c) : multiply(h.lo, none, main, main, c);
+        } else {
+            c = FIRST ? multiply(main, rest, h.hi, h.hi, c) : multiply(h.hi, h.hi, main, rest, c);
+            c = FIRST ? multiply(main, rest, h.mid, h.mid, c) : multiply(h.mid, h.mid, main, rest, c);
+            return FIRST ? multiply(main, rest, h.lo, h.lo, c) : multiply(h.lo, h.lo, main, rest, c);
         }
     }
 };
@@ -359,12 +373,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
                                                                                                          int64_t m, int r) {
     constexpr int kGroups = (FEW ? kFewTile : kTile / kShares) / 16;
     constexpr int kBlocks = FEW ? 1 : 8;       // of 16 ranks, whose H is in LDS at once
-    struct Pair {
-        uint2_t hi, lo;
-    };
     __shared__ int place[FEW ? sizeof(FewPlace) / sizeof(int) : 1];
     // H of the tile as the matrix unit takes it, which the four waves share: read by each for itself it was as many requests as Y.
-    __shared__ __attribute__((aligned(16))) Pair shared[FEW ? 1 : kBlocks][FEW ? 1 : kGroups][64];
+    __shared__ __attribute__((aligned(16))) uint4_t shared_upper[FEW ? 1 : kBlocks][FEW ? 1 : kGroups][64];
+    __shared__ __attribute__((aligned(8))) uint2_t shared_lo[FEW ? 1 : kBlocks][FEW ? 1 : kGroups][64];
     Members<FEW> tile;
     if (!members<FEW>(index, order, t, (int)(FEW ? blockIdx.x : blockIdx.x / kShares), place, &tile)) return;
     if constexpr (!FEW) {
@@ -418,7 +430,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
             return v;
         };
         // H of four ranks of a token, from its parts where there are any.
-        auto pair_of = [&](int64_t row, int rank) {
+        auto thirds_of = [&](int64_t row, int rank) {
             const float* const p = H + row * r16 + rank + 4 * g;
             float4_t h = *reinterpret_cast<const float4_t*>(p);
             if constexpr (FEW) {
@@ -430,8 +442,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
                     if (q < parts) h += part[q];
             }
             const float hv[4] = {h[0] * scale, h[1] * scale, h[2] * scale, h[3] * scale};
-            const Halves two = halves(hv);
-            return Pair{two.hi, two.lo};
+            return thirds(hv);
         };
         Slab next = {};
         if (active) next = load(0);
@@ -441,8 +452,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
                 if (rank0) __syncthreads();
                 const int group = wave % kGroups;
                 const int64_t row = tile.at(16 * group + c);
-                for (int rank = rank0 + 16 * (wave / kGroups); rank < last; rank += 16 * (4 / kGroups))
-                    shared[(rank - rank0) / 16][group][lane] = pair_of(row, rank);
+                for (int rank = rank0 + 16 * (wave / kGroups); rank < last; rank += 16 * (4 / kGroups)) {
+                    const Thirds h = thirds_of(row, rank);
+                    shared_upper[(rank - rank0) / 16][group][lane] = (uint4_t){h.hi[0], h.hi[1], h.mid[0], h.mid[1]};
+                    shared_lo[(rank - rank0) / 16][group][lane] = h.lo;
+                }
                 __syncthreads();
             }
             if (!active) continue;
@@ -453,23 +467,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
                 for (int s = 0; s < 4; ++s)
 #pragma unroll
                     for (int w = 0; w < 4; ++w) v.rows[s][w] = rank + 4 * g + s < r ? v.rows[s][w] : 0u;
-                Fours<T> f;
-                f.from(v.rows);
+                Thirds h[kGroups];
 #pragma unroll
                 for (int i = 0; i < kGroups; ++i) {
-                    if (16 * i >= tile.count) break;
-                    Pair k;
-                    if constexpr (FEW) k = pair_of(token[i], rank);
-                    else k = shared[(rank - rank0) / 16][i][lane];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        acc[i][q] = multiply(f.main[q], k.hi, acc[i][q]);
-                        acc[i][q] = multiply(f.main[q], k.lo, acc[i][q]);
-                        if constexpr (std::is_same<T, F16>::value) {
-                            acc[i][q] = multiply(f.rest[q], k.hi, acc[i][q]);
-                            acc[i][q] = multiply(f.rest[q], k.lo, acc[i][q]);
-                        }
+                    if constexpr (FEW) {
+                        h[i] = thirds_of(token[i], rank);
+                    } else {
+                        const uint4_t u = shared_upper[(rank - rank0) / 16][i][lane];
+                        h[i] = {{u[0], u[1]}, {u[2], u[3]}, shared_lo[(rank - rank0) / 16][i][lane]};
                     }
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const Column<T> column(v.rows, q);
+#pragma unroll
+                    for (int i = 0; i < kGroups; ++i) acc[i][q] = column.template times<true>(h[i], acc[i][q]);
                 }
             }
         }
@@ -591,22 +603,13 @@ __global__ __launch_bounds__(1024) void rsh_adapters_few_kernel(const uint16_t* 
         for (int i = 0; i < RT; ++i) {
             const float4_t h = sums[i][lane];
             const float hv[4] = {h[0], h[1], h[2], h[3]};
-            const Halves two = halves(hv);
+            const Thirds three = thirds(hv);
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) rows[i][s][w] = 16 * i + 4 * g + s < r ? rows[i][s][w] : 0u;
-            Fours<T> f;
-            f.from(rows[i]);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                acc[q] = multiply(f.main[q], two.hi, acc[q]);
-                acc[q] = multiply(f.main[q], two.lo, acc[q]);
-                if constexpr (std::is_same<T, F16>::value) {
-                    acc[q] = multiply(f.rest[q], two.hi, acc[q]);
-                    acc[q] = multiply(f.rest[q], two.lo, acc[q]);
-                }
-            }
+            for (int q = 0; q < 8; ++q) acc[q] = Column<T>(rows[i], q).template times<true>(three, acc[q]);
         }
     }
     if (c >= tile.count) return;
@@ -691,20 +694,11 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
                     for (int j = 0; j < RT; ++j) s.h[j][i] = in ? s.h[j][i] : 0.f;
                 }
             }
-            Fours<T> f;
-            f.from(s.x);
 #pragma unroll
             for (int j = 0; j < RT; ++j) {
-                const Halves h = halves(s.h[j]);
+                const Thirds h = thirds(s.h[j]);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    acc[j][q] = multiply(h.hi, f.main[q], acc[j][q]);
-                    acc[j][q] = multiply(h.lo, f.main[q], acc[j][q]);
-                    if constexpr (std::is_same<T, F16>::value) {
-                        acc[j][q] = multiply(h.hi, f.rest[q], acc[j][q]);
-                        acc[j][q] = multiply(h.lo, f.rest[q], acc[j][q]);
-                    }
-                }
+                for (int q = 0; q < 8; ++q) acc[j][q] = Column<T>(s.x, q).template times<false>(h, acc[j][q]);
             }
         }
     }
