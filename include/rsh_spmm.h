@@ -398,8 +398,8 @@ int rsh_join_backward(const rsh_join_t *join, const rsh_join_gradients_t *gradie
  *   rsh_adapters_forward   kept not NULL: what the gradients need of H and of the tokens' order, 16-byte aligned, rsh_adapters_kept bytes
  *   rsh_adapters_backward  for dout (rows ld_dout apart): dX [t][k], dA and dB of A's and B's shapes, each NULL where not wanted, from what
  *                          was kept for these tokens and indexes.  The gradient of Y is dout.
- * Sums are fp32.  Between the products H is held in fp32 and enters the second with all of its bits; each result is rounded once.  An infinite
- * element of B, or of dout or X in a factor's gradient, may make NaN of what would be infinite.  work: 16-byte aligned, of the bytes that the *_work function
+ * Sums are fp32.  Between the products H is held in fp32 and enters the second with all of its bits; each result is rounded once.  Infinities
+ * and NaN come out where the formula has them, and in no other token, adapter or column.  work: 16-byte aligned, of the bytes that the *_work function
  * of the same sizes reports (keep: whether `kept` is there; 0 bytes: may be NULL), rewritten by every call.  Results never depend on the order in which waves run.
  * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE for widths
  * above RSH_FFN_MAX_WIDTH, more than RSH_ADAPTERS_MAX adapters or a rank above RSH_ADAPTERS_MAX_RANK.

@@ -363,6 +363,41 @@ struct Column {
         }
     }
 };
+// The pieces' products make NaN of an infinity: a piece that is zero times it, or pieces of either sign.  So where a sum has come out as NaN, it is
+// formed again from the numbers themselves, and is NaN where the formula is.  That way is taken whole, in a loop behind the other: between its steps it
+// cost one token 0.8 us, since every jump over it went to instructions that were not there yet.
+__device__ __forceinline__ bool is_nan(const Eight& e) {
+    bool is = false;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) is |= e.v[q] != e.v[q];
+    return is;
+}
+__device__ __forceinline__ void add_products(Eight& e, float h, const Eight& v) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) e.v[q] += h * v.v[q];
+}
+// A lane's four pieces of 128 columns of a token's row: Y, and sum(u) where the token has an adapter, or again(u) where one of those is NaN.
+template <class T, class SUM, class AGAIN>
+__device__ __forceinline__ void store_token(const uint16_t* Y, const uint4_t* y, uint16_t* out, int64_t col, int64_t m, bool some, SUM sum, AGAIN again) {
+    bool is = false;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) is |= is_nan(sum(u));      // zeros where the token has no adapter
+    auto store = [&](int u, Eight e, const Eight& s) {
+        if (some) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) e.v[q] += s.v[q];
+        }
+        store_eight<T>(out, col + 32 * u, e, (int)min(m - col - 32 * u, (int64_t)8));
+    };
+    if (__builtin_expect(!is, 1)) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) store(u, widen8<T>(y[u]), sum(u));
+        return;
+    }
+#pragma unroll 1
+    for (int u = 0; u < 4; ++u) store(u, Y ? widen8<T>(run_of(Y, col + 32 * u, m)) : Eight{}, again(col + 32 * u));
+}
+
 // out = Y + s H B_i of a tile's tokens and 128 columns a wave.  A lane's loads of B are eight columns of four rows, four for each of eight
 // results of 16 columns by 16 tokens; which eight is chosen so that lanes store pieces of a row that lie side by side.  The sums of all tokens
 // of a tile stay in registers while B goes by once, 16 rows at a time and the next 16 on their way.
@@ -497,16 +532,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
     for (int i = 0; i < kGroups; ++i) {
         if (16 * i >= tile.count) break;
         if (16 * i + c >= tile.count) continue;
+        store_token<T>(
+            Y ? Y + token[i] * ld_y : nullptr, y[i].y, out + token[i] * m, col0 + 8 * g, m, some,
+            [&](int u) {
+                Eight e;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t to = col0 + 32 * u + 8 * g;
-            Eight e = widen8<T>(y[i].y[u]);
-            if (some) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) e.v[q] += acc[i][q][u];
-            }
-            store_eight<T>(out, token[i] * m + to, e, (int)min(m - to, (int64_t)8));
-        }
+                for (int q = 0; q < 8; ++q) e.v[q] = acc[i][q][u];
+                return e;
+            },
+            [&](int64_t to) {
+                Eight e = {};
+#pragma unroll 1
+                for (int rank = 0; rank < r; ++rank) {
+                    float h = H[token[i] * r16 + rank];
+                    for (int p = 1; p < (FEW ? parts : 1); ++p) h += H[((int64_t)p * t + token[i]) * r16 + rank];
+                    add_products(e, h * (scales ? scales[tile.adapter] : 1.f), widen8<T>(run_of(B + ((int64_t)tile.adapter * r + rank) * m, to, m)));
+                }
+                return e;
+            });
     }
 }
 
@@ -613,16 +656,22 @@ __global__ __launch_bounds__(1024) void rsh_adapters_few_kernel(const uint16_t* 
         }
     }
     if (c >= tile.count) return;
+    store_token<T>(
+        Y ? Y + token * ld_y : nullptr, y, out + token * m, col0 + 8 * g, m, some,
+        [&](int u) {
+            Eight e;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int64_t to = col0 + 32 * u + 8 * g;
-        Eight e = widen8<T>(y[u]);
-        if (some) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) e.v[q] += acc[q][u];
-        }
-        store_eight<T>(out, token * m + to, e, (int)min(m - to, (int64_t)8));
-    }
+            for (int q = 0; q < 8; ++q) e.v[q] = acc[q][u];
+            return e;
+        },
+        [&](int64_t to) {
+            Eight e = {};
+#pragma unroll 1
+            for (int rank = 0; rank < r; ++rank)
+                add_products(e, sums[rank / 16][16 * (rank % 16 / 4) + c][rank % 4],
+                             widen8<T>(run_of(B + ((int64_t)tile.adapter * r + rank) * m, to, m)));
+            return e;
+        });
 }
 
 // H of all tokens from its parts.
@@ -717,9 +766,19 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
                 float s = joined[0][q][lane][v];
 #pragma unroll
                 for (int w = 1; w < WAVES; ++w) s += joined[w][q][lane][v];
-                e.v[q] = s * scale;
+                e.v[q] = s;
             }
             if (rank >= r || col >= k) continue;
+            if (__builtin_expect(is_nan(e), 0)) {
+                e = {};
+#pragma unroll 1
+                for (int n = begin; n < end; ++n) {
+                    const int64_t token = order.token[n];
+                    add_products(e, H[token * r16 + rank], widen8<T>(run_of(X + token * ld_x, col, k)));
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) e.v[q] *= scale;
             const int64_t at = ((int64_t)adapter * r + rank) * k + col;
             if (parts == 1) store_eight<T>(out, at, e, valid);
             else store_eight<F32>(sums, (int64_t)part * n * r * k + at, e, valid);
