@@ -751,7 +751,8 @@ __global__ __launch_bounds__(64 * WAVES) void rsh_adapters_outer_kernel(const ui
             }
         }
     }
-    const float scale = scales ? scales[adapter] : 1.f;
+    // No tokens, no product: the scale of an adapter that nothing uses may be anything, and an infinite one leaves an empty part out.
+    const float scale = scales && begin < end ? scales[adapter] : 1.f;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         __syncthreads();
