@@ -180,7 +180,7 @@ __device__ __forceinline__ float2_t statistics(const rsh_norm_t& norm, int d, Te
     };
     attempt(1.f);
     if (m - m + q < INFINITY) return (float2_t){m, __builtin_amdgcn_rsqf(q + norm.eps)};      // one step of fp32 off at most, a normal number
-    const float c = 0x1p-70f;
+    const float c = 0x1p-80f;      // 2^21 squares of numbers of 2^128 stay in range
     attempt(c);
     return (float2_t){m / c, c / sqrtf(q + fmaxf(norm.eps * c * c, 0x1p-149f))};
 }
