@@ -457,25 +457,24 @@ struct Backward {
 #pragma unroll
             for (int i = 0; i < 8; ++i) n.v[i] = n.v[i] * w.v[i] + b.v[i];
         }
-        if (j.drop.share) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) n.v[i] = x.kept >> i & 1 ? n.v[i] : 0.f;
-        }
+        drop(n, x);
         return n;
     }
     __device__ __forceinline__ float factor() const { return j.drop.share ? j.scale * random.keep : j.scale; }
-    // scale * gate, zero where dropped, times dropout's factor.
-    __device__ __forceinline__ Eight factors(const Run& x, const Place& row, int col) const {
+    // scale * gate times dropout's factor.
+    __device__ __forceinline__ Eight factors(const Place& row, int col) const {
         Eight f;
         if (j.ld_gate) f = load_vector<T, SHORT>(row.of(j.gate, j.ld_gate, j.gate_type == RSH_F32 ? 4 : 2), j.gate_type, col, d);
         else f = given.gate_of(col);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f.v[i] *= factor();
-        if (j.drop.share) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f.v[i] = x.kept >> i & 1 ? f.v[i] : 0.f;
-        }
         return f;
+    }
+    // What is dropped becomes zero, infinities and NaN too, in either direction.
+    __device__ __forceinline__ void drop(Eight& e, const Run& x) const {
+        if (!j.drop.share) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = x.kept >> i & 1 ? e.v[i] : 0.f;
     }
     __device__ __forceinline__ void store_gate(const Place& row, int col, const Eight& gate) const {
         if (std::is_same<T, F32>::value || j.gate_type == RSH_F32) store_run<F32>(g.dgate, row, col, d, gate);
@@ -494,7 +493,7 @@ struct Backward {
         if (!first) return;
         x.xh = value(in, in.x, col);
         if constexpr (JOIN) {
-            const Eight n = inner(x, col), f = factors(x, row, col);
+            const Eight n = inner(x, col), f = factors(row, col);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x.xh.v[i] += f.v[i] * n.v[i];
         }
@@ -522,7 +521,7 @@ struct Backward {
     }
     // From there to the gradient of N1's result; returns what the gate's gradient gets.
     __device__ __forceinline__ Eight through(const Inputs<T>&, const Place& row, int col, Run& x, SUMS& sums) const {
-        const Eight f = factors(x, row, col);
+        const Eight f = factors(row, col);
         Eight gate = {};
         if (g.dgate) {
             gate = inner(x, col);
@@ -532,6 +531,7 @@ struct Backward {
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) x.gb.v[i] = x.ds.v[i] * f.v[i];
+        drop(x.gb, x);
         if (second) {
             const Eight w = given.after_weight(col);
             Eight term;
@@ -658,14 +658,18 @@ __global__ __launch_bounds__(1024) void rsh_join_means_kernel(rsh_join_t j, rsh_
                 for (int i = 0; i < 8; ++i) a1 += x.g.v[i], a2 += x.g.v[i] * x.xh.v[i];
             }
             if (JOIN && back.second && g.dB) {
-                Eight fw = back.factors(x, row, col), ds = g.dS ? back.value(in, in.ds, col) : Eight{};
+                Eight fw = back.factors(row, col), ds = g.dS ? back.value(in, in.ds, col) : Eight{};
                 const Eight w = given.after_weight(col);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) fw.v[i] *= w.v[i];
                 clear_from(fw, d - col);
+                back.drop(fw, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ds.v[i] = (back.first ? ds.v[i] + in.before[1] * x.g.v[i] : ds.v[i]) * fw.v[i];
+                back.drop(ds, x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float f = fw.v[i], xb = x.xb.v[i], p = (back.first ? ds.v[i] + in.before[1] * x.g.v[i] : ds.v[i]) * f;
+                    const float f = fw.v[i], xb = x.xb.v[i], p = ds.v[i];
                     b1 += p, b2 += p * xb;
                     if (back.first) {
                         const float h = x.xh.v[i] * f;
