@@ -362,7 +362,7 @@ int rsh_dropout(const void *X_dev, int32_t type, int64_t t, int64_t d, int64_t l
  * without gaps), gradients of the parameters in their types.  work: 16-byte aligned, of the bytes that rsh_join_backward_work reports,
  * rewritten by every call (0: may be NULL); vectors: how many results are [d].
  * Results never depend on the order in which waves run.  RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride,
- * alignment or number out of range (eps is a finite normal number above 0), RSH_ERR_TOO_LARGE for a d above RSH_FFN_MAX_WIDTH.
+ * alignment or number out of range (eps is a finite normal number above 0; scale is finite, and scale * 65536 / (65536 - share) in fp32 where not all is dropped), RSH_ERR_TOO_LARGE for a d above RSH_FFN_MAX_WIDTH.
  */
 enum { RSH_NORM_NONE = 0, RSH_NORM_RMS = 1, RSH_NORM_LAYER = 2 };
 typedef struct {

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <chrono>
+#include <cmath>
 #include <cstring>
 #include <initializer_list>
 #include <new>
@@ -757,6 +758,7 @@ int join_ok(const rsh_join_t* j, bool forward) {
     if (!norm_ok(j->after, j->type) || !norm_ok(j->before, j->type) || !aligned_to({j->X, j->B, j->S, j->Y}, type_bytes(j->type)) || (j->X && !stride_ok(j->ld_x, j->d)) ||
         (j->B && !stride_ok(j->ld_b, j->d)) || !drop_ok(j->drop) || !(j->scale - j->scale == 0))
         return RSH_ERR_BAD_OPTION;
+    if (j->drop.share < 65536 && !(std::fabs(j->scale) * (65536.f / (float)(65536 - j->drop.share)) < INFINITY)) return RSH_ERR_BAD_OPTION;
     if (!parameter_ok(j->gate, j->gate_type, j->type) || (j->gate ? j->ld_gate && !stride_ok(j->ld_gate, j->d) : j->ld_gate != 0)) return RSH_ERR_BAD_OPTION;
     if (forward && ((j->B && (j->S == j->X || j->S == j->B)) || (j->Y && (j->Y == j->X || j->Y == j->B || j->Y == j->S)))) return RSH_ERR_BAD_OPTION;
     return RSH_OK;

@@ -155,11 +155,11 @@ __device__ __forceinline__ void store_eight(void* base, int64_t at, const Eight&
 // of them a block: 16 bits an element keep that below what the memory takes.
 struct Random {
     uint32_t k0, k1, c2, c3, share;
-    float keep;        // what is kept is multiplied by it: 1 / (1 - share / 65536)
+    float keep;        // what is kept is multiplied by it: 1 / (1 - share / 65536); with nothing kept 1, which nothing is multiplied by
     __device__ __forceinline__ Random(const rsh_drop_t& d) {
         const uint64_t seed = d.seed_dev && d.share ? *d.seed_dev : d.seed;
         k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32), c2 = (uint32_t)d.offset, c3 = (uint32_t)(d.offset >> 32), share = d.share;
-        keep = 65536.f / (float)(share < 65536u ? 65536u - share : 1u);
+        keep = share < 65536u ? 65536.f / (float)(65536u - share) : 1.f;
     }
     __device__ __forceinline__ uint4_t bits(uint32_t place, uint32_t row) const {
         asm volatile("" : "+v"(place));       // its first product is not kept from row to row

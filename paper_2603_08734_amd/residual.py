@@ -231,4 +231,6 @@ def join(X, B, after: Norm | None = None, gate=None, scale: float = 1.0, drop: D
         raise TypeError("B: expected a tensor; the norm alone is residual.norm")
     if not abs(scale) < 2.0 ** 127:
         raise ValueError(f"scale: expected a finite number of fp32, got {scale}")
+    if isinstance(drop, Drop) and 0 < drop.share < 65536 and not abs(scale) * 65536 / (65536 - drop.share) < 2.0 ** 128:
+        raise ValueError(f"scale: {scale} / (1 - {drop.share / 65536}) is beyond fp32")
     return _run(X, B, after, gate, float(scale), drop, before)
