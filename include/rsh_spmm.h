@@ -402,8 +402,9 @@ int rsh_join_backward(const rsh_join_t *join, const rsh_join_gradients_t *gradie
  * and NaN come out where the formula has them, and in no other token, adapter or column.  work: 16-byte aligned, of the bytes that the *_work function
  * of the same sizes reports (keep: whether `kept` is there; 0 bytes: may be NULL), rewritten by every call.  Results never depend on the order in which waves run.
  * RSH_ERR_NULL for a missing operand, RSH_ERR_BAD_OPTION for a type, size, stride or alignment out of range, RSH_ERR_TOO_LARGE for widths
- * above RSH_FFN_MAX_WIDTH, more than RSH_ADAPTERS_MAX adapters or a rank above RSH_ADAPTERS_MAX_RANK.
+ * above RSH_FFN_MAX_WIDTH, more than RSH_ADAPTERS_MAX adapters or RSH_ADAPTERS_MAX_TOKENS tokens, or a rank above RSH_ADAPTERS_MAX_RANK.
  */
+#define RSH_ADAPTERS_MAX_TOKENS (1 << 28)
 #define RSH_ADAPTERS_MAX 4096
 #define RSH_ADAPTERS_MAX_RANK 512
 typedef struct {

@@ -22,7 +22,7 @@ RSH_F32, RSH_F16, RSH_BF16, RSH_MX4 = range(4)
 RSH_FFN_MAX_WIDTH = 1 << 21
 RSH_ACT_SILU, RSH_ACT_GELU, RSH_ACT_RELU = range(3)
 RSH_NORM_NONE, RSH_NORM_RMS, RSH_NORM_LAYER = range(3)
-RSH_ADAPTERS_MAX, RSH_ADAPTERS_MAX_RANK = 4096, 512
+RSH_ADAPTERS_MAX, RSH_ADAPTERS_MAX_RANK, RSH_ADAPTERS_MAX_TOKENS = 4096, 512, 1 << 28
 RSH_ROWS_MAX_STRIDE = 1 << 29
 (RSH_TILES_PRODUCT, RSH_TILES_PRODUCT4, RSH_TILES_GATED, RSH_TILES_GATED4, RSH_TILES_DX, RSH_TILES_DW, RSH_TILES_DW_ONE) = range(7)
 

@@ -809,7 +809,8 @@ int rsh_join_backward(const rsh_join_t* join, const rsh_join_gradients_t* g, voi
 namespace {
 int adapter_sizes_ok(int64_t t, int64_t k, int64_t m, int32_t n, int32_t r) {
     if (t <= 0 || k <= 0 || m <= 0 || n <= 0 || r <= 0 || t >= kMaxSize) return RSH_ERR_BAD_OPTION;
-    return k > kMaxWidth || m > kMaxWidth || n > RSH_ADAPTERS_MAX || r > RSH_ADAPTERS_MAX_RANK ? RSH_ERR_TOO_LARGE : RSH_OK;
+    // A launch takes fewer than 2^32 threads, and of a tile of 64 tokens 512 are threads of one.
+    return t > RSH_ADAPTERS_MAX_TOKENS || k > kMaxWidth || m > kMaxWidth || n > RSH_ADAPTERS_MAX || r > RSH_ADAPTERS_MAX_RANK ? RSH_ERR_TOO_LARGE : RSH_OK;
 }
 int adapters_ok(const rsh_adapters_t* a, const void* work, bool forward) {
     if (!a) return RSH_ERR_NULL;
