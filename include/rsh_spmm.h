@@ -331,7 +331,7 @@ int rsh_ffn_tiles(int32_t which, int32_t aligned, int64_t t, int64_t a, int64_t 
  * (low, high half of the seed); of its four words, low half before high half, elements take theirs in order.  An element whose bits are
  * below `share` becomes zero (an infinity or a NaN too), the others are multiplied by 65536 / (65536 - share).
  *   rsh_dropout    Y = drop(X); its gradient is the same call on the gradient of Y.  Y without gaps, or X itself (ld = d)
- * ld: elements from row to row, d .. RSH_ROWS_MAX_STRIDE.  share: 0 .. 65536.  seed_dev: device, 8-byte aligned, read by the kernels in place of `seed`, or NULL.
+ * t: 1 .. 2^31 - 1.  d: 1 .. RSH_FFN_MAX_WIDTH (RSH_ERR_TOO_LARGE above).  ld: elements from row to row, d .. RSH_ROWS_MAX_STRIDE.  share: 0 .. 65536.  seed_dev: device, 8-byte aligned, read by the kernels in place of `seed`, or NULL.
  */
 #define RSH_ROWS_MAX_STRIDE (1 << 29)
 typedef struct {

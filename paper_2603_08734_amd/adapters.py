@@ -5,7 +5,8 @@
 
 A [n, r, k] and B [n, r, m]: n adapters of rank r, both factors rank first (products along their rows serve the forward and the backward
 pass alike).  Tokens may come in any order; one whose index is not 0 .. n - 1 has no adapter and keeps its row of Y.  Binary16 or bfloat16;
-X A[i]^T stays in fp32 between the two products, and results are rounded once.  Autograd-aware (reverse mode, first derivatives) in Y, X, A
+X A[i]^T stays in fp32 between the two products and enters the second with all of its bits, and results are rounded once.  Up to 4096 adapters of
+rank up to 512 and 2^28 tokens.  Autograd-aware (reverse mode, first derivatives) in Y, X, A
 and B; scales are constants.
 """
 from __future__ import annotations

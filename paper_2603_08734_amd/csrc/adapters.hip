@@ -9,10 +9,10 @@
 //
 // Ranks are small, so all three are passes over X, Y and dout, bound by memory; operands go from memory to the matrix unit through registers
 // alone, a step ahead of their use.  Measured (bfloat16): 4096 tokens of 28672 features at rank 16, shrink 57 us (235 MB, 4.1 TB/s),
-// expand to 8192 columns 33 us (134 MB, 4.1); 4096 tokens at rank 64 between 4096 and 16384 features: shrink 16.5 and 48 us, expand 20.5
-// and 80, outer 24 and 46 (a copy of the bytes would take 7, 26, 7, 53, 7 and 26): what counts there is the time until a workgroup's first
-// loads have come, since all of them fit the chip at once or nearly so.  One token at rank 16 between 8192 and 28672 features 13.6 us in one
-// launch, 7.0 at 1024 features: one compute unit's reading of A, 35 KB a us; 77 tokens of 61 adapters at 4100 by 1003 11.1 us.
+// expand to 8192 columns 33 us (134 MB, 4.1); 4096 tokens at rank 64 between 4096 and 16384 features: shrink 17 and 48 us, expand 23
+// and 86, outer 26 and 55 (a copy of the bytes would take 7, 26, 7, 53, 7 and 26): what counts there is the time until a workgroup's first
+// loads have come, since all of them fit the chip at once or nearly so.  One token at rank 16 between 8192 and 28672 features 13.9 us in one
+// launch, 7.0 at 1024 features: one compute unit's reading of A, 35 KB a us; 77 tokens of 61 adapters at 4100 by 1003 11.2 us.
 #include <algorithm>
 
 #include "rows.hpp"
@@ -25,7 +25,7 @@ constexpr int kFewTokens = 256, kFewTile = 16, kFewParts = 8, kFewColumns = 1024
 constexpr int kSortThreads = 1024, kSortWords = 7 * (RSH_ADAPTERS_MAX + 1);     // counters in LDS
 
 struct Tile {
-    int adapter, first, count, pad;        // adapter: -1 for none; first: in the order
+    int adapter, first, count, pad;        // adapter: n for none; first: in the order
 };
 
 // Of the tokens: int32 or int64, anything but 0 .. n - 1 for none.
@@ -303,8 +303,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(RT =
 
 // Four fp32 numbers as three of bfloat16 each, hi + mid + lo: cut into eight bits at a time, so the three are the number itself (its last bits
 // may be lost below 2^-110, where lo is subnormal); of an infinity or a NaN mid and lo are zero.  Sums of r or t products of one of them with 16-bit
-// numbers are formed by the matrix unit's 16-bit instructions, whose products and sums are fp32: two instructions for bfloat16, three for binary16, of which
-// one takes 32 terms.  Its fp32 form, at an eighth of the rate, took 55 of the 100 us of 4096 tokens at rank 64 by 16384 columns.
+// numbers are formed by the matrix unit's 16-bit instructions, whose products and sums are fp32: 16 terms take two of them for bfloat16, three for binary16.
+// Its fp32 form takes four times as long as two and was 55 of the 100 us of 4096 tokens at rank 64 by 16384 columns.  (Two numbers of bfloat16, 2^-17
+// off, make that step 80 us, three 86.)
 struct Thirds {
     uint2_t hi, mid, lo;
 };
@@ -838,15 +839,18 @@ struct Sorted {
 };
 
 // Whether a few tokens go in one launch, in which every workgroup reads its A for itself.  It takes 4.4 us and 1 us for every 30 KB of A (7.0 us at
-// k = 1024 and rank 16, 13.6 at 8192); two launches take 10.1 us at 8192 and, called one by one, 4 us more on the host.  So up to 256 KB, and
-// while what all workgroups read together stays below 64 MB.
+// k = 1024 and rank 16, 13.9 at 8192).  Called one by one two launches cost the host 3 to 4 us more (16.4 for 12.6 us at 1024, 16.7 for 13.7 at
+// 8192): so one up to 256 KB, and while what all workgroups read together stays below 64 MB.  Inside a graph of many calls the host does not count, and
+// two would be as good at 1024 (8.1 for 7.5 us) and better at 8192 (8.9 for 13.6).
 bool in_one(int64_t t, int64_t k, int64_t m, int r) {
     const int64_t factor = 2 * k * wide_rank(r), columns = (m + kFewColumns - 1) / kFewColumns;
     return t <= kFewTokens && r <= 32 && factor <= (1 << 18) && factor * columns * t <= (1 << 26);
 }
 
 // Parts of the long axis of a shrinking product, and the steps of 64 in each: as many as bring all compute units their fill of workgroups at
-// once, since a second round costs as much as the first (4096 tokens at rank 64 by 16384 columns in 16 parts and four rounds 63 us).
+// once, since a second round costs as much as the first (4096 tokens at rank 64 by 16384 columns in 16 parts and four rounds 63 us; the training
+// step between 4096 and 16384 columns with half as many 273 us, with twice as many 291, for 267).  Tiles are counted as if every adapter had some: 512
+// tokens of four adapters at 28672 features take 31 us with 4 of them loaded, 40 with 64 and 147 with 512.
 constexpr int kFewWaves = 8, kOuterWaves = 4;
 constexpr int shrink_waves(int r) { return r <= 16 ? 8 : 4; }      // fewer parts to add up where the registers leave room (63 -> 60 us)
 int slots_of(int r) { return r <= 16 ? 1024 : r <= 32 ? 768 : 512; }     // workgroups of four waves that fit the chip, by their registers
@@ -862,7 +866,9 @@ struct Split {
     }
 };
 
-// Parts of the tokens in a factor's gradient.
+// Parts of the tokens in a factor's gradient: as many as fill the chip if all adapters have tokens alike (8 or 32 in place of 16 take the same time).  With
+// 4096 tokens of one adapter at 4096 features and rank 64 a step takes 163 us if it is the only one loaded, 184 of 4, 343 of 64 and 443 of
+// 256, whose gradients are 268 MB of zeros.
 int outer_parts(int64_t t, int64_t k, int n, int r) {
     const int64_t blocks = (k + 127) / 128 * n * ((r + 63) / 64);
     return (int)std::max<int64_t>(1, std::min<int64_t>({16, slots_of(r) / blocks, t / 64}));

@@ -3,14 +3,14 @@
 // with m the mean (RSH_NORM_LAYER) or zero, and backwards, xh = (S - m) r and g = dY w2:
 //   dS' = dS + r (g - mean(g) - xh mean(g xh)),  dX = dS',  dn = dS' scale gate (1 / (1 - p) or zero),  dB as dS' from dn w1 and B's xh,
 //   dw = sum of dY xh over the rows, db = sum of dY, dgate = dS' scale D (summed where the gate is a vector)
-// (mean(g) without a mean in the forward pass is zero).  Each tensor is read once and written once, a few dozen operations an element: bound
-// by memory, if the work of a row leaves it busy.  So a row is eight columns to a lane, whatever number of lanes that takes (8 to 1024),
+// (mean(g) without a mean in the forward pass is zero).  Each tensor is read once and written once (gradients of rows beyond 8192 columns read theirs
+// twice), a few dozen operations an element: bound by memory, if the work of a row leaves it busy.  So a row is eight columns to a lane, whatever number of lanes that takes (8 to 1024),
 // and a workgroup goes through many rows: parameters stay in its registers, the gradients' sums over the rows in LDS, the next row is on
 // its way while one is computed, and the only waits within a row are for the sums over its lanes, one a norm (two with a mean).
 // Measured (a copy too large for the caches runs at 5.1 TB/s, reading and writing; smaller ones up to 7.2): 2048 x 8192 bfloat16, sum and norm
 // 24.0 us (134 MB, 5.6 TB/s); 2^20 x 64 binary16, norm 53.7 and its gradients 78 us (5.0, 5.2); 8192 x 8192 bfloat16 with both norms, gate and
-// dropout 125 us forward and 171 to 185 backward (4.3, 4.4 to 4.7), where dropout's random numbers cost 16 us and each wait for sums about 10; 1001 x 500 fp32
-// 7.1 and 10.6 us, 16 x 4096 4.8, 1 x 8192 2.7 (the norm alone), where a launch's latency counts.
+// dropout 126 us forward and 170 to 189 backward (4.3, 4.3 to 4.7), where dropout's random numbers cost 16 us and each wait for sums about 10; 1001 x 500 fp32
+// 7.2 and 10.8 us, 16 x 4096 4.8, 1 x 8192 2.7 (the norm alone), where a launch's latency counts.
 #pragma once
 #include <algorithm>
 
@@ -547,7 +547,9 @@ struct Backward {
 };
 
 // One pass over the rows, each in its lanes' registers, and the vectors' sums with it, a part of them from every workgroup.  The next
-// row is on its way while one is computed.
+// row is on its way while one is computed.  128 registers are all that 1024 lanes have: in 16 bits without biases they do, with biases 48 to 68 bytes
+// of a lane go to scratch memory, in fp32 12, with biases 112.  8192 x 8192 with dropout, forward and backward: bfloat16 RMS without biases 293 us, layer norms with biases 429 (a
+// copy of the bytes 211); fp32 525 and 757 (421).
 template <class T, int LANES, bool JOIN, bool BIAS>
 __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_eu(!JOIN || LANES > 256 ? 4 : LANES > 64 ? 3 : 2))) void rsh_join_backward_kernel(rsh_join_t j, rsh_join_gradients_t g, Vectors vectors, float* parts) {
     constexpr int kThreads = kThreadsOf<LANES>, kRows = kRowsOf<LANES>;
@@ -634,7 +636,8 @@ __global__ __launch_bounds__(kThreadsOf<LANES>) __attribute__((amdgpu_waves_per_
 // Longer rows: this kernel forms the four means of a row, means[4 row] = those of g and g xh and those of N1's, and the next one goes through the
 // columns.  N1's means are of gb = (dS + r g - r mean(g) - r xh mean(g xh)) fw with fw = w1 scale gate drop, so of (dS + r g) fw, fw and xh fw,
 // which need no other mean: one pass has them all.  (With three passes over
-// the rows, and a fourth for the vectors, a step of 1677 x 20000 bfloat16 took 448 us, with these two 353.)
+// the rows, and a fourth for the vectors, a step of 1677 x 20000 bfloat16 took 448 us, with these two 353.)  The price is a difference of sums: where g is
+// nearly a constant, 100 times its spread, dB is 3.0e-7 off in fp32 for 1.3e-7 from finished terms (8192 columns); elsewhere both are 0.8e-7.
 template <class T, bool JOIN>
 __global__ __launch_bounds__(1024) void rsh_join_means_kernel(rsh_join_t j, rsh_join_gradients_t g, float* means) {
     __shared__ Team<1024>::Meeting meeting;
@@ -732,7 +735,8 @@ __global__ __launch_bounds__(256) void rsh_join_columns_kernel(rsh_join_t j, rsh
 }
 
 // f(lanes) of the kernels that have a row in registers, a run a lane: the fewest that do.
-constexpr int64_t kRegisterWidth = 8192, kColumnBlocks = 512;      // workgroups of the columns' kernel that fit the chip at once
+// Workgroups of the columns' kernel: as many as fit the chip at once (a step of 1677 x 20000 353 us, with 256 395, with 1024 358).
+constexpr int64_t kRegisterWidth = 8192, kColumnBlocks = 512;
 template <class F>
 void by_width(int64_t d, F f) {
     using std::integral_constant;
@@ -768,8 +772,10 @@ void join_backward_of(const rsh_join_t& j, const rsh_join_gradients_t& g, const 
 template <class T>
 void join_forward_launch(const rsh_join_t& j, hipStream_t st) {
     if (j.d > kRegisterWidth) {
-        // Joins keep a row in registers while it fits (1170 x 28672 bfloat16 79 us, 104 read again at every pass, 1677 x 20000 106 and 97); a norm alone is
-        // faster read again, from the caches (28 and 32 us, 26 and 43; 3276 x 10240 27.5 and 37).
+        // Joins keep a row in registers up to 32768 columns, or read it again, from the caches, at every pass.  With both norms and a gate, in us, the former
+        // and the latter of 10240, 16384, 20000 and 28672 columns (67 MB a tensor): bfloat16 93 118, 67 96, 107 107, 83 118; fp32, where 108 to 136 bytes
+        // of a lane go to scratch memory, 85 85, 73 98, 101 106, 89 110.  A sum and a norm: bfloat16 69 73, 57 65, 81 68, 63 76; fp32 70 60, 66 82, 86 86, 77 91.
+        // A norm alone: bfloat16 35 26, 29 26, 42 26, 33 29; fp32 31 26, 26 28, 35 31, 31 33: read again.
         const dim3 rows((unsigned)std::min<int64_t>(j.t, 1 << 16));
         if (!j.B) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 1024, 0, false>), rows, dim3(1024), 0, st, j);
         else if (j.d <= 2 * kRegisterWidth) hipLaunchKernelGGL((rsh_join_forward_long_kernel<T, 512, 4, true>), rows, dim3(512), 0, st, j);

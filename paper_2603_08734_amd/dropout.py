@@ -1,11 +1,12 @@
 """Dropout whose random numbers are a function of a seed, an offset and an element's place, so that no mask is stored.
 
     drop = dropout.Drop(0.1, seed, offset)       # offset: what tells apart the layers and steps of a program, say
-    Y = dropout.dropout(X, drop)                 # fp32, binary16 or bfloat16, any shape; autograd-aware, derivatives of any order
+    Y = dropout.dropout(X, drop)                 # fp32, binary16 or bfloat16, [..., d] with d up to 2^21; autograd-aware, derivatives of any order
     S = residual.join(X, B, drop=drop)           # the same numbers inside the join after a block
 
 An element is dropped (becomes zero, whatever it was) with probability p, rounded to a multiple of 2^-16, and multiplied by
-1 / (1 - p) otherwise.  ``include/rsh_spmm.h`` says which random number an element has: rows are the last dimension, counted over the others.
+1 / (1 - p) otherwise, in the join too and for the gradients.  ``include/rsh_spmm.h`` says which random number an element has: rows are the last
+dimension, counted over the others.
 """
 from __future__ import annotations
 

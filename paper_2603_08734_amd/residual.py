@@ -6,7 +6,7 @@
 
 All of a row's steps run in one kernel (``rsh_join_forward``) in fp32; S and Y are each rounded once, Y being the norm of the sum as it was
 before its rounding.  Autograd-aware (reverse mode, first derivatives) in X, B, the gate and the norms' parameters; one pass over the
-rows (``rsh_join_backward``) forms all gradients, from X, B and two numbers a row and norm: S is added up again,
+rows (two beyond 8192 columns, ``rsh_join_backward``) forms all gradients, from X, B and two numbers a row and norm: S is added up again,
 since the rounded one would bring its error into them.
 """
 from __future__ import annotations
@@ -226,7 +226,7 @@ def norm(X, norm: Norm):
 
 def join(X, B, after: Norm | None = None, gate=None, scale: float = 1.0, drop: Drop | None = None, before: Norm | None = None):
     """S = X + scale * gate * drop(after(B)), and with ``before`` the pair (S, before(S)).  X, B [..., d] of one type; gate: [d] or of X's
-    shape, in fp32 or X's type; scale: a number."""
+    shape, in fp32 or X's type; scale: a number, finite in fp32 also when divided by 1 - p of drop."""
     if B is None:
         raise TypeError("B: expected a tensor; the norm alone is residual.norm")
     if not abs(scale) < 2.0 ** 127:
